@@ -430,9 +430,96 @@ ipkv_status ipkv_pack_blocks(const ipkv_attn_shape* shape, int32_t layout, const
 /* Bytes of one block for a shape. */
 int64_t ipkv_block_bytes(const ipkv_attn_shape* shape);
 
+/* ---- what comes before the cache: head norm and rotation (no handle) ----------------------------------------
+ * The paper starts at finished queries and keys; models that it evaluates (Qwen3) normalise every query and key head and
+ * rotate it by its token's position right before the append.  One call does both for all heads of a step or a prompt:
+ *   y = x * rsqrt(mean(x^2) + eps) * weight            (over the head's dim columns; skipped where weight_dev is NULL)
+ *   (a, b) -> (a cos t - b sin t, b cos t + a sin t)   (pair i of y's first rot_dim columns; the others stay)
+ *   t = positions[pair_axis[i]][token] * frequency i
+ * bf16 in and out, fp32 in between, one rounding.  The angle is the product modulo a turn, off by at most 2^-24 of a
+ * turn for every 32-bit position and frequencies up to one turn per position (an fp32 product of a far position is not). */
+typedef struct {
+  int32_t dim;               /* columns of a head: 64, 128 or 256                                              */
+  int32_t rot_dim;           /* columns that are rotated, from the first: a multiple of 16 up to dim; 0: none   */
+  int32_t n_axes;            /* 1..4 positions per token (time, height, width of images and video)              */
+  int32_t interleaved;       /* pair i is columns (2i, 2i+1) if nonzero, else (i, i + rot_dim/2)                */
+  float eps;
+  double theta;              /* frequency of pair i is theta^(-2i/rot_dim) ...                                  */
+  const double* inv_freq;    /* ... or, if not NULL, inv_freq[i] radians per position: host [rot_dim/2]         */
+  const uint8_t* pair_axis;  /* host [rot_dim/2]: the axis that pair i follows; NULL: axis 0                    */
+} ipkv_rope;
+
+/* Some heads of every token (the queries, the keys).  Strides in elements, multiples of 8; pointers 16-byte aligned.  out_dev
+ * may be in_dev with the same strides (in place); otherwise no output may share bytes with an input or another output. */
+typedef struct {
+  const void* in_dev;        /* head h of token t begins at in_dev + t * in_token_stride + h * in_head_stride   */
+  void* out_dev;
+  const void* weight_dev;    /* [dim] bf16, or NULL: no norm                                                    */
+  int32_t n_heads;
+  int64_t in_token_stride, in_head_stride, out_token_stride, out_head_stride;
+} ipkv_heads;
+
+/* parts: host array of 1..4.  positions_dev: device int32 [n_axes][n_tokens] (may be NULL when rot_dim is 0).  Works on the
+ * current device; the launch keeps copies of everything on the host side, so it can be captured into a CUDA graph. */
+ipkv_status ipkv_norm_rope(const ipkv_rope* rope, int64_t n_tokens, const ipkv_heads* parts, int32_t n_parts,
+                           const int32_t* positions_dev, void* stream);
+
 const char* ipkv_status_str(ipkv_status s);
 const char* ipkv_last_error(const ipkv_t* h);
 const char* ipkv_version(void);
+
+/* ---- a cache held in 4 bits (no handle) ------------------------------------------------------------------------
+ * Blocks of 4-bit codes: 140 bytes per token and KV head of 128 columns (72 for 64) where TILE blocks take 512 (256).
+ * A group of values — the 64 columns of one panel for K, all columns for V, of one token and KV head — is held as codes with
+ * a bf16 scale and zero:
+ *   zero = min x,  scale = bf16((max x - min x) / 15),  code = min(round_half_even((x - zero) / scale), 15)      (fp32)
+ * and a code stands for scale * code + zero.  Where scale is below 2^-126 every code is 0.  Inputs have to be finite and
+ * below 2^126 in magnitude; what a group with other values holds is unspecified (other groups are not affected).
+ * Grouped-query shapes only: kind IPKV_GQA, dim 64 or 128, block_tokens a multiple of 64.
+ *
+ * NIBBLE block layout.  For each KV head: block_tokens/64 tiles of 64 tokens.  A tile of width D (P = D/64 panels) is K codes
+ * (32 D bytes), K scales and zeros (256 P), V codes (32 D), V scales and zeros (256).  Nibble j of a 32-bit word is its bits
+ * 4j..4j+3.  K codes: token 16u+8h+g, column 64p+16t+8w+j is nibble j of word ((((u*P+p)*8+g)*4+t)*2+h)*2+w.  V codes: column
+ * 16d+8h+g, token 32w+8i+2t+e is nibble i+4e of word ((((d*8+g)*4+t)*2+h)*2+w.  Scale (low half) and zero (high half of a
+ * 32-bit word) of token 16u+8h+g: row 16u+2g+h, one word per panel for K, one word for V.
+ *
+ * Some consecutive tokens of one run of consecutive blocks. */
+typedef struct {
+  void* blocks_dev;      /* first block of the run, 16-byte aligned                                        */
+  int64_t first_token;   /* first token of the span, counted from the run's first                          */
+  int64_t n_tokens;
+} ipkv_span;
+
+/* Bytes of one NIBBLE block for a shape; -1 for a shape that the format does not have. */
+int64_t ipkv_nibble_block_bytes(const ipkv_attn_shape* shape);
+
+/* Write token-major K/V into NIBBLE blocks: the tokens of span 0, then those of span 1, and so on, from k_dev and v_dev
+ * [tokens][n_kv_heads][dim] bf16; k_token_stride, v_token_stride: elements between tokens (multiples of 8; 0: dense).
+ * One call serves prompts, chunks of prompts that begin or end inside a block, and a decode step (one token per span).  Tokens
+ * outside the spans keep their codes.  spans: host array, copied by the call (so the call can be captured into a CUDA
+ * graph).  No two spans of a call may touch the same block (IPKV_EINVAL), and calls that touch the same block must be
+ * ordered on the device: neighbouring tokens share bytes.  Works on the current device. */
+ipkv_status ipkv_nibble_pack(const ipkv_attn_shape* shape, int32_t n_spans, const ipkv_span* spans, const void* k_dev, const void* v_dev,
+                             int64_t k_token_stride, int64_t v_token_stride, void* stream);
+
+/* The inverse: the values that the codes of the spans' tokens stand for, rounded to bf16, into k_dev and v_dev (which no
+ * block may overlap).  Several spans may read the same block. */
+ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* shape, int32_t n_spans, const ipkv_span* spans, void* k_dev, void* v_dev,
+                               int64_t k_token_stride, int64_t v_token_stride, void* stream);
+
+/* Decode attention over runs of NIBBLE blocks: ipkv_attend_runs for this format.  n_rows queries, row r over the tokens of
+ * runs[row_run_start[r] .. row_run_start[r+1]) (a run: consecutive blocks and how many of their first tokens count; what
+ * the blocks hold behind them may be anything).  runs and row_run_start are host arrays, copied by the call; small tables travel
+ * with the launch, so that the call can be captured into a CUDA graph like ipkv_attend_runs.  q_dev [n_rows][n_q_heads][dim] bf16.
+ * Outputs fp32: o_part_dev [n_rows][n_q_heads][dim] normalised, lse_part_dev [n_rows][n_q_heads] natural log; a row without
+ * tokens gives (0, -inf).  They join partials over other tokens (a bf16 window, the CPU side) through ipkv_merge.
+ * scratch_dev: at least ipkv_nibble_scratch_bytes, 256-byte aligned, private to this call until its work on `stream` has
+ * completed (calls captured into graphs that may run at the same time need scratch of their own).  status_dev as in
+ * ipkv_attend_runs, may be NULL.  Results are bit-reproducible.  Works on the current device. */
+ipkv_status ipkv_nibble_scratch_bytes(const ipkv_attn_shape* shape, int32_t n_rows, int32_t n_runs, size_t* out_bytes);
+ipkv_status ipkv_nibble_attend(const ipkv_attn_shape* shape, int32_t n_rows, const ipkv_run* runs, const int32_t* row_run_start,
+                               const void* q_dev, void* scratch_dev, size_t scratch_bytes, float* o_part_dev, float* lse_part_dev,
+                               uint32_t* status_dev, void* stream);
 
 #ifdef __cplusplus
 }

@@ -28,6 +28,8 @@ EXPORTS = [
     "ipkv_policy_create", "ipkv_policy_destroy", "ipkv_policy_observe", "ipkv_policy_update", "ipkv_policy_prefill_share",
     "ipkv_block_bytes", "ipkv_status_str", "ipkv_last_error", "ipkv_version", "ipkv_probe_read_bandwidth",
     "ipkv_selftest_expire_wait", "ipkv_selftest_fail_next_launch", "ipkv_selftest_declare_bounds", "ipkv_probe_umma",
+    "ipkv_norm_rope", "ipkv_nibble_block_bytes", "ipkv_nibble_pack", "ipkv_nibble_unpack",
+    "ipkv_nibble_scratch_bytes", "ipkv_nibble_attend",
 ]
 
 
@@ -72,6 +74,20 @@ class AttnShape(C.Structure):
 
 class Run(C.Structure):
     _fields_ = [("blocks_dev", C.c_void_p), ("n_tokens", C.c_int64)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("rot_dim", C.c_int32), ("n_axes", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float),
+                ("theta", C.c_double), ("inv_freq", C.c_void_p), ("pair_axis", C.c_void_p)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("in_dev", C.c_void_p), ("out_dev", C.c_void_p), ("weight_dev", C.c_void_p), ("n_heads", C.c_int32),
+                ("in_token_stride", C.c_int64), ("in_head_stride", C.c_int64), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64)]
+
+
+class Span(C.Structure):
+    _fields_ = [("blocks_dev", C.c_void_p), ("first_token", C.c_int64), ("n_tokens", C.c_int64)]
 
 
 class Roofline(C.Structure):
@@ -127,6 +143,11 @@ def lib():
         "ipkv_attend_scratch_bytes": [C.POINTER(AttnShape), i32, i32, i64, i32, C.POINTER(C.c_size_t)],
         "ipkv_attend_runs": [C.POINTER(AttnShape), i32, C.POINTER(Run), C.POINTER(i32), vp, i32, vp, C.c_size_t, vp, vp, vp, vp],
         "ipkv_pack_blocks": [C.POINTER(AttnShape), i32, vp, vp, i64, vp, vp],
+        "ipkv_norm_rope": [C.POINTER(Rope), i64, C.POINTER(Heads), i32, vp, vp],
+        "ipkv_nibble_pack": [C.POINTER(AttnShape), i32, vp, vp, vp, i64, i64, vp],
+        "ipkv_nibble_unpack": [C.POINTER(AttnShape), i32, vp, vp, vp, i64, i64, vp],
+        "ipkv_nibble_scratch_bytes": [C.POINTER(AttnShape), i32, i32, C.POINTER(C.c_size_t)],
+        "ipkv_nibble_attend": [C.POINTER(AttnShape), i32, vp, vp, vp, vp, C.c_size_t, vp, vp, vp, vp],
         "ipkv_attend_runs_noalloc": [C.POINTER(AttnShape), i32, C.POINTER(Run), C.POINTER(i32), vp, i32, vp, vp, vp, vp],
     }
     L.ipkv_version.restype = C.c_char_p
@@ -137,6 +158,8 @@ def lib():
         f.restype = C.c_int
     L.ipkv_block_bytes.argtypes = [C.POINTER(AttnShape)]
     L.ipkv_block_bytes.restype = C.c_int64
+    L.ipkv_nibble_block_bytes.argtypes = [C.POINTER(AttnShape)]
+    L.ipkv_nibble_block_bytes.restype = C.c_int64
     L.ipkv_roofline_share.argtypes = [C.POINTER(Roofline), C.c_double]
     L.ipkv_roofline_share.restype = C.c_double
     L.ipkv_roofline_step_time.argtypes = [C.POINTER(Roofline), C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double), C.POINTER(C.c_double)]
@@ -516,3 +539,166 @@ def ipkv_pack_blocks(shape, layout, k, v, n_tokens, dst, stream=None):
     rc = lib().ipkv_pack_blocks(C.byref(shape), layout, _ptr(k), _ptr(v), n_tokens, _ptr(dst), _stream(stream))
     if rc != OK:
         raise IpkvError(rc, "ipkv_pack_blocks")
+
+
+# ---- head norm and rotation ---------------------------------------------------------------------------------------
+
+def _device_call(stream, *tensors):
+    """The stream of a stateless call, as a number: the given one, or the current device's current one.  The call runs on the
+    current device, so every tensor has to live there."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, the call runs on the current CUDA device ({dev})")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def make_rope(dim, rot_dim=None, *, theta=10000.0, sections=None, interleaved=False, eps=1e-6, inv_freq=None, pair_axis=None):
+    """What ipkv_norm_rope does to a head.  sections: how many pairs of columns follow each axis, in order (their sum is
+    rot_dim / 2); pair_axis: the axis of every pair instead, for other arrangements; neither: one axis."""
+    rot_dim = dim if rot_dim is None else rot_dim
+    pairs = rot_dim // 2
+    if pair_axis is None:
+        pair_axis = [a for a, n in enumerate(sections) for _ in range(n)] if sections is not None else None
+    elif sections is not None:
+        raise ValueError("sections and pair_axis exclude each other")
+    r = Rope(dim, rot_dim, 1, 1 if interleaved else 0, eps, theta, None, None)
+    if pair_axis is not None:
+        if len(pair_axis) != pairs:
+            raise ValueError(f"{len(pair_axis)} pairs have an axis, {pairs} are rotated")
+        r._axes = bytes(pair_axis)
+        r.n_axes = len(sections) if sections is not None else max(pair_axis, default=0) + 1
+        if r.n_axes > 1:
+            r.pair_axis = C.cast(C.c_char_p(r._axes), C.c_void_p)
+    if inv_freq is not None:
+        if len(inv_freq) != pairs:
+            raise ValueError(f"{len(inv_freq)} frequencies, {pairs} pairs are rotated")
+        r._freq = (C.c_double * max(1, pairs))(*[float(f) for f in inv_freq])
+        r.inv_freq = C.cast(r._freq, C.c_void_p)
+    return r
+
+
+def ipkv_norm_rope(rope, parts, positions, stream=None):
+    """parts: 1..4 tuples (x, weight or None, out or None): x and out [n_tokens, heads, dim] bf16 with any token and head
+    strides, out None means in place.  positions: int32 [n_axes, n_tokens] (or [n_tokens]), contiguous; None without a rotation."""
+    import torch
+    n = len(parts)
+    arr = (Heads * n)()
+    n_tokens, tensors = parts[0][0].shape[0], [positions]
+    for a, (x, w, out) in zip(arr, parts):
+        out = x if out is None else out
+        if x.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16 or (w is not None and w.dtype is not torch.bfloat16):
+            raise ValueError("heads and weights are bfloat16")
+        heads = x.shape
+        if len(heads) != 3 or heads != out.shape or heads[0] != n_tokens or heads[2] != rope.dim:
+            raise ValueError(f"heads are [n_tokens, n_heads, {rope.dim}], the output's like the input's: got {tuple(heads)} and {tuple(out.shape)}")
+        i, o = x.stride(), out.stride()
+        if i[2] != 1 or o[2] != 1 or (w is not None and (w.numel() != rope.dim or not w.is_contiguous())):
+            raise ValueError("the columns of a head and of a weight are contiguous")
+        a.in_dev, a.out_dev, a.weight_dev, a.n_heads = x.data_ptr(), out.data_ptr(), _ptr(w), heads[1]
+        t, h = n_tokens > 1, heads[1] > 1               # the stride of a dimension of one is never used
+        a.in_token_stride, a.in_head_stride, a.out_token_stride, a.out_head_stride = i[0] * t, i[1] * h, o[0] * t, o[1] * h
+        tensors += (x, w, out)
+    if positions is not None and (positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.numel() != rope.n_axes * n_tokens):
+        raise ValueError(f"positions are contiguous int32 [{rope.n_axes}, {n_tokens}]")
+    rc = lib().ipkv_norm_rope(C.byref(rope), n_tokens, arr, n, _ptr(positions), _device_call(stream, *tensors))
+    if rc != OK:
+        raise IpkvError(rc, "ipkv_norm_rope")
+
+
+# ---- a cache held in 4 bits -----------------------------------------------------------------------------------------
+
+def ipkv_nibble_block_bytes(shape):
+    """Bytes of one NIBBLE block (grouped-query shapes, dim 64 or 128, block_tokens a multiple of 64)."""
+    n = int(lib().ipkv_nibble_block_bytes(C.byref(shape)))
+    if n < 0:
+        raise IpkvError(1, "ipkv_nibble_block_bytes")
+    return n
+
+
+def _table(rows, width):
+    """A host table of 64-bit words, [n][width]: a NumPy int64 array as it is, or rows whose first entry may be a tensor."""
+    import numpy as np
+    if not isinstance(rows, np.ndarray):
+        rows = np.array([[_ptr(r[0]) or 0, *r[1:]] for r in rows], dtype=np.int64).reshape(-1, width)
+    if rows.dtype != np.int64 or rows.ndim != 2 or rows.shape[1] != width or not rows.flags.c_contiguous:
+        raise ValueError(f"expected a contiguous int64 array [n][{width}]: got {rows.dtype} {rows.shape}")
+    return rows
+
+
+def _token_rows(x, shape, what):
+    """Elements between the tokens of K or V [tokens][n_kv_heads][dim]; the heads of a token lie side by side."""
+    import torch
+    d = x.shape
+    if x.dtype is not torch.bfloat16 or len(d) != 3 or d[1] != shape.n_kv_heads or d[2] != shape.dim_qk:
+        raise ValueError(f"{what} is bfloat16 [tokens, {shape.n_kv_heads}, {shape.dim_qk}]: got {x.dtype} {tuple(d)}")
+    st = x.stride()
+    if st[2] != 1 or (d[1] > 1 and st[1] != d[2]):
+        raise ValueError(f"the heads of a token of {what} lie side by side")
+    return st[0] if d[0] > 1 else 0
+
+
+def _move(name, shape, spans, k, v, stream):
+    t = _table(spans, 3)
+    ks, vs = _token_rows(k, shape, "K"), _token_rows(v, shape, "V")
+    n = int(t[:, 2].sum())
+    if k.shape[0] != n or v.shape[0] != n:
+        raise ValueError(f"the spans hold {n} tokens, K and V {k.shape[0]} and {v.shape[0]}")
+    if n > 1 and (ks == 0 or vs == 0):
+        raise ValueError("the tokens of K and V lie apart")
+    rc = getattr(lib(), name)(C.byref(shape), t.shape[0], t.__array_interface__["data"][0], k.data_ptr(), v.data_ptr(), ks, vs,
+                              _device_call(stream, k, v))
+    if rc != OK:
+        raise IpkvError(rc, name)
+
+
+def ipkv_nibble_pack(shape, spans, k, v, stream=None):
+    """Write the tokens of k and v [tokens][n_kv_heads][dim] into NIBBLE blocks: spans is a list of (blocks, first token, tokens),
+    or an int64 array [n][3] of addresses and counts; the tokens of one span follow those of the one before."""
+    _move("ipkv_nibble_pack", shape, spans, k, v, stream)
+
+
+def ipkv_nibble_unpack(shape, spans, k, v, stream=None):
+    """The inverse of ipkv_nibble_pack: the values that the spans' codes stand for, into k and v."""
+    _move("ipkv_nibble_unpack", shape, spans, k, v, stream)
+
+
+def ipkv_nibble_scratch_bytes(shape, n_rows, n_runs):
+    out = C.c_size_t()
+    rc = lib().ipkv_nibble_scratch_bytes(C.byref(shape), n_rows, n_runs, C.byref(out))
+    if rc != OK:
+        raise IpkvError(rc, "ipkv_nibble_scratch_bytes")
+    return out.value
+
+
+def ipkv_nibble_attend(shape, runs, row_start, q, scratch, o_part, lse_part, status=None, stream=None):
+    """Attention of one query per row over runs of NIBBLE blocks.  runs: int64 array [n][2] of (address, tokens) with row_start,
+    an int32 array [rows + 1]; or, with row_start None, one list per row of (blocks, tokens) as for ipkv_attend_runs."""
+    import numpy as np
+    import torch
+    if row_start is None:
+        row_start = np.cumsum([0] + [len(r) for r in runs]).astype(np.int32)
+        runs = _table([x for r in runs for x in r], 2)
+    else:
+        runs = _table(runs, 2)
+        if not isinstance(row_start, np.ndarray) or row_start.dtype != np.int32 or not row_start.flags.c_contiguous or row_start.ndim != 1:
+            raise ValueError("row_start is a contiguous int32 array [rows + 1]")
+    rows = row_start.shape[0] - 1
+    if rows < 1 or row_start[-1] > runs.shape[0]:
+        raise ValueError(f"row_start names runs up to {row_start[-1] if rows >= 0 else None}: there are {runs.shape[0]}")
+    want = (rows, shape.n_q_heads, shape.dim_qk)
+    if q.dtype is not torch.bfloat16 or q.shape != want or not q.is_contiguous():
+        raise ValueError(f"q is contiguous bfloat16 {want}: got {q.dtype} {tuple(q.shape)}")
+    if o_part.dtype is not torch.float32 or o_part.shape != want or not o_part.is_contiguous():
+        raise ValueError(f"o_part is contiguous float32 {want}: got {o_part.dtype} {tuple(o_part.shape)}")
+    if lse_part.dtype is not torch.float32 or lse_part.shape != want[:2] or not lse_part.is_contiguous():
+        raise ValueError(f"lse_part is contiguous float32 {want[:2]}: got {lse_part.dtype} {tuple(lse_part.shape)}")
+    s = _device_call(stream, q, scratch, o_part, lse_part, status)
+    rc = lib().ipkv_nibble_attend(C.byref(shape), rows, runs.__array_interface__["data"][0], row_start.__array_interface__["data"][0], q.data_ptr(),
+                                  scratch.data_ptr(), scratch.numel() * scratch.element_size(), o_part.data_ptr(), lse_part.data_ptr(),
+                                  _ptr(status), s)
+    if rc != OK:
+        raise IpkvError(rc, "ipkv_nibble_attend")

@@ -1,0 +1,570 @@
+// Decode attention over a cache held in 4 bits (format: nibble.cuh): one query per row, partial output and log-sum-exp.
+//
+// With key = sk * code + zk per 64-column panel and value = sv * code + zv per token,
+//   q . key = sum over panels of sk (q . codes) + zk sum(q),      O = sum_t (p_t sv_t) codes_t + sum_t p_t zv_t,
+// so the tensor cores multiply the bare codes and the scales are applied to scores and weights, one value per token instead
+// of one per element.  Codes become fp16 operands as they lie in the word, by a mask (nibble.cuh): below 2^11 the bits of an fp16
+// number are the number times 2^24, so a code that a mask leaves in place is the code times a power of two, exactly, and the
+// powers of two go into the other operand.
+//
+// Tokens are the rows (M = 16) of the score product and columns of the head the rows of the output product; 8 query heads
+// are the columns (N = 8): no row of a product is wasted on a missing head, and codes are never the operand that would have
+// to be moved between lanes.  Scores come out as [token][head]; movmatrix turns the weights, two 16-bit rows at a time,
+// into the [token][head] operand of the second product.
+//
+// Exactness.  q (bf16) times a power of two per head is exact in fp16; products are exact and sums are fp32.  A weight p sv is
+// held as two fp16 numbers, head and remainder (22 bits): with at most 4 query heads per KV head they share one product (columns
+// 0-3 and 4-7), otherwise there are two.  sv is brought near 1 by a power of two per warp (the largest scale so far), so that
+// fp16's range is spent on p: weights down to 2^-31 of the largest keep their share.
+// The tensor cores add with two bits more than fp32 has and round towards zero, both counted from the largest exponent that
+// an operand's FORMAT shows (a subnormal counts as 2^-14).  Two things follow for V, whose sums are long.  The codes are shifted up
+// so that they fill fp16's subnormal range (bits 3..6 and 7..10).  And sums must not be much larger than the result:
+// codes are never negative, but an output is a mean of many values of either sign, so a sum of p sv code would exceed it by
+// 2.5 sqrt(tokens); every other eight tokens enter complemented, code = 15 - (15 - code): the complement costs nothing in the
+// mask, its weight is negative, 15 sv joins zv, and the excesses of the two halves meet in the same product.  Without
+// the two the output of 32K tokens was off by 5e-4 of itself.  Score accumulators start at -7.5 sum(q) for the same reason.
+//
+// One warp works on one tile (64 tokens of a KV head) at a time, alone: its online softmax has its own reference maximum, raised
+// only when a score exceeds it by 2^8 (then everything is rescaled), which costs one vote per tile in place of a reduction over lanes.  A
+// producer warp streams tiles (one bulk copy each, they are contiguous) into a ring of stages on mbarriers; the warps of a CTA
+// take them in turn.  At the end of a (row, head group) the warps' states are joined through shared memory, in a fixed order.
+// More than 8 query heads per KV head: several warps (one per octet of heads) share a tile, so it is still read once.
+// Every wait is bounded; a warp whose wait ran out does no more work but still comes to the barriers, so nobody waits for it.
+#include <cuda_fp16.h>
+
+#include "kernels.h"
+#include "launch.cuh"
+#include "ops.h"
+#include "ptx.cuh"
+
+namespace ipkvi {
+
+namespace {
+
+constexpr int kWarps = kNibbleWarps;
+constexpr int kThreads = (kWarps + 1) * 32;
+constexpr int kMaxStages = 32;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kRaise = 8.f;                    // the reference maximum is raised when a score exceeds it by this (log2)
+constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;         // K codes: times 2^-24 and 2^-20
+constexpr uint32_t kLowV = 0x00780078u, kHighV = 0x07800780u;       // V codes, shifted: times 2^-21 and 2^-17
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
+
+struct Smem {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    int32_t n_valid[kMaxStages];
+    float m[kWarps][8], l[kWarps][8];
+};
+
+// A chunk's walk over (row, head group) pairs: which pair unit u belongs to, and how many of the chunk's tiles follow in it.
+struct Pair {
+    int row, gh, tile0, n, slot;
+};
+__device__ __forceinline__ Pair pair_at(const NibbleAttend& p, const NibbleRowArg* rows, int u, int u1) {
+    int lo = 0, hi = p.n_rows - 1;
+    while (lo < hi) {                            // the last row that begins at or before u (rows without tiles lie in front of it)
+        const int mid = (lo + hi + 1) >> 1;
+        if (rows[mid].unit0 <= u) lo = mid; else hi = mid - 1;
+    }
+    const NibbleRowArg r = rows[lo];
+    Pair x;
+    x.row = lo;
+    x.gh = (u - r.unit0) / r.tiles;
+    x.tile0 = (u - r.unit0) - x.gh * r.tiles;
+    x.n = min(r.tiles - x.tile0, u1 - u);
+    x.slot = int(blockIdx.x) + r.pair0 + x.gh;
+    return x;
+}
+
+template <int D, bool HALF>                      // HALF: at most 4 query heads per KV head
+__global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kernel(const __grid_constant__ NibbleAttend p) {
+    constexpr int P = D / 64;
+    constexpr int kTile = 64 * D + 256 * (P + 1), kKMeta = 32 * D, kV = kKMeta + 256 * P, kVMeta = kV + 32 * D;
+    constexpr int kPitch = D + 4;                // floats of a head's row in the joining buffer: heads 0, 2, 4, 6 on distinct banks
+    extern __shared__ unsigned char smem_dyn[];
+    unsigned char* ring = smem_dyn + ((128u - (ptx::smem_addr(smem_dyn) & 127u)) & 127u);
+    Smem& sm = *reinterpret_cast<Smem*>(ring + p.stages * kTile);
+    float* joined = reinterpret_cast<float*>(ring + p.stages * kTile + sizeof(Smem));
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int stages = p.stages, octets = p.octets, teams = kWarps / octets;
+    if (tid == 0) {
+        for (int s = 0; s < stages; ++s) {
+            ptx::mbar_init(ptx::smem_addr(&sm.full[s]), 1);
+            ptx::mbar_init(ptx::smem_addr(&sm.empty[s]), octets);
+        }
+        ptx::mbar_fence_init();
+    }
+    __syncthreads();
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+
+    const NibbleRowArg* rows = p.rows ? p.rows : p.row;
+    const NibbleRunArg* runs = p.runs ? p.runs : p.run;
+    const int u0 = int(int64_t(p.n_units) * blockIdx.x / p.n_ctas), u1 = int(int64_t(p.n_units) * (blockIdx.x + 1) / p.n_ctas);
+
+    if (warp == kWarps) {
+        // ---------------- producer ----------------
+        if (lane != 0) return;
+        const uint64_t pol = ptx::l2_evict_first_policy();
+        int st = 0, lap = 0;
+        bool ok = true;
+        for (int u = u0; u < u1 && ok;) {
+            const Pair x = pair_at(p, rows, u, u1);
+            const int kv = x.gh / p.groups_per_kv;
+            int k = rows[x.row].run0;
+            // the run of the first tile, then run after run
+            {
+                int lo = k, hi = k;
+                for (int step = 1; ; step <<= 1) {       // the row's runs end where the next row's begin, or where their tiles do
+                    const int64_t last = int64_t(k) + step;
+                    const int end = x.row + 1 < p.n_rows ? rows[x.row + 1].run0 : p.n_runs;
+                    hi = last < end ? int(last) : end - 1;
+                    if (hi == end - 1 || runs[hi].tile0 > x.tile0) break;
+                    lo = hi;
+                }
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (runs[mid].tile0 <= x.tile0) lo = mid; else hi = mid - 1;
+                }
+                k = lo;
+            }
+            // the address moves from tile to tile by additions: a division per tile would make this one thread the bottleneck
+            const int per = p.g.bt / kTileTokens;
+            const int64_t to_next_block = p.g.block_bytes() - int64_t(per - 1) * kTile;
+            NibbleRunArg run = runs[k];
+            int tile = x.tile0 - run.tile0, left = run.n_tokens - tile * kTileTokens, in_block = tile % per;
+            const char* src = run.blocks + p.g.tile_off(tile, kv);
+            for (int i = 0; i < x.n; ++i) {
+                if (left <= 0) {
+                    run = runs[++k];
+                    left = run.n_tokens; in_block = 0;
+                    src = run.blocks + p.g.tile_off(0, kv);
+                }
+                if (lap > 0 && !ptx::mbar_wait(ptx::smem_addr(&sm.empty[st]), (lap - 1) & 1)) { ok = false; break; }
+                sm.n_valid[st] = left < kTileTokens ? left : kTileTokens;
+                const uint32_t bar = ptx::smem_addr(&sm.full[st]);
+                ptx::mbar_expect_tx(bar, kTile);
+                const int64_t extent = kChecked && p.status ? (int64_t(run.n_tokens) + p.g.bt - 1) / p.g.bt * p.g.block_bytes() : 0;
+                ptx::bulk_g2s_hint(ptx::smem_addr(ring + st * kTile), ptx::checked_src<kChecked>(src, kTile, run.blocks, extent, p.status, kStatusBadIndex),
+                                   kTile, bar, pol);
+                left -= kTileTokens;
+                if (++in_block == per) { in_block = 0; src += to_next_block; } else src += kTile;
+                if (++st == stages) { st = 0; ++lap; }
+            }
+            u += x.n;
+        }
+        if (!ok && p.status) atomicOr(p.status, kStatusNoFreeStage);
+        // do not leave the CTA while copies of ours may still be in flight
+        for (int i = 0; i < stages; ++i) {
+            const int last = i < st ? lap : lap - 1;         // the stage's last lap
+            if (last >= 0 && !ptx::mbar_wait(ptx::smem_addr(&sm.full[i]), last & 1) && p.status) atomicOr(p.status, kStatusCopyNotLanded);
+        }
+        return;
+    }
+
+    // ---------------- consumers ----------------
+    const int g = lane >> 2, t = lane & 3;
+    const int team = warp / octets, octet = warp - team * octets;
+    const bool works = team < teams;
+    bool dead = false;
+    auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory"); };
+
+    int it0 = 0;                                 // tiles of this CTA before the current pair
+    int st = team, phase = 0;                    // stage of the team's next tile and its parity (teams <= stages)
+    for (int u = u0; u < u1;) {
+        const Pair x = pair_at(p, rows, u, u1);
+        const int in_kv = (x.gh % p.groups_per_kv) * p.rows_per_part;      // the head group's first head among those of its KV head
+        const int n_heads = min(p.group - in_kv, p.rows_per_part), head0 = (x.gh / p.groups_per_kv) * p.group + in_kv;
+
+        // ---- queries: operands of head g (columns 64p+16t+8w+{0,4},{1,5},{2,6},{3,7}), normalised to [2^14, 2^15) ----
+        uint32_t qf[P][2][4];
+        float qs[P][2], c[2];                    // per panel 2^-24 sum(q), and log2 units per score, of heads 2t and 2t+1
+        {
+            const int hq = octet * 8 + (HALF ? (g & 3) : g);
+            const bool live = works && hq < n_heads;
+            const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t(x.row) * p.n_q_heads + head0 + hq) * (2 * D) + 32 * t);
+            float v[P][16], top = 0.f;
+#pragma unroll
+            for (int pn = 0; pn < P; ++pn)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const uint4 y = live ? __ldg(src + pn * 8 + w) : make_uint4(0, 0, 0, 0);
+                    const uint32_t yy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { v[pn][8 * w + 2 * i] = ptx::bf16_lo(yy[i]); v[pn][8 * w + 2 * i + 1] = ptx::bf16_hi(yy[i]); }
+                }
+#pragma unroll
+            for (int pn = 0; pn < P; ++pn)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(v[pn][i]));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = min(max(int(__float_as_uint(top) >> 23), 15), 230);
+            const float f = __uint_as_float(uint32_t(268 - e) << 23);                    // 2^14 / 2^(exponent of the largest)
+            const float cg = p.scale * kLog2e * __uint_as_float(uint32_t(10 + e) << 23); // ... undone, with the codes' 2^24
+            float sum[P];
+#pragma unroll
+            for (int pn = 0; pn < P; ++pn) {
+                sum[pn] = 0.f;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    float* y = &v[pn][8 * w];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { y[i] *= f; sum[pn] += y[i]; }
+                    qf[pn][w][0] = pack_f16(y[0], y[4]);
+                    qf[pn][w][1] = pack_f16(y[1] * 0.0625f, y[5] * 0.0625f);
+                    qf[pn][w][2] = pack_f16(y[2], y[6]);
+                    qf[pn][w][3] = pack_f16(y[3] * 0.0625f, y[7] * 0.0625f);
+                }
+                sum[pn] += __shfl_xor_sync(0xffffffffu, sum[pn], 1);
+                sum[pn] += __shfl_xor_sync(0xffffffffu, sum[pn], 2);
+                sum[pn] *= 0x1p-24f;
+                qs[pn][0] = __shfl_sync(0xffffffffu, sum[pn], 8 * t);                    // lane 4 (2t): head 2t
+                qs[pn][1] = __shfl_sync(0xffffffffu, sum[pn], 8 * t + 4);
+            }
+            c[0] = __shfl_sync(0xffffffffu, cg, 8 * t);
+            c[1] = __shfl_sync(0xffffffffu, cg, 8 * t + 4);
+        }
+
+        // ---- the warp's state over its tiles of this pair ----
+        float o[D / 16][4];                      // [column g / g+8 of 16][head 2t / 2t+1], times 64 fv / 2^21
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][i] = 0.f;
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, oz[2] = {0.f, 0.f};      // l and oz: this lane's tokens only
+        float limit[2] = {-INFINITY, -INFINITY};                                          // scores above it raise m
+        float v_limit = -1.f, fv = 0.f;          // value scales from v_limit on raise the power of two behind fv
+
+        // the tiles of team `team`: it = team modulo teams
+        const int it_end = it0 + x.n;
+        int first = it0 / teams * teams + team;
+        if (first < it0) first += teams;
+        for (int it = works ? first : it_end; it < it_end; it += teams) {
+            if (!dead && !ptx::mbar_wait(ptx::smem_addr(&sm.full[st]), phase)) {
+                if (lane == 0 && p.status) atomicOr(p.status, kStatusNoTile);
+                dead = true;
+            }
+            dead = __any_sync(0xffffffffu, dead);
+            if (dead) break;
+            const unsigned char* tile = ring + st * kTile;
+            const int nv = sm.n_valid[st];
+
+            // scores of tokens 16u+g (0, 1) and 16u+8+g (2, 3) for heads 2t and 2t+1
+            float s[4][4];
+            float sv[4][2], zv[4][2];
+#pragma unroll
+            for (int un = 0; un < 4; ++un) {
+                float acc[P][4];
+#pragma unroll
+                for (int pn = 0; pn < P; ++pn) {
+                    acc[pn][0] = acc[pn][2] = -7.5f * qs[pn][0]; acc[pn][1] = acc[pn][3] = -7.5f * qs[pn][1];
+                    const uint4 y = *reinterpret_cast<const uint4*>(tile + ((un * P + pn) * 32 + lane) * 16);
+                    const uint32_t ya[2] = {y.x, y.y}, yb[2] = {y.z, y.w};
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        mma_f16(acc[pn], ya[w] & kLow, yb[w] & kLow, ya[w] & kHigh, yb[w] & kHigh, qf[pn][w][0], qf[pn][w][1]);
+                        const uint32_t a8 = ya[w] >> 8, b8 = yb[w] >> 8;
+                        mma_f16(acc[pn], a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, qf[pn][w][2], qf[pn][w][3]);
+                    }
+                }
+                uint32_t km[2][P];
+                if (P == 2) {
+                    const uint4 y = *reinterpret_cast<const uint4*>(tile + kKMeta + (un * 8 + g) * 16);
+                    km[0][0] = y.x; km[0][P - 1] = y.y; km[1][0] = y.z; km[1][P - 1] = y.w;
+                } else {
+                    const uint2 y = *reinterpret_cast<const uint2*>(tile + kKMeta + (un * 8 + g) * 8);
+                    km[0][0] = y.x; km[1][0] = y.y;
+                }
+                const uint2 vm = *reinterpret_cast<const uint2*>(tile + kVMeta + (un * 8 + g) * 8);
+                const uint32_t vmm[2] = {vm.x, vm.y};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float y = 0.f;
+#pragma unroll
+                        for (int pn = 0; pn < P; ++pn) {
+                            y = fmaf(ptx::bf16_lo(km[h][pn]), acc[pn][2 * h + e], y);
+                            y = fmaf(fmaf(ptx::bf16_lo(km[h][pn]), 7.5f, ptx::bf16_hi(km[h][pn])), qs[pn][e], y);
+                        }
+                        s[un][2 * h + e] = y;
+                    }
+                    sv[un][h] = ptx::bf16_lo(vmm[h]);
+                    zv[un][h] = h ? fmaf(ptx::bf16_lo(vmm[h]), 15.f, ptx::bf16_hi(vmm[h])) : ptx::bf16_hi(vmm[h]);
+                }
+            }
+            if (nv < kTileTokens) {              // what lies behind the last token may be anything, NaN too
+#pragma unroll
+                for (int un = 0; un < 4; ++un)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (un * 16 + h * 8 + g >= nv) { s[un][2 * h] = s[un][2 * h + 1] = -INFINITY; sv[un][h] = zv[un][h] = 0.f; }
+            }
+
+            // raise the references where a score or a scale has outgrown them (the first tile always does)
+            float top[2] = {s[0][0], s[0][1]}, v_top = fmaxf(sv[0][0], sv[0][1]);
+#pragma unroll
+            for (int un = 0; un < 4; ++un) {
+                top[0] = fmaxf(top[0], fmaxf(s[un][0], s[un][2]));
+                top[1] = fmaxf(top[1], fmaxf(s[un][1], s[un][3]));
+                v_top = fmaxf(v_top, fmaxf(sv[un][0], sv[un][1]));
+            }
+            if (__any_sync(0xffffffffu, top[0] > limit[0] || top[1] > limit[1] || v_top >= v_limit)) {
+                float alpha[2];
+#pragma unroll
+                for (int d = 4; d <= 16; d <<= 1) {
+                    top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
+                    top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], d));
+                    v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, d));
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float m_new = fmaxf(m[e], top[e] * c[e]);
+                    alpha[e] = m[e] == -INFINITY ? 0.f : ptx::ex2(m[e] - m_new);
+                    m[e] = m_new;
+                    limit[e] = (m_new + kRaise) / c[e];
+                    l[e] *= alpha[e]; oz[e] *= alpha[e];
+                }
+                if (v_top >= v_limit) {
+                    const int e = min(max(int(__float_as_uint(v_top) >> 23), 8), 250);
+                    const float f_new = __uint_as_float(uint32_t(254 - e) << 23);        // scales times f_new lie below 2
+                    const float r = fv == 0.f ? 0.f : f_new / fv;
+                    alpha[0] *= r; alpha[1] *= r;
+                    fv = f_new;
+                    v_limit = __uint_as_float(uint32_t(e + 1) << 23);
+                }
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) {
+                    o[d][0] *= alpha[0]; o[d][1] *= alpha[1]; o[d][2] *= alpha[0]; o[d][3] *= alpha[1];
+                }
+            }
+
+            // weights, and their products with the value scales as operands [token][head]
+            uint32_t hi[4][2], lo[4][2];
+            const float f0 = fv * 64.f, f1 = fv * -4.f;                  // tokens 8-15 of a unit meet complements, times 2^4
+#pragma unroll
+            for (int un = 0; un < 4; ++un)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float w[2];
+                    const float svf = sv[un][h] * (h ? f1 : f0);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float pr = ptx::ex2(fmaf(s[un][2 * h + e], c[e], -m[e]));
+                        l[e] += pr;
+                        oz[e] = fmaf(pr, zv[un][h], oz[e]);
+                        w[e] = pr * svf;
+                    }
+                    const uint32_t big = pack_f16(w[0], w[1]);
+                    const float2 back = unpack_f16(big);
+                    const uint32_t rest = pack_f16(w[0] - back.x, w[1] - back.y);
+                    if (HALF) hi[un][h] = transpose8x8(t < 2 ? big : rest);              // columns 4-7 repeat heads 0-3
+                    else { hi[un][h] = transpose8x8(big); lo[un][h] = transpose8x8(rest); }
+                }
+
+            // output: 16 columns of the head a time, the tile's 64 tokens
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+                const uint4 y = *reinterpret_cast<const uint4*>(tile + kV + (d * 32 + lane) * 16);
+                const uint32_t ya[2] = {y.x, y.y}, yb[2] = {y.z, y.w};
+#pragma unroll
+                for (int un = 0; un < 4; ++un) {
+                    const uint32_t va = (un & 1) ? ya[un >> 1] >> 5 : ya[un >> 1] << 3, vb = (un & 1) ? yb[un >> 1] >> 5 : yb[un >> 1] << 3;
+                    const uint32_t a0 = va & kLowV, a1 = vb & kLowV, a2 = ~va & kHighV, a3 = ~vb & kHighV;
+                    mma_f16(o[d], a0, a1, a2, a3, hi[un][0], hi[un][1]);
+                    if (!HALF) mma_f16(o[d], a0, a1, a2, a3, lo[un][0], lo[un][1]);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[st]));
+            st += teams;
+            if (st >= stages) { st -= stages; phase ^= 1; }
+        }
+
+        // ---- join the teams' states into the pair's partial ----
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int d = 4; d <= 16; d <<= 1) {
+                l[e] += __shfl_xor_sync(0xffffffffu, l[e], d);
+                oz[e] += __shfl_xor_sync(0xffffffffu, oz[e], d);
+            }
+        if (HALF) {
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[d][i] += __shfl_xor_sync(0xffffffffu, o[d][i], 2);
+        }
+        const float undo = fv > 0.f ? 0x1p15f : 0.f, inv_fv = fv > 0.f ? 1.f / fv : 0.f;   // 2^21 / 64, then 1 / fv
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][i] = fmaf(o[d][i] * undo, inv_fv, oz[i & 1]);
+
+        const int n_act = min(x.n, teams);       // teams with tiles of this pair, from team it0 % teams on
+        int turn_of = team - it0 % teams;
+        if (turn_of < 0) turn_of += teams;
+        const bool active = works && turn_of < n_act;
+        float big_m[2] = {m[0], m[1]}, sum_l[2] = {l[0], l[1]};
+        if (n_act > 1) {
+            if (g == 0) { sm.m[warp][2 * t] = m[0]; sm.m[warp][2 * t + 1] = m[1]; sm.l[warp][2 * t] = l[0]; sm.l[warp][2 * t + 1] = l[1]; }
+            sync();
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float mm = -INFINITY, ll = 0.f;
+                for (int k = 0; k < n_act; ++k) mm = fmaxf(mm, sm.m[(it0 + k) % teams * octets + octet][2 * t + e]);
+                for (int k = 0; k < n_act; ++k) {
+                    const int wk = (it0 + k) % teams * octets + octet;
+                    const float mk = sm.m[wk][2 * t + e];
+                    if (mk != -INFINITY) ll += ptx::ex2(mk - mm) * sm.l[wk][2 * t + e];
+                }
+                big_m[e] = mm; sum_l[e] = ll;
+            }
+        }
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) f[e] = (m[e] != -INFINITY && sum_l[e] > 0.f) ? ptx::ex2(m[e] - big_m[e]) / sum_l[e] : 0.f;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][i] *= f[i & 1];
+        float* buf = joined + (octet * 8 + 2 * t) * kPitch + g;
+        const int hb = octet * 8 + 2 * t;        // of the head group
+        const bool writes = (!HALF || t < 2);
+        for (int turn = 0; turn < n_act; ++turn) {
+            if (active && turn == turn_of) {
+                if (turn > 0) {
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) {
+                        o[d][0] += buf[16 * d]; o[d][1] += buf[16 * d + kPitch];
+                        o[d][2] += buf[16 * d + 8]; o[d][3] += buf[16 * d + 8 + kPitch];
+                    }
+                }
+                if (turn + 1 < n_act) {
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) {
+                        buf[16 * d] = o[d][0]; buf[16 * d + kPitch] = o[d][1];
+                        buf[16 * d + 8] = o[d][2]; buf[16 * d + 8 + kPitch] = o[d][3];
+                    }
+                } else if (writes) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (hb + e >= n_heads) continue;
+                        const int64_t row = int64_t(x.slot) * p.rows_per_part + hb + e;
+                        if (kChecked && (row < 0 || row >= p.part_rows)) {       // the partial must lie inside the scratch
+                            if (p.status) atomicOr(p.status, kStatusBadIndex);
+                            continue;
+                        }
+                        float* dst = p.part_o + row * D + g;
+#pragma unroll
+                        for (int d = 0; d < D / 16; ++d) { dst[16 * d] = o[d][e]; dst[16 * d + 8] = o[d][2 + e]; }
+                        if (g == 0) p.part_ml[row] = make_float2(big_m[e], sum_l[e]);
+                    }
+                }
+            }
+            if (turn + 1 < n_act) sync();
+        }
+        it0 = it_end;
+        u += x.n;
+    }
+}
+
+// Joins the partials of every (row, query head): LSE = m + ln sum exp(LSE_i - m), O = sum exp(LSE_i - LSE) O_i, in a fixed order.
+// One CTA per (row, head): D/4 column groups times 512/D slices of the partials.
+template <int D>
+__global__ void __launch_bounds__(128) nibble_reduce_kernel(const __grid_constant__ NibbleAttend p) {
+    constexpr int kCols = D / 4, kSlices = 128 / kCols;
+    __shared__ float4 s_o[kSlices][kCols];
+    __shared__ float s_z[kSlices], s_m[4];
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+    const int row = blockIdx.x / p.n_q_heads, head = blockIdx.x - row * p.n_q_heads;
+    const NibbleRowArg r = (p.rows ? p.rows : p.row)[row];
+    const int tid = threadIdx.x, col = tid % kCols, slice = tid / kCols;
+    float4* out = reinterpret_cast<float4*>(p.out_o + int64_t(blockIdx.x) * D) + col;
+    if (r.tiles == 0) {                          // nothing attended: (0, -inf)
+        if (slice == 0) *out = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (tid == 0) p.out_lse[blockIdx.x] = -INFINITY;
+        return;
+    }
+    const int in_kv = head % p.group;
+    const int gh = head / p.group * p.groups_per_kv + in_kv / p.rows_per_part, rin = in_kv % p.rows_per_part;
+    const int64_t a = int64_t(r.unit0) + int64_t(gh) * r.tiles, b = a + r.tiles - 1;
+    const int j = r.pair0 + gh;
+    const int e0 = int(((a + 1) * p.n_ctas - 1) / p.n_units) + j, e1 = int(((b + 1) * p.n_ctas - 1) / p.n_units) + j;   // first, last partial
+    const int n = e1 - e0 + 1;
+    const float2* ml = p.part_ml + int64_t(e0) * p.rows_per_part + rin;
+    const float4* part = reinterpret_cast<const float4*>(p.part_o + (int64_t(e0) * p.rows_per_part + rin) * D) + col;
+    const int64_t stride = int64_t(p.rows_per_part) * kCols;
+
+    float m = -INFINITY;
+    for (int i = tid; i < n; i += 128) m = fmaxf(m, ml[int64_t(i) * p.rows_per_part].x);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    if ((tid & 31) == 0) s_m[tid >> 5] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float z = 0.f;
+#pragma unroll 4
+    for (int i = slice; i < n; i += kSlices) {
+        const float2 x = ml[int64_t(i) * p.rows_per_part];
+        const float4 v = part[int64_t(i) * stride];
+        const float w = x.x == -INFINITY ? 0.f : ptx::ex2(x.x - m) * x.y;
+        acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+        z += w;
+    }
+    s_o[slice][col] = acc;
+    if (col == 0) s_z[slice] = z;
+    __syncthreads();
+    if (slice != 0) return;
+    for (int k = 1; k < kSlices; ++k) {
+        const float4 v = s_o[k][col];
+        acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        z += s_z[k];
+    }
+    const float inv = z > 0.f ? 1.f / z : 0.f;
+    *out = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    if (col == 0) p.out_lse[blockIdx.x] = z > 0.f ? m * kLn2 + logf(z) : -INFINITY;
+}
+
+}  // namespace
+
+cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s) {
+    const bool wide = a.g.dim == 128, half = a.group <= 4;
+    if (a.n_units > 0) {
+        const int tile = a.g.tile_bytes(), teams = kWarps / a.octets;
+        const int joined = teams > 1 ? a.octets * 8 * (a.g.dim + 4) * int(sizeof(float)) : 0;
+        const int fixed = int(sizeof(Smem)) + joined + 128;
+        constexpr int kSmemPerCta = 228 * 1024 / kNibbleCtasPerSm - 1024;
+        const int room = kSmemPerCta - fixed;
+        a.stages = room / tile < kMaxStages ? room / tile : kMaxStages;
+        const size_t smem = size_t(a.stages) * tile + fixed;
+        auto kernel = wide ? (half ? nibble_attend_kernel<128, true> : nibble_attend_kernel<128, false>)
+                           : (half ? nibble_attend_kernel<64, true> : nibble_attend_kernel<64, false>);
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerCta);
+        if (e != cudaSuccess) return e;
+        e = launch_ordered(!a.plain_launch, kernel, a.n_ctas, kThreads, smem, s, a);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_ordered(a.n_units > 0, wide ? nibble_reduce_kernel<128> : nibble_reduce_kernel<64>, a.n_rows * a.n_q_heads, 128, size_t(0), s, a);
+}
+
+}  // namespace ipkvi

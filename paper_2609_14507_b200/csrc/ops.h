@@ -1,0 +1,103 @@
+// Launch interface of the operators beside the cache (ops_api.cu checks the arguments and fills these): head norm with
+// rotation, and the cache held in 4 bits.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "nibble.cuh"
+
+namespace ipkvi {
+
+// ---- head norm and rotation (norm_rope.cu) ------------------------------------------------------------------------
+constexpr int kRopeMaxParts = 4;
+constexpr int kRopeMaxPairs = 128;
+struct RopePart {
+    const char* in;
+    char* out;
+    const char* weight;                          // [dim] bf16, null: no norm
+    int64_t in_token, in_head, out_token, out_head;   // strides in bytes
+    int32_t n_heads;
+    int32_t step0;                               // steps (groups of heads that one warp takes at once) of the parts before this one
+};
+struct RopeLaunch {
+    uint64_t turn[kRopeMaxPairs];                // frequency of a pair as a fraction of a turn per position, times 2^64
+    uint8_t axis[kRopeMaxPairs];
+    RopePart part[kRopeMaxParts];
+    const int32_t* positions;                    // [n_axes][n_tokens]
+    int64_t n_tokens;
+    int32_t n_parts, n_steps, split, dim, rot_dim, n_axes, interleaved;
+    float eps;
+};
+// heads that one warp takes in one step, for a head width
+inline int rope_heads_per_step(int dim) { return 512 / dim; }
+cudaError_t launch_norm_rope(RopeLaunch& a, cudaStream_t s);
+
+// ---- the cache in 4 bits: writing and reading back (nibble_pack.cu) --------------------------------------------------
+constexpr int kNibbleSpansPerLaunch = 96;
+struct NibbleSpanArg {
+    char* blocks;                                // first block of the run
+    int64_t first;                               // first token of the span inside the run
+    int64_t src;                                 // its row among the token-major tokens
+    int32_t n;                                   // tokens
+    int32_t tile0;                               // tiles of the launch's spans before this one
+};
+struct NibbleMove {
+    NibbleSpanArg span[kNibbleSpansPerLaunch];
+    NibbleGeom g;
+    char* k;                                     // token-major [tokens][n_kv_heads][dim] bf16
+    char* v;
+    int64_t k_token, v_token;                    // bytes between tokens
+    int32_t n_spans, n_tiles;
+};
+// All spans hold one token (a decode step): one group of lanes per token and head, no tile is moved.
+cudaError_t launch_nibble_pack(const NibbleMove& a, bool single_tokens, cudaStream_t s);
+cudaError_t launch_nibble_unpack(const NibbleMove& a, bool single_tokens, cudaStream_t s);
+
+// ---- the cache in 4 bits: decode attention (nibble_attend.cu) --------------------------------------------------------
+// Work is counted in units: (row, head group, tile of 64 tokens), tiles innermost; a head group is a KV head and some of
+// its query heads.  CTA c of n takes units [units c / n, units (c + 1) / n).  Where such a chunk meets a (row, head group)
+// that has tiles, a partial (O, maximum, sum) results; with j the index of the pair among those with tiles, partial c + j is its
+// place: distinct, and consecutive for a pair.  So neither the spans nor the partials need tables.
+struct NibbleRunArg {
+    const char* blocks;
+    int32_t n_tokens;
+    int32_t tile0;                               // tiles of the row's runs before this one
+};
+struct NibbleRowArg {
+    int32_t unit0;                               // units of the rows before this one
+    int32_t tiles;                               // tiles of the row
+    int32_t run0;                                // its first run (runs without tokens are left out)
+    int32_t pair0;                               // (row, head group) pairs with tiles before this row's
+};
+constexpr int kNibbleWarps = 7, kNibbleCtasPerSm = 2;              // warps that compute, beside the one that copies
+constexpr int kNibbleInlineRows = 64, kNibbleInlineRuns = 128;      // tables up to this size travel as launch parameters
+struct NibbleAttend {
+    NibbleRowArg row[kNibbleInlineRows];
+    NibbleRunArg run[kNibbleInlineRuns];
+    const NibbleRowArg* rows;                    // tables on the device, null: the ones above
+    const NibbleRunArg* runs;
+    NibbleGeom g;
+    const char* q;                               // [n_rows][n_q_heads][dim] bf16
+    float* part_o;                               // [partials][rows_per_part][dim]
+    float2* part_ml;                             // [partials][rows_per_part]: reference maximum (log2) and sum of weights against it
+    float* out_o;
+    float* out_lse;
+    uint32_t* status;                            // may be null
+    int64_t part_rows;                           // partial rows that the scratch holds (bounds-checked build)
+    int32_t n_rows, n_units, n_ctas, n_q_heads, group, groups_per_kv, n_gh, rows_per_part;
+    int32_t octets;                              // groups of 8 query heads in a head group
+    int32_t stages, n_runs;
+    int32_t plain_launch;                        // the tables were written by the kernel in front of this launch: no overlap with it
+    float scale;
+};
+// Head groups of a KV head's `group` query heads, and heads in each: one warp per 8 heads works on a tile, so a group has at most
+// 8 per computing warp; larger groups are cut into equal parts (each reads the tiles once more).
+inline int nibble_groups_per_kv(int group) { return (group + 8 * kNibbleWarps - 1) / (8 * kNibbleWarps); }
+inline int nibble_rows_per_part(int group) {
+    const int n = nibble_groups_per_kv(group);
+    return n == 1 ? group : ((group + n - 1) / n + 7) / 8 * 8;
+}
+cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s);
+
+}  // namespace ipkvi
