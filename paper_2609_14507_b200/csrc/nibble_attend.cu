@@ -17,12 +17,13 @@
 // 0-3 and 4-7), otherwise there are two.  sv is brought near 1 by a power of two per warp (the largest scale so far), so that
 // fp16's range is spent on p: weights down to 2^-31 of the largest keep their share.
 // The tensor cores add with two bits more than fp32 has and round towards zero, both counted from the largest exponent that
-// an operand's FORMAT shows (a subnormal counts as 2^-14).  Two things follow for V, whose sums are long.  The codes are shifted up
-// so that they fill fp16's subnormal range (bits 3..6 and 7..10).  And sums must not be much larger than the result:
+// an operand's FORMAT shows (a subnormal counts as 2^-14).  Two things follow.  The codes are shifted up so that they fill fp16's
+// subnormal range (bits 3..6 and 7..10): in place they lost up to six bits of their products.  And the sums over tokens must not be
+// much larger than the result:
 // codes are never negative, but an output is a mean of many values of either sign, so a sum of p sv code would exceed it by
 // 2.5 sqrt(tokens); every other eight tokens enter complemented, code = 15 - (15 - code): the complement costs nothing in the
 // mask, its weight is negative, 15 sv joins zv, and the excesses of the two halves meet in the same product.  Without
-// the two the output of 32K tokens was off by 5e-4 of itself.  Score accumulators start at -7.5 sum(q) for the same reason.
+// the two the output of 32K tokens was off by 5e-4 of itself.
 //
 // One warp works on one tile (64 tokens of a KV head) at a time, alone: its online softmax has its own reference maximum, raised
 // only when a score exceeds it by 2^8 (then everything is rescaled), which costs one vote per tile in place of a reduction over lanes.  A
@@ -43,12 +44,10 @@ namespace {
 
 constexpr int kWarps = kNibbleWarps;
 constexpr int kThreads = (kWarps + 1) * 32;
-constexpr int kMaxStages = 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.f;                    // the reference maximum is raised when a score exceeds it by this (log2)
-constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;         // K codes: times 2^-24 and 2^-20
-constexpr uint32_t kLowV = 0x00780078u, kHighV = 0x07800780u;       // V codes, shifted: times 2^-21 and 2^-17
+constexpr uint32_t kLow = 0x00780078u, kHigh = 0x07800780u;         // codes in bits 3..6 and 7..10: times 2^-21 and 2^-17
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -66,23 +65,24 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
-struct Smem {
-    uint64_t full[kMaxStages], empty[kMaxStages];
-    int32_t n_valid[kMaxStages];
-    float m[kWarps][8], l[kWarps][8];
-};
+using Smem = NibbleSmem;
+
+// The tables: launch parameters, or device memory when they are too large.  (Both are indexed where they are: a pointer to one or the
+// other would take the address of a launch parameter.)
+__device__ __forceinline__ NibbleRowArg row_at(const NibbleAttend& p, int i) { return p.rows ? p.rows[i] : p.row[i]; }
+__device__ __forceinline__ NibbleRunArg run_at(const NibbleAttend& p, int i) { return p.runs ? p.runs[i] : p.run[i]; }
 
 // A chunk's walk over (row, head group) pairs: which pair unit u belongs to, and how many of the chunk's tiles follow in it.
 struct Pair {
     int row, gh, tile0, n, slot;
 };
-__device__ __forceinline__ Pair pair_at(const NibbleAttend& p, const NibbleRowArg* rows, int u, int u1) {
+__device__ __forceinline__ Pair pair_at(const NibbleAttend& p, int u, int u1) {
     int lo = 0, hi = p.n_rows - 1;
     while (lo < hi) {                            // the last row that begins at or before u (rows without tiles lie in front of it)
         const int mid = (lo + hi + 1) >> 1;
-        if (rows[mid].unit0 <= u) lo = mid; else hi = mid - 1;
+        if (row_at(p, mid).unit0 <= u) lo = mid; else hi = mid - 1;
     }
-    const NibbleRowArg r = rows[lo];
+    const NibbleRowArg r = row_at(p, lo);
     Pair x;
     x.row = lo;
     x.gh = (u - r.unit0) / r.tiles;
@@ -114,8 +114,6 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
 
-    const NibbleRowArg* rows = p.rows ? p.rows : p.row;
-    const NibbleRunArg* runs = p.runs ? p.runs : p.run;
     const int u0 = int(int64_t(p.n_units) * blockIdx.x / p.n_ctas), u1 = int(int64_t(p.n_units) * (blockIdx.x + 1) / p.n_ctas);
 
     if (warp == kWarps) {
@@ -125,34 +123,22 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         int st = 0, lap = 0;
         bool ok = true;
         for (int u = u0; u < u1 && ok;) {
-            const Pair x = pair_at(p, rows, u, u1);
+            const Pair x = pair_at(p, u, u1);
             const int kv = x.gh / p.groups_per_kv;
-            int k = rows[x.row].run0;
-            // the run of the first tile, then run after run
-            {
-                int lo = k, hi = k;
-                for (int step = 1; ; step <<= 1) {       // the row's runs end where the next row's begin, or where their tiles do
-                    const int64_t last = int64_t(k) + step;
-                    const int end = x.row + 1 < p.n_rows ? rows[x.row + 1].run0 : p.n_runs;
-                    hi = last < end ? int(last) : end - 1;
-                    if (hi == end - 1 || runs[hi].tile0 > x.tile0) break;
-                    lo = hi;
-                }
-                while (lo < hi) {
-                    const int mid = (lo + hi + 1) >> 1;
-                    if (runs[mid].tile0 <= x.tile0) lo = mid; else hi = mid - 1;
-                }
-                k = lo;
+            int k = row_at(p, x.row).run0, hi = (x.row + 1 < p.n_rows ? row_at(p, x.row + 1).run0 : p.n_runs) - 1;
+            while (k < hi) {                     // the row's last run that begins at or before the first tile
+                const int mid = (k + hi + 1) >> 1;
+                if (run_at(p, mid).tile0 <= x.tile0) k = mid; else hi = mid - 1;
             }
             // the address moves from tile to tile by additions: a division per tile would make this one thread the bottleneck
             const int per = p.g.bt / kTileTokens;
             const int64_t to_next_block = p.g.block_bytes() - int64_t(per - 1) * kTile;
-            NibbleRunArg run = runs[k];
+            NibbleRunArg run = run_at(p, k);
             int tile = x.tile0 - run.tile0, left = run.n_tokens - tile * kTileTokens, in_block = tile % per;
             const char* src = run.blocks + p.g.tile_off(tile, kv);
             for (int i = 0; i < x.n; ++i) {
                 if (left <= 0) {
-                    run = runs[++k];
+                    run = run_at(p, ++k);
                     left = run.n_tokens; in_block = 0;
                     src = run.blocks + p.g.tile_off(0, kv);
                 }
@@ -183,18 +169,21 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
     const int team = warp / octets, octet = warp - team * octets;
     const bool works = team < teams;
     bool dead = false;
-    auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory"); };
+    auto sync = [&]() {
+        __syncwarp();
+        asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+    };
 
     int it0 = 0;                                 // tiles of this CTA before the current pair
-    int st = team, phase = 0;                    // stage of the team's next tile and its parity (teams <= stages)
+    int st = team, phase = 0;                    // stage of the team's next tile and its parity (stages is a multiple of teams)
     for (int u = u0; u < u1;) {
-        const Pair x = pair_at(p, rows, u, u1);
+        const Pair x = pair_at(p, u, u1);
         const int in_kv = (x.gh % p.groups_per_kv) * p.rows_per_part;      // the head group's first head among those of its KV head
         const int n_heads = min(p.group - in_kv, p.rows_per_part), head0 = (x.gh / p.groups_per_kv) * p.group + in_kv;
 
         // ---- queries: operands of head g (columns 64p+16t+8w+{0,4},{1,5},{2,6},{3,7}), normalised to [2^14, 2^15) ----
         uint32_t qf[P][2][4];
-        float qs[P][2], c[2];                    // per panel 2^-24 sum(q), and log2 units per score, of heads 2t and 2t+1
+        float qs[P][2], c[2];                    // per panel 2^-21 sum(q), and log2 units per score, of heads 2t and 2t+1
         {
             const int hq = octet * 8 + (HALF ? (g & 3) : g);
             const bool live = works && hq < n_heads;
@@ -217,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int e = min(max(int(__float_as_uint(top) >> 23), 15), 230);
             const float f = __uint_as_float(uint32_t(268 - e) << 23);                    // 2^14 / 2^(exponent of the largest)
-            const float cg = p.scale * kLog2e * __uint_as_float(uint32_t(10 + e) << 23); // ... undone, with the codes' 2^24
+            const float cg = p.scale * kLog2e * __uint_as_float(uint32_t(7 + e) << 23);  // ... undone, with the codes' 2^21
             float sum[P];
 #pragma unroll
             for (int pn = 0; pn < P; ++pn) {
@@ -234,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 }
                 sum[pn] += __shfl_xor_sync(0xffffffffu, sum[pn], 1);
                 sum[pn] += __shfl_xor_sync(0xffffffffu, sum[pn], 2);
-                sum[pn] *= 0x1p-24f;
+                sum[pn] *= 0x1p-21f;
                 qs[pn][0] = __shfl_sync(0xffffffffu, sum[pn], 8 * t);                    // lane 4 (2t): head 2t
                 qs[pn][1] = __shfl_sync(0xffffffffu, sum[pn], 8 * t + 4);
             }
@@ -274,14 +263,14 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 float acc[P][4];
 #pragma unroll
                 for (int pn = 0; pn < P; ++pn) {
-                    acc[pn][0] = acc[pn][2] = -7.5f * qs[pn][0]; acc[pn][1] = acc[pn][3] = -7.5f * qs[pn][1];
+                    acc[pn][0] = acc[pn][1] = acc[pn][2] = acc[pn][3] = 0.f;
                     const uint4 y = *reinterpret_cast<const uint4*>(tile + ((un * P + pn) * 32 + lane) * 16);
                     const uint32_t ya[2] = {y.x, y.y}, yb[2] = {y.z, y.w};
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
-                        mma_f16(acc[pn], ya[w] & kLow, yb[w] & kLow, ya[w] & kHigh, yb[w] & kHigh, qf[pn][w][0], qf[pn][w][1]);
-                        const uint32_t a8 = ya[w] >> 8, b8 = yb[w] >> 8;
-                        mma_f16(acc[pn], a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, qf[pn][w][2], qf[pn][w][3]);
+                        const uint32_t a3 = ya[w] << 3, b3 = yb[w] << 3, a5 = ya[w] >> 5, b5 = yb[w] >> 5;
+                        mma_f16(acc[pn], a3 & kLow, b3 & kLow, a3 & kHigh, b3 & kHigh, qf[pn][w][0], qf[pn][w][1]);
+                        mma_f16(acc[pn], a5 & kLow, b5 & kLow, a5 & kHigh, b5 & kHigh, qf[pn][w][2], qf[pn][w][3]);
                     }
                 }
                 uint32_t km[2][P];
@@ -302,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
 #pragma unroll
                         for (int pn = 0; pn < P; ++pn) {
                             y = fmaf(ptx::bf16_lo(km[h][pn]), acc[pn][2 * h + e], y);
-                            y = fmaf(fmaf(ptx::bf16_lo(km[h][pn]), 7.5f, ptx::bf16_hi(km[h][pn])), qs[pn][e], y);
+                            y = fmaf(ptx::bf16_hi(km[h][pn]), qs[pn][e], y);
                         }
                         s[un][2 * h + e] = y;
                     }
@@ -387,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
 #pragma unroll
                 for (int un = 0; un < 4; ++un) {
                     const uint32_t va = (un & 1) ? ya[un >> 1] >> 5 : ya[un >> 1] << 3, vb = (un & 1) ? yb[un >> 1] >> 5 : yb[un >> 1] << 3;
-                    const uint32_t a0 = va & kLowV, a1 = vb & kLowV, a2 = ~va & kHighV, a3 = ~vb & kHighV;
+                    const uint32_t a0 = va & kLow, a1 = vb & kLow, a2 = ~va & kHigh, a3 = ~vb & kHigh;
                     mma_f16(o[d], a0, a1, a2, a3, hi[un][0], hi[un][1]);
                     if (!HALF) mma_f16(o[d], a0, a1, a2, a3, lo[un][0], lo[un][1]);
                 }
@@ -496,7 +485,7 @@ __global__ void __launch_bounds__(128) nibble_reduce_kernel(const __grid_constan
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     const int row = blockIdx.x / p.n_q_heads, head = blockIdx.x - row * p.n_q_heads;
-    const NibbleRowArg r = (p.rows ? p.rows : p.row)[row];
+    const NibbleRowArg r = row_at(p, row);
     const int tid = threadIdx.x, col = tid % kCols, slice = tid / kCols;
     float4* out = reinterpret_cast<float4*>(p.out_o + int64_t(blockIdx.x) * D) + col;
     if (r.tiles == 0) {                          // nothing attended: (0, -inf)
@@ -550,16 +539,12 @@ __global__ void __launch_bounds__(128) nibble_reduce_kernel(const __grid_constan
 cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s) {
     const bool wide = a.g.dim == 128, half = a.group <= 4;
     if (a.n_units > 0) {
-        const int tile = a.g.tile_bytes(), teams = kWarps / a.octets;
-        const int joined = teams > 1 ? a.octets * 8 * (a.g.dim + 4) * int(sizeof(float)) : 0;
-        const int fixed = int(sizeof(Smem)) + joined + 128;
-        constexpr int kSmemPerCta = 228 * 1024 / kNibbleCtasPerSm - 1024;
-        const int room = kSmemPerCta - fixed;
-        a.stages = room / tile < kMaxStages ? room / tile : kMaxStages;
-        const size_t smem = size_t(a.stages) * tile + fixed;
+        a.stages = nibble_stages(a.g.dim, a.octets);
+        if (a.stages <= 0) return cudaErrorInvalidValue;
+        const size_t smem = size_t(a.stages) * a.g.tile_bytes() + nibble_fixed_smem(a.g.dim, a.octets);
         auto kernel = wide ? (half ? nibble_attend_kernel<128, true> : nibble_attend_kernel<128, false>)
                            : (half ? nibble_attend_kernel<64, true> : nibble_attend_kernel<64, false>);
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemPerCta);
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNibbleSmemPerCta);
         if (e != cudaSuccess) return e;
         e = launch_ordered(!a.plain_launch, kernel, a.n_ctas, kThreads, smem, s, a);
         if (e != cudaSuccess) return e;

@@ -70,8 +70,32 @@ struct NibbleRowArg {
     int32_t run0;                                // its first run (runs without tokens are left out)
     int32_t pair0;                               // (row, head group) pairs with tiles before this row's
 };
-constexpr int kNibbleWarps = 7, kNibbleCtasPerSm = 2;              // warps that compute, beside the one that copies
+constexpr int kNibbleWarps = 4, kNibbleCtasPerSm = 3;              // warps that compute, beside the one that copies
 constexpr int kNibbleInlineRows = 64, kNibbleInlineRuns = 128;      // tables up to this size travel as launch parameters
+// Shared memory of a CTA: the stages, this, and the buffer in which the teams' outputs are joined.
+constexpr int kNibbleMaxStages = 16;
+struct NibbleSmem {
+    uint64_t full[kNibbleMaxStages], empty[kNibbleMaxStages];
+    int32_t n_valid[kNibbleMaxStages];
+    float m[kNibbleWarps][8], l[kNibbleWarps][8];
+};
+constexpr int kNibbleSmemPerCta = 228 * 1024 / kNibbleCtasPerSm - 1024;
+// A tile is worked on by one team of `octets` warps.
+inline int nibble_teams(int octets) { return kNibbleWarps / octets; }
+inline int nibble_fixed_smem(int dim, int octets) {
+    const int joined = nibble_teams(octets) > 1 ? octets * 8 * (dim + 4) * int(sizeof(float)) : 0;
+    return int(sizeof(NibbleSmem)) + joined + 128;       // 128: to align the stages
+}
+// Stages of the copy ring: as many as fit, in a multiple of the teams, so that every stage has one team.  A warp that waits for a lap of
+// a stage can tell that lap from the one before only if it has seen the one before complete itself; with another team's
+// tile in the stage before its own it could run ahead of a copy that lands late, take the old tile for the new one and release the stage.
+inline int nibble_stages(int dim, int octets) {
+    const int teams = nibble_teams(octets), tile = NibbleGeom{1, dim, kTileTokens}.tile_bytes();
+    if (teams < 1) return 0;
+    int n = (kNibbleSmemPerCta - nibble_fixed_smem(dim, octets)) / tile;
+    if (n > kNibbleMaxStages) n = kNibbleMaxStages;
+    return n / teams * teams;
+}
 struct NibbleAttend {
     NibbleRowArg row[kNibbleInlineRows];
     NibbleRunArg run[kNibbleInlineRuns];

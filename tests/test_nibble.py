@@ -277,11 +277,11 @@ ATTEND_CASES = [  # hq, hkv, d, bt, run lengths of every row
     (12, 4, 64, 64, [[1500, 77], [2]]),          # three
     (10, 2, 128, 64, [[90], [640]]),             # five: more than four share no product
     (16, 1, 128, 64, [[450, 70], [5000]]),       # two octets on a tile
-    (24, 1, 64, 64, [[1000], [64]]),             # three octets: two warps idle
+    (24, 1, 64, 64, [[1000], [64]]),             # three octets
     (40, 1, 128, 64, [[450]]),                   # five octets
-    (56, 1, 64, 64, [[700, 300]]),               # seven: one team
-    (64, 1, 64, 256, [[700, 300]]),              # eight: two head groups
-    (119, 1, 128, 64, [[300], [65]]),            # three head groups, the last one smaller
+    (32, 1, 64, 64, [[700, 300]]),               # four octets: one team
+    (64, 1, 64, 256, [[700, 300]]),              # eight
+    (119, 1, 128, 64, [[300], [65]]),            # more than 64: two head groups, the last one smaller
     (32, 4, 128, 256, [[5000, 100], [256]]),
     (4, 1, 64, 64, [[1]] * 200),                 # tables too large to travel with the launch
     (8, 2, 128, 64, [[64] * 150, [1, 64, 3] * 30]),      # pages: runs of one block
