@@ -368,18 +368,21 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                     else { hi[un][h] = transpose8x8(big); lo[un][h] = transpose8x8(rest); }
                 }
 
-            // output: 16 columns of the head a time, the tile's 64 tokens
+            // output: 16 columns of the head a time, the tile's 64 tokens; a sum per tile, added to the state in fp32 (to nearest)
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
                 const uint4 y = *reinterpret_cast<const uint4*>(tile + kV + (d * 32 + lane) * 16);
                 const uint32_t ya[2] = {y.x, y.y}, yb[2] = {y.z, y.w};
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int un = 0; un < 4; ++un) {
                     const uint32_t va = (un & 1) ? ya[un >> 1] >> 5 : ya[un >> 1] << 3, vb = (un & 1) ? yb[un >> 1] >> 5 : yb[un >> 1] << 3;
                     const uint32_t a0 = va & kLow, a1 = vb & kLow, a2 = ~va & kHigh, a3 = ~vb & kHigh;
-                    mma_f16(o[d], a0, a1, a2, a3, hi[un][0], hi[un][1]);
-                    if (!HALF) mma_f16(o[d], a0, a1, a2, a3, lo[un][0], lo[un][1]);
+                    mma_f16(sum, a0, a1, a2, a3, hi[un][0], hi[un][1]);
+                    if (!HALF) mma_f16(sum, a0, a1, a2, a3, lo[un][0], lo[un][1]);
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[d][i] += sum[i];
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[st]));
