@@ -494,18 +494,18 @@ typedef struct {
 int64_t ipkv_nibble_block_bytes(const ipkv_attn_shape* shape);
 
 /* Write token-major K/V into NIBBLE blocks: the tokens of span 0, then those of span 1, and so on, from k_dev and v_dev
- * [tokens][n_kv_heads][dim] bf16; k_token_stride, v_token_stride: elements between tokens (multiples of 8; 0: dense).
+ * [n_tokens][n_kv_heads][dim] bf16 (n_tokens: what the spans hold together, IPKV_EINVAL otherwise); k_token_stride, v_token_stride: elements between tokens (multiples of 8; 0: dense).
  * One call serves prompts, chunks of prompts that begin or end inside a block, and a decode step (one token per span).  Tokens
  * outside the spans keep their codes.  spans: host array, copied by the call (so the call can be captured into a CUDA
  * graph).  No two spans of a call may touch the same block (IPKV_EINVAL), and calls that touch the same block must be
  * ordered on the device: neighbouring tokens share bytes.  Works on the current device. */
-ipkv_status ipkv_nibble_pack(const ipkv_attn_shape* shape, int32_t n_spans, const ipkv_span* spans, const void* k_dev, const void* v_dev,
-                             int64_t k_token_stride, int64_t v_token_stride, void* stream);
+ipkv_status ipkv_nibble_pack(const ipkv_attn_shape* shape, int32_t n_spans, const ipkv_span* spans, int64_t n_tokens,
+                             const void* k_dev, const void* v_dev, int64_t k_token_stride, int64_t v_token_stride, void* stream);
 
 /* The inverse: the values that the codes of the spans' tokens stand for, rounded to bf16, into k_dev and v_dev (which no
  * block may overlap).  Several spans may read the same block. */
-ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* shape, int32_t n_spans, const ipkv_span* spans, void* k_dev, void* v_dev,
-                               int64_t k_token_stride, int64_t v_token_stride, void* stream);
+ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* shape, int32_t n_spans, const ipkv_span* spans, int64_t n_tokens,
+                               void* k_dev, void* v_dev, int64_t k_token_stride, int64_t v_token_stride, void* stream);
 
 /* Decode attention over runs of NIBBLE blocks: ipkv_attend_runs for this format.  n_rows queries, row r over the tokens of
  * runs[row_run_start[r] .. row_run_start[r+1]) (a run: consecutive blocks and how many of their first tokens count; what

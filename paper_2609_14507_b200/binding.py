@@ -8,6 +8,7 @@ Tensors are passed as ``torch`` tensors (device or host); this module only takes
 """
 import ctypes as C
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libipkv.so")
@@ -143,9 +144,9 @@ def lib():
         "ipkv_attend_scratch_bytes": [C.POINTER(AttnShape), i32, i32, i64, i32, C.POINTER(C.c_size_t)],
         "ipkv_attend_runs": [C.POINTER(AttnShape), i32, C.POINTER(Run), C.POINTER(i32), vp, i32, vp, C.c_size_t, vp, vp, vp, vp],
         "ipkv_pack_blocks": [C.POINTER(AttnShape), i32, vp, vp, i64, vp, vp],
-        "ipkv_norm_rope": [C.POINTER(Rope), i64, C.POINTER(Heads), i32, vp, vp],
-        "ipkv_nibble_pack": [C.POINTER(AttnShape), i32, vp, vp, vp, i64, i64, vp],
-        "ipkv_nibble_unpack": [C.POINTER(AttnShape), i32, vp, vp, vp, i64, i64, vp],
+        "ipkv_norm_rope": [C.POINTER(Rope), i64, vp, i32, vp, vp],
+        "ipkv_nibble_pack": [C.POINTER(AttnShape), i32, vp, i64, vp, vp, i64, i64, vp],
+        "ipkv_nibble_unpack": [C.POINTER(AttnShape), i32, vp, i64, vp, vp, i64, i64, vp],
         "ipkv_nibble_scratch_bytes": [C.POINTER(AttnShape), i32, i32, C.POINTER(C.c_size_t)],
         "ipkv_nibble_attend": [C.POINTER(AttnShape), i32, vp, vp, vp, vp, C.c_size_t, vp, vp, vp, vp],
         "ipkv_attend_runs_noalloc": [C.POINTER(AttnShape), i32, C.POINTER(Run), C.POINTER(i32), vp, i32, vp, vp, vp, vp],
@@ -541,19 +542,34 @@ def ipkv_pack_blocks(shape, layout, k, v, n_tokens, dst, stream=None):
         raise IpkvError(rc, "ipkv_pack_blocks")
 
 
-# ---- head norm and rotation ---------------------------------------------------------------------------------------
+# ---- operators beside the cache -------------------------------------------------------------------------------------
+# A decode step calls these once a layer, so what they check is checked with few attribute reads, and tables go to the
+# library as packed bytes.
 
-def _device_call(stream, *tensors):
-    """The stream of a stateless call, as a number: the given one, or the current device's current one.  The call runs on the
-    current device, so every tensor has to live there."""
+_torch = _np = None
+
+
+def _modules():
+    global _torch, _np
+    import numpy
     import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"a tensor is on {t.device}, the call runs on the current CUDA device ({dev})")
+    _np, _torch = numpy, torch
+    return torch
+
+
+def _call_stream(stream, dev):
+    """The stream of a stateless call on tensors of CUDA device `dev`, as a number: the given one, or the current device's current
+    one.  The call runs on the current device, so the tensors have to live there."""
+    if dev < 0 or dev != _torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on device {dev} (-1: the host), the call runs on the current CUDA device")
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(dev)
+        return _torch._C._cuda_getCurrentRawStream(dev)
     return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+# ---- head norm and rotation ----
+
+_HEADS_FORMAT = struct.Struct("<QQQi4xqqqq")         # ipkv_heads
 
 
 def make_rope(dim, rot_dim=None, *, theta=10000.0, sections=None, interleaved=False, eps=1e-6, inv_freq=None, pair_axis=None):
@@ -561,18 +577,23 @@ def make_rope(dim, rot_dim=None, *, theta=10000.0, sections=None, interleaved=Fa
     rot_dim / 2); pair_axis: the axis of every pair instead, for other arrangements; neither: one axis."""
     rot_dim = dim if rot_dim is None else rot_dim
     pairs = rot_dim // 2
-    if pair_axis is None:
-        pair_axis = [a for a, n in enumerate(sections) for _ in range(n)] if sections is not None else None
-    elif sections is not None:
-        raise ValueError("sections and pair_axis exclude each other")
     r = Rope(dim, rot_dim, 1, 1 if interleaved else 0, eps, theta, None, None)
-    if pair_axis is not None:
+    if sections is not None:
+        if pair_axis is not None:
+            raise ValueError("sections and pair_axis exclude each other")
+        if sum(sections) != pairs or min(sections, default=0) < 0:
+            raise ValueError(f"{sum(sections)} pairs have an axis, {pairs} are rotated")
+        r.n_axes = len(sections)
+        if len(sections) > 1:
+            pair_axis = b"".join([bytes((a,)) * n for a, n in enumerate(sections)])
+    elif pair_axis is not None:
         if len(pair_axis) != pairs:
             raise ValueError(f"{len(pair_axis)} pairs have an axis, {pairs} are rotated")
-        r._axes = bytes(pair_axis)
-        r.n_axes = len(sections) if sections is not None else max(pair_axis, default=0) + 1
-        if r.n_axes > 1:
-            r.pair_axis = C.cast(C.c_char_p(r._axes), C.c_void_p)
+        r.n_axes = max(pair_axis, default=0) + 1
+        pair_axis = bytes(pair_axis)
+    if pair_axis:
+        r._axes = pair_axis                              # stays alive with r
+        r.pair_axis = C.cast(pair_axis, C.c_void_p)
     if inv_freq is not None:
         if len(inv_freq) != pairs:
             raise ValueError(f"{len(inv_freq)} frequencies, {pairs} pairs are rotated")
@@ -584,32 +605,51 @@ def make_rope(dim, rot_dim=None, *, theta=10000.0, sections=None, interleaved=Fa
 def ipkv_norm_rope(rope, parts, positions, stream=None):
     """parts: 1..4 tuples (x, weight or None, out or None): x and out [n_tokens, heads, dim] bf16 with any token and head
     strides, out None means in place.  positions: int32 [n_axes, n_tokens] (or [n_tokens]), contiguous; None without a rotation."""
-    import torch
-    n = len(parts)
-    arr = (Heads * n)()
-    n_tokens, tensors = parts[0][0].shape[0], [positions]
-    for a, (x, w, out) in zip(arr, parts):
-        out = x if out is None else out
-        if x.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16 or (w is not None and w.dtype is not torch.bfloat16):
-            raise ValueError("heads and weights are bfloat16")
-        heads = x.shape
-        if len(heads) != 3 or heads != out.shape or heads[0] != n_tokens or heads[2] != rope.dim:
-            raise ValueError(f"heads are [n_tokens, n_heads, {rope.dim}], the output's like the input's: got {tuple(heads)} and {tuple(out.shape)}")
-        i, o = x.stride(), out.stride()
-        if i[2] != 1 or o[2] != 1 or (w is not None and (w.numel() != rope.dim or not w.is_contiguous())):
-            raise ValueError("the columns of a head and of a weight are contiguous")
-        a.in_dev, a.out_dev, a.weight_dev, a.n_heads = x.data_ptr(), out.data_ptr(), _ptr(w), heads[1]
-        t, h = n_tokens > 1, heads[1] > 1               # the stride of a dimension of one is never used
-        a.in_token_stride, a.in_head_stride, a.out_token_stride, a.out_head_stride = i[0] * t, i[1] * h, o[0] * t, o[1] * h
-        tensors += (x, w, out)
-    if positions is not None and (positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.numel() != rope.n_axes * n_tokens):
-        raise ValueError(f"positions are contiguous int32 [{rope.n_axes}, {n_tokens}]")
-    rc = lib().ipkv_norm_rope(C.byref(rope), n_tokens, arr, n, _ptr(positions), _device_call(stream, *tensors))
+    torch = _torch or _modules()
+    bf16, dim = torch.bfloat16, rope.dim
+    x = parts[0][0]
+    n_tokens, dev = x.shape[0], x.get_device()
+    packed = b""
+    for x, w, out in parts:
+        shape = x.shape
+        if x.dtype is not bf16 or len(shape) != 3 or shape[0] != n_tokens or shape[2] != dim:
+            raise ValueError(f"heads are bfloat16 [{n_tokens}, n_heads, {dim}]: got {x.dtype} {tuple(shape)}")
+        n_heads, (it, ih, ic), at = shape[1], x.stride(), x.data_ptr()
+        if n_tokens <= 1:                                # the stride of a dimension of one is never used
+            it = 0
+        if n_heads <= 1:
+            ih = 0
+        if out is None:
+            ot, oh, to = it, ih, at
+        else:
+            if out.dtype is not bf16 or out.shape != shape:
+                raise ValueError(f"an output is like its input: got {out.dtype} {tuple(out.shape)} for {tuple(shape)}")
+            (ot, oh, oc), to = out.stride(), out.data_ptr()
+            if n_tokens <= 1:
+                ot = 0
+            if n_heads <= 1:
+                oh = 0
+            if oc != 1 or out.get_device() != dev:
+                raise ValueError("the columns of a head are contiguous, and all tensors are on one device")
+        if ic != 1 or x.get_device() != dev:
+            raise ValueError("the columns of a head are contiguous, and all tensors are on one device")
+        if w is None:
+            wp = 0
+        else:
+            if w.dtype is not bf16 or w.numel() != dim or not w.is_contiguous() or w.get_device() != dev:
+                raise ValueError(f"a weight is contiguous bfloat16 [{dim}] on the device of the heads")
+            wp = w.data_ptr()
+        packed += _HEADS_FORMAT.pack(at, to, wp, n_heads, it, ih, ot, oh)
+    if positions is not None:
+        if positions.dtype is not torch.int32 or positions.numel() != rope.n_axes * n_tokens or not positions.is_contiguous() or positions.get_device() != dev:
+            raise ValueError(f"positions are contiguous int32 [{rope.n_axes}, {n_tokens}] on the device of the heads")
+        positions = positions.data_ptr()
+    rc = lib().ipkv_norm_rope(C.byref(rope), n_tokens, packed, len(parts), positions, _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, "ipkv_norm_rope")
 
 
-# ---- a cache held in 4 bits -----------------------------------------------------------------------------------------
+# ---- a cache held in 4 bits ----
 
 def ipkv_nibble_block_bytes(shape):
     """Bytes of one NIBBLE block (grouped-query shapes, dim 64 or 128, block_tokens a multiple of 64)."""
@@ -621,36 +661,32 @@ def ipkv_nibble_block_bytes(shape):
 
 def _table(rows, width):
     """A host table of 64-bit words, [n][width]: a NumPy int64 array as it is, or rows whose first entry may be a tensor."""
-    import numpy as np
-    if not isinstance(rows, np.ndarray):
-        rows = np.array([[_ptr(r[0]) or 0, *r[1:]] for r in rows], dtype=np.int64).reshape(-1, width)
-    if rows.dtype != np.int64 or rows.ndim != 2 or rows.shape[1] != width or not rows.flags.c_contiguous:
+    if not isinstance(rows, _np.ndarray):
+        rows = _np.array([[_ptr(r[0]) or 0, *r[1:]] for r in rows], dtype=_np.int64).reshape(-1, width)
+    if rows.dtype != _np.int64 or rows.ndim != 2 or rows.shape[1] != width or not rows.flags.c_contiguous:
         raise ValueError(f"expected a contiguous int64 array [n][{width}]: got {rows.dtype} {rows.shape}")
     return rows
 
 
-def _token_rows(x, shape, what):
-    """Elements between the tokens of K or V [tokens][n_kv_heads][dim]; the heads of a token lie side by side."""
-    import torch
-    d = x.shape
-    if x.dtype is not torch.bfloat16 or len(d) != 3 or d[1] != shape.n_kv_heads or d[2] != shape.dim_qk:
-        raise ValueError(f"{what} is bfloat16 [tokens, {shape.n_kv_heads}, {shape.dim_qk}]: got {x.dtype} {tuple(d)}")
-    st = x.stride()
-    if st[2] != 1 or (d[1] > 1 and st[1] != d[2]):
-        raise ValueError(f"the heads of a token of {what} lie side by side")
-    return st[0] if d[0] > 1 else 0
+def _address(a):
+    return a.__array_interface__["data"][0]
 
 
 def _move(name, shape, spans, k, v, stream):
+    torch = _torch or _modules()
     t = _table(spans, 3)
-    ks, vs = _token_rows(k, shape, "K"), _token_rows(v, shape, "V")
-    n = int(t[:, 2].sum())
-    if k.shape[0] != n or v.shape[0] != n:
-        raise ValueError(f"the spans hold {n} tokens, K and V {k.shape[0]} and {v.shape[0]}")
-    if n > 1 and (ks == 0 or vs == 0):
-        raise ValueError("the tokens of K and V lie apart")
-    rc = getattr(lib(), name)(C.byref(shape), t.shape[0], t.__array_interface__["data"][0], k.data_ptr(), v.data_ptr(), ks, vs,
-                              _device_call(stream, k, v))
+    heads, dim, n, dev = shape.n_kv_heads, shape.dim_qk, k.shape[0], k.get_device()
+    strides = []
+    for x in (k, v):
+        d = x.shape
+        if x.dtype is not torch.bfloat16 or len(d) != 3 or d[0] != n or d[1] != heads or d[2] != dim:
+            raise ValueError(f"K and V are bfloat16 [{n}, {heads}, {dim}]: got {x.dtype} {tuple(d)}")
+        token, head, column = x.stride()
+        if column != 1 or (heads > 1 and head != dim) or (n > 1 and token == 0) or x.get_device() != dev:
+            raise ValueError("the heads of a token lie side by side, its tokens apart, and K and V are on one device")
+        strides.append(token if n > 1 else 0)
+    rc = getattr(lib(), name)(C.byref(shape), t.shape[0], _address(t), n, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
+                              _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, name)
 
@@ -677,28 +713,24 @@ def ipkv_nibble_scratch_bytes(shape, n_rows, n_runs):
 def ipkv_nibble_attend(shape, runs, row_start, q, scratch, o_part, lse_part, status=None, stream=None):
     """Attention of one query per row over runs of NIBBLE blocks.  runs: int64 array [n][2] of (address, tokens) with row_start,
     an int32 array [rows + 1]; or, with row_start None, one list per row of (blocks, tokens) as for ipkv_attend_runs."""
-    import numpy as np
-    import torch
+    torch = _torch or _modules()
     if row_start is None:
-        row_start = np.cumsum([0] + [len(r) for r in runs]).astype(np.int32)
+        row_start = _np.cumsum([0] + [len(r) for r in runs]).astype(_np.int32)
         runs = _table([x for r in runs for x in r], 2)
     else:
         runs = _table(runs, 2)
-        if not isinstance(row_start, np.ndarray) or row_start.dtype != np.int32 or not row_start.flags.c_contiguous or row_start.ndim != 1:
+        if not isinstance(row_start, _np.ndarray) or row_start.dtype != _np.int32 or row_start.ndim != 1 or not row_start.flags.c_contiguous:
             raise ValueError("row_start is a contiguous int32 array [rows + 1]")
     rows = row_start.shape[0] - 1
     if rows < 1 or row_start[-1] > runs.shape[0]:
-        raise ValueError(f"row_start names runs up to {row_start[-1] if rows >= 0 else None}: there are {runs.shape[0]}")
-    want = (rows, shape.n_q_heads, shape.dim_qk)
-    if q.dtype is not torch.bfloat16 or q.shape != want or not q.is_contiguous():
-        raise ValueError(f"q is contiguous bfloat16 {want}: got {q.dtype} {tuple(q.shape)}")
-    if o_part.dtype is not torch.float32 or o_part.shape != want or not o_part.is_contiguous():
-        raise ValueError(f"o_part is contiguous float32 {want}: got {o_part.dtype} {tuple(o_part.shape)}")
-    if lse_part.dtype is not torch.float32 or lse_part.shape != want[:2] or not lse_part.is_contiguous():
-        raise ValueError(f"lse_part is contiguous float32 {want[:2]}: got {lse_part.dtype} {tuple(lse_part.shape)}")
-    s = _device_call(stream, q, scratch, o_part, lse_part, status)
-    rc = lib().ipkv_nibble_attend(C.byref(shape), rows, runs.__array_interface__["data"][0], row_start.__array_interface__["data"][0], q.data_ptr(),
-                                  scratch.data_ptr(), scratch.numel() * scratch.element_size(), o_part.data_ptr(), lse_part.data_ptr(),
-                                  _ptr(status), s)
+        raise ValueError(f"row_start names runs that are not there: there are {runs.shape[0]}")
+    want, dev = (rows, shape.n_q_heads, shape.dim_qk), q.get_device()
+    for x, dtype, size, what in ((q, torch.bfloat16, want, "q"), (o_part, torch.float32, want, "o_part"), (lse_part, torch.float32, want[:2], "lse_part")):
+        if x.dtype is not dtype or x.shape != size or not x.is_contiguous() or x.get_device() != dev:
+            raise ValueError(f"{what} is contiguous {dtype} {size} on the device of q: got {x.dtype} {tuple(x.shape)}")
+    if scratch.get_device() != dev or not scratch.is_contiguous() or (status is not None and (status.get_device() != dev or status.dtype not in (torch.int32, torch.uint32))):
+        raise ValueError("scratch and the status word (32 bits) are on the device of q")
+    rc = lib().ipkv_nibble_attend(C.byref(shape), rows, _address(runs), _address(row_start), q.data_ptr(), scratch.data_ptr(), scratch.nbytes,
+                                  o_part.data_ptr(), lse_part.data_ptr(), _ptr(status), _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, "ipkv_nibble_attend")

@@ -47,6 +47,7 @@ constexpr int kThreads = (kWarps + 1) * 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.f;                    // the reference maximum is raised when a score exceeds it by this (log2)
+constexpr int kManyParts = 16;                   // partials of a (row, head) from which the join is spread over more threads
 constexpr uint32_t kLow = 0x00780078u, kHigh = 0x07800780u;         // codes in bits 3..6 and 7..10: times 2^-21 and 2^-17
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -478,22 +479,25 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
     }
 }
 
-// Joins the partials of every (row, query head): LSE = m + ln sum exp(LSE_i - m), O = sum exp(LSE_i - LSE) O_i, in a fixed order.
-// One CTA per (row, head): D/4 column groups times 512/D slices of the partials.
-template <int D>
-__global__ void __launch_bounds__(128) nibble_reduce_kernel(const __grid_constant__ NibbleAttend p) {
-    constexpr int kCols = D / 4, kSlices = 128 / kCols;
+// Joins the partials of every (row, query head): with partial i's maximum m_i (log2), sum l_i and normalised O_i,
+//   m = max m_i,  z = sum 2^(m_i - m) l_i,  O = sum 2^(m_i - m) l_i O_i / z,  LSE = m ln 2 + ln z,   in a fixed order.
+// One CTA per (row, head, COLS columns): COLS/4 column groups times THREADS / (COLS/4) slices of the partials.  Bound by the latency of
+// its two dependent reads; many partials per head (few heads, a long sequence) want many slices, see the launch.
+template <int D, int COLS, int THREADS>
+__global__ void __launch_bounds__(THREADS) nibble_reduce_kernel(const __grid_constant__ NibbleAttend p) {
+    constexpr int kCols = COLS / 4, kSlices = THREADS / kCols, kSlabs = D / COLS;
     __shared__ float4 s_o[kSlices][kCols];
-    __shared__ float s_z[kSlices], s_m[4];
+    __shared__ float s_z[kSlices], s_m[THREADS / 32];
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const int row = blockIdx.x / p.n_q_heads, head = blockIdx.x - row * p.n_q_heads;
+    const int item = blockIdx.x / kSlabs, slab = blockIdx.x - item * kSlabs;     // item: row * n_q_heads + head
+    const int row = item / p.n_q_heads, head = item - row * p.n_q_heads;
     const NibbleRowArg r = row_at(p, row);
     const int tid = threadIdx.x, col = tid % kCols, slice = tid / kCols;
-    float4* out = reinterpret_cast<float4*>(p.out_o + int64_t(blockIdx.x) * D) + col;
+    float4* out = reinterpret_cast<float4*>(p.out_o + int64_t(item) * D + slab * COLS) + col;
     if (r.tiles == 0) {                          // nothing attended: (0, -inf)
         if (slice == 0) *out = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (tid == 0) p.out_lse[blockIdx.x] = -INFINITY;
+        if (tid == 0 && slab == 0) p.out_lse[item] = -INFINITY;
         return;
     }
     const int in_kv = head % p.group;
@@ -503,16 +507,17 @@ __global__ void __launch_bounds__(128) nibble_reduce_kernel(const __grid_constan
     const int e0 = int(((a + 1) * p.n_ctas - 1) / p.n_units) + j, e1 = int(((b + 1) * p.n_ctas - 1) / p.n_units) + j;   // first, last partial
     const int n = e1 - e0 + 1;
     const float2* ml = p.part_ml + int64_t(e0) * p.rows_per_part + rin;
-    const float4* part = reinterpret_cast<const float4*>(p.part_o + (int64_t(e0) * p.rows_per_part + rin) * D) + col;
-    const int64_t stride = int64_t(p.rows_per_part) * kCols;
+    const float4* part = reinterpret_cast<const float4*>(p.part_o + (int64_t(e0) * p.rows_per_part + rin) * D + slab * COLS) + col;
+    const int64_t stride = int64_t(p.rows_per_part) * (D / 4);
 
     float m = -INFINITY;
-    for (int i = tid; i < n; i += 128) m = fmaxf(m, ml[int64_t(i) * p.rows_per_part].x);
+    for (int i = tid; i < n; i += THREADS) m = fmaxf(m, ml[int64_t(i) * p.rows_per_part].x);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     if ((tid & 31) == 0) s_m[tid >> 5] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) m = fmaxf(m, s_m[w]);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float z = 0.f;
 #pragma unroll 4
@@ -527,6 +532,7 @@ __global__ void __launch_bounds__(128) nibble_reduce_kernel(const __grid_constan
     if (col == 0) s_z[slice] = z;
     __syncthreads();
     if (slice != 0) return;
+#pragma unroll
     for (int k = 1; k < kSlices; ++k) {
         const float4 v = s_o[k][col];
         acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
@@ -534,7 +540,7 @@ __global__ void __launch_bounds__(128) nibble_reduce_kernel(const __grid_constan
     }
     const float inv = z > 0.f ? 1.f / z : 0.f;
     *out = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    if (col == 0) p.out_lse[blockIdx.x] = z > 0.f ? m * kLn2 + logf(z) : -INFINITY;
+    if (tid == 0 && slab == 0) p.out_lse[item] = z > 0.f ? m * kLn2 + logf(z) : -INFINITY;
 }
 
 }  // namespace
@@ -552,7 +558,11 @@ cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s) {
         e = launch_ordered(!a.plain_launch, kernel, a.n_ctas, kThreads, smem, s, a);
         if (e != cudaSuccess) return e;
     }
-    return launch_ordered(a.n_units > 0, wide ? nibble_reduce_kernel<128> : nibble_reduce_kernel<64>, a.n_rows * a.n_q_heads, 128, size_t(0), s, a);
+    const int items = a.n_rows * a.n_q_heads;
+    if (a.max_parts > kManyParts)
+        return launch_ordered(true, wide ? nibble_reduce_kernel<128, 32, 256> : nibble_reduce_kernel<64, 32, 256>, items * (a.g.dim / 32), 256,
+                              size_t(0), s, a);
+    return launch_ordered(a.n_units > 0, wide ? nibble_reduce_kernel<128, 128, 128> : nibble_reduce_kernel<64, 64, 128>, items, 128, size_t(0), s, a);
 }
 
 }  // namespace ipkvi

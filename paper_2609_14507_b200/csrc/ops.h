@@ -112,6 +112,7 @@ struct NibbleAttend {
     int32_t n_rows, n_units, n_ctas, n_q_heads, group, groups_per_kv, n_gh, rows_per_part;
     int32_t octets;                              // groups of 8 query heads in a head group
     int32_t stages, n_runs;
+    int32_t max_parts;                           // partials of a (row, head group) at most
     int32_t plain_launch;                        // the tables were written by the kernel in front of this launch: no overlap with it
     float scale;
 };

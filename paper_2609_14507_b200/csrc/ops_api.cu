@@ -58,7 +58,7 @@ NibbleGeom nibble_geom(const ipkv_attn_shape* sh) { return NibbleGeom{sh->n_kv_h
 constexpr int64_t kMaxRunTokens = int64_t(1) << 36;      // keeps every product with a block's bytes inside 63 bits
 
 // Checks the arguments of pack and unpack and issues their launches.
-ipkv_status move_spans(const ipkv_attn_shape* sh, int32_t n_spans, const ipkv_span* spans, const void* k, const void* v, int64_t k_token_stride,
+ipkv_status move_spans(const ipkv_attn_shape* sh, int32_t n_spans, const ipkv_span* spans, int64_t n_tokens, const void* k, const void* v, int64_t k_token_stride,
                        int64_t v_token_stride, bool pack, cudaStream_t stream) {
     if (!nibble_shape_ok(sh) || n_spans < 0 || (n_spans > 0 && !spans)) return IPKV_EINVAL;
     const NibbleGeom g = nibble_geom(sh);
@@ -82,6 +82,7 @@ ipkv_status move_spans(const ipkv_attn_shape* sh, int32_t n_spans, const ipkv_sp
                                  base + uintptr_t(((sp.first_token + sp.n_tokens - 1) / g.bt + 1) * g.block_bytes()));
         }
     }
+    if (tokens != n_tokens) return IPKV_EINVAL;
     if (tokens == 0) return IPKV_OK;
     if (!k || !v) return IPKV_EINVAL;
     std::sort(touched.begin(), touched.end());
@@ -134,7 +135,7 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
     if (!(sh->softmax_scale >= 0.f) || std::isinf(sh->softmax_scale)) return IPKV_EINVAL;
     if (!aligned16(q) || !aligned16(o) || (reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(status) & 3u)) return IPKV_EINVAL;
     if (reinterpret_cast<uintptr_t>(scratch) & 255u) return IPKV_EINVAL;
-    if (int64_t(n_rows) * sh->n_q_heads > INT32_MAX) return IPKV_EINVAL;
+    if (int64_t(n_rows) * sh->n_q_heads > INT32_MAX / 4) return IPKV_EINVAL;          // the join's grid
     const NibblePlan plan(sh);
     if (row_run_start[0] < 0) return IPKV_EINVAL;
     for (int r = 0; r < n_rows; ++r)
@@ -159,7 +160,7 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
         row = reinterpret_cast<NibbleRowArg*>(image.data());
         run = reinterpret_cast<NibbleRunArg*>(row + n_rows);
     }
-    int64_t units = 0;
+    int64_t units = 0, longest = 0;
     int32_t n_runs = 0, pairs = 0;
     for (int r = 0; r < n_rows; ++r) {
         int64_t tiles = 0;
@@ -171,6 +172,7 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
             if (tiles > INT32_MAX) return IPKV_EINVAL;
         }
         row[r].tiles = int32_t(tiles);
+        longest = std::max(longest, tiles);
         units += tiles * plan.n_gh;
         pairs += tiles > 0 ? plan.n_gh : 0;
         if (units > INT32_MAX) return IPKV_EINVAL;
@@ -199,6 +201,7 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
     a.out_o = o; a.out_lse = lse; a.status = status;
     a.n_rows = n_rows; a.n_units = int32_t(units); a.n_runs = n_runs;
     a.n_ctas = units < NibblePlan::kCtas ? int32_t(units) : NibblePlan::kCtas;
+    a.max_parts = units > 0 ? int32_t((longest * a.n_ctas + units - 1) / units + 1) : 0;
     a.n_q_heads = sh->n_q_heads; a.group = plan.group; a.groups_per_kv = plan.groups_per_kv; a.n_gh = plan.n_gh; a.rows_per_part = plan.rows_per_part;
     a.octets = (plan.rows_per_part + 7) / 8;
     a.scale = sh->softmax_scale > 0.f ? sh->softmax_scale : 1.0f / std::sqrt(float(sh->dim_qk));
@@ -269,15 +272,15 @@ ipkv_status ipkv_norm_rope(const ipkv_rope* rope, int64_t n_tokens, const ipkv_h
             if (i != k && may_overlap(out[i], out[k])) return IPKV_EINVAL;
             if (may_overlap(out[i], in[k]) && !(i == k && same_view(out[i], in[k]))) return IPKV_EINVAL;
         }
-    constexpr long double kTwoPi = 6.283185307179586476925286766559005768L;
+    constexpr long double kTurnsPerRadian = 0.159154943091895335768883763372514362L;
     // theta^(-2i / rot_dim) by repeated multiplication (one power a call instead of one a pair): at most 127 roundings of 2^-64
     const long double ratio = pairs > 0 && !rope->inv_freq ? powl(static_cast<long double>(rope->theta), -2.0L / rope->rot_dim) : 1.0L;
     long double power = 1.0L;
     for (int i = 0; i < pairs; ++i) {
-        long double turns = (rope->inv_freq ? static_cast<long double>(rope->inv_freq[i]) : power) / kTwoPi;
+        long double turns = (rope->inv_freq ? static_cast<long double>(rope->inv_freq[i]) : power) * kTurnsPerRadian;
         power *= ratio;
-        turns -= floorl(turns);                                      // whole turns change nothing: positions are integers
-        long double scaled = roundl(turns * 18446744073709551616.0L);
+        if (turns < 0.0L || turns >= 1.0L) turns -= floorl(turns);   // whole turns change nothing: positions are integers
+        const long double scaled = turns * 18446744073709551616.0L + 0.5L;
         a.turn[i] = scaled >= 18446744073709551616.0L ? 0u : static_cast<uint64_t>(scaled);
         a.axis[i] = rope->pair_axis ? rope->pair_axis[i] : uint8_t(0);
     }
@@ -288,14 +291,14 @@ ipkv_status ipkv_norm_rope(const ipkv_rope* rope, int64_t n_tokens, const ipkv_h
 
 int64_t ipkv_nibble_block_bytes(const ipkv_attn_shape* sh) { return nibble_shape_ok(sh) ? nibble_geom(sh).block_bytes() : -1; }
 
-ipkv_status ipkv_nibble_pack(const ipkv_attn_shape* sh, int32_t n_spans, const ipkv_span* spans, const void* k_dev, const void* v_dev,
-                             int64_t k_token_stride, int64_t v_token_stride, void* stream) {
-    return guarded([&] { return move_spans(sh, n_spans, spans, k_dev, v_dev, k_token_stride, v_token_stride, true, static_cast<cudaStream_t>(stream)); });
+ipkv_status ipkv_nibble_pack(const ipkv_attn_shape* sh, int32_t n_spans, const ipkv_span* spans, int64_t n_tokens,
+                             const void* k_dev, const void* v_dev, int64_t k_token_stride, int64_t v_token_stride, void* stream) {
+    return guarded([&] { return move_spans(sh, n_spans, spans, n_tokens, k_dev, v_dev, k_token_stride, v_token_stride, true, static_cast<cudaStream_t>(stream)); });
 }
 
-ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* sh, int32_t n_spans, const ipkv_span* spans, void* k_dev, void* v_dev,
-                               int64_t k_token_stride, int64_t v_token_stride, void* stream) {
-    return guarded([&] { return move_spans(sh, n_spans, spans, k_dev, v_dev, k_token_stride, v_token_stride, false, static_cast<cudaStream_t>(stream)); });
+ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* sh, int32_t n_spans, const ipkv_span* spans, int64_t n_tokens,
+                               void* k_dev, void* v_dev, int64_t k_token_stride, int64_t v_token_stride, void* stream) {
+    return guarded([&] { return move_spans(sh, n_spans, spans, n_tokens, k_dev, v_dev, k_token_stride, v_token_stride, false, static_cast<cudaStream_t>(stream)); });
 }
 
 ipkv_status ipkv_nibble_scratch_bytes(const ipkv_attn_shape* sh, int32_t n_rows, int32_t n_runs, size_t* out_bytes) {

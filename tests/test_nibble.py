@@ -27,8 +27,8 @@ def test_shapes_without_the_format_are_refused(sh):
     L = binding.lib()
     assert L.ipkv_nibble_block_bytes(C.byref(sh)) == -1
     spans = (binding.Span * 1)(binding.Span(BASE, 0, 1))
-    assert L.ipkv_nibble_pack(C.byref(sh), 1, spans, BASE, BASE, 0, 0, None) == EINVAL
-    assert L.ipkv_nibble_unpack(C.byref(sh), 1, spans, BASE, BASE, 0, 0, None) == EINVAL
+    assert L.ipkv_nibble_pack(C.byref(sh), 1, spans, 1, BASE, BASE, 0, 0, None) == EINVAL
+    assert L.ipkv_nibble_unpack(C.byref(sh), 1, spans, 1, BASE, BASE, 0, 0, None) == EINVAL
     n = C.c_size_t()
     assert L.ipkv_nibble_scratch_bytes(C.byref(sh), 1, 1, C.byref(n)) == EINVAL
     runs, start = (binding.Run * 1)(binding.Run(BASE, 5)), (C.c_int32 * 2)(0, 1)
@@ -42,9 +42,9 @@ def test_block_bytes():
     assert binding.ipkv_nibble_block_bytes(shape_of(12, 4, 64, 256)) == 4 * 4 * 4608 == ref.block_bytes(4, 64, 256)
 
 
-def move(fn, sh, spans, k=BASE, v=BASE, ks=0, vs=0, n=None):
+def move(fn, sh, spans, k=BASE, v=BASE, ks=0, vs=0, n=None, tokens=None):
     arr = (binding.Span * max(1, len(spans)))(*[binding.Span(*s) for s in spans])
-    return fn(C.byref(sh), len(spans) if n is None else n, arr, k, v, ks, vs, None)
+    return fn(C.byref(sh), len(spans) if n is None else n, arr, sum(s[2] for s in spans) if tokens is None else tokens, k, v, ks, vs, None)
 
 
 @pytest.mark.parametrize("name", ["ipkv_nibble_pack", "ipkv_nibble_unpack"])
@@ -57,7 +57,8 @@ def test_bad_spans_are_refused(name):
     assert move(fn, sh, ok, k=BASE + 2) == EINVAL and move(fn, sh, ok, v=BASE + 8) == EINVAL
     assert move(fn, sh, ok, ks=504) == EINVAL and move(fn, sh, ok, vs=-512) == EINVAL and move(fn, sh, ok, ks=516) == EINVAL
     assert move(fn, sh, ok, n=-1) == EINVAL
-    assert fn(C.byref(sh), 1, None, BASE, BASE, 0, 0, None) == EINVAL
+    assert move(fn, sh, ok, tokens=2) == EINVAL and move(fn, sh, ok, tokens=4) == EINVAL
+    assert fn(C.byref(sh), 1, None, 1, BASE, BASE, 0, 0, None) == EINVAL
     assert move(fn, sh, []) == 0 and move(fn, sh, [(BASE, 3, 0), (None, 0, 0)], k=None, v=None) == 0      # nothing to do
 
 
