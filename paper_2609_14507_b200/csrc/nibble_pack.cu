@@ -41,35 +41,80 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
     return r;
 }
 
-struct Group { float zero, scale, inverse; };
-
-// Zero, scale and reciprocal of a group that lies in LANES neighbouring lanes, eight values each.
-template <int LANES>
-__device__ __forceinline__ Group group_of(const uint4& x) {
-    uint32_t lo = min2(min2(x.x, x.y), min2(x.z, x.w)), hi = max2(max2(x.x, x.y), max2(x.z, x.w));
-#pragma unroll
-    for (int d = LANES / 2; d > 0; d >>= 1) {
-        lo = min2(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        hi = max2(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-    }
+// A group's smallest value and the negative of its largest, as bf16 in the low and high half of a word: one minimum serves both.
+__device__ __forceinline__ uint32_t extremes(const uint4& x) {
+    const uint32_t lo = min2(min2(x.x, x.y), min2(x.z, x.w)), hi = max2(max2(x.x, x.y), max2(x.z, x.w)) ^ 0x80008000u;
+    return min2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+}
+// What a group's codes are made with: scale and zero as they are stored (low and high half), and 1 / scale (0: all codes are 0).
+struct Group { uint32_t meta; float inverse; };
+__device__ __forceinline__ Group group_of(uint32_t ends) {
+    const float zero = ptx::bf16_lo(ends), top = -ptx::bf16_hi(ends);
     Group g;
-    g.zero = fminf(ptx::bf16_lo(lo), ptx::bf16_hi(lo));
-    const float top = fmaxf(ptx::bf16_lo(hi), ptx::bf16_hi(hi));
-    g.scale = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(top - g.zero, 15.f)));
-    g.inverse = g.scale >= 0x1p-126f ? __frcp_rn(g.scale) : 0.f;
+    g.meta = ptx::pack_bf16(__fdiv_rn(top - zero, 15.f), zero);
+    const float scale = ptx::bf16_lo(g.meta);
+    g.inverse = scale >= 0x1p-126f ? __frcp_rn(scale) : 0.f;
     return g;
 }
-__device__ __forceinline__ uint32_t meta_of(const Group& g) { return ptx::pack_bf16(g.scale, g.zero); }
+// Groups of eight tokens that LANES neighbouring lanes hold in parts, ends[k] of token k: lane c ends up with token (c & 7)'s whole
+// extremes (each step halves the tokens a lane still carries), and computes that group's scale.  group_k() hands them out.
+template <int LANES>
+__device__ __forceinline__ Group own_group(uint32_t (&ends)[8], int c) {
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+        for (int k = 0; k < d; ++k) {
+            const bool up = c & d;               // keeps tokens k + d, gives away k
+            const uint32_t give = up ? ends[k] : ends[k + d], keep = up ? ends[k + d] : ends[k];
+            ends[k] = min2(keep, __shfl_xor_sync(0xffffffffu, give, d));
+        }
+    uint32_t e = ends[0];
+    if (LANES == 16) e = min2(e, __shfl_xor_sync(0xffffffffu, e, 8));
+    return group_of(e);
+}
+__device__ __forceinline__ Group group_k(const Group& own, int lane, int k) {
+    Group g;
+    g.meta = __shfl_sync(0xffffffffu, own.meta, (lane & 24) | k);
+    g.inverse = __shfl_sync(0xffffffffu, own.inverse, (lane & 24) | k);
+    return g;
+}
 
 // The code of a value in the low bits of a word whose other bits are kMagic's.
-__device__ __forceinline__ uint32_t code_bits(float x, const Group& g) {
-    const float d = __fsub_rn(x, g.zero);
-    const float t = __fmul_rn(d, g.inverse);
-    const float q = __fmaf_rn(__fmaf_rn(-t, g.scale, d), g.inverse, t);
-    return __float_as_uint(__fadd_rn(fminf(q, 15.f), kMagic));
+__device__ __forceinline__ uint32_t code_bits(float x, float scale, float zero, float inverse) {
+    const float d = __fsub_rn(x, zero);
+    const float t = __fmul_rn(d, inverse);
+    const float q = __fmaf_rn(__fmaf_rn(-t, scale, d), inverse, t);
+    return __float_as_uint(__fadd_rn(fminf(q, 15.f), kMagic));           // a NaN becomes 15: no other code is touched
 }
-__device__ __forceinline__ float value_of(uint32_t code, uint32_t meta) {
-    return __fmaf_rn(ptx::bf16_lo(meta), float(code), ptx::bf16_hi(meta));
+
+// Two codes (bits 0..3 of either half of x) -> their two values, rounded to bf16 once: under the exponent of 128 the bits are 128 +
+// code, the difference is exact, and scale * code + zero is one bf16 multiply-add.  meta2: {scale, scale}, {zero, zero}.
+__device__ __forceinline__ uint32_t two_values(uint32_t x, const __nv_bfloat162& scale, const __nv_bfloat162& zero) {
+    const uint32_t y = (x & 0x000f000fu) | 0x43004300u, bias = 0xc300c300u;
+    const __nv_bfloat162 code = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&y), *reinterpret_cast<const __nv_bfloat162*>(&bias));
+    const __nv_bfloat162 v = __hfma2(code, scale, zero);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+struct Meta2 { __nv_bfloat162 scale, zero; };
+__device__ __forceinline__ Meta2 meta2(uint32_t meta) {
+    const uint32_t s = __byte_perm(meta, meta, 0x1010), z = __byte_perm(meta, meta, 0x3232);
+    return Meta2{*reinterpret_cast<const __nv_bfloat162*>(&s), *reinterpret_cast<const __nv_bfloat162*>(&z)};
+}
+// The eight values of a K word (nibble j is column j), in order.
+__device__ __forceinline__ uint4 values_of_k(uint32_t w, uint32_t meta) {
+    const Meta2 m = meta2(meta);
+    const uint32_t v04 = two_values(w, m.scale, m.zero), v15 = two_values(w >> 4, m.scale, m.zero);
+    const uint32_t v26 = two_values(w >> 8, m.scale, m.zero), v37 = two_values(w >> 12, m.scale, m.zero);
+    return make_uint4(__byte_perm(v04, v15, 0x5410), __byte_perm(v26, v37, 0x5410), __byte_perm(v04, v15, 0x7632), __byte_perm(v26, v37, 0x7632));
+}
+// The values of one token in the V words of eight columns: nibble k of each.
+__device__ __forceinline__ uint4 values_of_v(const uint32_t (&w)[8], int k, uint32_t meta) {
+    const Meta2 m = meta2(meta);
+    const uint32_t byte = k >> 1, sel = byte | (4u + byte) << 8;         // byte k/2 of either word into bytes 0 and 2 (what is in 1 and 3 is masked)
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = two_values(__byte_perm(w[2 * i], w[2 * i + 1], sel) >> (4 * (k & 1)), m.scale, m.zero);
+    return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // The span of a tile of the launch.
@@ -139,37 +184,47 @@ __global__ void __launch_bounds__(kThreads) nibble_pack_kernel(const __grid_cons
         for (int i = r; i < kWords / 4; i += D) s_image[su][i] = reinterpret_cast<const uint4*>(job.image)[i];
     __syncthreads();
 
+    const int lane = threadIdx.x & 31;
     uint32_t covered = 0;                        // bits of the nibbles of this thread's V words that the span writes
+    uint32_t ends[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) ends[k] = extremes(kx[k]);
+    Group own = own_group<8>(ends, c);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int t = 32 * w + 8 * (k & 3) + 2 * tt + (k >> 2);
         const bool in = t >= job.first && t < job.end;
         covered |= in ? 15u << (4 * k) : 0u;
-        const Group g = group_of<8>(kx[k]);
+        const Group g = group_k(own, lane, k);
+        const float scale = ptx::bf16_lo(g.meta), zero = ptx::bf16_hi(g.meta);
         const uint32_t x[4] = {kx[k].x, kx[k].y, kx[k].z, kx[k].w};
         uint32_t word = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            word += code_bits(ptx::bf16_lo(x[i]), g) << (8 * i);
-            word += code_bits(ptx::bf16_hi(x[i]), g) << (8 * i + 4);
+            word += code_bits(ptx::bf16_lo(x[i]), scale, zero, g.inverse) << (8 * i);
+            word += code_bits(ptx::bf16_hi(x[i]), scale, zero, g.inverse) << (8 * i + 4);
         }
         if (in) {
             image[nibble_k_word(kPanels, t, c)] = word - kMagicSum;
-            if ((c & 7) == 0) image[kKMeta + nibble_meta_row(t) * kPanels + (c >> 3)] = meta_of(g);
+            if ((c & 7) == 0) image[kKMeta + nibble_meta_row(t) * kPanels + (c >> 3)] = g.meta;
         }
     }
     uint32_t words[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
+    for (int k = 0; k < 8; ++k) ends[k] = extremes(vx[k]);
+    own = own_group<kLanes>(ends, c);
+#pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int t = 32 * w + 8 * (k & 3) + 2 * tt + (k >> 2);
-        const Group g = group_of<kLanes>(vx[k]);
+        const Group g = group_k(own, lane, k);
+        const float scale = ptx::bf16_lo(g.meta), zero = ptx::bf16_hi(g.meta);
         const uint32_t x[4] = {vx[k].x, vx[k].y, vx[k].z, vx[k].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            words[2 * i] += code_bits(ptx::bf16_lo(x[i]), g) << (4 * k);
-            words[2 * i + 1] += code_bits(ptx::bf16_hi(x[i]), g) << (4 * k);
+            words[2 * i] += code_bits(ptx::bf16_lo(x[i]), scale, zero, g.inverse) << (4 * k);
+            words[2 * i + 1] += code_bits(ptx::bf16_hi(x[i]), scale, zero, g.inverse) << (4 * k);
         }
-        if (c == 0 && t >= job.first && t < job.end) image[kVMeta + nibble_meta_row(t)] = meta_of(g);
+        if (c == 0 && t >= job.first && t < job.end) image[kVMeta + nibble_meta_row(t)] = g.meta;
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -208,16 +263,10 @@ __global__ void __launch_bounds__(kThreads) nibble_unpack_kernel(const __grid_co
     for (int k = 0; k < 8; ++k) {
         const int t = 32 * w + 8 * (k & 3) + 2 * tt + (k >> 2);
         if (t < job.first || t >= job.end) continue;
-        const uint32_t kw = image[nibble_k_word(kPanels, t, c)], km = image[kKMeta + nibble_meta_row(t) * kPanels + (c >> 3)];
-        const uint32_t vm = image[kVMeta + nibble_meta_row(t)];
-        uint32_t ko[4], vo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            ko[i] = ptx::pack_bf16(value_of((kw >> (8 * i)) & 15u, km), value_of((kw >> (8 * i + 4)) & 15u, km));
-            vo[i] = ptx::pack_bf16(value_of((words[2 * i] >> (4 * k)) & 15u, vm), value_of((words[2 * i + 1] >> (4 * k)) & 15u, vm));
-        }
-        __stcs(reinterpret_cast<uint4*>(p.k + (job.src + t) * p.k_token + at), make_uint4(ko[0], ko[1], ko[2], ko[3]));
-        __stcs(reinterpret_cast<uint4*>(p.v + (job.src + t) * p.v_token + at), make_uint4(vo[0], vo[1], vo[2], vo[3]));
+        const uint4 ko = values_of_k(image[nibble_k_word(kPanels, t, c)], image[kKMeta + nibble_meta_row(t) * kPanels + (c >> 3)]);
+        const uint4 vo = values_of_v(words, k, image[kVMeta + nibble_meta_row(t)]);
+        __stcs(reinterpret_cast<uint4*>(p.k + (job.src + t) * p.k_token + at), ko);
+        __stcs(reinterpret_cast<uint4*>(p.v + (job.src + t) * p.v_token + at), vo);
     }
 }
 
@@ -253,22 +302,30 @@ __global__ void __launch_bounds__(kThreads) nibble_pack_token_kernel(const __gri
 #pragma unroll
         for (int j = 0; j < 8; ++j) old[j] = job.image[kV + nibble_v_word(8 * c + j, job.t >> 5, (job.t & 7) >> 1)];
     }
-    const Group gk = group_of<8>(kx), gv = group_of<kLanes>(vx);
+    uint32_t ke = extremes(kx), ve = extremes(vx);
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) {
+        ke = min2(ke, __shfl_xor_sync(0xffffffffu, ke, d));
+        ve = min2(ve, __shfl_xor_sync(0xffffffffu, ve, d));
+    }
+    if (kLanes == 16) ve = min2(ve, __shfl_xor_sync(0xffffffffu, ve, 8));
     if (!job.live) return;
+    const Group gk = group_of(ke), gv = group_of(ve);
+    const float ks = ptx::bf16_lo(gk.meta), kz = ptx::bf16_hi(gk.meta), vs = ptx::bf16_lo(gv.meta), vz = ptx::bf16_hi(gv.meta);
     const uint32_t x[4] = {kx.x, kx.y, kx.z, kx.w}, y[4] = {vx.x, vx.y, vx.z, vx.w};
     uint32_t word = 0;
     const int shift = 4 * nibble_v_of(job.t);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        word += code_bits(ptx::bf16_lo(x[i]), gk) << (8 * i);
-        word += code_bits(ptx::bf16_hi(x[i]), gk) << (8 * i + 4);
-        const uint32_t a = code_bits(ptx::bf16_lo(y[i]), gv) & 15u, b = code_bits(ptx::bf16_hi(y[i]), gv) & 15u;
+        word += code_bits(ptx::bf16_lo(x[i]), ks, kz, gk.inverse) << (8 * i);
+        word += code_bits(ptx::bf16_hi(x[i]), ks, kz, gk.inverse) << (8 * i + 4);
+        const uint32_t a = code_bits(ptx::bf16_lo(y[i]), vs, vz, gv.inverse) & 15u, b = code_bits(ptx::bf16_hi(y[i]), vs, vz, gv.inverse) & 15u;
         old[2 * i] = (old[2 * i] & ~(15u << shift)) | (a << shift);
         old[2 * i + 1] = (old[2 * i + 1] & ~(15u << shift)) | (b << shift);
     }
     job.image[nibble_k_word(kPanels, job.t, c)] = word - kMagicSum;
-    if ((c & 7) == 0) job.image[kKMeta + nibble_meta_row(job.t) * kPanels + (c >> 3)] = meta_of(gk);
-    if (c == 0) job.image[kVMeta + nibble_meta_row(job.t)] = meta_of(gv);
+    if ((c & 7) == 0) job.image[kKMeta + nibble_meta_row(job.t) * kPanels + (c >> 3)] = gk.meta;
+    if (c == 0) job.image[kVMeta + nibble_meta_row(job.t)] = gv.meta;
 #pragma unroll
     for (int j = 0; j < 8; ++j) job.image[kV + nibble_v_word(8 * c + j, job.t >> 5, (job.t & 7) >> 1)] = old[j];
 }
@@ -284,16 +341,11 @@ __global__ void __launch_bounds__(kThreads) nibble_unpack_token_kernel(const __g
     const int64_t at = int64_t(job.head) * D * 2 + c * 16;
     const uint32_t kw = job.image[nibble_k_word(kPanels, job.t, c)], km = job.image[kKMeta + nibble_meta_row(job.t) * kPanels + (c >> 3)];
     const uint32_t vm = job.image[kVMeta + nibble_meta_row(job.t)];
-    uint32_t words[8], ko[4], vo[4];
+    uint32_t words[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) words[j] = job.image[kV + nibble_v_word(8 * c + j, job.t >> 5, (job.t & 7) >> 1)] >> (4 * nibble_v_of(job.t));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        ko[i] = ptx::pack_bf16(value_of((kw >> (8 * i)) & 15u, km), value_of((kw >> (8 * i + 4)) & 15u, km));
-        vo[i] = ptx::pack_bf16(value_of(words[2 * i] & 15u, vm), value_of(words[2 * i + 1] & 15u, vm));
-    }
-    *reinterpret_cast<uint4*>(p.k + job.src * p.k_token + at) = make_uint4(ko[0], ko[1], ko[2], ko[3]);
-    *reinterpret_cast<uint4*>(p.v + job.src * p.v_token + at) = make_uint4(vo[0], vo[1], vo[2], vo[3]);
+    for (int j = 0; j < 8; ++j) words[j] = job.image[kV + nibble_v_word(8 * c + j, job.t >> 5, (job.t & 7) >> 1)];
+    *reinterpret_cast<uint4*>(p.k + job.src * p.k_token + at) = values_of_k(kw, km);
+    *reinterpret_cast<uint4*>(p.v + job.src * p.v_token + at) = values_of_v(words, nibble_v_of(job.t), vm);
 }
 
 cudaError_t launch(const NibbleMove& a, bool single, void (*tile64)(NibbleMove), void (*tile128)(NibbleMove), void (*token64)(NibbleMove),
