@@ -8,9 +8,9 @@
 // q + (d - q scale) r with fused multiply-adds: Markstein's theorem (IBM J. Res. Dev. 34, 1990) gives the rounded
 // quotient from a rounded reciprocal.  Adding 1.5 * 2^23 then leaves the code in the low bits of the sum.
 //
-// Bound by memory (per token and head of 128 columns: 512 bytes on the bf16 side, 140 on the 4-bit side).  One tile (64 tokens of one head)
-// at a time: D threads, thread (c, w, t) takes the 8 columns 8c.. of the eight tokens 32w + 8i + 2t + e, which are exactly
-// the tokens that share its words of V.  All 16 loads of a thread are issued before the first is used.  Groups are reduced
+// Bound by memory (per token and head of 128 columns: 512 bytes on the bf16 side, 140 on the 4-bit side).  K or V of one tile (64 tokens
+// of one head) at a time: D threads, thread (c, w, t) takes the 8 columns 8c.. of the eight tokens 32w + 8i + 2t + e, which are
+// exactly the tokens that share its words of V.  All 8 loads of a thread are issued before the first is used.  Groups are reduced
 // among the lanes of a token by shuffles; the tile's image is put together in shared memory and leaves in 16-byte stores.
 // A tile that the span covers in part keeps the other tokens' codes: its image is loaded first.
 //
@@ -46,14 +46,14 @@ __device__ __forceinline__ uint32_t extremes(const uint4& x) {
     const uint32_t lo = min2(min2(x.x, x.y), min2(x.z, x.w)), hi = max2(max2(x.x, x.y), max2(x.z, x.w)) ^ 0x80008000u;
     return min2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
 }
-// What a group's codes are made with: scale and zero as they are stored (low and high half), and 1 / scale (0: all codes are 0).
-struct Group { uint32_t meta; float inverse; };
+// What a group's codes are made with: scale and zero as they are stored (low and high half), and 1 / (16 scale) (0: all codes are 0).
+struct Group { uint32_t meta; float inverse16; };
 __device__ __forceinline__ Group group_of(uint32_t ends) {
     const float zero = ptx::bf16_lo(ends), top = -ptx::bf16_hi(ends);
     Group g;
     g.meta = ptx::pack_bf16(__fdiv_rn(top - zero, 15.f), zero);
     const float scale = ptx::bf16_lo(g.meta);
-    g.inverse = scale >= 0x1p-126f ? __frcp_rn(scale) : 0.f;
+    g.inverse16 = scale >= 0x1p-126f ? __frcp_rn(scale) * 0.0625f : 0.f;
     return g;
 }
 // Groups of eight tokens that LANES neighbouring lanes hold in parts, ends[k] of token k: lane c ends up with token (c & 7)'s whole
@@ -75,16 +75,18 @@ __device__ __forceinline__ Group own_group(uint32_t (&ends)[8], int c) {
 __device__ __forceinline__ Group group_k(const Group& own, int lane, int k) {
     Group g;
     g.meta = __shfl_sync(0xffffffffu, own.meta, (lane & 24) | k);
-    g.inverse = __shfl_sync(0xffffffffu, own.inverse, (lane & 24) | k);
+    g.inverse16 = __shfl_sync(0xffffffffu, own.inverse16, (lane & 24) | k);
     return g;
 }
 
-// The code of a value in the low bits of a word whose other bits are kMagic's.
-__device__ __forceinline__ uint32_t code_bits(float x, float scale, float zero, float inverse) {
+// The code of a value in the low bits of a word whose other bits are kMagic's.  Everything is done on a sixteenth of the code, so that
+// the last multiply-add can saturate to [0, 1]: a NaN becomes 0 there, and no value touches another one's code.
+__device__ __forceinline__ uint32_t code_bits(float x, float scale16, float zero, float inverse16) {
     const float d = __fsub_rn(x, zero);
-    const float t = __fmul_rn(d, inverse);
-    const float q = __fmaf_rn(__fmaf_rn(-t, scale, d), inverse, t);
-    return __float_as_uint(__fadd_rn(fminf(q, 15.f), kMagic));           // a NaN becomes 15: no other code is touched
+    const float t = __fmul_rn(d, inverse16);
+    float q;
+    asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(q) : "f"(__fmaf_rn(-t, scale16, d)), "f"(inverse16), "f"(t));
+    return __float_as_uint(__fmaf_rn(q, 16.f, kMagic));
 }
 
 // Two codes (bits 0..3 of either half of x) -> their two values, rounded to bf16 once: under the exponent of 128 the bits are 128 +
@@ -156,117 +158,126 @@ __device__ __forceinline__ TileJob tile_job(const NibbleMove& p, int64_t unit) {
 template <int D>
 __global__ void __launch_bounds__(kThreads) nibble_pack_kernel(const __grid_constant__ NibbleMove p) {
     constexpr int kLanes = D / 8, kUnits = kThreads / D, kPanels = D / 64;
-    constexpr int kWords = (64 * D + 256 * (kPanels + 1)) / 4, kKMeta = 8 * D, kV = kKMeta + 64 * kPanels, kVMeta = kV + 8 * D;
-    __shared__ uint4 s_image[kUnits][kWords / 4];
+    constexpr int kKWords = 8 * D + 64 * kPanels, kVWords = 8 * D + 64;          // of either half of a tile
+    __shared__ uint4 s_image[kUnits][kKWords / 4];
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const int su = threadIdx.x / D, r = threadIdx.x % D;
+    const int su = threadIdx.x / D, r = threadIdx.x % D, lane = threadIdx.x & 31;
     const int c = r % kLanes, wt = r / kLanes, w = wt >> 2, tt = wt & 3;
-    const TileJob job = tile_job<D>(p, int64_t(blockIdx.x) * kUnits + su);
+    const int64_t unit = int64_t(blockIdx.x) * kUnits + su;
+    const bool is_v = unit & 1;
+    const TileJob job = tile_job<D>(p, unit >> 1);
     uint32_t* image = reinterpret_cast<uint32_t*>(s_image[su]);
+    uint4* const out = reinterpret_cast<uint4*>(job.image + (is_v ? 4 * kKWords : 0));
+    const int n16 = (is_v ? kVWords : kKWords) / 4;
     const bool whole = job.live && job.first == 0 && job.end == kTileTokens;
 
-    uint4 kx[8], vx[8];
-    const int64_t at = int64_t(job.head) * D * 2 + c * 16;
+    // token k = i + 4e of this thread: 32w + 8i + 2tt + e
+    const int t0 = 32 * w + 2 * tt;
+    auto token = [&](int k) { return t0 + 8 * (k & 3) + (k >> 2); };
+    uint4 x[8];
+    uint32_t in = 0;                             // which of the eight the span covers
+    {
+        const int64_t pitch = is_v ? p.v_token : p.k_token;
+        const char* src = (is_v ? p.v : p.k) + (job.src + t0) * pitch + int64_t(job.head) * D * 2 + c * 16;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int t = 32 * w + 8 * (k & 3) + 2 * tt + (k >> 2);
-        const bool in = t >= job.first && t < job.end;
-        kx[k] = in ? __ldcs(reinterpret_cast<const uint4*>(p.k + (job.src + t) * p.k_token + at)) : make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < 8; ++k) {
+            const bool there = token(k) >= job.first && token(k) < job.end;
+            in |= there ? 1u << k : 0u;
+            x[k] = there ? __ldcs(reinterpret_cast<const uint4*>(src + (8 * (k & 3) + (k >> 2)) * pitch)) : make_uint4(0, 0, 0, 0);
+        }
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int t = 32 * w + 8 * (k & 3) + 2 * tt + (k >> 2);
-        const bool in = t >= job.first && t < job.end;
-        vx[k] = in ? __ldcs(reinterpret_cast<const uint4*>(p.v + (job.src + t) * p.v_token + at)) : make_uint4(0, 0, 0, 0);
+    if (job.live && !whole) {
+        for (int i = r; i < n16; i += D) s_image[su][i] = out[i];
     }
-    if (job.live && !whole)
-        for (int i = r; i < kWords / 4; i += D) s_image[su][i] = reinterpret_cast<const uint4*>(job.image)[i];
-    __syncthreads();
-
-    const int lane = threadIdx.x & 31;
-    uint32_t covered = 0;                        // bits of the nibbles of this thread's V words that the span writes
     uint32_t ends[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) ends[k] = extremes(kx[k]);
-    Group own = own_group<8>(ends, c);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int t = 32 * w + 8 * (k & 3) + 2 * tt + (k >> 2);
-        const bool in = t >= job.first && t < job.end;
-        covered |= in ? 15u << (4 * k) : 0u;
-        const Group g = group_k(own, lane, k);
-        const float scale = ptx::bf16_lo(g.meta), zero = ptx::bf16_hi(g.meta);
-        const uint32_t x[4] = {kx[k].x, kx[k].y, kx[k].z, kx[k].w};
-        uint32_t word = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            word += code_bits(ptx::bf16_lo(x[i]), scale, zero, g.inverse) << (8 * i);
-            word += code_bits(ptx::bf16_hi(x[i]), scale, zero, g.inverse) << (8 * i + 4);
-        }
-        if (in) {
-            image[nibble_k_word(kPanels, t, c)] = word - kMagicSum;
-            if ((c & 7) == 0) image[kKMeta + nibble_meta_row(t) * kPanels + (c >> 3)] = g.meta;
-        }
-    }
+    for (int k = 0; k < 8; ++k) ends[k] = extremes(x[k]);
+    const Group own = is_v ? own_group<kLanes>(ends, c) : own_group<8>(ends, c);
+    __syncthreads();
+
+    const int row0 = nibble_meta_row(t0);
     uint32_t words[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) ends[k] = extremes(vx[k]);
-    own = own_group<kLanes>(ends, c);
-#pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int t = 32 * w + 8 * (k & 3) + 2 * tt + (k >> 2);
         const Group g = group_k(own, lane, k);
-        const float scale = ptx::bf16_lo(g.meta), zero = ptx::bf16_hi(g.meta);
-        const uint32_t x[4] = {vx[k].x, vx[k].y, vx[k].z, vx[k].w};
+        const float scale16 = 16.f * ptx::bf16_lo(g.meta), zero = ptx::bf16_hi(g.meta);
+        const uint32_t xx[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+        const int row = row0 + 16 * ((k & 3) >> 1) + 2 * (k >> 2) + (k & 1);
+        uint32_t bits[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            words[2 * i] += code_bits(ptx::bf16_lo(x[i]), scale, zero, g.inverse) << (4 * k);
-            words[2 * i + 1] += code_bits(ptx::bf16_hi(x[i]), scale, zero, g.inverse) << (4 * k);
+            bits[2 * i] = code_bits(ptx::bf16_lo(xx[i]), scale16, zero, g.inverse16);
+            bits[2 * i + 1] = code_bits(ptx::bf16_hi(xx[i]), scale16, zero, g.inverse16);
         }
-        if (c == 0 && t >= job.first && t < job.end) image[kVMeta + nibble_meta_row(t)] = g.meta;
-    }
+        if (is_v) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        uint32_t& dst = image[kV + nibble_v_word(8 * c + j, w, tt)];
-        const uint32_t word = words[j] - kMagicSum;
-        if (whole) dst = word;
-        else if (covered) dst = (dst & ~covered) | (word & covered);
+            for (int j = 0; j < 8; ++j) words[j] += bits[j] << (4 * k);
+            if (c == 0 && (in >> k & 1)) image[8 * D + row] = g.meta;
+        } else {
+            uint32_t word = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) word += bits[j] << (4 * j);
+            if (in >> k & 1) {
+                image[nibble_k_word(kPanels, t0, c) + ((k & 3) >> 1) * kPanels * 128 + (k >> 2) * 16 + (k & 1) * 2] = word - kMagicSum;
+                if ((c & 7) == 0) image[8 * D + row * kPanels + (c >> 3)] = g.meta;
+            }
+        }
+    }
+    if (is_v) {
+        uint32_t covered = 0;                    // bits of the nibbles that the span writes
+#pragma unroll
+        for (int k = 0; k < 8; ++k) covered |= (in >> k & 1) ? 15u << (4 * k) : 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint32_t& dst = image[nibble_v_word(8 * c, w, tt) + 16 * j];
+            const uint32_t word = words[j] - kMagicSum;
+            if (whole) dst = word;
+            else if (covered) dst = (dst & ~covered) | (word & covered);
+        }
     }
     __syncthreads();
     if (job.live)
-        for (int i = r; i < kWords / 4; i += D) reinterpret_cast<uint4*>(job.image)[i] = s_image[su][i];
+        for (int i = r; i < n16; i += D) out[i] = s_image[su][i];
 }
 
 template <int D>
 __global__ void __launch_bounds__(kThreads) nibble_unpack_kernel(const __grid_constant__ NibbleMove p) {
     constexpr int kLanes = D / 8, kUnits = kThreads / D, kPanels = D / 64;
-    constexpr int kWords = (64 * D + 256 * (kPanels + 1)) / 4, kKMeta = 8 * D, kV = kKMeta + 64 * kPanels, kVMeta = kV + 8 * D;
-    __shared__ uint4 s_image[kUnits][kWords / 4];
+    constexpr int kKWords = 8 * D + 64 * kPanels, kVWords = 8 * D + 64;
+    __shared__ uint4 s_image[kUnits][kKWords / 4];
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     const int su = threadIdx.x / D, r = threadIdx.x % D;
     const int c = r % kLanes, wt = r / kLanes, w = wt >> 2, tt = wt & 3;
-    const TileJob job = tile_job<D>(p, int64_t(blockIdx.x) * kUnits + su);
+    const int64_t unit = int64_t(blockIdx.x) * kUnits + su;
+    const bool is_v = unit & 1;
+    const TileJob job = tile_job<D>(p, unit >> 1);
     const uint32_t* image = reinterpret_cast<const uint32_t*>(s_image[su]);
     if (job.live) {
+        const uint4* from = reinterpret_cast<const uint4*>(job.image + (is_v ? 4 * kKWords : 0));
+        const int n16 = (is_v ? kVWords : kKWords) / 4;
 #pragma unroll
-        for (int i = 0; i < (kWords / 4 + D - 1) / D; ++i)
-            if (i * D + r < kWords / 4) s_image[su][i * D + r] = reinterpret_cast<const uint4*>(job.image)[i * D + r];
+        for (int i = 0; i < (kKWords / 4 + D - 1) / D; ++i)
+            if (i * D + r < n16) s_image[su][i * D + r] = from[i * D + r];
     }
     __syncthreads();
+    const int t0 = 32 * w + 2 * tt, row0 = nibble_meta_row(t0);
+    const int64_t pitch = is_v ? p.v_token : p.k_token;
+    char* dst = (is_v ? p.v : p.k) + (job.src + t0) * pitch + int64_t(job.head) * D * 2 + c * 16;
     uint32_t words[8];
+    if (is_v) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) words[j] = image[kV + nibble_v_word(8 * c + j, w, tt)];
-    const int64_t at = int64_t(job.head) * D * 2 + c * 16;
+        for (int j = 0; j < 8; ++j) words[j] = image[nibble_v_word(8 * c, w, tt) + 16 * j];
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int t = 32 * w + 8 * (k & 3) + 2 * tt + (k >> 2);
+        const int t = t0 + 8 * (k & 3) + (k >> 2), row = row0 + 16 * ((k & 3) >> 1) + 2 * (k >> 2) + (k & 1);
         if (t < job.first || t >= job.end) continue;
-        const uint4 ko = values_of_k(image[nibble_k_word(kPanels, t, c)], image[kKMeta + nibble_meta_row(t) * kPanels + (c >> 3)]);
-        const uint4 vo = values_of_v(words, k, image[kVMeta + nibble_meta_row(t)]);
-        __stcs(reinterpret_cast<uint4*>(p.k + (job.src + t) * p.k_token + at), ko);
-        __stcs(reinterpret_cast<uint4*>(p.v + (job.src + t) * p.v_token + at), vo);
+        const uint4 v = is_v ? values_of_v(words, k, image[8 * D + row])
+                             : values_of_k(image[nibble_k_word(kPanels, t0, c) + ((k & 3) >> 1) * kPanels * 128 + (k >> 2) * 16 + (k & 1) * 2],
+                                           image[8 * D + row * kPanels + (c >> 3)]);
+        __stcs(reinterpret_cast<uint4*>(dst + (8 * (k & 3) + (k >> 2)) * pitch), v);
     }
 }
 
@@ -311,15 +322,15 @@ __global__ void __launch_bounds__(kThreads) nibble_pack_token_kernel(const __gri
     if (kLanes == 16) ve = min2(ve, __shfl_xor_sync(0xffffffffu, ve, 8));
     if (!job.live) return;
     const Group gk = group_of(ke), gv = group_of(ve);
-    const float ks = ptx::bf16_lo(gk.meta), kz = ptx::bf16_hi(gk.meta), vs = ptx::bf16_lo(gv.meta), vz = ptx::bf16_hi(gv.meta);
+    const float ks = 16.f * ptx::bf16_lo(gk.meta), kz = ptx::bf16_hi(gk.meta), vs = 16.f * ptx::bf16_lo(gv.meta), vz = ptx::bf16_hi(gv.meta);
     const uint32_t x[4] = {kx.x, kx.y, kx.z, kx.w}, y[4] = {vx.x, vx.y, vx.z, vx.w};
     uint32_t word = 0;
     const int shift = 4 * nibble_v_of(job.t);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        word += code_bits(ptx::bf16_lo(x[i]), ks, kz, gk.inverse) << (8 * i);
-        word += code_bits(ptx::bf16_hi(x[i]), ks, kz, gk.inverse) << (8 * i + 4);
-        const uint32_t a = code_bits(ptx::bf16_lo(y[i]), vs, vz, gv.inverse) & 15u, b = code_bits(ptx::bf16_hi(y[i]), vs, vz, gv.inverse) & 15u;
+        word += code_bits(ptx::bf16_lo(x[i]), ks, kz, gk.inverse16) << (8 * i);
+        word += code_bits(ptx::bf16_hi(x[i]), ks, kz, gk.inverse16) << (8 * i + 4);
+        const uint32_t a = code_bits(ptx::bf16_lo(y[i]), vs, vz, gv.inverse16) & 15u, b = code_bits(ptx::bf16_hi(y[i]), vs, vz, gv.inverse16) & 15u;
         old[2 * i] = (old[2 * i] & ~(15u << shift)) | (a << shift);
         old[2 * i + 1] = (old[2 * i + 1] & ~(15u << shift)) | (b << shift);
     }
@@ -351,7 +362,7 @@ __global__ void __launch_bounds__(kThreads) nibble_unpack_token_kernel(const __g
 cudaError_t launch(const NibbleMove& a, bool single, void (*tile64)(NibbleMove), void (*tile128)(NibbleMove), void (*token64)(NibbleMove),
                    void (*token128)(NibbleMove), cudaStream_t s) {
     const bool wide = a.g.dim == 128;
-    const int64_t units = int64_t(single ? a.n_spans : a.n_tiles) * a.g.n_kv_heads;
+    const int64_t units = int64_t(single ? a.n_spans : 2 * int64_t(a.n_tiles)) * a.g.n_kv_heads;     // K and V of a tile apart
     const int per_cta = single ? kThreads / (a.g.dim / 8) : kThreads / a.g.dim;
     const int64_t grid = (units + per_cta - 1) / per_cta;
     if (grid > INT32_MAX) return cudaErrorInvalidValue;
