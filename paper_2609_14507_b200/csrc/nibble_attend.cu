@@ -28,9 +28,10 @@
 // One warp works on one tile (64 tokens of a KV head) at a time, alone: its online softmax has its own reference maximum, raised
 // only when a score exceeds it by 2^8 (then everything is rescaled), which costs one vote per tile in place of a reduction over lanes.  A
 // producer warp streams tiles (one bulk copy each, they are contiguous) into a ring of stages on mbarriers; the warps of a CTA
-// take them in turn.  At the end of a (row, head group) the warps' states are joined through shared memory, in a fixed order.
+// take them in turn.  At the end of a (row, head group) every warp writes its partial and goes on, and a second kernel joins the partials
+// in a fixed order.  (Joining a CTA's warps through shared memory first made each wait for the slowest: 2.7 us per pair and CTA.)
 // More than 8 query heads per KV head: several warps (one per octet of heads) share a tile, so it is still read once.
-// Every wait is bounded; a warp whose wait ran out does no more work but still comes to the barriers, so nobody waits for it.
+// Every wait is bounded; a warp whose wait ran out does no more work.
 #include <cuda_fp16.h>
 
 #include "kernels.h"
@@ -73,9 +74,11 @@ using Smem = NibbleSmem;
 __device__ __forceinline__ NibbleRowArg row_at(const NibbleAttend& p, int i) { return p.rows ? p.rows[i] : p.row[i]; }
 __device__ __forceinline__ NibbleRunArg run_at(const NibbleAttend& p, int i) { return p.runs ? p.runs[i] : p.run[i]; }
 
-// A chunk's walk over (row, head group) pairs: which pair unit u belongs to, and how many of the chunk's tiles follow in it.
+// A chunk's walk over (row, head group) pairs: the pair that unit u belongs to, and how many of the chunk's tiles follow in it.
 struct Pair {
-    int row, gh, tile0, n, slot;
+    NibbleRowArg r;
+    int row, kv, part;           // row, KV head, and which part of its query heads
+    int tile0, n, slot;
 };
 __device__ __forceinline__ Pair pair_at(const NibbleAttend& p, int u, int u1) {
     int lo = 0, hi = p.n_rows - 1;
@@ -83,27 +86,40 @@ __device__ __forceinline__ Pair pair_at(const NibbleAttend& p, int u, int u1) {
         const int mid = (lo + hi + 1) >> 1;
         if (row_at(p, mid).unit0 <= u) lo = mid; else hi = mid - 1;
     }
-    const NibbleRowArg r = row_at(p, lo);
     Pair x;
+    x.r = row_at(p, lo);
     x.row = lo;
-    x.gh = (u - r.unit0) / r.tiles;
-    x.tile0 = (u - r.unit0) - x.gh * r.tiles;
-    x.n = min(r.tiles - x.tile0, u1 - u);
-    x.slot = int(blockIdx.x) + r.pair0 + x.gh;
+    const int gh = (u - x.r.unit0) / x.r.tiles;
+    x.tile0 = (u - x.r.unit0) - gh * x.r.tiles;
+    x.kv = p.groups_per_kv == 1 ? gh : gh / p.groups_per_kv;
+    x.part = gh - x.kv * p.groups_per_kv;
+    x.n = min(x.r.tiles - x.tile0, u1 - u);
+    x.slot = int(blockIdx.x) + x.r.pair0 + gh;
     return x;
+}
+// The next pair of the chunk, u its first unit.
+__device__ __forceinline__ void next_pair(const NibbleAttend& p, Pair& x, int u, int u1) {
+    ++x.slot;
+    if (++x.part == p.groups_per_kv) {
+        x.part = 0;
+        if (++x.kv == p.g.n_kv_heads) {
+            x.kv = 0;
+            do x.r = row_at(p, ++x.row); while (x.r.tiles == 0);
+        }
+    }
+    x.tile0 = 0;
+    x.n = min(x.r.tiles, u1 - u);
 }
 
 template <int D, bool HALF>                      // HALF: at most 4 query heads per KV head
 __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kernel(const __grid_constant__ NibbleAttend p) {
     constexpr int P = D / 64;
     constexpr int kTile = 64 * D + 256 * (P + 1), kKMeta = 32 * D, kV = kKMeta + 256 * P, kVMeta = kV + 32 * D;
-    constexpr int kPitch = D + 4;                // floats of a head's row in the joining buffer: heads 0, 2, 4, 6 on distinct banks
     extern __shared__ unsigned char smem_dyn[];
     unsigned char* ring = smem_dyn + ((128u - (ptx::smem_addr(smem_dyn) & 127u)) & 127u);
     Smem& sm = *reinterpret_cast<Smem*>(ring + p.stages * kTile);
-    float* joined = reinterpret_cast<float*>(ring + p.stages * kTile + sizeof(Smem));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int stages = p.stages, octets = p.octets, teams = kWarps / octets;
+    const int stages = p.stages, octets = p.octets, teams = p.teams;
     if (tid == 0) {
         for (int s = 0; s < stages; ++s) {
             ptx::mbar_init(ptx::smem_addr(&sm.full[s]), 1);
@@ -111,11 +127,12 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         }
         ptx::mbar_fence_init();
     }
+    // The tables are launch parameters, or were there before the previous kernel of the stream began: they may be read under its tail.
+    const int u0 = int(int64_t(p.n_units) * blockIdx.x / p.n_ctas), u1 = int(int64_t(p.n_units) * (blockIdx.x + 1) / p.n_ctas);
+    Pair x = pair_at(p, u0, u1);
     __syncthreads();
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-
-    const int u0 = int(int64_t(p.n_units) * blockIdx.x / p.n_ctas), u1 = int(int64_t(p.n_units) * (blockIdx.x + 1) / p.n_ctas);
 
     if (warp == kWarps) {
         // ---------------- producer ----------------
@@ -124,9 +141,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         int st = 0, lap = 0;
         bool ok = true;
         for (int u = u0; u < u1 && ok;) {
-            const Pair x = pair_at(p, u, u1);
-            const int kv = x.gh / p.groups_per_kv;
-            int k = row_at(p, x.row).run0, hi = (x.row + 1 < p.n_rows ? row_at(p, x.row + 1).run0 : p.n_runs) - 1;
+            int k = x.r.run0, hi = (x.row + 1 < p.n_rows ? row_at(p, x.row + 1).run0 : p.n_runs) - 1;
             while (k < hi) {                     // the row's last run that begins at or before the first tile
                 const int mid = (k + hi + 1) >> 1;
                 if (run_at(p, mid).tile0 <= x.tile0) k = mid; else hi = mid - 1;
@@ -136,12 +151,12 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             const int64_t to_next_block = p.g.block_bytes() - int64_t(per - 1) * kTile;
             NibbleRunArg run = run_at(p, k);
             int tile = x.tile0 - run.tile0, left = run.n_tokens - tile * kTileTokens, in_block = tile % per;
-            const char* src = run.blocks + p.g.tile_off(tile, kv);
+            const char* src = run.blocks + p.g.tile_off(tile, x.kv);
             for (int i = 0; i < x.n; ++i) {
                 if (left <= 0) {
                     run = run_at(p, ++k);
                     left = run.n_tokens; in_block = 0;
-                    src = run.blocks + p.g.tile_off(0, kv);
+                    src = run.blocks + p.g.tile_off(0, x.kv);
                 }
                 if (lap > 0 && !ptx::mbar_wait(ptx::smem_addr(&sm.empty[st]), (lap - 1) & 1)) { ok = false; break; }
                 sm.n_valid[st] = left < kTileTokens ? left : kTileTokens;
@@ -155,6 +170,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 if (++st == stages) { st = 0; ++lap; }
             }
             u += x.n;
+            if (u < u1) next_pair(p, x, u, u1);
         }
         if (!ok && p.status) atomicOr(p.status, kStatusNoFreeStage);
         // do not leave the CTA while copies of ours may still be in flight
@@ -170,17 +186,12 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
     const int team = warp / octets, octet = warp - team * octets;
     const bool works = team < teams;
     bool dead = false;
-    auto sync = [&]() {
-        __syncwarp();
-        asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-    };
 
     int it0 = 0;                                 // tiles of this CTA before the current pair
     int st = team, phase = 0;                    // stage of the team's next tile and its parity (stages is a multiple of teams)
     for (int u = u0; u < u1;) {
-        const Pair x = pair_at(p, u, u1);
-        const int in_kv = (x.gh % p.groups_per_kv) * p.rows_per_part;      // the head group's first head among those of its KV head
-        const int n_heads = min(p.group - in_kv, p.rows_per_part), head0 = (x.gh / p.groups_per_kv) * p.group + in_kv;
+        const int in_kv = x.part * p.rows_per_part;      // the head group's first head among those of its KV head
+        const int n_heads = min(p.group - in_kv, p.rows_per_part), head0 = x.kv * p.group + in_kv;
 
         // ---- queries: operands of head g (columns 64p+16t+8w+{0,4},{1,5},{2,6},{3,7}), normalised to [2^14, 2^15) ----
         uint32_t qf[P][2][4];
@@ -391,91 +402,45 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             if (st >= stages) { st -= stages; phase ^= 1; }
         }
 
-        // ---- join the teams' states into the pair's partial ----
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int d = 4; d <= 16; d <<= 1) {
-                l[e] += __shfl_xor_sync(0xffffffffu, l[e], d);
-                oz[e] += __shfl_xor_sync(0xffffffffu, oz[e], d);
-            }
-        if (HALF) {
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[d][i] += __shfl_xor_sync(0xffffffffu, o[d][i], 2);
-        }
-        const float undo = fv > 0.f ? 0x1p15f : 0.f, inv_fv = fv > 0.f ? 1.f / fv : 0.f;   // 2^21 / 64, then 1 / fv
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[d][i] = fmaf(o[d][i] * undo, inv_fv, oz[i & 1]);
-
-        const int n_act = min(x.n, teams);       // teams with tiles of this pair, from team it0 % teams on
-        int turn_of = team - it0 % teams;
-        if (turn_of < 0) turn_of += teams;
-        const bool active = works && turn_of < n_act;
-        float big_m[2] = {m[0], m[1]}, sum_l[2] = {l[0], l[1]};
-        if (n_act > 1) {
-            if (g == 0) { sm.m[warp][2 * t] = m[0]; sm.m[warp][2 * t + 1] = m[1]; sm.l[warp][2 * t] = l[0]; sm.l[warp][2 * t + 1] = l[1]; }
-            sync();
+        // ---- the warp's partial: every team writes its own (nobody waits for another warp), one without a tile an empty one ----
+        if (works) {
+            float f[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float mm = -INFINITY, ll = 0.f;
-                for (int k = 0; k < n_act; ++k) mm = fmaxf(mm, sm.m[(it0 + k) % teams * octets + octet][2 * t + e]);
-                for (int k = 0; k < n_act; ++k) {
-                    const int wk = (it0 + k) % teams * octets + octet;
-                    const float mk = sm.m[wk][2 * t + e];
-                    if (mk != -INFINITY) ll += ptx::ex2(mk - mm) * sm.l[wk][2 * t + e];
+#pragma unroll
+                for (int d = 4; d <= 16; d <<= 1) {
+                    l[e] += __shfl_xor_sync(0xffffffffu, l[e], d);
+                    oz[e] += __shfl_xor_sync(0xffffffffu, oz[e], d);
                 }
-                big_m[e] = mm; sum_l[e] = ll;
+                f[e] = l[e] > 0.f ? 1.f / l[e] : 0.f;
             }
-        }
-        float f[2];
+            const float undo = fv > 0.f ? 0x1p15f : 0.f, inv_fv = fv > 0.f ? 1.f / fv : 0.f;   // 2^21 / 64, then 1 / fv
+            const int hb = octet * 8 + 2 * t;    // of the head group
+            const int64_t row0 = (int64_t(x.slot) * teams + team) * p.rows_per_part + hb;
+            const bool inside = !kChecked || (row0 >= 0 && row0 + min(2, n_heads - hb) <= p.part_rows);      // the partial must lie inside the scratch
+            if (kChecked && !inside && hb < n_heads && p.status) atomicOr(p.status, kStatusBadIndex);
+            const bool writes = (!HALF || t < 2) && inside;
+            float* dst = p.part_o + row0 * D + g;
+            if (x.n > (team - it0 % teams + teams) % teams) {            // the team had a tile
 #pragma unroll
-        for (int e = 0; e < 2; ++e) f[e] = (m[e] != -INFINITY && sum_l[e] > 0.f) ? ptx::ex2(m[e] - big_m[e]) / sum_l[e] : 0.f;
+                for (int d = 0; d < D / 16; ++d) {
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[d][i] *= f[i & 1];
-        float* buf = joined + (octet * 8 + 2 * t) * kPitch + g;
-        const int hb = octet * 8 + 2 * t;        // of the head group
-        const bool writes = (!HALF || t < 2);
-        for (int turn = 0; turn < n_act; ++turn) {
-            if (active && turn == turn_of) {
-                if (turn > 0) {
-#pragma unroll
-                    for (int d = 0; d < D / 16; ++d) {
-                        o[d][0] += buf[16 * d]; o[d][1] += buf[16 * d + kPitch];
-                        o[d][2] += buf[16 * d + 8]; o[d][3] += buf[16 * d + 8 + kPitch];
+                    for (int i = 0; i < 4; ++i) {
+                        if (HALF) o[d][i] += __shfl_xor_sync(0xffffffffu, o[d][i], 2);
+                        o[d][i] = fmaf(o[d][i] * undo, inv_fv, oz[i & 1]) * f[i & 1];
                     }
-                }
-                if (turn + 1 < n_act) {
 #pragma unroll
-                    for (int d = 0; d < D / 16; ++d) {
-                        buf[16 * d] = o[d][0]; buf[16 * d + kPitch] = o[d][1];
-                        buf[16 * d + 8] = o[d][2]; buf[16 * d + 8 + kPitch] = o[d][3];
-                    }
-                } else if (writes) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        if (hb + e >= n_heads) continue;
-                        const int64_t row = int64_t(x.slot) * p.rows_per_part + hb + e;
-                        if (kChecked && (row < 0 || row >= p.part_rows)) {       // the partial must lie inside the scratch
-                            if (p.status) atomicOr(p.status, kStatusBadIndex);
-                            continue;
-                        }
-                        float* dst = p.part_o + row * D + g;
-#pragma unroll
-                        for (int d = 0; d < D / 16; ++d) { dst[16 * d] = o[d][e]; dst[16 * d + 8] = o[d][2 + e]; }
-                        if (g == 0) p.part_ml[row] = make_float2(big_m[e], sum_l[e]);
-                    }
+                    for (int e = 0; e < 2; ++e)
+                        if (writes && hb + e < n_heads) { dst[e * D + 16 * d] = o[d][e]; dst[e * D + 16 * d + 8] = o[d][2 + e]; }
                 }
             }
-            if (turn + 1 < n_act) sync();
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (g == 0 && writes && hb + e < n_heads) p.part_ml[row0 + e] = make_float2(m[e], l[e]);
         }
         it0 = it_end;
         u += x.n;
+        if (u < u1) next_pair(p, x, u, u1);
     }
 }
 
@@ -488,27 +453,30 @@ __global__ void __launch_bounds__(THREADS) nibble_reduce_kernel(const __grid_con
     constexpr int kCols = COLS / 4, kSlices = THREADS / kCols, kSlabs = D / COLS;
     __shared__ float4 s_o[kSlices][kCols];
     __shared__ float s_z[kSlices], s_m[THREADS / 32];
-    ptx::grid_dependency_wait();
-    ptx::grid_launch_dependents();
     const int item = blockIdx.x / kSlabs, slab = blockIdx.x - item * kSlabs;     // item: row * n_q_heads + head
     const int row = item / p.n_q_heads, head = item - row * p.n_q_heads;
     const NibbleRowArg r = row_at(p, row);
     const int tid = threadIdx.x, col = tid % kCols, slice = tid / kCols;
     float4* out = reinterpret_cast<float4*>(p.out_o + int64_t(item) * D + slab * COLS) + col;
-    if (r.tiles == 0) {                          // nothing attended: (0, -inf)
+    const int kv = head / p.group, in_kv = head - kv * p.group, part_of = in_kv / p.rows_per_part, rin = in_kv - part_of * p.rows_per_part;
+    const int gh = kv * p.groups_per_kv + part_of, teams = p.teams;
+    const int64_t a = int64_t(r.unit0) + int64_t(gh) * r.tiles, b = a + r.tiles - 1;
+    const int j = r.pair0 + gh;
+    int e0 = 0, n = 0;
+    if (r.tiles > 0) {                           // the CTAs that hold the pair's first and last unit, hence its first and last partial
+        const int c0 = int(((a + 1) * p.n_ctas - 1) / p.n_units), c1 = int(((b + 1) * p.n_ctas - 1) / p.n_units);
+        e0 = (c0 + j) * teams; n = (c1 - c0 + 1) * teams;
+    }
+    const float2* ml = p.part_ml + int64_t(e0) * p.rows_per_part + rin;
+    const float4* part = reinterpret_cast<const float4*>(p.part_o + (int64_t(e0) * p.rows_per_part + rin) * D + slab * COLS) + col;
+    const int64_t stride = int64_t(p.rows_per_part) * (D / 4);
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+    if (n == 0) {                                // nothing attended: (0, -inf)
         if (slice == 0) *out = make_float4(0.f, 0.f, 0.f, 0.f);
         if (tid == 0 && slab == 0) p.out_lse[item] = -INFINITY;
         return;
     }
-    const int in_kv = head % p.group;
-    const int gh = head / p.group * p.groups_per_kv + in_kv / p.rows_per_part, rin = in_kv % p.rows_per_part;
-    const int64_t a = int64_t(r.unit0) + int64_t(gh) * r.tiles, b = a + r.tiles - 1;
-    const int j = r.pair0 + gh;
-    const int e0 = int(((a + 1) * p.n_ctas - 1) / p.n_units) + j, e1 = int(((b + 1) * p.n_ctas - 1) / p.n_units) + j;   // first, last partial
-    const int n = e1 - e0 + 1;
-    const float2* ml = p.part_ml + int64_t(e0) * p.rows_per_part + rin;
-    const float4* part = reinterpret_cast<const float4*>(p.part_o + (int64_t(e0) * p.rows_per_part + rin) * D + slab * COLS) + col;
-    const int64_t stride = int64_t(p.rows_per_part) * (D / 4);
 
     float m = -INFINITY;
     for (int i = tid; i < n; i += THREADS) m = fmaxf(m, ml[int64_t(i) * p.rows_per_part].x);
@@ -524,9 +492,11 @@ __global__ void __launch_bounds__(THREADS) nibble_reduce_kernel(const __grid_con
     for (int i = slice; i < n; i += kSlices) {
         const float2 x = ml[int64_t(i) * p.rows_per_part];
         const float4 v = part[int64_t(i) * stride];
-        const float w = x.x == -INFINITY ? 0.f : ptx::ex2(x.x - m) * x.y;
-        acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
-        z += w;
+        if (x.x != -INFINITY) {                  // an empty one's output may hold anything
+            const float w = ptx::ex2(x.x - m) * x.y;
+            acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+            z += w;
+        }
     }
     s_o[slice][col] = acc;
     if (col == 0) s_z[slice] = z;
@@ -550,7 +520,7 @@ cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s) {
     if (a.n_units > 0) {
         a.stages = nibble_stages(a.g.dim, a.octets);
         if (a.stages <= 0) return cudaErrorInvalidValue;
-        const size_t smem = size_t(a.stages) * a.g.tile_bytes() + nibble_fixed_smem(a.g.dim, a.octets);
+        const size_t smem = size_t(a.stages) * a.g.tile_bytes() + nibble_fixed_smem();
         auto kernel = wide ? (half ? nibble_attend_kernel<128, true> : nibble_attend_kernel<128, false>)
                            : (half ? nibble_attend_kernel<64, true> : nibble_attend_kernel<64, false>);
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNibbleSmemPerCta);

@@ -57,8 +57,8 @@ cudaError_t launch_nibble_unpack(const NibbleMove& a, bool single_tokens, cudaSt
 // ---- the cache in 4 bits: decode attention (nibble_attend.cu) --------------------------------------------------------
 // Work is counted in units: (row, head group, tile of 64 tokens), tiles innermost; a head group is a KV head and some of
 // its query heads.  CTA c of n takes units [units c / n, units (c + 1) / n).  Where such a chunk meets a (row, head group)
-// that has tiles, a partial (O, maximum, sum) results; with j the index of the pair among those with tiles, partial c + j is its
-// place: distinct, and consecutive for a pair.  So neither the spans nor the partials need tables.
+// that has tiles, a partial (O, maximum, sum) of every team results; with j the index of the pair among those with tiles, their
+// place is c + j: distinct, and consecutive for a pair.  So neither the spans nor the partials need tables.
 struct NibbleRunArg {
     const char* blocks;
     int32_t n_tokens;
@@ -72,27 +72,23 @@ struct NibbleRowArg {
 };
 constexpr int kNibbleWarps = 4, kNibbleCtasPerSm = 3;              // warps that compute, beside the one that copies
 constexpr int kNibbleInlineRows = 64, kNibbleInlineRuns = 128;      // tables up to this size travel as launch parameters
-// Shared memory of a CTA: the stages, this, and the buffer in which the teams' outputs are joined.
+// Shared memory of a CTA: the stages and this.
 constexpr int kNibbleMaxStages = 16;
 struct NibbleSmem {
     uint64_t full[kNibbleMaxStages], empty[kNibbleMaxStages];
     int32_t n_valid[kNibbleMaxStages];
-    float m[kNibbleWarps][8], l[kNibbleWarps][8];
 };
 constexpr int kNibbleSmemPerCta = 228 * 1024 / kNibbleCtasPerSm - 1024;
 // A tile is worked on by one team of `octets` warps.
 inline int nibble_teams(int octets) { return kNibbleWarps / octets; }
-inline int nibble_fixed_smem(int dim, int octets) {
-    const int joined = nibble_teams(octets) > 1 ? octets * 8 * (dim + 4) * int(sizeof(float)) : 0;
-    return int(sizeof(NibbleSmem)) + joined + 128;       // 128: to align the stages
-}
+inline int nibble_fixed_smem() { return int(sizeof(NibbleSmem)) + 128; }         // 128: to align the stages
 // Stages of the copy ring: as many as fit, in a multiple of the teams, so that every stage has one team.  A warp that waits for a lap of
 // a stage can tell that lap from the one before only if it has seen the one before complete itself; with another team's
 // tile in the stage before its own it could run ahead of a copy that lands late, take the old tile for the new one and release the stage.
 inline int nibble_stages(int dim, int octets) {
     const int teams = nibble_teams(octets), tile = NibbleGeom{1, dim, kTileTokens}.tile_bytes();
     if (teams < 1) return 0;
-    int n = (kNibbleSmemPerCta - nibble_fixed_smem(dim, octets)) / tile;
+    int n = (kNibbleSmemPerCta - nibble_fixed_smem()) / tile;
     if (n > kNibbleMaxStages) n = kNibbleMaxStages;
     return n / teams * teams;
 }
@@ -103,13 +99,14 @@ struct NibbleAttend {
     const NibbleRunArg* runs;
     NibbleGeom g;
     const char* q;                               // [n_rows][n_q_heads][dim] bf16
-    float* part_o;                               // [partials][rows_per_part][dim]
-    float2* part_ml;                             // [partials][rows_per_part]: reference maximum (log2) and sum of weights against it
+    float* part_o;                               // [partials][teams][rows_per_part][dim]
+    float2* part_ml;                             // [partials][teams][rows_per_part]: reference maximum (log2) and sum of weights against it
     float* out_o;
     float* out_lse;
     uint32_t* status;                            // may be null
     int64_t part_rows;                           // partial rows that the scratch holds (bounds-checked build)
     int32_t n_rows, n_units, n_ctas, n_q_heads, group, groups_per_kv, n_gh, rows_per_part;
+    int32_t teams;                               // teams of warps in a CTA
     int32_t octets;                              // groups of 8 query heads in a head group
     int32_t stages, n_runs;
     int32_t max_parts;                           // partials of a (row, head group) at most

@@ -114,12 +114,12 @@ ipkv_status move_spans(const ipkv_attn_shape* sh, int32_t n_spans, const ipkv_sp
 
 // Head groups of a row, partials that a launch of n_rows rows can have, and the scratch for them behind the tables.
 struct NibblePlan {
-    int group, groups_per_kv, n_gh, rows_per_part;
+    int group, groups_per_kv, n_gh, rows_per_part, octets, teams;
     explicit NibblePlan(const ipkv_attn_shape* sh)
         : group(sh->n_q_heads / sh->n_kv_heads), groups_per_kv(nibble_groups_per_kv(group)), n_gh(sh->n_kv_heads * groups_per_kv),
-          rows_per_part(nibble_rows_per_part(group)) {}
+          rows_per_part(nibble_rows_per_part(group)), octets((rows_per_part + 7) / 8), teams(nibble_teams(octets)) {}
     static constexpr int kCtas = kSmCount * kNibbleCtasPerSm;
-    size_t part_rows(int32_t n_rows) const { return (size_t(kCtas) + size_t(n_rows) * n_gh) * rows_per_part; }
+    size_t part_rows(int32_t n_rows) const { return (size_t(kCtas) + size_t(n_rows) * n_gh) * teams * rows_per_part; }
     static bool inlined(int32_t n_rows, int64_t n_runs) { return n_rows <= kNibbleInlineRows && n_runs <= kNibbleInlineRuns; }
     static size_t table_bytes(int32_t n_rows, int64_t n_runs) {
         return inlined(n_rows, n_runs) ? 0 : align_up(size_t(n_rows) * sizeof(NibbleRowArg) + size_t(n_runs) * sizeof(NibbleRunArg), 256);
@@ -201,9 +201,9 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
     a.out_o = o; a.out_lse = lse; a.status = status;
     a.n_rows = n_rows; a.n_units = int32_t(units); a.n_runs = n_runs;
     a.n_ctas = units < NibblePlan::kCtas ? int32_t(units) : NibblePlan::kCtas;
-    a.max_parts = units > 0 ? int32_t((longest * a.n_ctas + units - 1) / units + 1) : 0;
+    a.max_parts = units > 0 ? int32_t(((longest * a.n_ctas + units - 1) / units + 1) * plan.teams) : 0;
     a.n_q_heads = sh->n_q_heads; a.group = plan.group; a.groups_per_kv = plan.groups_per_kv; a.n_gh = plan.n_gh; a.rows_per_part = plan.rows_per_part;
-    a.octets = (plan.rows_per_part + 7) / 8;
+    a.octets = plan.octets; a.teams = plan.teams;
     a.scale = sh->softmax_scale > 0.f ? sh->softmax_scale : 1.0f / std::sqrt(float(sh->dim_qk));
     return launch_nibble_attend(a, stream) == cudaSuccess ? IPKV_OK : IPKV_ECUDA;
 }

@@ -8,7 +8,7 @@ int shim_nibble_warps() { return kNibbleWarps; }
 int shim_nibble_teams(int octets) { return nibble_teams(octets); }
 int shim_nibble_stages(int dim, int octets) { return nibble_stages(dim, octets); }
 int shim_nibble_smem(int dim, int octets) {
-    return nibble_stages(dim, octets) * NibbleGeom{1, dim, kTileTokens}.tile_bytes() + nibble_fixed_smem(dim, octets);
+    return nibble_stages(dim, octets) * NibbleGeom{1, dim, kTileTokens}.tile_bytes() + nibble_fixed_smem();
 }
 int shim_nibble_smem_limit() { return kNibbleSmemPerCta; }
 int shim_nibble_groups(int group) { return nibble_groups_per_kv(group); }
