@@ -3,23 +3,24 @@
 // With key = sk * code + zk per 64-column panel and value = sv * code + zv per token,
 //   q . key = sum over panels of sk (q . codes) + zk sum(q),      O = sum_t (p_t sv_t) codes_t + sum_t p_t zv_t,
 // so the tensor cores multiply the bare codes and the scales are applied to scores and weights, one value per token instead
-// of one per element.  Codes become fp16 operands as they lie in the word, by a mask (nibble.cuh): below 2^11 the bits of an fp16
-// number are the number times 2^24, so a code that a mask leaves in place is the code times a power of two, exactly, and the
-// powers of two go into the other operand.
+// of one per element.  Codes become 16-bit operands as they lie in the word, by a mask (nibble.cuh): below the smallest normal
+// number the bits of a bf16 (fp16) number are the number times 2^133 (2^24), so a code that a mask leaves in place is the code times a
+// power of two, exactly, and the powers of two go into the other operand.  The zeros' share of the scores is a product of its own,
+// over panels times terms of sum(q), and cheaper there than as multiply-adds.
 //
 // Tokens are the rows (M = 16) of the score product and columns of the head the rows of the output product; 8 query heads
 // are the columns (N = 8): no row of a product is wasted on a missing head, and codes are never the operand that would have
 // to be moved between lanes.  Scores come out as [token][head]; movmatrix turns the weights, two 16-bit rows at a time,
 // into the [token][head] operand of the second product.
 //
-// Exactness.  q (bf16) times a power of two per head is exact in fp16; products are exact and sums are fp32.  A weight p sv is
+// Exactness.  q (bf16) times a power of two per head is exact; products are exact and sums are fp32.  A weight p sv is
 // held as two fp16 numbers, head and remainder (22 bits): with at most 4 query heads per KV head they share one product (columns
 // 0-3 and 4-7), otherwise there are two.  sv is brought near 1 by a power of two per warp (the largest scale so far), so that
 // fp16's range is spent on p: weights down to 2^-31 of the largest keep their share.
 // The tensor cores add with two bits more than fp32 has and round towards zero, both counted from the largest exponent that
-// an operand's FORMAT shows (a subnormal counts as 2^-14).  Two things follow.  The codes are shifted up so that they fill fp16's
-// subnormal range (bits 3..6 and 7..10): in place they lost up to six bits of their products.  And the sums over tokens must not be
-// much larger than the result:
+// an operand's FORMAT shows (a subnormal counts as the smallest normal number).  Two things follow.  The codes must fill the
+// subnormal range: K's do in place as bf16 (7 bits of mantissa; bits 0..3 and 4..7), V's are shifted up to bits 3..6 and 7..10 of fp16,
+// in place they lost up to six bits of their products.  And the sums over tokens must not be much larger than the result:
 // codes are never negative, but an output is a mean of many values of either sign, so a sum of p sv code would exceed it by
 // 2.5 sqrt(tokens); every other eight tokens enter complemented, code = 15 - (15 - code): the complement costs nothing in the
 // mask, its weight is negative, 15 sv joins zv, and the excesses of the two halves meet in the same product.  Without
@@ -49,12 +50,33 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.f;                    // the reference maximum is raised when a score exceeds it by this (log2)
 constexpr int kManyParts = 16;                   // partials of a (row, head) from which the join is spread over more threads
-constexpr uint32_t kLow = 0x00780078u, kHigh = 0x07800780u;         // codes in bits 3..6 and 7..10: times 2^-21 and 2^-17
+constexpr uint32_t kLowK = 0x000f000fu, kHighK = 0x00f000f0u;       // K codes as bf16 in bits 0..3 and 4..7: times 2^-133 and 2^-129
+constexpr uint32_t kLow = 0x00780078u, kHigh = 0x07800780u;         // V codes as fp16 in bits 3..6 and 7..10: times 2^-21 and 2^-17
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16_k8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(b0));
+}
+// Two fp32 operations in one instruction, each rounded as if alone.
+__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
+    asm("{.reg .b64 p, q; mov.b64 p, {%0,%1}; mov.b64 q, {%2,%3}; add.rn.f32x2 p, p, q; mov.b64 {%0,%1}, p;}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+__device__ __forceinline__ float2 fma2(float a0, float a1, float b0, float b1, float c0, float c1) {
+    float2 r;
+    asm("{.reg .b64 p, q, s; mov.b64 p, {%2,%3}; mov.b64 q, {%4,%5}; mov.b64 s, {%6,%7}; fma.rn.f32x2 p, p, q, s; mov.b64 {%0,%1}, p;}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+    return r;
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t r;
@@ -193,9 +215,10 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         const int in_kv = x.part * p.rows_per_part;      // the head group's first head among those of its KV head
         const int n_heads = min(p.group - in_kv, p.rows_per_part), head0 = x.kv * p.group + in_kv;
 
-        // ---- queries: operands of head g (columns 64p+16t+8w+{0,4},{1,5},{2,6},{3,7}), normalised to [2^14, 2^15) ----
+        // ---- queries: operands of head g (columns 64p+16t+8w+{0,4},{1,5},{2,6},{3,7}), normalised to [2^110, 2^111) ----
         uint32_t qf[P][2][4];
-        float qs[P][2], c[2];                    // per panel 2^-21 sum(q), and log2 units per score, of heads 2t and 2t+1
+        uint32_t qz;                             // 2^-133 sum(q) of each panel and head g: its t-th term of three bf16 (24 bits), 0 for t = 3
+        float c[2];                              // log2 units per score, of heads 2t and 2t+1
         {
             const int hq = octet * 8 + (HALF ? (g & 3) : g);
             const bool live = works && hq < n_heads;
@@ -216,9 +239,9 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(v[pn][i]));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int e = min(max(int(__float_as_uint(top) >> 23), 15), 230);
-            const float f = __uint_as_float(uint32_t(268 - e) << 23);                    // 2^14 / 2^(exponent of the largest)
-            const float cg = p.scale * kLog2e * __uint_as_float(uint32_t(7 + e) << 23);  // ... undone, with the codes' 2^21
+            const int e = min(max(int(__float_as_uint(top) >> 23), 110), 231);
+            const float f = __uint_as_float(uint32_t(364 - e) << 23);                    // 2^110 / 2^(exponent of the largest)
+            const float cg = p.scale * kLog2e * __uint_as_float(uint32_t(23 + e) << 23); // ... undone, with the codes' 2^133
             float sum[P];
 #pragma unroll
             for (int pn = 0; pn < P; ++pn) {
@@ -228,18 +251,24 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                     float* y = &v[pn][8 * w];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) { y[i] *= f; sum[pn] += y[i]; }
-                    qf[pn][w][0] = pack_f16(y[0], y[4]);
-                    qf[pn][w][1] = pack_f16(y[1] * 0.0625f, y[5] * 0.0625f);
-                    qf[pn][w][2] = pack_f16(y[2], y[6]);
-                    qf[pn][w][3] = pack_f16(y[3] * 0.0625f, y[7] * 0.0625f);
+                    qf[pn][w][0] = ptx::pack_bf16(y[0], y[4]);
+                    qf[pn][w][1] = ptx::pack_bf16(y[1] * 0.0625f, y[5] * 0.0625f);
+                    qf[pn][w][2] = ptx::pack_bf16(y[2], y[6]);
+                    qf[pn][w][3] = ptx::pack_bf16(y[3] * 0.0625f, y[7] * 0.0625f);
                 }
                 sum[pn] += __shfl_xor_sync(0xffffffffu, sum[pn], 1);
                 sum[pn] += __shfl_xor_sync(0xffffffffu, sum[pn], 2);
-                sum[pn] *= 0x1p-21f;
-                qs[pn][0] = __shfl_sync(0xffffffffu, sum[pn], 8 * t);                    // lane 4 (2t): head 2t
-                qs[pn][1] = __shfl_sync(0xffffffffu, sum[pn], 8 * t + 4);
+                float rest = sum[pn] * 0x1p-100f * 0x1p-33f, term = 0.f;
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    const float y = ptx::bf16_lo(ptx::pack_bf16(rest, rest));
+                    if (k == t) term = y;
+                    rest -= y;
+                }
+                sum[pn] = term;
             }
-            c[0] = __shfl_sync(0xffffffffu, cg, 8 * t);
+            qz = ptx::pack_bf16(sum[0], P == 2 ? sum[P - 1] : 0.f);
+            c[0] = __shfl_sync(0xffffffffu, cg, 8 * t);                                  // lane 4 (2t): head 2t
             c[1] = __shfl_sync(0xffffffffu, cg, 8 * t + 4);
         }
 
@@ -280,9 +309,9 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                     const uint32_t ya[2] = {y.x, y.y}, yb[2] = {y.z, y.w};
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
-                        const uint32_t a3 = ya[w] << 3, b3 = yb[w] << 3, a5 = ya[w] >> 5, b5 = yb[w] >> 5;
-                        mma_f16(acc[pn], a3 & kLow, b3 & kLow, a3 & kHigh, b3 & kHigh, qf[pn][w][0], qf[pn][w][1]);
-                        mma_f16(acc[pn], a5 & kLow, b5 & kLow, a5 & kHigh, b5 & kHigh, qf[pn][w][2], qf[pn][w][3]);
+                        const uint32_t a8 = ya[w] >> 8, b8 = yb[w] >> 8;
+                        mma_bf16(acc[pn], ya[w] & kLowK, yb[w] & kLowK, ya[w] & kHighK, yb[w] & kHighK, qf[pn][w][0], qf[pn][w][1]);
+                        mma_bf16(acc[pn], a8 & kLowK, b8 & kLowK, a8 & kHighK, b8 & kHighK, qf[pn][w][2], qf[pn][w][3]);
                     }
                 }
                 uint32_t km[2][P];
@@ -295,17 +324,16 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 }
                 const uint2 vm = *reinterpret_cast<const uint2*>(tile + kVMeta + (un * 8 + g) * 8);
                 const uint32_t vmm[2] = {vm.x, vm.y};
+                // the zeros' share, sum over panels of zk sum(q): columns 2t and 2t+1 of A are both panels' zeros, rows of B the terms of qz
+                float zeros[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_bf16_k8(zeros, __byte_perm(km[0][0], km[0][P - 1], 0x7632), __byte_perm(km[1][0], km[1][P - 1], 0x7632), qz);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float y = 0.f;
+                        s[un][2 * h + e] = zeros[2 * h + e];
 #pragma unroll
-                        for (int pn = 0; pn < P; ++pn) {
-                            y = fmaf(ptx::bf16_lo(km[h][pn]), acc[pn][2 * h + e], y);
-                            y = fmaf(ptx::bf16_hi(km[h][pn]), qs[pn][e], y);
-                        }
-                        s[un][2 * h + e] = y;
+                        for (int pn = 0; pn < P; ++pn) s[un][2 * h + e] = fmaf(ptx::bf16_lo(km[h][pn]), acc[pn][2 * h + e], s[un][2 * h + e]);
                     }
                     sv[un][h] = ptx::bf16_lo(vmm[h]);
                     zv[un][h] = h ? fmaf(ptx::bf16_lo(vmm[h]), 15.f, ptx::bf16_hi(vmm[h])) : ptx::bf16_hi(vmm[h]);
@@ -366,16 +394,18 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 for (int h = 0; h < 2; ++h) {
                     float w[2];
                     const float svf = sv[un][h] * (h ? f1 : f0);
+                    const float2 y = fma2(s[un][2 * h], s[un][2 * h + 1], c[0], c[1], -m[0], -m[1]);
+                    const float pr[2] = {ptx::ex2(y.x), ptx::ex2(y.y)};
+                    add2(l[0], l[1], pr[0], pr[1]);
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float pr = ptx::ex2(fmaf(s[un][2 * h + e], c[e], -m[e]));
-                        l[e] += pr;
-                        oz[e] = fmaf(pr, zv[un][h], oz[e]);
-                        w[e] = pr * svf;
+                        oz[e] = fmaf(pr[e], zv[un][h], oz[e]);
+                        w[e] = pr[e] * svf;
                     }
                     const uint32_t big = pack_f16(w[0], w[1]);
                     const float2 back = unpack_f16(big);
-                    const uint32_t rest = pack_f16(w[0] - back.x, w[1] - back.y);
+                    add2(w[0], w[1], -back.x, -back.y);
+                    const uint32_t rest = pack_f16(w[0], w[1]);
                     if (HALF) hi[un][h] = transpose8x8(t < 2 ? big : rest);              // columns 4-7 repeat heads 0-3
                     else { hi[un][h] = transpose8x8(big); lo[un][h] = transpose8x8(rest); }
                 }
@@ -394,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                     if (!HALF) mma_f16(sum, a0, a1, a2, a3, lo[un][0], lo[un][1]);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[d][i] += sum[i];
+                for (int i = 0; i < 4; i += 2) add2(o[d][i], o[d][i + 1], sum[i], sum[i + 1]);
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[st]));
