@@ -668,10 +668,6 @@ def _table(rows, width):
     return rows
 
 
-def _address(a):
-    return a.__array_interface__["data"][0]
-
-
 def _move(name, shape, spans, k, v, stream):
     torch = _torch or _modules()
     t = _table(spans, 3)
@@ -685,7 +681,7 @@ def _move(name, shape, spans, k, v, stream):
         if column != 1 or (heads > 1 and head != dim) or (n > 1 and token == 0) or x.get_device() != dev:
             raise ValueError("the heads of a token lie side by side, its tokens apart, and K and V are on one device")
         strides.append(token if n > 1 else 0)
-    rc = getattr(lib(), name)(C.byref(shape), t.shape[0], _address(t), n, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
+    rc = getattr(lib(), name)(C.byref(shape), t.shape[0], t.tobytes(), n, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
                               _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, name)
@@ -730,7 +726,7 @@ def ipkv_nibble_attend(shape, runs, row_start, q, scratch, o_part, lse_part, sta
             raise ValueError(f"{what} is contiguous {dtype} {size} on the device of q: got {x.dtype} {tuple(x.shape)}")
     if scratch.get_device() != dev or not scratch.is_contiguous() or (status is not None and (status.get_device() != dev or status.dtype not in (torch.int32, torch.uint32))):
         raise ValueError("scratch and the status word (32 bits) are on the device of q")
-    rc = lib().ipkv_nibble_attend(C.byref(shape), rows, _address(runs), _address(row_start), q.data_ptr(), scratch.data_ptr(), scratch.nbytes,
+    rc = lib().ipkv_nibble_attend(C.byref(shape), rows, runs.tobytes(), row_start.tobytes(), q.data_ptr(), scratch.data_ptr(), scratch.nbytes,
                                   o_part.data_ptr(), lse_part.data_ptr(), _ptr(status), _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, "ipkv_nibble_attend")
