@@ -474,7 +474,8 @@ const char* ipkv_version(void);
  * a bf16 scale and zero:
  *   zero = min x,  scale = bf16((max x - min x) / 15),  code = min(round_half_even((x - zero) / scale), 15)      (fp32)
  * and a code stands for scale * code + zero.  Where scale is below 2^-126 every code is 0.  Inputs have to be finite and
- * below 2^126 in magnitude; what a group with other values holds is unspecified (other groups are not affected).
+ * below 2^126 in magnitude: a group with an infinity decodes to NaN, what one with a NaN or larger values holds is unspecified
+ * (other groups are not affected).
  * Grouped-query shapes only: kind IPKV_GQA, dim 64 or 128, block_tokens a multiple of 64.
  *
  * NIBBLE block layout.  For each KV head: block_tokens/64 tiles of 64 tokens.  A tile of width D (P = D/64 panels) is K codes
@@ -512,7 +513,7 @@ ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* shape, int32_t n_spans, co
  * the blocks hold behind them may be anything).  runs and row_run_start are host arrays, copied by the call; small tables travel
  * with the launch, so that the call can be captured into a CUDA graph like ipkv_attend_runs.  q_dev [n_rows][n_q_heads][dim] bf16.
  * Outputs fp32: o_part_dev [n_rows][n_q_heads][dim] normalised, lse_part_dev [n_rows][n_q_heads] natural log; a row without
- * tokens gives (0, -inf).  They join partials over other tokens (a bf16 window, the CPU side) through ipkv_merge.
+ * tokens gives (0, -inf), a head whose query or tokens hold a NaN gives NaN.  They join partials over other tokens (a bf16 window, the CPU side) through ipkv_merge.
  * scratch_dev: at least ipkv_nibble_scratch_bytes, 256-byte aligned, private to this call until its work on `stream` has
  * completed (calls captured into graphs that may run at the same time need scratch of their own).  status_dev as in
  * ipkv_attend_runs, may be NULL.  Results are bit-reproducible.  Works on the current device. */

@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                     l[e] += __shfl_xor_sync(0xffffffffu, l[e], d);
                     oz[e] += __shfl_xor_sync(0xffffffffu, oz[e], d);
                 }
-                f[e] = l[e] > 0.f ? 1.f / l[e] : 0.f;
+                f[e] = l[e] == 0.f ? 0.f : 1.f / l[e];
             }
             const float undo = fv > 0.f ? 0x1p15f : 0.f, inv_fv = fv > 0.f ? 1.f / fv : 0.f;   // 2^21 / 64, then 1 / fv
             const int hb = octet * 8 + 2 * t;    // of the head group
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(THREADS) nibble_reduce_kernel(const __grid_con
     for (int i = slice; i < n; i += kSlices) {
         const float2 x = ml[int64_t(i) * p.rows_per_part];
         const float4 v = part[int64_t(i) * stride];
-        if (x.x != -INFINITY) {                  // an empty one's output may hold anything
+        if (x.y != 0.f) {                        // an empty one's output may hold anything (a sum of NaN is not empty: it must be seen)
             const float w = ptx::ex2(x.x - m) * x.y;
             acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
             z += w;
@@ -538,9 +538,9 @@ __global__ void __launch_bounds__(THREADS) nibble_reduce_kernel(const __grid_con
         acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
         z += s_z[k];
     }
-    const float inv = z > 0.f ? 1.f / z : 0.f;
+    const float inv = z == 0.f ? 0.f : 1.f / z;
     *out = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    if (tid == 0 && slab == 0) p.out_lse[item] = z > 0.f ? m * kLn2 + logf(z) : -INFINITY;
+    if (tid == 0 && slab == 0) p.out_lse[item] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
 }
 
 }  // namespace

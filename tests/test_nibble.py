@@ -327,6 +327,29 @@ def test_attention_on_hard_values(what):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hq", [8, 16, 32])              # heads that share one product, one octet and two
+def test_what_is_not_a_number_is_seen_where_it_counts_and_nowhere_else(hq):
+    """A NaN in a query makes that head NaN, an infinite key (its group decodes to NaN) its KV head in its row; nothing else changes."""
+    hkv, d, n = 2, 128, 700
+    rng = np.random.default_rng(hq)
+    sh = shape_of(hq, hkv, d, 64)
+    k, v = synth.normal_bf16(rng, (2 * n, hkv, d)), synth.normal_bf16(rng, (2 * n, hkv, d))
+    q = synth.normal_bf16(rng, (2, hq, d))
+    buf = torch.full((2, -(-n // 64) * ref.block_bytes(hkv, d, 64)), 255, dtype=torch.uint8, device="cuda")
+    spans, runs = [(buf[0], 0, n), (buf[1], 0, n)], [[(buf[0], n)], [(buf[1], n)]]
+    binding.ipkv_nibble_pack(sh, spans, synth.bits_to_torch(k, "cuda"), synth.bits_to_torch(v, "cuda"))
+    o, lse = attend(sh, runs, q)
+    q[0, 1, 5] = 0x7fc0
+    k[n + 333, 1, 70] = 0x7f80
+    binding.ipkv_nibble_pack(sh, spans, synth.bits_to_torch(k, "cuda"), synth.bits_to_torch(v, "cuda"))
+    o2, lse2 = attend(sh, runs, q)
+    hit = np.zeros((2, hq), bool)
+    hit[0, 1] = hit[1, hq // 2:] = True
+    assert np.isnan(o2[hit]).all() and np.isnan(lse2[hit]).all()
+    assert np.array_equal(o2[~hit], o[~hit]) and np.array_equal(lse2[~hit], lse[~hit])
+
+
+@pytest.mark.gpu
 def test_a_run_whose_offsets_pass_32_bits():
     """More than 4 GB in one run: the first and last tokens carry all the weight."""
     hkv, d, bt, n = 8, 128, 64, 64 * 62000 + 17
