@@ -80,8 +80,8 @@ __global__ void __launch_bounds__(kRopeWarps * 32, kRopeCtasPerSm) norm_rope_ker
         if (p.split > 1) {
             const uint32_t split = uint32_t(p.split), item = uint32_t(w.item), token = item / split, share = item - token * split;   // few tokens
             w.token = token;
-            w.step = int(uint32_t(p.n_steps) * share / split);
-            w.last = int(uint32_t(p.n_steps) * (share + 1) / split);
+            w.step = int(uint64_t(p.n_steps) * share / split);       // 2^21 steps times 2^11 warps pass 32 bits
+            w.last = int(uint64_t(p.n_steps) * (share + 1) / split);
         }
         enter_part(w);
     };

@@ -226,3 +226,20 @@ def test_replays_from_a_graph_and_runs_on_another_stream():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal((out.float() * 2).bfloat16(), again)
+
+
+@pytest.mark.gpu
+def test_one_token_of_more_heads_than_32_bits_can_divide():
+    """The steps of a token are divided among warps: four parts of 2^20 heads of 256, the most that a call takes."""
+    d, heads = 256, 1 << 20
+    x = torch.randn((1, 1000, d), device="cuda").bfloat16()
+    x = x.repeat(1, heads // 1000 + 1, 1)[:, :heads].contiguous()
+    parts = [x.clone() for _ in range(4)]
+    pos = torch.tensor([[7]], dtype=torch.int32, device="cuda")
+    rope = binding.make_rope(d, eps=1e-6)
+    few = torch.empty((1, 1000, d), dtype=torch.bfloat16, device="cuda")
+    binding.ipkv_norm_rope(rope, [(x[:, :1000], None, few)], pos)
+    want = few.repeat(1, heads // 1000 + 1, 1)[:, :heads]
+    binding.ipkv_norm_rope(rope, [(p, None, None) for p in parts], pos)
+    for p in parts:
+        assert torch.equal(p, want)
