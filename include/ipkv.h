@@ -504,7 +504,8 @@ ipkv_status ipkv_nibble_pack(const ipkv_attn_shape* shape, int32_t n_spans, cons
                              const void* k_dev, const void* v_dev, int64_t k_token_stride, int64_t v_token_stride, void* stream);
 
 /* The inverse: the values that the codes of the spans' tokens stand for, rounded to bf16, into k_dev and v_dev (which no
- * block may overlap).  Several spans may read the same block. */
+ * block may overlap, nor one the other: they may lie side by side in one buffer).  Several spans may read
+ * the same block. */
 ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* shape, int32_t n_spans, const ipkv_span* spans, int64_t n_tokens,
                                void* k_dev, void* v_dev, int64_t k_token_stride, int64_t v_token_stride, void* stream);
 
@@ -513,7 +514,8 @@ ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* shape, int32_t n_spans, co
  * the blocks hold behind them may be anything).  runs and row_run_start are host arrays, copied by the call; small tables travel
  * with the launch, so that the call can be captured into a CUDA graph like ipkv_attend_runs.  q_dev [n_rows][n_q_heads][dim] bf16.
  * Outputs fp32: o_part_dev [n_rows][n_q_heads][dim] normalised, lse_part_dev [n_rows][n_q_heads] natural log; a row without
- * tokens gives (0, -inf), a head whose query or tokens hold a NaN gives NaN.  They join partials over other tokens (a bf16 window, the CPU side) through ipkv_merge.
+ * tokens gives (0, -inf), a head whose query or tokens hold a NaN gives NaN.  They join partials over other tokens (a bf16
+ * window, the CPU side) through ipkv_merge.
  * scratch_dev: at least ipkv_nibble_scratch_bytes, 256-byte aligned, private to this call until its work on `stream` has
  * completed (calls captured into graphs that may run at the same time need scratch of their own).  status_dev as in
  * ipkv_attend_runs, may be NULL.  Results are bit-reproducible.  Works on the current device. */

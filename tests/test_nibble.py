@@ -465,3 +465,75 @@ def test_a_decode_run_from_prompt_to_merge():
                 to, tl = to + 2e-3, tl + 1e-3                             # the bf16 kernel's documented tolerance
             want_o, want_lse = ref.attend(synth.torch_bits(qc)[s], kv, vv, d ** -0.5)
             assert np.abs(got[s] - want_o).max() <= to and np.abs(got_lse[s] - want_lse).max() <= tl + 2.0 ** -18
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_rows", [1, 70])              # tables in the launch, tables uploaded
+def test_a_batch_without_tokens_and_a_block_that_rows_share(n_rows):
+    rng = np.random.default_rng(41)
+    sh = shape_of(8, 2, 128, 64)
+    q = synth.normal_bf16(rng, (n_rows, 8, 128))
+    o, lse = attend(sh, [[] if r % 2 else [(0, 0)] for r in range(n_rows)], q)
+    assert not o.any() and np.isneginf(lse).all()
+    buf, runs, kvs = fill(rng, sh, [[100]])
+    (k, v), = kvs
+    twice = [runs[0] * 2] * n_rows                       # the same tokens twice in a row, and in every row
+    o, lse = attend(sh, twice, q)
+    check(sh, q, [(np.concatenate([k, k]), np.concatenate([v, v]))] * n_rows, o, lse)
+
+
+@pytest.mark.gpu
+def test_k_and_v_side_by_side_and_spans_that_read_a_block_twice():
+    """K and V interleaved per token in one buffer, with a column of other data between tokens that has to stay."""
+    rng = np.random.default_rng(43)
+    hkv, d, n = 2, 64, 150
+    sh = shape_of(4, hkv, d, 64)
+    row = hkv * d
+    x = synth.normal_bf16(rng, (n, 2 * row + 8))
+    src = synth.bits_to_torch(x, "cuda")
+    k, v = src[:, :row].view(n, hkv, d), src[:, row:2 * row].view(n, hkv, d)
+    buf = torch.full((3 * ref.block_bytes(hkv, d, 64),), 255, dtype=torch.uint8, device="cuda")
+    binding.ipkv_nibble_pack(sh, [(buf, 0, n)], k, v)
+    dst = torch.full((2 * n, 2 * row + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    ko, vo = dst[:, :row].view(2 * n, hkv, d), dst[:, row:2 * row].view(2 * n, hkv, d)
+    binding.ipkv_nibble_unpack(sh, [(buf, 0, n), (buf, 0, n)], ko, vo)
+    kv, vv = ref.quantised_values(x[:, :row].reshape(n, hkv, d), x[:, row:2 * row].reshape(n, hkv, d))
+    for got, want in ((ko, kv), (vo, vv)):
+        want = synth.f32_to_bf16_bits(want.astype(np.float32))
+        assert np.array_equal(synth.torch_bits(got[:n].contiguous()), want) and np.array_equal(synth.torch_bits(got[n:].contiguous()), want)
+    assert bool((dst[:, 2 * row:] == 7).all())
+
+
+@pytest.mark.gpu
+def test_calls_at_once_from_two_threads_on_their_own_streams():
+    import threading
+    rng = np.random.default_rng(47)
+    sh = shape_of(16, 2, 128, 64)
+    rows = [[2000], [], [65, 700]]
+    jobs = []
+    for i in range(2):
+        buf, runs, _ = fill(rng, sh, rows, spread=1.0 + i)
+        q = synth.bits_to_torch(synth.normal_bf16(rng, (3, 16, 128)), "cuda")
+        o, lse = attend(sh, runs, q)
+        scratch = torch.empty(binding.ipkv_nibble_scratch_bytes(sh, 3, 4), dtype=torch.uint8, device="cuda")
+        jobs.append((runs, q, scratch, torch.empty((20, 3, 16, 128), device="cuda"), torch.empty((20, 3, 16), device="cuda"), o, lse, buf))
+    errors = []
+
+    def work(job):
+        try:
+            runs, q, scratch, o, lse = job[:5]
+            s = torch.cuda.Stream()
+            for i in range(20):
+                binding.ipkv_nibble_attend(sh, runs, None, q, scratch, o[i], lse[i], stream=s)
+            s.synchronize()
+        except Exception as e:                           # a thread's exception would be lost
+            errors.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(j,)) for j in jobs]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not errors
+    for _, _, _, o, lse, want_o, want_lse, _ in jobs:
+        for i in range(20):
+            assert np.array_equal(o[i].cpu().numpy(), want_o.astype(np.float32)) and np.array_equal(lse[i].cpu().numpy(), want_lse.astype(np.float32))
