@@ -96,26 +96,44 @@ using Smem = NibbleSmem;
 __device__ __forceinline__ NibbleRowArg row_at(const NibbleAttend& p, int i) { return p.rows ? p.rows[i] : p.row[i]; }
 __device__ __forceinline__ NibbleRunArg run_at(const NibbleAttend& p, int i) { return p.runs ? p.runs[i] : p.run[i]; }
 
-// A chunk's walk over (row, head group) pairs: the pair that unit u belongs to, and how many of the chunk's tiles follow in it.
+// A CTA's walk over (row, head group) pairs: the pair, and which of its tiles are the CTA's.
 struct Pair {
     NibbleRowArg r;
     int row, kv, part;           // row, KV head, and which part of its query heads
-    int tile0, n, slot;
+    int tile0, n;                // the CTA's tiles of it (none where only units of its cost are in the CTA's chunk)
+    int units, slot;             // units of the chunk that belong to it; where its partials go
 };
+__device__ __forceinline__ void set_pair(const NibbleAttend& p, Pair& x, int gh) {
+    x.kv = p.groups_per_kv == 1 ? gh : gh / p.groups_per_kv;
+    x.part = gh - x.kv * p.groups_per_kv;
+}
+// The tiles of units [first, first + x.units) of a pair: its cost comes first.
+__device__ __forceinline__ void set_tiles(Pair& x, int first) {
+    x.tile0 = max(first - kNibblePairCost, 0);
+    x.n = max(first + x.units - kNibblePairCost, 0) - x.tile0;
+}
 __device__ __forceinline__ Pair pair_at(const NibbleAttend& p, int u, int u1) {
     int lo = 0, hi = p.n_rows - 1;
     while (lo < hi) {                            // the last row that begins at or before u (rows without tiles lie in front of it)
         const int mid = (lo + hi + 1) >> 1;
-        if (row_at(p, mid).unit0 <= u) lo = mid; else hi = mid - 1;
+        if (row_at(p, mid).first <= u) lo = mid; else hi = mid - 1;
     }
     Pair x;
     x.r = row_at(p, lo);
     x.row = lo;
-    const int gh = (u - x.r.unit0) / x.r.tiles;
-    x.tile0 = (u - x.r.unit0) - gh * x.r.tiles;
-    x.kv = p.groups_per_kv == 1 ? gh : gh / p.groups_per_kv;
-    x.part = gh - x.kv * p.groups_per_kv;
-    x.n = min(x.r.tiles - x.tile0, u1 - u);
+    if (p.share > 0) {                           // whole CTAs to every pair, u is the CTA
+        const int ctas = (x.r.tiles + p.share - 1) / p.share, gh = (u - x.r.first) / ctas, piece = u - x.r.first - gh * ctas;
+        set_pair(p, x, gh);
+        x.tile0 = int(int64_t(x.r.tiles) * piece / ctas);
+        x.n = int(int64_t(x.r.tiles) * (piece + 1) / ctas) - x.tile0;
+        x.units = 1;
+        x.slot = u;
+        return x;
+    }
+    const int all = x.r.tiles + kNibblePairCost, gh = (u - x.r.first) / all, first = u - x.r.first - gh * all;
+    set_pair(p, x, gh);
+    x.units = min(all - first, u1 - u);
+    set_tiles(x, first);
     x.slot = int(blockIdx.x) + x.r.pair0 + gh;
     return x;
 }
@@ -129,8 +147,8 @@ __device__ __forceinline__ void next_pair(const NibbleAttend& p, Pair& x, int u,
             do x.r = row_at(p, ++x.row); while (x.r.tiles == 0);
         }
     }
-    x.tile0 = 0;
-    x.n = min(x.r.tiles, u1 - u);
+    x.units = min(x.r.tiles + kNibblePairCost, u1 - u);
+    set_tiles(x, 0);
 }
 
 template <int D, bool HALF>                      // HALF: at most 4 query heads per KV head
@@ -150,7 +168,8 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         ptx::mbar_fence_init();
     }
     // The tables are launch parameters, or were there before the previous kernel of the stream began: they may be read under its tail.
-    const int u0 = int(int64_t(p.n_units) * blockIdx.x / p.n_ctas), u1 = int(int64_t(p.n_units) * (blockIdx.x + 1) / p.n_ctas);
+    const int u0 = p.share > 0 ? int(blockIdx.x) : int(int64_t(p.n_units) * blockIdx.x / p.n_ctas);
+    const int u1 = p.share > 0 ? u0 + 1 : int(int64_t(p.n_units) * (blockIdx.x + 1) / p.n_ctas);
     Pair x = pair_at(p, u0, u1);
     __syncthreads();
     ptx::grid_dependency_wait();
@@ -191,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 if (++in_block == per) { in_block = 0; src += to_next_block; } else src += kTile;
                 if (++st == stages) { st = 0; ++lap; }
             }
-            u += x.n;
+            u += x.units;
             if (u < u1) next_pair(p, x, u, u1);
         }
         if (!ok && p.status) atomicOr(p.status, kStatusNoFreeStage);
@@ -469,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 if (g == 0 && writes && hb + e < n_heads) p.part_ml[row0 + e] = make_float2(m[e], l[e]);
         }
         it0 = it_end;
-        u += x.n;
+        u += x.units;
         if (u < u1) next_pair(p, x, u, u1);
     }
 }
@@ -490,12 +509,14 @@ __global__ void __launch_bounds__(THREADS) nibble_reduce_kernel(const __grid_con
     float4* out = reinterpret_cast<float4*>(p.out_o + int64_t(item) * D + slab * COLS) + col;
     const int kv = head / p.group, in_kv = head - kv * p.group, part_of = in_kv / p.rows_per_part, rin = in_kv - part_of * p.rows_per_part;
     const int gh = kv * p.groups_per_kv + part_of, teams = p.teams;
-    const int64_t a = int64_t(r.unit0) + int64_t(gh) * r.tiles, b = a + r.tiles - 1;
-    const int j = r.pair0 + gh;
     int e0 = 0, n = 0;
-    if (r.tiles > 0) {                           // the CTAs that hold the pair's first and last unit, hence its first and last partial
+    if (r.tiles > 0 && p.share > 0) {
+        const int ctas = (r.tiles + p.share - 1) / p.share;
+        e0 = (r.first + gh * ctas) * teams; n = ctas * teams;
+    } else if (r.tiles > 0) {                    // the CTAs that hold the pair's first and last unit, hence its first and last partial
+        const int64_t a = int64_t(r.first) + int64_t(gh) * (r.tiles + kNibblePairCost), b = a + r.tiles + kNibblePairCost - 1;
         const int c0 = int(((a + 1) * p.n_ctas - 1) / p.n_units), c1 = int(((b + 1) * p.n_ctas - 1) / p.n_units);
-        e0 = (c0 + j) * teams; n = (c1 - c0 + 1) * teams;
+        e0 = (c0 + r.pair0 + gh) * teams; n = (c1 - c0 + 1) * teams;
     }
     const float2* ml = p.part_ml + int64_t(e0) * p.rows_per_part + rin;
     const float4* part = reinterpret_cast<const float4*>(p.part_o + (int64_t(e0) * p.rows_per_part + rin) * D + slab * COLS) + col;

@@ -55,17 +55,24 @@ cudaError_t launch_nibble_pack(const NibbleMove& a, bool single_tokens, cudaStre
 cudaError_t launch_nibble_unpack(const NibbleMove& a, bool single_tokens, cudaStream_t s);
 
 // ---- the cache in 4 bits: decode attention (nibble_attend.cu) --------------------------------------------------------
-// Work is counted in units: (row, head group, tile of 64 tokens), tiles innermost; a head group is a KV head and some of
-// its query heads.  CTA c of n takes units [units c / n, units (c + 1) / n).  Where such a chunk meets a (row, head group)
-// that has tiles, a partial (O, maximum, sum) of every team results; with j the index of the pair among those with tiles, their
-// place is c + j: distinct, and consecutive for a pair.  So neither the spans nor the partials need tables.
+// A pair is a row and a head group (a KV head and some of its query heads); its tiles of 64 tokens are work for one CTA or several,
+// which leave a partial (O, maximum, sum) of every team.  Two ways to share the pairs out, see nibble_share:
+//  - whole CTAs to every pair: ceil(tiles / share) of them, each an equal part of the pair's tiles; partials in the CTAs' order;
+//  - equal chunks: work is counted in units, a pair's tiles and its cost in front of them, pair after pair, and CTA c of n takes units
+//    [units c / n, units (c + 1) / n).  With j the index of the pair among those with tiles, the partials that CTA c has of
+//    it go to place c + j: distinct, and consecutive for a pair.
+// So neither needs tables beside the rows'.
+// The cost of a pair, in tiles: queries read, a partial written, the pipeline drained.  Without it the CTA with the shortest
+// sequences was the last: 64 ragged rows of up to 24K tokens 183 us, 162 with 4 (171 with 2, 163 with 12); rows of up to 2K
+// tokens 48 and 29 us.
+constexpr int kNibblePairCost = 4;
 struct NibbleRunArg {
     const char* blocks;
     int32_t n_tokens;
     int32_t tile0;                               // tiles of the row's runs before this one
 };
 struct NibbleRowArg {
-    int32_t unit0;                               // units of the rows before this one
+    int32_t first;                               // units (whole CTAs to every pair: CTAs) of the rows before this one
     int32_t tiles;                               // tiles of the row
     int32_t run0;                                // its first run (runs without tokens are left out)
     int32_t pair0;                               // (row, head group) pairs with tiles before this row's
@@ -109,6 +116,7 @@ struct NibbleAttend {
     int32_t teams;                               // teams of warps in a CTA
     int32_t octets;                              // groups of 8 query heads in a head group
     int32_t stages, n_runs;
+    int32_t share;                               // whole CTAs to every pair: tiles that one takes at most; 0: equal chunks of all units
     int32_t max_parts;                           // partials of a (row, head group) at most
     int32_t plain_launch;                        // the tables were written by the kernel in front of this launch: no overlap with it
     float scale;
@@ -119,6 +127,43 @@ inline int nibble_groups_per_kv(int group) { return (group + 8 * kNibbleWarps - 
 inline int nibble_rows_per_part(int group) {
     const int n = nibble_groups_per_kv(group);
     return n == 1 ? group : ((group + n - 1) / n + 7) / 8 * 8;
+}
+// How to share out the pairs: the tiles that a CTA takes at most where every pair has whole CTAs, or 0 for equal chunks.
+// A team that works off k tiles takes about (us, 128 columns, 4 query heads per KV head; 8 take a sixth more)
+//   7 + 1.3 k with one CTA to an SM,   9.3 + 1.75 k with two,   9.5 + 2.5 k with three,
+// and the chunks, which fill all SMs to the same degree but meet two pairs and more, with r rounds of tiles on three CTAs,
+//   11.5 + 2.4 r, 5.5 more if there are several pairs.
+// Whole CTAs win where there is little work for each SM (one row of 4K tokens of 4 KV heads 8.6 us against 10.6, 16 rows of 2K 12.7 against
+// 18.2, 32 ragged rows of up to 2K and 8 KV heads 17.5 against 27), chunks with more (16 rows of 32K 66 us against 71, 48 ragged rows
+// of up to 8K 45 against 58).
+inline int nibble_share(const NibbleRowArg* row, int n_rows, int n_gh, int teams, int64_t units, int64_t pairs, int sms) {
+    const int64_t most = int64_t(sms) * kNibbleCtasPerSm;
+    const float rounds = float(units) / float(most * teams);
+    if (pairs == 0 || pairs > most || rounds > 24.f) return 0;
+    const float at0[kNibbleCtasPerSm] = {7.f, 9.3f, 9.5f}, per_tile[kNibbleCtasPerSm] = {1.3f, 1.75f, 2.5f};
+    auto ctas = [&](int share) {
+        int64_t n = 0;
+        for (int r = 0; r < n_rows; ++r) n += (row[r].tiles + share - 1) / share;
+        return n * n_gh;
+    };
+    float best = 11.5f + 2.4f * rounds + (pairs > 1 ? 5.5f : 0.f);
+    int share = 0;
+    for (int w = 0; w < kNibbleCtasPerSm; ++w) {
+        const int64_t limit = int64_t(sms) * (w + 1);
+        if (pairs > limit) continue;
+        // the fewest tiles a team with which the CTAs stay within the limit; they only get fewer with more tiles a team
+        const float most_tiles = (best - at0[w]) / per_tile[w];          // not better from here on
+        if (most_tiles < 1.f) continue;
+        int lo = 1, hi = int(most_tiles);
+        if (ctas(hi * teams) > limit) continue;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (ctas(mid * teams) <= limit) hi = mid; else lo = mid + 1;
+        }
+        const float t = at0[w] + per_tile[w] * float(lo);
+        if (t < best) { best = t; share = lo * teams; }
+    }
+    return share;
 }
 cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s);
 

@@ -164,7 +164,7 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
     int32_t n_runs = 0, pairs = 0;
     for (int r = 0; r < n_rows; ++r) {
         int64_t tiles = 0;
-        row[r].run0 = n_runs; row[r].pair0 = pairs; row[r].unit0 = int32_t(units);
+        row[r].run0 = n_runs; row[r].pair0 = pairs; row[r].first = int32_t(units);
         for (int32_t k = row_run_start[r]; k < row_run_start[r + 1]; ++k) {
             if (runs[k].n_tokens == 0) continue;
             run[n_runs++] = NibbleRunArg{static_cast<const char*>(runs[k].blocks_dev), int32_t(runs[k].n_tokens), int32_t(tiles)};
@@ -173,9 +173,18 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
         }
         row[r].tiles = int32_t(tiles);
         longest = std::max(longest, tiles);
-        units += tiles * plan.n_gh;
+        if (tiles > 0) units += (tiles + kNibblePairCost) * plan.n_gh;
         pairs += tiles > 0 ? plan.n_gh : 0;
         if (units > INT32_MAX) return IPKV_EINVAL;
+    }
+    a.n_ctas = units < NibblePlan::kCtas ? int32_t(units) : NibblePlan::kCtas;
+    a.max_parts = units > 0 ? int32_t((((longest + kNibblePairCost) * a.n_ctas + units - 1) / units + 1) * plan.teams) : 0;
+    a.share = nibble_share(row, n_rows, plan.n_gh, plan.teams, units, pairs, kSmCount);
+    if (a.share > 0) {
+        int64_t ctas = 0;
+        for (int r = 0; r < n_rows; ++r) { row[r].first = int32_t(ctas); ctas += plan.n_gh * ((row[r].tiles + a.share - 1) / a.share); }
+        a.n_ctas = int32_t(ctas);
+        a.max_parts = int32_t((longest + a.share - 1) / a.share * plan.teams);
     }
     a.rows = nullptr; a.runs = nullptr; a.plain_launch = 0;
     if (!inlined) {
@@ -200,8 +209,6 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
     a.part_rows = int64_t(plan.part_rows(n_rows));
     a.out_o = o; a.out_lse = lse; a.status = status;
     a.n_rows = n_rows; a.n_units = int32_t(units); a.n_runs = n_runs;
-    a.n_ctas = units < NibblePlan::kCtas ? int32_t(units) : NibblePlan::kCtas;
-    a.max_parts = units > 0 ? int32_t(((longest * a.n_ctas + units - 1) / units + 1) * plan.teams) : 0;
     a.n_q_heads = sh->n_q_heads; a.group = plan.group; a.groups_per_kv = plan.groups_per_kv; a.n_gh = plan.n_gh; a.rows_per_part = plan.rows_per_part;
     a.octets = plan.octets; a.teams = plan.teams;
     a.scale = sh->softmax_scale > 0.f ? sh->softmax_scale : 1.0f / std::sqrt(float(sh->dim_qk));

@@ -12,5 +12,19 @@ int shim_nibble_smem(int dim, int octets) {
 }
 int shim_nibble_smem_limit() { return kNibbleSmemPerCta; }
 int shim_nibble_groups(int group) { return nibble_groups_per_kv(group); }
+int shim_nibble_ctas_per_sm() { return kNibbleCtasPerSm; }
+// rows of `tiles` tiles -> the share, and how many CTAs it takes
+int shim_nibble_share(const int* tiles, int n_rows, int n_gh, int teams, int sms, int* ctas) {
+    NibbleRowArg row[4096];
+    int64_t units = 0, pairs = 0;
+    for (int i = 0; i < n_rows; ++i) {
+        row[i] = NibbleRowArg{0, tiles[i], 0, 0};
+        if (tiles[i] > 0) { units += int64_t(tiles[i] + kNibblePairCost) * n_gh; pairs += n_gh; }
+    }
+    const int share = nibble_share(row, n_rows, n_gh, teams, units, pairs, sms);
+    *ctas = 0;
+    for (int i = 0; i < n_rows && share > 0; ++i) *ctas += (tiles[i] + share - 1) / share * n_gh;
+    return share;
+}
 int shim_nibble_rows(int group) { return nibble_rows_per_part(group); }
 }
