@@ -49,7 +49,10 @@ constexpr int kThreads = (kWarps + 1) * 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.f;                    // the reference maximum is raised when a score exceeds it by this (log2)
-constexpr int kManyParts = 16;                   // partials of a (row, head) from which the join is spread over more threads
+// Partials of a (row, head) above which its join is cut into slabs of 32 columns by 256 and by 512 threads.  Under 64 one CTA a head is
+// better (16 rows of 32K tokens, 32 partials: 61.9 us in all, with slabs 65.4; 4 rows of 50K, 60 partials: 49 and 59), over 256 more
+// threads are (one row of 1M, 888 partials: 61.2 and 66.9 with 256 threads; one of 64K, 148 partials: 21.9 and 19.2).
+constexpr int kManyParts = 64, kVeryManyParts = 256;
 constexpr uint32_t kLowK = 0x000f000fu, kHighK = 0x00f000f0u;       // K codes as bf16 in bits 0..3 and 4..7: times 2^-133 and 2^-129
 constexpr uint32_t kLow = 0x00780078u, kHigh = 0x07800780u;         // V codes as fp16 in bits 3..6 and 7..10: times 2^-21 and 2^-17
 
@@ -580,6 +583,9 @@ cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
     }
     const int items = a.n_rows * a.n_q_heads;
+    if (a.max_parts > kVeryManyParts)
+        return launch_ordered(true, wide ? nibble_reduce_kernel<128, 32, 512> : nibble_reduce_kernel<64, 32, 512>, items * (a.g.dim / 32), 512,
+                              size_t(0), s, a);
     if (a.max_parts > kManyParts)
         return launch_ordered(true, wide ? nibble_reduce_kernel<128, 32, 256> : nibble_reduce_kernel<64, 32, 256>, items * (a.g.dim / 32), 256,
                               size_t(0), s, a);

@@ -303,6 +303,36 @@ def test_attention_matches_64_bits(hq, hkv, d, bt, rows):
     assert np.array_equal(o, again[0]) and np.array_equal(lse, again[1])         # bit-reproducible
 
 
+def ragged(n_rows, most, seed):
+    rng = np.random.default_rng(seed)
+    rows = [[int(x)] for x in rng.integers(0, most, n_rows)]
+    rows[0], rows[1], rows[2], rows[-2], rows[-1] = [0], [1, 0, 64], [most], [65], []
+    return rows
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,bt,rows", [
+    (8, 8, 64, 64, ragged(64, 300, 1)),          # more pairs than CTAs: equal chunks that meet many pairs, tables in the launch
+    (32, 4, 64, 64, ragged(130, 200, 2)),        # ... and uploaded
+    (16, 8, 128, 128, ragged(60, 3000, 3)),      # chunks that end inside pairs
+    (16, 1, 64, 64, ragged(500, 130, 4)),        # two octets a tile
+    (4, 1, 64, 64, [[40000]]),                   # one pair, hundreds of partials
+    (8, 1, 128, 64, [[40000]]),
+    (16, 1, 128, 64, [[40000, 7]]),
+    (16, 4, 128, 64, ragged(12, 5000, 5)),       # whole CTAs to ragged pairs
+    (24, 2, 64, 64, ragged(30, 1000, 6)),
+])
+def test_attention_however_the_work_is_shared_out(hq, hkv, d, bt, rows):
+    rng = np.random.default_rng(len(rows) + hq)
+    sh = shape_of(hq, hkv, d, bt)
+    buf, runs, kvs = fill(rng, sh, rows)
+    q = synth.normal_bf16(rng, (len(rows), hq, d))
+    o, lse = attend(sh, runs, q)
+    check(sh, q, kvs, o, lse)
+    again = attend(sh, runs, q)
+    assert np.array_equal(o, again[0]) and np.array_equal(lse, again[1])
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("what", ["peaked", "rising", "tiny values", "huge values", "scales that grow", "zero queries", "large queries", "one constant"])
 def test_attention_on_hard_values(what):
