@@ -22,9 +22,11 @@
 // subnormal range: K's do in place as bf16 (7 bits of mantissa; bits 0..3 and 4..7), V's are shifted up to bits 3..6 and 7..10 of fp16,
 // in place they lost up to six bits of their products.  And the sums over tokens must not be much larger than the result:
 // codes are never negative, but an output is a mean of many values of either sign, so a sum of p sv code would exceed it by
-// 2.5 sqrt(tokens); every other eight tokens enter complemented, code = 15 - (15 - code): the complement costs nothing in the
-// mask, its weight is negative, 15 sv joins zv, and the excesses of the two halves meet in the same product.  Without
-// the two the output of 32K tokens was off by 5e-4 of itself.
+// 2.5 sqrt(tokens); every other token enters complemented, code = 15 - (15 - code): the complement costs nothing in the mask, its
+// weight is negative, 15 sv joins zv, and the excesses of the two halves meet in the same product (and in either half of its
+// 16 tokens: with tokens 0-7 plain and 8-15 complemented the cut was one-sided, 4.2e-6 of the output at 1M tokens instead of 8e-7).
+// Remainders have sums of their own: added to the heads' they would be cut at the heads' exponent.  Without all this the output of
+// 32K tokens was off by 5e-4 of itself; it is off by 1e-6 (a computation in fp32: 6e-7).
 //
 // One warp works on one tile (64 tokens of a KV head) at a time, alone: its online softmax has its own reference maximum, raised
 // only when a score exceeds it by 2^8 (then everything is rescaled), which costs one vote per tile in place of a reduction over lanes.  A
@@ -79,6 +81,17 @@ __device__ __forceinline__ float2 fma2(float a0, float a1, float b0, float b1, f
     float2 r;
     asm("{.reg .b64 p, q, s; mov.b64 p, {%2,%3}; mov.b64 q, {%4,%5}; mov.b64 s, {%6,%7}; fma.rn.f32x2 p, p, q, s; mov.b64 {%0,%1}, p;}"
         : "=f"(r.x), "=f"(r.y) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+    return r;
+}
+// (a ^ b) & c and (a ^ ~b) & c
+__device__ __forceinline__ uint32_t differ(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0x28;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t agree(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0x82;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
@@ -230,6 +243,9 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
     const int team = warp / octets, octet = warp - team * octets;
     const bool works = team < teams;
     bool dead = false;
+    // Which tokens enter the output product complemented: 16u + 8h + g with g + h odd.
+    const uint32_t odd = p.odd_tokens;           // g odd, as the halves of a word of V (an immediate here would cost an instruction a use)
+    const float k15 = (g & 1) ? 15.f : 0.f;
 
     int it0 = 0;                                 // tiles of this CTA before the current pair
     int st = team, phase = 0;                    // stage of the team's next tile and its parity (stages is a multiple of teams)
@@ -358,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                         for (int pn = 0; pn < P; ++pn) s[un][2 * h + e] = fmaf(ptx::bf16_lo(km[h][pn]), acc[pn][2 * h + e], s[un][2 * h + e]);
                     }
                     sv[un][h] = ptx::bf16_lo(vmm[h]);
-                    zv[un][h] = h ? fmaf(ptx::bf16_lo(vmm[h]), 15.f, ptx::bf16_hi(vmm[h])) : ptx::bf16_hi(vmm[h]);
+                    zv[un][h] = fmaf(ptx::bf16_lo(vmm[h]), h ? 15.f - k15 : k15, ptx::bf16_hi(vmm[h]));
                 }
             }
             if (nv < kTileTokens) {              // what lies behind the last token may be anything, NaN too
@@ -409,7 +425,8 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
 
             // weights, and their products with the value scales as operands [token][head]
             uint32_t hi[4][2], lo[4][2];
-            const float f0 = fv * 64.f, f1 = fv * -4.f;                  // tokens 8-15 of a unit meet complements, times 2^4
+            float zt[2] = {0.f, 0.f};
+            const float f0 = (g & 1) ? fv * -64.f : fv * 64.f, f1 = f0 * -0.0625f;   // a complement's weight is negative; codes of h = 1 are times 2^4
 #pragma unroll
             for (int un = 0; un < 4; ++un)
 #pragma unroll
@@ -421,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                     add2(l[0], l[1], pr[0], pr[1]);
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        oz[e] = fmaf(pr[e], zv[un][h], oz[e]);
+                        zt[e] = fmaf(pr[e], zv[un][h], zt[e]);
                         w[e] = pr[e] * svf;
                     }
                     const uint32_t big = pack_f16(w[0], w[1]);
@@ -432,21 +449,26 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                     else { hi[un][h] = transpose8x8(big); lo[un][h] = transpose8x8(rest); }
                 }
 
-            // output: 16 columns of the head a time, the tile's 64 tokens; a sum per tile, added to the state in fp32 (to nearest)
+            add2(oz[0], oz[1], zt[0], zt[1]);
+
+            // output: 16 columns of the head a time, the tile's 64 tokens; sums per tile, added to the state in fp32 (to nearest)
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
                 const uint4 y = *reinterpret_cast<const uint4*>(tile + kV + (d * 32 + lane) * 16);
                 const uint32_t ya[2] = {y.x, y.y}, yb[2] = {y.z, y.w};
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                float sum[4] = {0.f, 0.f, 0.f, 0.f}, low[4] = {0.f, 0.f, 0.f, 0.f};      // of the weights' heads and remainders
 #pragma unroll
                 for (int un = 0; un < 4; ++un) {
                     const uint32_t va = (un & 1) ? ya[un >> 1] >> 5 : ya[un >> 1] << 3, vb = (un & 1) ? yb[un >> 1] >> 5 : yb[un >> 1] << 3;
-                    const uint32_t a0 = va & kLow, a1 = vb & kLow, a2 = ~va & kHigh, a3 = ~vb & kHigh;
+                    const uint32_t a0 = differ(va, odd, kLow), a1 = differ(vb, odd, kLow), a2 = agree(va, odd, kHigh), a3 = agree(vb, odd, kHigh);
                     mma_f16(sum, a0, a1, a2, a3, hi[un][0], hi[un][1]);
-                    if (!HALF) mma_f16(sum, a0, a1, a2, a3, lo[un][0], lo[un][1]);
+                    if (!HALF) mma_f16(low, a0, a1, a2, a3, lo[un][0], lo[un][1]);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) add2(o[d][i], o[d][i + 1], sum[i], sum[i + 1]);
+                for (int i = 0; i < 4; i += 2) {
+                    if (!HALF) add2(sum[i], sum[i + 1], low[i], low[i + 1]);
+                    add2(o[d][i], o[d][i + 1], sum[i], sum[i + 1]);
+                }
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[st]));

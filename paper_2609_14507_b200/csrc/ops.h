@@ -118,6 +118,7 @@ struct NibbleAttend {
     int32_t stages, n_runs;
     int32_t share;                               // whole CTAs to every pair: tiles that one takes at most; 0: equal chunks of all units
     int32_t max_parts;                           // partials of a (row, head group) at most
+    uint32_t odd_tokens;                         // 0xffff0000, see the kernel
     int32_t plain_launch;                        // the tables were written by the kernel in front of this launch: no overlap with it
     float scale;
 };

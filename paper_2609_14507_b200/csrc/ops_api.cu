@@ -186,7 +186,7 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
         a.n_ctas = int32_t(ctas);
         a.max_parts = int32_t((longest + a.share - 1) / a.share * plan.teams);
     }
-    a.rows = nullptr; a.runs = nullptr; a.plain_launch = 0;
+    a.rows = nullptr; a.runs = nullptr; a.plain_launch = 0; a.odd_tokens = 0xffff0000u;
     if (!inlined) {
         // as ipkv_attend_runs: a captured copy would be replayed from the image's address long after it is gone
         cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
