@@ -32,9 +32,17 @@
 // only when a score exceeds it by 2^8 (then everything is rescaled), which costs one vote per tile in place of a reduction over lanes.  A
 // producer warp streams tiles (one bulk copy each, they are contiguous) into a ring of stages on mbarriers; the warps of a CTA
 // take them in turn.  At the end of a (row, head group) every warp writes its partial and goes on, and a second kernel joins the partials
-// in a fixed order.  (Joining a CTA's warps through shared memory first made each wait for the slowest: 2.7 us per pair and CTA.)
+// in a fixed order.  (Joining a CTA's warps through shared memory first made each wait for the slowest: ragged 64 192 us, now 175
+// with that change alone.)  How rows and heads are shared out among CTAs: ops.h.
 // More than 8 query heads per KV head: several warps (one per octet of heads) share a tile, so it is still read once.
 // Every wait is bounded; a warp whose wait ran out does no more work.
+//
+// Bound by instruction issue, then by the copies: a product of 16 x 8 x 16 keeps its quarter of an SM busy for eight cycles, and a tile of
+// 128 columns takes 68 of them (4 query heads per KV head) or 100, beside 750 to 900 other instructions; the tiles of three
+// CTAs with four such warps and 73 KB of ring each are under way on an SM (fewer or larger CTAs: 3 to 15 % slower).  Measured, 128 columns:
+// 64 ragged rows of up to 24K tokens, 8 KV heads of 4 query heads: 158 us for 932 MB, 5.9 TB/s, 0.90 of a copy's rate; 16 rows of 32K,
+// 4 KV heads of 8: 62.7 us, 4.7 TB/s; one of 1M, 16 query heads on one KV head (every tile unpacked by two warps): 64 us,
+// 2.2 TB/s; one of 4K: 8.6 us, two launches of which neither does much.
 #include <cuda_fp16.h>
 
 #include "kernels.h"
@@ -521,7 +529,8 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
 // Joins the partials of every (row, query head): with partial i's maximum m_i (log2), sum l_i and normalised O_i,
 //   m = max m_i,  z = sum 2^(m_i - m) l_i,  O = sum 2^(m_i - m) l_i O_i / z,  LSE = m ln 2 + ln z,   in a fixed order.
 // One CTA per (row, head, COLS columns): COLS/4 column groups times THREADS / (COLS/4) slices of the partials.  Bound by the latency of
-// its two dependent reads; many partials per head (few heads, a long sequence) want many slices, see the launch.
+// its two dependent reads (16 rows of 32K tokens, 512 heads of 32 partials: 10 us by itself, most of it under the kernel before and after);
+// many partials per head (few heads, a long sequence) want many slices, see kManyParts.
 template <int D, int COLS, int THREADS>
 __global__ void __launch_bounds__(THREADS) nibble_reduce_kernel(const __grid_constant__ NibbleAttend p) {
     constexpr int kCols = COLS / 4, kSlices = THREADS / kCols, kSlabs = D / COLS;
