@@ -13,7 +13,7 @@
 // exactly the tokens that share its words of V.  All 8 loads of a thread are issued before the first is used.  Groups are reduced
 // among the lanes of a token by shuffles; the tile's image is put together in shared memory and leaves in 16-byte stores.
 // A tile that the span covers in part keeps the other tokens' codes: its image is loaded first.
-// 32K tokens of 4 heads of 128 columns, written and read back: 34 us for 171 MB, 5.0 TB/s, 0.77 of a copy's rate (issue slots 79 %
+// 32K tokens of 4 heads of 128 columns, written and read back: 33 us for 171 MB, 5.2 TB/s, 0.79 of a copy's rate (issue slots 79 %
 // busy in pack, 72 % in unpack); with K and V of a tile in one CTA 36, seven ragged chunks of up to 2.5K tokens 8.3 and 15 (half as many
 // CTAs, each twice as long); a scale computed by every lane, and fp32 values in unpack, 45.5.
 //
@@ -82,14 +82,30 @@ __device__ __forceinline__ Group group_k(const Group& own, int lane, int k) {
     return g;
 }
 
-// The code of a value in the low bits of a word whose other bits are kMagic's.  Everything is done on a sixteenth of the code, so that
-// the last multiply-add can saturate to [0, 1]: a NaN becomes 0 there, and no value touches another one's code.
-__device__ __forceinline__ uint32_t code_bits(float x, float scale16, float zero, float inverse16) {
-    const float d = __fsub_rn(x, zero);
-    const float t = __fmul_rn(d, inverse16);
-    float q;
-    asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(q) : "f"(__fmaf_rn(-t, scale16, d)), "f"(inverse16), "f"(t));
-    return __float_as_uint(__fmaf_rn(q, 16.f, kMagic));
+// Two fp32 numbers as the operand of an instruction that does both.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1,%2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+// What the codes of a group are made with, twice each.
+struct Quotient { uint64_t minus_zero, inverse16, minus_scale16; float inverse; };
+__device__ __forceinline__ Quotient quotient_of(const Group& g) {
+    const float z = -ptx::bf16_hi(g.meta), s = -16.f * ptx::bf16_lo(g.meta);
+    return Quotient{two(z, z), two(g.inverse16, g.inverse16), two(s, s), g.inverse16};
+}
+// The codes of two values in the low bits of words whose other bits are kMagic's.  Everything is done on a sixteenth of the code, so that
+// the last multiply-add of the quotient can saturate to [0, 1]: a NaN becomes 0 there, and no value touches another one's code.  (All but
+// that one for both values at once: 32.9 us for 32K tokens both ways, one value a time 34.0.)
+__device__ __forceinline__ void two_codes(uint32_t x, const Quotient& g, uint32_t& a, uint32_t& b) {
+    float r0, r1, t0, t1, q0, q1;
+    asm("{.reg .b64 d, t, r; add.rn.f32x2 d, %4, %5; mul.rn.f32x2 t, d, %6; fma.rn.f32x2 r, t, %7, d; mov.b64 {%0,%1}, r; mov.b64 {%2,%3}, t;}"
+        : "=f"(r0), "=f"(r1), "=f"(t0), "=f"(t1)
+        : "l"(two(ptx::bf16_lo(x), ptx::bf16_hi(x))), "l"(g.minus_zero), "l"(g.inverse16), "l"(g.minus_scale16));
+    asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(q0) : "f"(r0), "f"(g.inverse), "f"(t0));
+    asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(q1) : "f"(r1), "f"(g.inverse), "f"(t1));
+    asm("{.reg .b64 c; fma.rn.f32x2 c, %2, %3, %4; mov.b64 {%0,%1}, c;}"
+        : "=r"(a), "=r"(b) : "l"(two(q0, q1)), "l"(two(16.f, 16.f)), "l"(two(kMagic, kMagic)));
 }
 
 // Two codes (bits 0..3 of either half of x) -> their two values, rounded to bf16 once: under the exponent of 128 the bits are 128 +
@@ -204,15 +220,12 @@ __global__ void __launch_bounds__(kThreads) nibble_pack_kernel(const __grid_cons
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const Group g = group_k(own, lane, k);
-        const float scale16 = 16.f * ptx::bf16_lo(g.meta), zero = ptx::bf16_hi(g.meta);
+        const Quotient quotient = quotient_of(g);
         const uint32_t xx[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
         const int row = row0 + 16 * ((k & 3) >> 1) + 2 * (k >> 2) + (k & 1);
         uint32_t bits[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bits[2 * i] = code_bits(ptx::bf16_lo(xx[i]), scale16, zero, g.inverse16);
-            bits[2 * i + 1] = code_bits(ptx::bf16_hi(xx[i]), scale16, zero, g.inverse16);
-        }
+        for (int i = 0; i < 4; ++i) two_codes(xx[i], quotient, bits[2 * i], bits[2 * i + 1]);
         if (is_v) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) words[j] += bits[j] << (4 * k);
@@ -325,17 +338,18 @@ __global__ void __launch_bounds__(kThreads) nibble_pack_token_kernel(const __gri
     if (kLanes == 16) ve = min2(ve, __shfl_xor_sync(0xffffffffu, ve, 8));
     if (!job.live) return;
     const Group gk = group_of(ke), gv = group_of(ve);
-    const float ks = 16.f * ptx::bf16_lo(gk.meta), kz = ptx::bf16_hi(gk.meta), vs = 16.f * ptx::bf16_lo(gv.meta), vz = ptx::bf16_hi(gv.meta);
+    const Quotient kq = quotient_of(gk), vq = quotient_of(gv);
     const uint32_t x[4] = {kx.x, kx.y, kx.z, kx.w}, y[4] = {vx.x, vx.y, vx.z, vx.w};
     uint32_t word = 0;
     const int shift = 4 * nibble_v_of(job.t);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        word += code_bits(ptx::bf16_lo(x[i]), ks, kz, gk.inverse16) << (8 * i);
-        word += code_bits(ptx::bf16_hi(x[i]), ks, kz, gk.inverse16) << (8 * i + 4);
-        const uint32_t a = code_bits(ptx::bf16_lo(y[i]), vs, vz, gv.inverse16) & 15u, b = code_bits(ptx::bf16_hi(y[i]), vs, vz, gv.inverse16) & 15u;
-        old[2 * i] = (old[2 * i] & ~(15u << shift)) | (a << shift);
-        old[2 * i + 1] = (old[2 * i + 1] & ~(15u << shift)) | (b << shift);
+        uint32_t a, b;
+        two_codes(x[i], kq, a, b);
+        word += (a << (8 * i)) + (b << (8 * i + 4));
+        two_codes(y[i], vq, a, b);
+        old[2 * i] = (old[2 * i] & ~(15u << shift)) | ((a & 15u) << shift);
+        old[2 * i + 1] = (old[2 * i + 1] & ~(15u << shift)) | ((b & 15u) << shift);
     }
     job.image[nibble_k_word(kPanels, job.t, c)] = word - kMagicSum;
     if ((c & 7) == 0) job.image[kKMeta + nibble_meta_row(job.t) * kPanels + (c >> 3)] = gk.meta;
