@@ -79,7 +79,7 @@ class Run(C.Structure):
 
 class Rope(C.Structure):
     _fields_ = [("dim", C.c_int32), ("rot_dim", C.c_int32), ("n_axes", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float),
-                ("theta", C.c_double), ("inv_freq", C.c_void_p), ("pair_axis", C.c_void_p)]
+                ("theta", C.c_double), ("inv_freq", C.c_void_p), ("pair_axis", C.c_char_p)]
 
 
 class Heads(C.Structure):
@@ -546,15 +546,15 @@ def ipkv_pack_blocks(shape, layout, k, v, n_tokens, dst, stream=None):
 # A decode step calls these once a layer, so what they check is checked with few attribute reads, and tables go to the
 # library as packed bytes.
 
-_torch = _np = None
+_torch = _np = _bf16 = _f32 = _i32 = _int64 = _int32 = None
 
 
 def _modules():
-    global _torch, _np
+    global _torch, _np, _bf16, _f32, _i32, _int64, _int32
     import numpy
     import torch
     _np, _torch = numpy, torch
-    return torch
+    _bf16, _f32, _i32, _int64, _int32 = torch.bfloat16, torch.float32, torch.int32, numpy.dtype(numpy.int64), numpy.dtype(numpy.int32)
 
 
 def _call_stream(stream, dev):
@@ -570,6 +570,7 @@ def _call_stream(stream, dev):
 # ---- head norm and rotation ----
 
 _HEADS_FORMAT = struct.Struct("<QQQi4xqqqq")         # ipkv_heads
+_AXIS = (b"\0", b"\1", b"\2", b"\3")
 
 
 def make_rope(dim, rot_dim=None, *, theta=10000.0, sections=None, interleaved=False, eps=1e-6, inv_freq=None, pair_axis=None):
@@ -577,23 +578,28 @@ def make_rope(dim, rot_dim=None, *, theta=10000.0, sections=None, interleaved=Fa
     rot_dim / 2); pair_axis: the axis of every pair instead, for other arrangements; neither: one axis."""
     rot_dim = dim if rot_dim is None else rot_dim
     pairs = rot_dim // 2
-    r = Rope(dim, rot_dim, 1, 1 if interleaved else 0, eps, theta, None, None)
+    n_axes = 1
     if sections is not None:
         if pair_axis is not None:
             raise ValueError("sections and pair_axis exclude each other")
-        if sum(sections) != pairs or min(sections, default=0) < 0:
-            raise ValueError(f"{sum(sections)} pairs have an axis, {pairs} are rotated")
-        r.n_axes = len(sections)
-        if len(sections) > 1:
-            pair_axis = b"".join([bytes((a,)) * n for a, n in enumerate(sections)])
+        n_axes = len(sections)
+        if n_axes > 1:
+            pair_axis = b""
+            for a, n in enumerate(sections):
+                if n < 0:
+                    raise ValueError(f"a section has {n} pairs")
+                pair_axis += _AXIS[a] * n if a < 4 else bytes((a,)) * n
+            total = len(pair_axis)
+        else:
+            total = sections[0] if n_axes else 0
+        if total != pairs:
+            raise ValueError(f"{total} pairs have an axis, {pairs} are rotated")
     elif pair_axis is not None:
         if len(pair_axis) != pairs:
             raise ValueError(f"{len(pair_axis)} pairs have an axis, {pairs} are rotated")
-        r.n_axes = max(pair_axis, default=0) + 1
+        n_axes = max(pair_axis, default=0) + 1
         pair_axis = bytes(pair_axis)
-    if pair_axis:
-        r._axes = pair_axis                              # stays alive with r
-        r.pair_axis = C.cast(pair_axis, C.c_void_p)
+    r = Rope(dim, rot_dim, n_axes, 1 if interleaved else 0, eps, theta, None, pair_axis or None)         # the field keeps the bytes
     if inv_freq is not None:
         if len(inv_freq) != pairs:
             raise ValueError(f"{len(inv_freq)} frequencies, {pairs} pairs are rotated")
@@ -605,8 +611,9 @@ def make_rope(dim, rot_dim=None, *, theta=10000.0, sections=None, interleaved=Fa
 def ipkv_norm_rope(rope, parts, positions, stream=None):
     """parts: 1..4 tuples (x, weight or None, out or None): x and out [n_tokens, heads, dim] bf16 with any token and head
     strides, out None means in place.  positions: int32 [n_axes, n_tokens] (or [n_tokens]), contiguous; None without a rotation."""
-    torch = _torch or _modules()
-    bf16, dim = torch.bfloat16, rope.dim
+    if _torch is None:
+        _modules()
+    bf16, dim = _bf16, rope.dim
     x = parts[0][0]
     n_tokens, dev = x.shape[0], x.get_device()
     packed = b""
@@ -615,24 +622,20 @@ def ipkv_norm_rope(rope, parts, positions, stream=None):
         if x.dtype is not bf16 or len(shape) != 3 or shape[0] != n_tokens or shape[2] != dim:
             raise ValueError(f"heads are bfloat16 [{n_tokens}, n_heads, {dim}]: got {x.dtype} {tuple(shape)}")
         n_heads, (it, ih, ic), at = shape[1], x.stride(), x.data_ptr()
-        if n_tokens <= 1:                                # the stride of a dimension of one is never used
-            it = 0
-        if n_heads <= 1:
-            ih = 0
         if out is None:
-            ot, oh, to = it, ih, at
+            ot, oh, oc, to = it, ih, ic, at
         else:
             if out.dtype is not bf16 or out.shape != shape:
                 raise ValueError(f"an output is like its input: got {out.dtype} {tuple(out.shape)} for {tuple(shape)}")
             (ot, oh, oc), to = out.stride(), out.data_ptr()
-            if n_tokens <= 1:
-                ot = 0
-            if n_heads <= 1:
-                oh = 0
-            if oc != 1 or out.get_device() != dev:
-                raise ValueError("the columns of a head are contiguous, and all tensors are on one device")
-        if ic != 1 or x.get_device() != dev:
+            if out.get_device() != dev:
+                oc = 0
+        if ic != 1 or oc != 1 or x.get_device() != dev:
             raise ValueError("the columns of a head are contiguous, and all tensors are on one device")
+        if n_tokens <= 1:                                # the stride of a dimension of one is never used
+            it = ot = 0
+        if n_heads <= 1:
+            ih = oh = 0
         if w is None:
             wp = 0
         else:
@@ -641,10 +644,10 @@ def ipkv_norm_rope(rope, parts, positions, stream=None):
             wp = w.data_ptr()
         packed += _HEADS_FORMAT.pack(at, to, wp, n_heads, it, ih, ot, oh)
     if positions is not None:
-        if positions.dtype is not torch.int32 or positions.numel() != rope.n_axes * n_tokens or not positions.is_contiguous() or positions.get_device() != dev:
+        if positions.dtype is not _i32 or positions.numel() != rope.n_axes * n_tokens or not positions.is_contiguous() or positions.get_device() != dev:
             raise ValueError(f"positions are contiguous int32 [{rope.n_axes}, {n_tokens}] on the device of the heads")
         positions = positions.data_ptr()
-    rc = lib().ipkv_norm_rope(C.byref(rope), n_tokens, packed, len(parts), positions, _call_stream(stream, dev))
+    rc = (_lib or lib()).ipkv_norm_rope(C.byref(rope), n_tokens, packed, len(parts), positions, _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, "ipkv_norm_rope")
 
@@ -663,26 +666,28 @@ def _table(rows, width):
     """A host table of 64-bit words, [n][width]: a NumPy int64 array as it is, or rows whose first entry may be a tensor."""
     if not isinstance(rows, _np.ndarray):
         rows = _np.array([[_ptr(r[0]) or 0, *r[1:]] for r in rows], dtype=_np.int64).reshape(-1, width)
-    if rows.dtype != _np.int64 or rows.ndim != 2 or rows.shape[1] != width or not rows.flags.c_contiguous:
-        raise ValueError(f"expected a contiguous int64 array [n][{width}]: got {rows.dtype} {rows.shape}")
+    shape = rows.shape
+    if rows.dtype != _int64 or len(shape) != 2 or shape[1] != width or not rows.flags.c_contiguous:
+        raise ValueError(f"expected a contiguous int64 array [n][{width}]: got {rows.dtype} {shape}")
     return rows
 
 
 def _move(name, shape, spans, k, v, stream):
-    torch = _torch or _modules()
+    if _torch is None:
+        _modules()
     t = _table(spans, 3)
-    heads, dim, n, dev = shape.n_kv_heads, shape.dim_qk, k.shape[0], k.get_device()
-    strides = []
-    for x in (k, v):
-        d = x.shape
-        if x.dtype is not torch.bfloat16 or len(d) != 3 or d[0] != n or d[1] != heads or d[2] != dim:
-            raise ValueError(f"K and V are bfloat16 [{n}, {heads}, {dim}]: got {x.dtype} {tuple(d)}")
-        token, head, column = x.stride()
-        if column != 1 or (heads > 1 and head != dim) or (n > 1 and token == 0) or x.get_device() != dev:
-            raise ValueError("the heads of a token lie side by side, its tokens apart, and K and V are on one device")
-        strides.append(token if n > 1 else 0)
-    rc = getattr(lib(), name)(C.byref(shape), t.shape[0], t.tobytes(), n, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
-                              _call_stream(stream, dev))
+    heads, dim, size, dev, bf16 = shape.n_kv_heads, shape.dim_qk, k.shape, k.get_device(), _bf16
+    n = size[0]
+    if k.dtype is not bf16 or v.dtype is not bf16 or len(size) != 3 or size[1] != heads or size[2] != dim or v.shape != size:
+        raise ValueError(f"K and V are bfloat16 [tokens, {heads}, {dim}]: got {k.dtype} {tuple(size)}, {v.dtype} {tuple(v.shape)}")
+    (kt, kh, kc), (vt, vh, vc) = k.stride(), v.stride()
+    if n <= 1:                                           # the stride of a dimension of one is never used
+        kt = vt = 0
+    elif kt == 0 or vt == 0:
+        kc = 0
+    if kc != 1 or vc != 1 or (heads > 1 and (kh != dim or vh != dim)) or v.get_device() != dev:
+        raise ValueError("the heads of a token lie side by side, its tokens apart, and K and V are on one device")
+    rc = getattr(_lib or lib(), name)(C.byref(shape), len(t), t.tobytes(), n, k.data_ptr(), v.data_ptr(), kt, vt, _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, name)
 
@@ -709,24 +714,28 @@ def ipkv_nibble_scratch_bytes(shape, n_rows, n_runs):
 def ipkv_nibble_attend(shape, runs, row_start, q, scratch, o_part, lse_part, status=None, stream=None):
     """Attention of one query per row over runs of NIBBLE blocks.  runs: int64 array [n][2] of (address, tokens) with row_start,
     an int32 array [rows + 1]; or, with row_start None, one list per row of (blocks, tokens) as for ipkv_attend_runs."""
-    torch = _torch or _modules()
+    if _torch is None:
+        _modules()
     if row_start is None:
         row_start = _np.cumsum([0] + [len(r) for r in runs]).astype(_np.int32)
         runs = _table([x for r in runs for x in r], 2)
     else:
         runs = _table(runs, 2)
-        if not isinstance(row_start, _np.ndarray) or row_start.dtype != _np.int32 or row_start.ndim != 1 or not row_start.flags.c_contiguous:
+        if not isinstance(row_start, _np.ndarray) or row_start.dtype != _int32 or row_start.ndim != 1 or not row_start.flags.c_contiguous:
             raise ValueError("row_start is a contiguous int32 array [rows + 1]")
-    rows = row_start.shape[0] - 1
-    if rows < 1 or row_start[-1] > runs.shape[0]:
-        raise ValueError(f"row_start names runs that are not there: there are {runs.shape[0]}")
-    want, dev = (rows, shape.n_q_heads, shape.dim_qk), q.get_device()
-    for x, dtype, size, what in ((q, torch.bfloat16, want, "q"), (o_part, torch.float32, want, "o_part"), (lse_part, torch.float32, want[:2], "lse_part")):
-        if x.dtype is not dtype or x.shape != size or not x.is_contiguous() or x.get_device() != dev:
-            raise ValueError(f"{what} is contiguous {dtype} {size} on the device of q: got {x.dtype} {tuple(x.shape)}")
-    if scratch.get_device() != dev or not scratch.is_contiguous() or (status is not None and (status.get_device() != dev or status.dtype not in (torch.int32, torch.uint32))):
+    rows = len(row_start) - 1
+    if rows < 1 or row_start.item(-1) > len(runs):
+        raise ValueError(f"row_start names runs that are not there: there are {len(runs)}")
+    heads, f32, dev = shape.n_q_heads, _f32, q.get_device()
+    want = (rows, heads, shape.dim_qk)
+    if (q.dtype is not _bf16 or o_part.dtype is not f32 or lse_part.dtype is not f32 or q.shape != want or o_part.shape != want
+            or lse_part.shape != (rows, heads) or not (q.is_contiguous() and o_part.is_contiguous() and lse_part.is_contiguous())
+            or o_part.get_device() != dev or lse_part.get_device() != dev):
+        raise ValueError(f"q is contiguous bfloat16 {want}, o_part float32 {want} and lse_part float32 {want[:2]} on one device: got "
+                         + ", ".join(f"{x.dtype} {tuple(x.shape)} {x.device}" for x in (q, o_part, lse_part)))
+    if scratch.get_device() != dev or not scratch.is_contiguous() or (status is not None and (status.get_device() != dev or status.dtype not in (_i32, _torch.uint32))):
         raise ValueError("scratch and the status word (32 bits) are on the device of q")
-    rc = lib().ipkv_nibble_attend(C.byref(shape), rows, runs.tobytes(), row_start.tobytes(), q.data_ptr(), scratch.data_ptr(), scratch.nbytes,
-                                  o_part.data_ptr(), lse_part.data_ptr(), _ptr(status), _call_stream(stream, dev))
+    rc = (_lib or lib()).ipkv_nibble_attend(C.byref(shape), rows, runs.tobytes(), row_start.tobytes(), q.data_ptr(), scratch.data_ptr(), scratch.nbytes,
+                                            o_part.data_ptr(), lse_part.data_ptr(), _ptr(status), _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, "ipkv_nibble_attend")
