@@ -32,7 +32,7 @@
 // only when a score exceeds it by 2^8 (then everything is rescaled), which costs one vote per tile in place of a reduction over lanes.  A
 // producer warp streams tiles (one bulk copy each, they are contiguous) into a ring of stages on mbarriers; the warps of a CTA
 // take them in turn.  At the end of a (row, head group) every warp writes its partial and goes on, and a second kernel joins the partials
-// in a fixed order.  (Joining a CTA's warps through shared memory first made each wait for the slowest: ragged 64 192 us, now 175
+// in a fixed order; where one CTA has the whole group (WHOLE: short sequences) it does that itself.  (Joining a CTA's warps through shared memory first made each wait for the slowest: ragged 64 192 us, now 175
 // with that change alone.)  How rows and heads are shared out among CTAs: ops.h.
 // More than 8 query heads per KV head: several warps (one per octet of heads) share a tile, so it is still read once.
 // Every wait is bounded; a warp whose wait ran out does no more work.
@@ -56,6 +56,7 @@ namespace {
 
 constexpr int kWarps = kNibbleWarps;
 constexpr int kThreads = (kWarps + 1) * 32;
+constexpr int kPartRows = 8 * kWarps;            // partials of a CTA's teams: a row per head and team
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.f;                    // the reference maximum is raised when a score exceeds it by this (log2)
@@ -113,6 +114,9 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
+// All warps that compute (the one that copies has left).
+__device__ __forceinline__ void consumers_meet() { asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory"); }
+
 using Smem = NibbleSmem;
 
 // The tables: launch parameters, or device memory when they are too large.  (Both are indexed where they are: a pointer to one or the
@@ -136,7 +140,16 @@ __device__ __forceinline__ void set_tiles(Pair& x, int first) {
     x.tile0 = max(first - kNibblePairCost, 0);
     x.n = max(first + x.units - kNibblePairCost, 0) - x.tile0;
 }
+template <bool WHOLE>
 __device__ __forceinline__ Pair pair_at(const NibbleAttend& p, int u, int u1) {
+    if (WHOLE) {                                 // a CTA for every pair, those without tiles too; u is the CTA
+        Pair x;
+        x.row = u / p.n_gh;
+        x.r = row_at(p, x.row);
+        set_pair(p, x, u - x.row * p.n_gh);
+        x.tile0 = 0; x.n = x.r.tiles; x.units = 1; x.slot = 0;
+        return x;
+    }
     int lo = 0, hi = p.n_rows - 1;
     while (lo < hi) {                            // the last row that begins at or before u (rows without tiles lie in front of it)
         const int mid = (lo + hi + 1) >> 1;
@@ -175,7 +188,8 @@ __device__ __forceinline__ void next_pair(const NibbleAttend& p, Pair& x, int u,
     set_tiles(x, 0);
 }
 
-template <int D, bool HALF>                      // HALF: at most 4 query heads per KV head
+// HALF: at most 4 query heads per KV head.  WHOLE: one CTA to every pair, which writes the result.
+template <int D, bool HALF, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kernel(const __grid_constant__ NibbleAttend p) {
     constexpr int P = D / 64;
     constexpr int kTile = 64 * D + 256 * (P + 1), kKMeta = 32 * D, kV = kKMeta + 256 * P, kVMeta = kV + 32 * D;
@@ -192,9 +206,10 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         ptx::mbar_fence_init();
     }
     // The tables are launch parameters, or were there before the previous kernel of the stream began: they may be read under its tail.
-    const int u0 = p.share > 0 ? int(blockIdx.x) : int(int64_t(p.n_units) * blockIdx.x / p.n_ctas);
-    const int u1 = p.share > 0 ? u0 + 1 : int(int64_t(p.n_units) * (blockIdx.x + 1) / p.n_ctas);
-    Pair x = pair_at(p, u0, u1);
+    const bool by_cta = WHOLE || p.share > 0;
+    const int u0 = by_cta ? int(blockIdx.x) : int(int64_t(p.n_units) * blockIdx.x / p.n_ctas);
+    const int u1 = by_cta ? u0 + 1 : int(int64_t(p.n_units) * (blockIdx.x + 1) / p.n_ctas);
+    Pair x = pair_at<WHOLE>(p, u0, u1);
     __syncthreads();
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
@@ -205,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         const uint64_t pol = ptx::l2_evict_first_policy();
         int st = 0, lap = 0;
         bool ok = true;
-        for (int u = u0; u < u1 && ok;) {
+        for (int u = u0; u < u1 && ok && x.r.tiles > 0;) {
             int k = x.r.run0, hi = (x.row + 1 < p.n_rows ? row_at(p, x.row + 1).run0 : p.n_runs) - 1;
             while (k < hi) {                     // the row's last run that begins at or before the first tile
                 const int mid = (k + hi + 1) >> 1;
@@ -484,6 +499,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             if (st >= stages) { st -= stages; phase ^= 1; }
         }
 
+        if (WHOLE) consumers_meet();             // the ring is free when every warp has done its tiles
         // ---- the warp's partial: every team writes its own (nobody waits for another warp), one without a tile an empty one ----
         if (works) {
             float f[2];
@@ -498,11 +514,12 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             }
             const float undo = fv > 0.f ? 0x1p15f : 0.f, inv_fv = fv > 0.f ? 1.f / fv : 0.f;   // 2^21 / 64, then 1 / fv
             const int hb = octet * 8 + 2 * t;    // of the head group
-            const int64_t row0 = (int64_t(x.slot) * teams + team) * p.rows_per_part + hb;
-            const bool inside = !kChecked || (row0 >= 0 && row0 + min(2, n_heads - hb) <= p.part_rows);      // the partial must lie inside the scratch
+            const int64_t row0 = (int64_t(x.slot) * teams + team) * p.rows_per_part + hb;      // (of the ring's memory: slot 0)
+            const bool inside = !kChecked || WHOLE || (row0 >= 0 && row0 + min(2, n_heads - hb) <= p.part_rows);      // the partial must lie inside the scratch
             if (kChecked && !inside && hb < n_heads && p.status) atomicOr(p.status, kStatusBadIndex);
             const bool writes = (!HALF || t < 2) && inside;
-            float* dst = p.part_o + row0 * D + g;
+            float* dst = (WHOLE ? reinterpret_cast<float*>(ring) : p.part_o) + row0 * D + g;
+            float2* dst_ml = (WHOLE ? reinterpret_cast<float2*>(ring + kPartRows * D * 4) : p.part_ml) + row0;
             if (x.n > (team - it0 % teams + teams) % teams) {            // the team had a tile
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) {
@@ -518,7 +535,31 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                if (g == 0 && writes && hb + e < n_heads) p.part_ml[row0 + e] = make_float2(m[e], l[e]);
+                if (g == 0 && writes && hb + e < n_heads) dst_ml[e] = make_float2(m[e], l[e]);
+        }
+        if (WHOLE) {                             // the teams' partials are all there are: join them here, as nibble_reduce_kernel does
+            consumers_meet();
+            const float4* part = reinterpret_cast<const float4*>(ring);
+            const float2* ml = reinterpret_cast<const float2*>(ring + kPartRows * D * 4);
+            for (int i = tid; i < n_heads * (D / 4); i += kWarps * 32) {
+                const int head = i / (D / 4), col = i - head * (D / 4);
+                float m_all = -INFINITY, z = 0.f;
+                for (int k = 0; k < teams; ++k) m_all = fmaxf(m_all, ml[k * p.rows_per_part + head].x);
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int k = 0; k < teams; ++k) {
+                    const float2 y = ml[k * p.rows_per_part + head];
+                    if (y.y != 0.f) {
+                        const float w = ptx::ex2(y.x - m_all) * y.y;
+                        const float4 v = part[(k * p.rows_per_part + head) * (D / 4) + col];
+                        acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+                        z += w;
+                    }
+                }
+                const float inv = z == 0.f ? 0.f : 1.f / z;
+                const int64_t item = int64_t(x.row) * p.n_q_heads + head0 + head;
+                reinterpret_cast<float4*>(p.out_o + item * D)[col] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+                if (col == 0) p.out_lse[item] = z == 0.f ? -INFINITY : m_all * kLn2 + logf(z);
+            }
         }
         it0 = it_end;
         u += x.units;
@@ -602,17 +643,20 @@ __global__ void __launch_bounds__(THREADS) nibble_reduce_kernel(const __grid_con
 
 cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s) {
     const bool wide = a.g.dim == 128, half = a.group <= 4;
-    if (a.n_units > 0) {
+    if (a.n_ctas > 0) {
         a.stages = nibble_stages(a.g.dim, a.octets);
         if (a.stages <= 0) return cudaErrorInvalidValue;
         const size_t smem = size_t(a.stages) * a.g.tile_bytes() + nibble_fixed_smem();
-        auto kernel = wide ? (half ? nibble_attend_kernel<128, true> : nibble_attend_kernel<128, false>)
-                           : (half ? nibble_attend_kernel<64, true> : nibble_attend_kernel<64, false>);
+#define IPKV_NIBBLE(D) (half ? (a.whole ? nibble_attend_kernel<D, true, true> : nibble_attend_kernel<D, true, false>) \
+                             : (a.whole ? nibble_attend_kernel<D, false, true> : nibble_attend_kernel<D, false, false>))
+        auto kernel = wide ? IPKV_NIBBLE(128) : IPKV_NIBBLE(64);
+#undef IPKV_NIBBLE
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNibbleSmemPerCta);
         if (e != cudaSuccess) return e;
         e = launch_ordered(!a.plain_launch, kernel, a.n_ctas, kThreads, smem, s, a);
         if (e != cudaSuccess) return e;
     }
+    if (a.whole) return cudaSuccess;
     const int items = a.n_rows * a.n_q_heads;
     if (a.max_parts > kVeryManyParts)
         return launch_ordered(true, wide ? nibble_reduce_kernel<128, 32, 512> : nibble_reduce_kernel<64, 32, 512>, items * (a.g.dim / 32), 512,

@@ -56,7 +56,8 @@ cudaError_t launch_nibble_unpack(const NibbleMove& a, bool single_tokens, cudaSt
 
 // ---- the cache in 4 bits: decode attention (nibble_attend.cu) --------------------------------------------------------
 // A pair is a row and a head group (a KV head and some of its query heads); its tiles of 64 tokens are work for one CTA or several,
-// which leave a partial (O, maximum, sum) of every team.  Two ways to share the pairs out, see nibble_share:
+// which leave a partial (O, maximum, sum) of every team.  Three ways to share the pairs out, see nibble_split:
+//  - one CTA to every pair, those without tiles too: it joins its teams' partials itself and writes the result, in one launch;
 //  - whole CTAs to every pair: ceil(tiles / share) of them, each an equal part of the pair's tiles; partials in the CTAs' order;
 //  - equal chunks: work is counted in units, a pair's tiles and its cost in front of them, pair after pair, and CTA c of n takes units
 //    [units c / n, units (c + 1) / n).  With j the index of the pair among those with tiles, the partials that CTA c has of
@@ -116,6 +117,7 @@ struct NibbleAttend {
     int32_t teams;                               // teams of warps in a CTA
     int32_t octets;                              // groups of 8 query heads in a head group
     int32_t stages, n_runs;
+    int32_t whole;                               // one CTA for every pair, which writes the result itself
     int32_t share;                               // whole CTAs to every pair: tiles that one takes at most; 0: equal chunks of all units
     int32_t max_parts;                           // partials of a (row, head group) at most
     uint32_t odd_tokens;                         // 0xffff0000, see the kernel
@@ -129,18 +131,23 @@ inline int nibble_rows_per_part(int group) {
     const int n = nibble_groups_per_kv(group);
     return n == 1 ? group : ((group + n - 1) / n + 7) / 8 * 8;
 }
-// How to share out the pairs: the tiles that a CTA takes at most where every pair has whole CTAs, or 0 for equal chunks.
+// How to share out the pairs: whole (one CTA to every pair); or else share, the tiles that a CTA takes at most where every pair has
+// whole CTAs, 0 for equal chunks.
 // A team that works off k tiles takes about (us, 128 columns, 4 query heads per KV head; 8 take a sixth more)
 //   7 + 1.3 k with one CTA to an SM,   9.3 + 1.75 k with two,   9.5 + 2.5 k with three,
 // and the chunks, which fill all SMs to the same degree but meet two pairs and more, with r rounds of tiles on three CTAs,
 //   11.5 + 2.4 r, 5.5 more if there are several pairs.
 // Whole CTAs win where there is little work for each SM (one row of 4K tokens of 4 KV heads 8.6 us against 10.6, 16 rows of 2K 12.7 against
 // 18.2, 32 ragged rows of up to 2K and 8 KV heads 17.5 against 27), chunks with more (16 rows of 32K 66 us against 71, 48 ragged rows
-// of up to 8K 45 against 58).
-inline int nibble_share(const NibbleRowArg* row, int n_rows, int n_gh, int teams, int64_t units, int64_t pairs, int sms) {
-    const int64_t most = int64_t(sms) * kNibbleCtasPerSm;
+// of up to 8K 45 against 58).  One CTA to a pair saves the join, 2.5 us, and its launch on the host: a call on one row of 768 tokens and 4 KV
+// heads (three tiles a team) 8.5 us and 9.2 with the tiles spread over more CTAs, 1024 tokens 9.7 and 9.2; 32 rows of 1024 11.0 and 14.7.
+struct NibbleSplit { bool whole; int share; };
+constexpr int kNibbleWholeTiles = 3;             // tiles a team up to which the launch saved decides
+inline NibbleSplit nibble_split(const NibbleRowArg* row, int n_rows, int n_gh, int teams, int64_t units, int64_t pairs, int64_t longest, int sms) {
+    const int64_t most = int64_t(sms) * kNibbleCtasPerSm, all = int64_t(n_rows) * n_gh, whole_tiles = (longest + teams - 1) / teams;
+    if (all <= most && whole_tiles <= kNibbleWholeTiles) return {true, 0};
     const float rounds = float(units) / float(most * teams);
-    if (pairs == 0 || pairs > most || rounds > 24.f) return 0;
+    if (pairs == 0 || pairs > most || rounds > 24.f) return {false, 0};
     const float at0[kNibbleCtasPerSm] = {7.f, 9.3f, 9.5f}, per_tile[kNibbleCtasPerSm] = {1.3f, 1.75f, 2.5f};
     auto ctas = [&](int share) {
         int64_t n = 0;
@@ -164,7 +171,11 @@ inline int nibble_share(const NibbleRowArg* row, int n_rows, int n_gh, int teams
         const float t = at0[w] + per_tile[w] * float(lo);
         if (t < best) { best = t; share = lo * teams; }
     }
-    return share;
+    if (all <= most) {
+        const int w = int((all - 1) / sms);
+        if (at0[w] - 2.5f + per_tile[w] * float(whole_tiles) < best) return {true, 0};
+    }
+    return {false, share};
 }
 cudaError_t launch_nibble_attend(NibbleAttend& a, cudaStream_t s);
 

@@ -179,7 +179,10 @@ ipkv_status attend_nibbles(const ipkv_attn_shape* sh, int32_t n_rows, const ipkv
     }
     a.n_ctas = units < NibblePlan::kCtas ? int32_t(units) : NibblePlan::kCtas;
     a.max_parts = units > 0 ? int32_t((((longest + kNibblePairCost) * a.n_ctas + units - 1) / units + 1) * plan.teams) : 0;
-    a.share = nibble_share(row, n_rows, plan.n_gh, plan.teams, units, pairs, kSmCount);
+    const NibbleSplit split = nibble_split(row, n_rows, plan.n_gh, plan.teams, units, pairs, longest, kSmCount);
+    a.whole = split.whole;
+    a.share = split.share;
+    if (a.whole) a.n_ctas = n_rows * plan.n_gh;
     if (a.share > 0) {
         int64_t ctas = 0;
         for (int r = 0; r < n_rows; ++r) { row[r].first = int32_t(ctas); ctas += plan.n_gh * ((row[r].tiles + a.share - 1) / a.share); }

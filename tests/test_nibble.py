@@ -321,6 +321,8 @@ def ragged(n_rows, most, seed):
     (16, 1, 128, 64, [[40000, 7]]),
     (16, 4, 128, 64, ragged(12, 5000, 5)),       # whole CTAs to ragged pairs
     (24, 2, 64, 64, ragged(30, 1000, 6)),
+    (4, 1, 64, 64, ragged(70, 6000, 7)),         # ... their tables uploaded
+    (8, 2, 128, 64, ragged(90, 700, 8)),         # one CTA to every pair, tables uploaded
 ])
 def test_attention_however_the_work_is_shared_out(hq, hkv, d, bt, rows):
     rng = np.random.default_rng(len(rows) + hq)

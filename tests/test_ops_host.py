@@ -46,16 +46,18 @@ def test_a_share_fits_the_gpu_and_is_whole_rounds(shim, n_gh, teams):
         most = rng.choice([1, 4, 60, 700, 30000])
         tiles = [rng.randint(0, most) for _ in range(rows)]
         share = shim.shim_nibble_share((ctypes.c_int * rows)(*tiles), rows, n_gh, teams, sms, ctypes.byref(n))
-        assert share >= 0 and share % teams == 0
-        if share:
+        assert share == -1 or (share >= 0 and share % teams == 0)
+        if share == -1:
+            assert n.value == rows * n_gh <= sms * shim.shim_nibble_ctas_per_sm()
+        elif share:
             assert sum(t > 0 for t in tiles) * n_gh <= n.value <= sms * shim.shim_nibble_ctas_per_sm()
 
 
 def test_little_work_gets_whole_ctas_and_much_work_equal_chunks(shim):
     n = ctypes.c_int()
     share = lambda tiles: shim.shim_nibble_share((ctypes.c_int * len(tiles))(*tiles), len(tiles), 4, 4, 148, ctypes.byref(n))
-    assert share([0, 0]) == 0                            # nothing to share out
-    assert share([1]) == 4 and n.value == 4
+    assert share([0, 0]) == -1 and share([1]) == -1 and n.value == 4                 # one CTA to every pair
+    assert share([0] * 200) == 0                         # ... if they fit
     assert share([65]) == 4 and n.value == 68
     assert share([32] * 16) in (8, 16) and n.value in (128, 256)
     assert share([512] * 16) == 0 and share([(1 << 31) - 300]) == 0
