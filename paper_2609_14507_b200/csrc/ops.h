@@ -124,13 +124,16 @@ struct NibbleAttend {
     int32_t plain_launch;                        // the tables were written by the kernel in front of this launch: no overlap with it
     float scale;
 };
-// Head groups of a KV head's `group` query heads, and heads in each: one warp per 8 heads works on a tile, so a group has at most
-// 8 per computing warp; larger groups are cut into equal parts (each reads the tiles once more).
-inline int nibble_groups_per_kv(int group) { return (group + 8 * kNibbleWarps - 1) / (8 * kNibbleWarps); }
-inline int nibble_rows_per_part(int group) {
-    const int n = nibble_groups_per_kv(group);
-    return n == 1 ? group : ((group + n - 1) / n + 7) / 8 * 8;
+// Head groups of a KV head's `group` query heads, and heads in each.  One warp per 8 heads works on a tile, and the tile is read once for a
+// group: as many octets as divide both the computing warps and the octets there are, so that no warp is idle (40 heads on one KV head, 200K
+// tokens: 36 us; in two groups of 24 and 16, three warps of four busy, 51, though the tiles were read twice in place of five times).
+inline int nibble_group_octets(int group) {
+    const int n = (group + 7) / 8;
+    return n % 4 == 0 ? 4 : n % 2 == 0 ? 2 : 1;
 }
+inline int nibble_groups_per_kv(int group) { return (group + 7) / 8 / nibble_group_octets(group); }
+inline int nibble_rows_per_part(int group) { return nibble_groups_per_kv(group) == 1 ? group : 8 * nibble_group_octets(group); }
+static_assert(kNibbleWarps == 4, "octets of a group");
 // How to share out the pairs: whole (one CTA to every pair); or else share, the tiles that a CTA takes at most where every pair has
 // whole CTAs, 0 for equal chunks.
 // A team that works off k tiles takes about (us, 128 columns, 4 query heads per KV head; 8 take a sixth more)
