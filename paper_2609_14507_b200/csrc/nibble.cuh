@@ -9,9 +9,9 @@
 // no value ever moves between lanes.  With lane = 4 g + t, nibble j = bits 4j..4j+3 of a 32-bit word:
 //   K: token 16u + 8h + g, column 64p + 16t + 8w + j  ->  nibble j of word ((((u P + p) 8 + g) 4 + t) 2 + h) 2 + w     (P = D/64)
 //   V: column 16d + 8h + g, token 32w + 8i + 2t + e   ->  nibble i + 4e of word ((((d 8 + g) 4 + t) 2 + h) 2 + w
-// Masking a word with 0x000f000f leaves nibbles 0 and 4 as the two halves of a register: read as fp16 these bits are the
-// code times 2^-24, exactly (a subnormal); nibbles 1 and 5 in place are the code times 2^-20.  So codes become fp16 operands with
-// one logical operation per two values, and the powers of two go into the other operand.
+// Masking a word with 0x000f000f leaves nibbles 0 and 4 as the two halves of a register: read as bf16 these bits are the code times
+// 2^-133, exactly (a subnormal), and nibbles 1 and 5 in place the code times 2^-129; shifted by three they are as good as fp16.  So codes
+// become 16-bit operands with one logical operation per two values, and the powers of two go into the other operand.
 // Scales and zeros (scale in the low half of a 32-bit word) are in the rows' order too: token 16u + 8h + g is row 16u + 2g + h.
 #pragma once
 #include <cstdint>
