@@ -1,0 +1,122 @@
+"""The 4-bit cache's attention against 64 bits under bounds that follow its arithmetic, head by head: what wider bounds would let
+pass (an output of zeros, a tile left out, weights of one half) fails here, which is checked on the host.
+
+The bound on a head's output.  With p_t the softmax weights and v_t the values in 64 bits, `size` = sqrt(sum p_t^2 |v_t|^2) is how
+large the output is when values are independent, and how large its error is when every token's share is off by a relative error
+that is independent of the others' (an error that all tokens have in common leaves with the denominator).  The parts of the relative error:
+  * a weight: fp32 products and ex2 2^-22, and its two fp16 halves 2^-22;
+  * a score: a tensor-core step adds 16 products and the sum so far, cut at 2^-26 of the largest exponent, and cuts the sum at 2^-24.  For
+    normal queries sums of q * code stay below 2^7 (64 columns, codes of 0..15), so a step is off by less than
+    17 * 2^-19 + 2^-17 = 2^-14.7, the eight steps of 128 columns by 2^-11.7 if all erred alike and by a quarter of that with
+    cuts of either sign; times a scale of key and softmax (1.2 * 0.09): 2^-16.9;
+  * the output's sums: 64 tokens a tile, products of either sign (every other token is complemented), sums below 2^7 of a value's
+    scale: four steps of 2^-14.7 if all erred alike, 2^-14.7 with cuts of either sign, against 24 scales (the size of the sum of 64 values
+    that lie within 15 scales): 2^-19.3.
+Together below 2^-16.
+"""
+import numpy as np
+import pytest
+
+from paper_2609_14507_b200 import synth
+from tests import nibble_ref as ref
+from tests.test_nibble import attend, fill, shape_of
+
+torch = pytest.importorskip("torch")
+
+RELATIVE = 2.0 ** -16
+LSE = 2.0 ** -15        # a score's error as above, common to all tokens, twice over; ln and its sum 2^-22 of the value
+
+
+def exact(sh, q, k, v):
+    """One row: q bits [Hq][D], K and V bits [n][Hkv][D] -> weights [Hq][n], values [n][Hkv][D], O, LSE."""
+    scale = float(np.float32(sh.softmax_scale if sh.softmax_scale > 0 else sh.dim_qk ** -0.5))
+    kd, vd = ref.quantised_values(k, v)
+    hq, d = q.shape
+    qd = synth.bf16_bits_to_f32(q).astype(np.float64).reshape(sh.n_kv_heads, -1, d)
+    s = np.matmul(qd, kd.transpose(1, 2, 0)) * scale
+    m = s.max(-1, keepdims=True)
+    e = np.exp(s - m)
+    z = e.sum(-1, keepdims=True)
+    p = e / z
+    o = np.matmul(p, vd.transpose(1, 0, 2))
+    return p, vd, o.reshape(hq, d), (m + np.log(z)).reshape(hq)
+
+
+def bounds(p, vd):
+    """Per query head: how far its output may be from 64 bits (Euclidean norm over its columns)."""
+    v2 = (vd ** 2).sum(-1).T[:, None]                                     # [Hkv][1][n]
+    return (np.sqrt((p ** 2 * v2).sum(-1)) * RELATIVE).reshape(-1)
+
+
+def miss(o, want, bound):
+    """The largest error over its bound among the heads."""
+    return float((np.linalg.norm(o - want, axis=-1) / bound).max())
+
+
+def check_exact(sh, q, kvs, o, lse):
+    for r, (k, v) in enumerate(kvs):
+        if not k.shape[0]:
+            assert not o[r].any() and np.isneginf(lse[r]).all()
+            continue
+        p, vd, want, want_lse = exact(sh, q[r], k, v)
+        assert np.isfinite(o[r]).all()
+        assert miss(o[r], want, bounds(p, vd)) <= 1, (r, k.shape[0], miss(o[r], want, bounds(p, vd)))
+        assert (np.abs(lse[r] - want_lse) <= LSE + np.abs(want_lse) * 2.0 ** -22).all(), (r, np.abs(lse[r] - want_lse).max())
+
+
+# ---- what the bound tells apart: mistakes made in a restatement on the host ------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv,d,n", [(4, 1, 64, 40000), (8, 2, 128, 9600), (16, 1, 128, 4097), (8, 8, 128, 64)])
+def test_the_bound_fails_what_is_wrong(hq, hkv, d, n):
+    rng = np.random.default_rng(n)
+    sh = shape_of(hq, hkv, d, 64)
+    k, v = synth.normal_bf16(rng, (n, hkv, d)), synth.normal_bf16(rng, (n, hkv, d))
+    q = synth.normal_bf16(rng, (hq, d))
+    p, vd, want, _ = exact(sh, q, k, v)
+    bound = bounds(p, vd)
+    product = lambda w: np.matmul(w, vd.transpose(1, 0, 2)).reshape(hq, d)
+    assert miss(product(p.astype(np.float32).astype(np.float64)), want, bound) < 0.1     # fp32 weights pass
+    assert miss(np.zeros_like(want), want, bound) > 100
+    left_out = p.copy()
+    left_out[..., n // 2:n // 2 + 16] = 0                                                # sixteen tokens
+    assert miss(product(left_out / left_out.sum(-1, keepdims=True)), want, bound) > 100
+    unit = p / p.max(-1, keepdims=True)                                                  # against the reference, as the kernel holds them
+    for cut in (lambda x: x.astype(np.float16).astype(np.float64), lambda x: synth.bf16_bits_to_f32(synth.f32_to_bf16_bits(x.astype(np.float32))).astype(np.float64)):
+        one_half = cut(unit)
+        assert miss(product(one_half / unit.sum(-1, keepdims=True)), want, bound) > 4    # the remainder left out
+    gone = vd.copy()
+    gone[1::2] -= np.abs(vd).max() * 2.0 ** -8                                           # half of the tokens a little low
+    assert miss(np.matmul(p, gone.transpose(1, 0, 2)).reshape(hq, d), want, bound) > 4
+
+
+# ---- outputs ---------------------------------------------------------------------------------------------------------
+
+def long_among(n_short, short, long):
+    """Rows of one length with a long one among them: more pairs than CTAs are resident, so work goes out in equal chunks, and the long
+    row meets so many that its join is cut into slabs."""
+    rows = [[short]] * n_short
+    rows[n_short // 2] = [long]
+    return rows
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,bt,rows", [
+    (32, 4, 128, 64, [[1]]), (32, 4, 128, 64, [[4097]]), (32, 8, 128, 64, [[700, 33], [64], [], [1000, 1, 129]]),
+    (8, 8, 64, 64, [[333]]), (6, 3, 64, 128, [[63, 65], [0], [200]]), (12, 4, 64, 64, [[1500, 77], [2]]),
+    (8, 2, 128, 64, [[64] * 150, [1, 64, 3] * 30]),                       # pages
+    # several heads on one tile and several groups of heads, the last one smaller: two octets, and four
+    (24, 1, 128, 64, [[300], [5000]]), (44, 1, 64, 64, [[300], [65], []]), (44, 1, 128, 64, [[20000]]), (57, 1, 128, 64, [[700], [64]]),
+    (60, 1, 64, 128, [[500, 3], [1]]), (60, 1, 128, 64, [[9000]]), (88, 2, 64, 64, [[130], [4000]]), (119, 1, 128, 64, [[300], [65]]),
+    # one pair of many partials: joins by one CTA a head, by slabs of 256 and of 512 threads
+    (4, 1, 64, 64, [[3000]]), (8, 1, 128, 64, [[9000]]), (4, 1, 64, 64, [[40000]]), (8, 1, 128, 64, [[40000]]), (16, 1, 128, 64, [[40000, 7]]),
+    # equal chunks with either join, tables in the launch (up to 64 rows) and uploaded
+    (8, 8, 64, 64, long_among(64, 64, 5000)), (32, 8, 128, 64, long_among(60, 100, 9000)), (16, 8, 64, 64, long_among(64, 64, 20000)),
+    (4, 1, 128, 64, long_among(450, 64, 10000)), (8, 1, 64, 64, long_among(450, 64, 40000)), (44, 1, 64, 64, long_among(160, 64, 12000)),
+])
+def test_attention_within_its_own_arithmetic(hq, hkv, d, bt, rows):
+    rng = np.random.default_rng(hq * 100 + d + len(rows))
+    sh = shape_of(hq, hkv, d, bt)
+    buf, runs, kvs = fill(rng, sh, rows)
+    q = synth.normal_bf16(rng, (len(rows), hq, d))
+    o, lse = attend(sh, runs, q)
+    check_exact(sh, q, kvs, o, lse)
