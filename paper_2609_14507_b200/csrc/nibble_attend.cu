@@ -16,7 +16,9 @@
 // Exactness.  q (bf16) times a power of two per head is exact; products are exact and sums are fp32.  A weight p sv is
 // held as two fp16 numbers, head and remainder (22 bits): with at most 4 query heads per KV head they share one product (columns
 // 0-3 and 4-7), otherwise there are two.  sv is brought near 1 by a power of two per warp (the largest scale so far), so that
-// fp16's range is spent on p: weights down to 2^-31 of the largest keep their share.
+// fp16's range is spent on p.  The remainder is held times 2^11: a head that is cut at fp16's smallest step, 2^-24, leaves its digits to a
+// remainder that is cut at 2^-35, and a weight p is known to 2^-38 of 1 (the reference) or to 22 bits, whichever is coarser.  Without the
+// factor both were cut at 2^-24: half of the tokens with weights of 2^-16 had lost ten digits.
 // The tensor cores add with two bits more than fp32 has and round towards zero, both counted from the largest exponent that
 // an operand's FORMAT shows (a subnormal counts as the smallest normal number).  Two things follow.  The codes must fill the
 // subnormal range: K's do in place as bf16 (7 bits of mantissa; bits 0..3 and 4..7), V's are shifted up to bits 3..6 and 7..10 of fp16,
@@ -64,6 +66,7 @@ constexpr float kRaise = 8.f;                    // the reference maximum is rai
 // better (16 rows of 32K tokens, 32 partials: 61.9 us in all, with slabs 65.4; 4 rows of 50K, 60 partials: 49 and 59), over 256 more
 // threads are (one row of 1M, 888 partials: 61.2 and 66.9 with 256 threads; one of 64K, 148 partials: 21.9 and 19.2).
 constexpr int kManyParts = 64, kVeryManyParts = 256;
+constexpr float kRest = 2048.f;                  // a weight's remainder is held times this
 constexpr uint32_t kLowK = 0x000f000fu, kHighK = 0x00f000f0u;       // K codes as bf16 in bits 0..3 and 4..7: times 2^-133 and 2^-129
 constexpr uint32_t kLow = 0x00780078u, kHigh = 0x07800780u;         // V codes as fp16 in bits 3..6 and 7..10: times 2^-21 and 2^-17
 
@@ -83,6 +86,11 @@ __device__ __forceinline__ void mma_bf16_k8(float (&d)[4], uint32_t a0, uint32_t
         : "r"(a0), "r"(a1), "r"(b0));
 }
 // Two fp32 operations in one instruction, each rounded as if alone.
+__device__ __forceinline__ float2 mul2(float a0, float a1, float b) {
+    float2 r;
+    asm("{.reg .b64 p, q; mov.b64 p, {%2,%3}; mov.b64 q, {%4,%4}; mul.rn.f32x2 p, p, q; mov.b64 {%0,%1}, p;}" : "=f"(r.x), "=f"(r.y) : "f"(a0), "f"(a1), "f"(b));
+    return r;
+}
 __device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
     asm("{.reg .b64 p, q; mov.b64 p, {%0,%1}; mov.b64 q, {%2,%3}; add.rn.f32x2 p, p, q; mov.b64 {%0,%1}, p;}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
@@ -454,20 +462,18 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             for (int un = 0; un < 4; ++un)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float w[2];
                     const float svf = sv[un][h] * (h ? f1 : f0);
                     const float2 y = fma2(s[un][2 * h], s[un][2 * h + 1], c[0], c[1], -m[0], -m[1]);
                     const float pr[2] = {ptx::ex2(y.x), ptx::ex2(y.y)};
                     add2(l[0], l[1], pr[0], pr[1]);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        zt[e] = fmaf(pr[e], zv[un][h], zt[e]);
-                        w[e] = pr[e] * svf;
-                    }
-                    const uint32_t big = pack_f16(w[0], w[1]);
+                    for (int e = 0; e < 2; ++e) zt[e] = fmaf(pr[e], zv[un][h], zt[e]);
+                    float2 w = mul2(pr[0], pr[1], svf);
+                    const uint32_t big = pack_f16(w.x, w.y);
                     const float2 back = unpack_f16(big);
-                    add2(w[0], w[1], -back.x, -back.y);
-                    const uint32_t rest = pack_f16(w[0], w[1]);
+                    add2(w.x, w.y, -back.x, -back.y);
+                    w = mul2(w.x, w.y, kRest);
+                    const uint32_t rest = pack_f16(w.x, w.y);
                     if (HALF) hi[un][h] = transpose8x8(t < 2 ? big : rest);              // columns 4-7 repeat heads 0-3
                     else { hi[un][h] = transpose8x8(big); lo[un][h] = transpose8x8(rest); }
                 }
@@ -489,8 +495,12 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 }
 #pragma unroll
                 for (int i = 0; i < 4; i += 2) {
-                    if (!HALF) add2(sum[i], sum[i + 1], low[i], low[i + 1]);
-                    add2(o[d][i], o[d][i + 1], sum[i], sum[i + 1]);
+                    if (!HALF) {
+                        const float2 both = fma2(low[i], low[i + 1], 1.f / kRest, 1.f / kRest, sum[i], sum[i + 1]);
+                        add2(o[d][i], o[d][i + 1], both.x, both.y);
+                    } else {
+                        add2(o[d][i], o[d][i + 1], sum[i], sum[i + 1]);
+                    }
                 }
             }
             __syncwarp();
@@ -525,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 for (int d = 0; d < D / 16; ++d) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (HALF) o[d][i] += __shfl_xor_sync(0xffffffffu, o[d][i], 2);
+                        if (HALF) o[d][i] = fmaf(__shfl_xor_sync(0xffffffffu, o[d][i], 2), 1.f / kRest, o[d][i]);
                         o[d][i] = fmaf(o[d][i] * undo, inv_fv, oz[i & 1]) * f[i & 1];
                     }
 #pragma unroll

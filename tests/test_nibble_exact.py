@@ -12,18 +12,19 @@ that is independent of the others' (an error that all tokens have in common leav
   * the output's sums: 64 tokens a tile, products of either sign (every other token is complemented), sums below 2^7 of a value's
     scale: four steps of 2^-14.7 if all erred alike, 2^-14.7 with cuts of either sign, against 24 scales (the size of the sum of 64 values
     that lie within 15 scales): 2^-19.3.
-Together below 2^-16.
+Together below 2^-16.  An absolute share comes on top: a weight is known to 2^-38 of the reference of its warp, which lies up to 2^8 below the
+largest one, times scales up to twice apart from where they are brought: an output is known to 2^-36 of the largest value (`floor`).
 """
 import numpy as np
 import pytest
 
-from paper_2609_14507_b200 import synth
+from paper_2609_14507_b200 import binding, synth
 from tests import nibble_ref as ref
 from tests.test_nibble import attend, fill, shape_of
 
 torch = pytest.importorskip("torch")
 
-RELATIVE = 2.0 ** -16
+RELATIVE, FLOOR = 2.0 ** -16, 2.0 ** -36
 LSE = 2.0 ** -15        # a score's error as above, common to all tokens, twice over; ln and its sum 2^-22 of the value
 
 
@@ -45,7 +46,8 @@ def exact(sh, q, k, v):
 def bounds(p, vd):
     """Per query head: how far its output may be from 64 bits (Euclidean norm over its columns)."""
     v2 = (vd ** 2).sum(-1).T[:, None]                                     # [Hkv][1][n]
-    return (np.sqrt((p ** 2 * v2).sum(-1)) * RELATIVE).reshape(-1)
+    size = np.sqrt((p ** 2 * v2).sum(-1))
+    return (size * RELATIVE + np.sqrt(v2.max(-1)) * FLOOR).reshape(-1)
 
 
 def miss(o, want, bound):
@@ -120,3 +122,37 @@ def test_attention_within_its_own_arithmetic(hq, hkv, d, bt, rows):
     q = synth.normal_bf16(rng, (len(rows), hq, d))
     o, lse = attend(sh, runs, q)
     check_exact(sh, q, kvs, o, lse)
+
+
+def packed(sh, k, v):
+    n = k.shape[0]
+    buf = torch.full((-(-n // 64) * ref.block_bytes(sh.n_kv_heads, sh.dim_qk, 64),), 255, dtype=torch.uint8, device="cuda")
+    binding.ipkv_nibble_pack(sh, [(buf, 0, n)], synth.bits_to_torch(k, "cuda"), synth.bits_to_torch(v, "cuda"))
+    return buf
+
+
+def controlled(rng, hq, hkv, d, n, log2_weight):
+    """Queries and keys whose scores are log2_weight[t] * ln 2 and a little noise, with softmax_scale 1."""
+    sign = np.where(rng.random(d) < 0.5, -1.0, 1.0)
+    a = np.asarray(log2_weight) * np.log(2) / d
+    k = a[:, None, None] * sign + rng.standard_normal((n, hkv, d)) * 0.02
+    q = np.broadcast_to(sign, (1, hq, d))
+    return synth.f32_to_bf16_bits(q.astype(np.float32)), synth.f32_to_bf16_bits(k.astype(np.float32))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (8, 1), (16, 1), (32, 2)])
+@pytest.mark.parametrize("at", [0, 5, 300])
+@pytest.mark.parametrize("gap", [12, 16, 20])
+def test_many_weak_tokens_beside_one_that_dominates(hq, hkv, at, gap):
+    """The token that a softmax rests on when nothing matters: nearly all the weight and no values.  The output is what the others leave."""
+    d, n = 128, 700
+    rng = np.random.default_rng(gap * 1000 + at)
+    sh = shape_of(hq, hkv, d, 64, 1.0)
+    level = np.zeros(n)
+    level[at] = gap
+    q, k = controlled(rng, hq, hkv, d, n, level)
+    v = synth.normal_bf16(rng, (n, hkv, d))
+    v[at] = 0
+    o, lse = attend(sh, [[(packed(sh, k, v), n)]], q)
+    check_exact(sh, q, [(k, v)], o, lse)
