@@ -15,10 +15,12 @@
 //
 // Exactness.  q (bf16) times a power of two per head is exact; products are exact and sums are fp32.  A weight p sv is
 // held as two fp16 numbers, head and remainder (22 bits): with at most 4 query heads per KV head they share one product (columns
-// 0-3 and 4-7), otherwise there are two.  sv is brought near 1 by a power of two per warp (the largest scale so far), so that
-// fp16's range is spent on p.  The remainder is held times 2^11: a head that is cut at fp16's smallest step, 2^-24, leaves its digits to a
-// remainder that is cut at 2^-35, and a weight p is known to 2^-38 of 1 (the reference) or to 22 bits, whichever is coarser.  Without the
-// factor both were cut at 2^-24: half of the tokens with weights of 2^-16 had lost ten digits.
+// 0-3 and 4-7), otherwise there are two.  The remainder is held times 2^11: a head that is cut at fp16's smallest step, 2^-24, leaves its
+// digits to a remainder that is cut at 2^-35.  (Without the factor both were cut at 2^-24: half of the tokens with weights of 2^-16 had
+// lost ten digits.)  sv is brought near 1 by a power of two per warp, so that fp16's range is spent on p.  It follows the largest scale among
+// tokens that count (with the largest of all, one token of no weight whose values were 2^20 times the others' took all but seven of their
+// digits) and leaves room for 2^4: a first token that outweighs the next by 2^12 and has no values would have every tile behind it
+// look again.  So a weight p is known to 22 bits or 2^-34 of the reference's, whichever is coarser.
 // The tensor cores add with two bits more than fp32 has and round towards zero, both counted from the largest exponent that
 // an operand's FORMAT shows (a subnormal counts as the smallest normal number).  Two things follow.  The codes must fill the
 // subnormal range: K's do in place as bf16 (7 bits of mantissa; bits 0..3 and 4..7), V's are shifted up to bits 3..6 and 7..10 of fp16,
@@ -66,6 +68,7 @@ constexpr float kRaise = 8.f;                    // the reference maximum is rai
 // better (16 rows of 32K tokens, 32 partials: 61.9 us in all, with slabs 65.4; 4 rows of 50K, 60 partials: 49 and 59), over 256 more
 // threads are (one row of 1M, 888 partials: 61.2 and 66.9 with 256 threads; one of 64K, 148 partials: 21.9 and 19.2).
 constexpr int kManyParts = 64, kVeryManyParts = 256;
+constexpr int kRoom = 4;                         // scales this many powers of two above the largest that counted need no other factor
 constexpr float kRest = 2048.f;                  // a weight's remainder is held times this
 constexpr uint32_t kLowK = 0x000f000fu, kHighK = 0x00f000f0u;       // K codes as bf16 in bits 0..3 and 4..7: times 2^-133 and 2^-129
 constexpr uint32_t kLow = 0x00780078u, kHigh = 0x07800780u;         // V codes as fp16 in bits 3..6 and 7..10: times 2^-21 and 2^-17
@@ -424,33 +427,56 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 top[1] = fmaxf(top[1], fmaxf(s[un][1], s[un][3]));
                 v_top = fmaxf(v_top, fmaxf(sv[un][0], sv[un][1]));
             }
-            if (__any_sync(0xffffffffu, top[0] > limit[0] || top[1] > limit[1] || v_top >= v_limit)) {
-                float alpha[2];
+            const bool outgrown = top[0] > limit[0] || top[1] > limit[1];
+            if (__any_sync(0xffffffffu, outgrown || v_top >= v_limit)) {
+                float alpha[2] = {1.f, 1.f};
+                bool rescale = __any_sync(0xffffffffu, outgrown);
 #pragma unroll
-                for (int d = 4; d <= 16; d <<= 1) {
-                    top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
-                    top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], d));
-                    v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, d));
-                }
+                for (int d = 4; d <= 16; d <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, d));
+                if (rescale) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float m_new = fmaxf(m[e], top[e] * c[e]);
-                    alpha[e] = m[e] == -INFINITY ? 0.f : ptx::ex2(m[e] - m_new);
-                    m[e] = m_new;
-                    limit[e] = (m_new + kRaise) / c[e];
-                    l[e] *= alpha[e]; oz[e] *= alpha[e];
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int d = 4; d <= 16; d <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], d));
+                        const float m_new = fmaxf(m[e], top[e] * c[e]);
+                        alpha[e] = m[e] == -INFINITY ? 0.f : ptx::ex2(m[e] - m_new);
+                        m[e] = m_new;
+                        limit[e] = (m_new + kRaise) / c[e];
+                        l[e] *= alpha[e]; oz[e] *= alpha[e];
+                    }
                 }
                 if (v_top >= v_limit) {
-                    const int e = min(max(int(__float_as_uint(v_top) >> 23), 8), 250);
-                    const float f_new = __uint_as_float(uint32_t(254 - e) << 23);        // scales times f_new lie below 2
-                    const float r = fv == 0.f ? 0.f : f_new / fv;
-                    alpha[0] *= r; alpha[1] *= r;
-                    fv = f_new;
-                    v_limit = __uint_as_float(uint32_t(e + 1) << 23);
-                }
+                    // scales of one order all count; otherwise a token's does in full from a weight of 2^-12 on, and less below
+                    float least = v_top, most = v_top;
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) {
-                    o[d][0] *= alpha[0]; o[d][1] *= alpha[1]; o[d][2] *= alpha[0]; o[d][3] *= alpha[1];
+                    for (int un = 0; un < 4; ++un) least = fminf(least, fminf(sv[un][0], sv[un][1]));
+                    if (__any_sync(0xffffffffu, least * float(1 << kRoom) < v_top)) {
+                        most = 0.f;
+#pragma unroll
+                        for (int un = 0; un < 4; ++un)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float y = fmaxf(fmaf(s[un][2 * h], c[0], 12.f - m[0]), fmaf(s[un][2 * h + 1], c[1], 12.f - m[1]));
+                                most = fmaxf(most, sv[un][h] * fminf(ptx::ex2(y), 1.f));
+                            }
+#pragma unroll
+                        for (int d = 1; d <= 16; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+                    }
+                    if (most >= v_limit) {
+                        const int e = min(max(int(__float_as_uint(most) >> 23) + kRoom, 8), 250);
+                        const float f_new = __uint_as_float(uint32_t(254 - e) << 23);    // such scales times f_new lie below 2^(1 - kRoom)
+                        const float r = fv == 0.f ? 0.f : f_new / fv;
+                        alpha[0] *= r; alpha[1] *= r;
+                        fv = f_new;
+                        v_limit = __uint_as_float(uint32_t(e + 1) << 23);
+                        rescale = true;
+                    }
+                }
+                if (rescale) {
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) {
+                        o[d][0] *= alpha[0]; o[d][1] *= alpha[1]; o[d][2] *= alpha[0]; o[d][3] *= alpha[1];
+                    }
                 }
             }
 

@@ -12,8 +12,10 @@ that is independent of the others' (an error that all tokens have in common leav
   * the output's sums: 64 tokens a tile, products of either sign (every other token is complemented), sums below 2^7 of a value's
     scale: four steps of 2^-14.7 if all erred alike, 2^-14.7 with cuts of either sign, against 24 scales (the size of the sum of 64 values
     that lie within 15 scales): 2^-19.3.
-Together below 2^-16.  An absolute share comes on top: a weight is known to 2^-38 of the reference of its warp, which lies up to 2^8 below the
-largest one, times scales up to twice apart from where they are brought: an output is known to 2^-36 of the largest value (`floor`).
+Together below 2^-16.  An absolute share comes on top: every other weight of a tile is held in steps of 2^-33 of the reference's, the rest in finer
+ones.  Off by 2^-34.8 (half a step over the root of three), half of the tokens, the root of the 192 tokens that a warp has here, times a
+code of 8 against values of 3 scales: 2^-30 of the values (`FLOOR`).  It counts only where one token outweighs the others by 2^14 and
+more and has no values.
 """
 import numpy as np
 import pytest
@@ -24,7 +26,7 @@ from tests.test_nibble import attend, fill, shape_of
 
 torch = pytest.importorskip("torch")
 
-RELATIVE, FLOOR = 2.0 ** -16, 2.0 ** -36
+RELATIVE, FLOOR = 2.0 ** -16, 2.0 ** -30
 LSE = 2.0 ** -15        # a score's error as above, common to all tokens, twice over; ln and its sum 2^-22 of the value
 
 
@@ -156,3 +158,26 @@ def test_many_weak_tokens_beside_one_that_dominates(hq, hkv, at, gap):
     v[at] = 0
     o, lse = attend(sh, [[(packed(sh, k, v), n)]], q)
     check_exact(sh, q, [(k, v)], o, lse)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (8, 1), (32, 2)])
+@pytest.mark.parametrize("at", [0, 300, 699])
+@pytest.mark.parametrize("factor,gap", [(12, 24), (20, 24), (20, 80), (30, 80), (60, 80), (20, 16), (30, 8)])
+def test_a_value_far_out_takes_no_digits_from_the_others(hq, hkv, at, factor, gap):
+    """One token whose values are 2^factor times the others' and whose weight is 2^-gap of theirs: what it adds counts, its scale does not."""
+    d, n = 128, 700
+    rng = np.random.default_rng(factor * 1000 + at + gap)
+    sh = shape_of(hq, hkv, d, 64, 1.0)
+    level = np.zeros(n)
+    level[at] = -gap
+    q, k = controlled(rng, hq, hkv, d, n, level)
+    v = rng.standard_normal((n, hkv, d)).astype(np.float32)
+    v[at] *= np.float32(2.0) ** factor
+    v = synth.f32_to_bf16_bits(v)
+    o, lse = attend(sh, [[(packed(sh, k, v), n)]], q)
+    p, vd, want, want_lse = exact(sh, q[0], k, v)
+    rest = np.delete(vd, at, 0)                          # the floor goes by the others' values
+    size = np.sqrt((p ** 2 * (vd ** 2).sum(-1).T[:, None]).sum(-1)).reshape(-1)
+    assert miss(o[0], want, size * RELATIVE + np.sqrt((rest ** 2).sum(-1).max()) * FLOOR) <= 1
+    assert (np.abs(lse[0] - want_lse) <= LSE + np.abs(want_lse) * 2.0 ** -22).all()
