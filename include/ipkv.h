@@ -450,7 +450,8 @@ typedef struct {
 } ipkv_rope;
 
 /* Some heads of every token (the queries, the keys).  Strides in elements, multiples of 8; pointers 16-byte aligned.  out_dev
- * may be in_dev with the same strides (in place); otherwise no output may share bytes with an input or another output. */
+ * may be in_dev with the same strides (in place); otherwise no output may share bytes with an input or another output (views of
+ * one buffer whose strides differ and whose ranges interleave are refused, too). */
 typedef struct {
   const void* in_dev;        /* head h of token t begins at in_dev + t * in_token_stride + h * in_head_stride   */
   void* out_dev;

@@ -33,17 +33,29 @@ bool same_view(const HeadView& a, const HeadView& b) {
            (a.n_heads == 1 || a.head == b.head);
 }
 
-// Whether two views may share a byte (views of one buffer whose tokens lie side by side are told apart; other interleavings
-// count as shared).
+// Whether two views may share a byte.  Exact where their tokens lie equally far apart and so do their heads (views of one buffer, q, k
+// and v of a token side by side or head by head among them); other interleavings count as shared.
 bool may_overlap(const HeadView& a, const HeadView& b) {
     if (a.end() <= b.base || b.end() <= a.base) return false;
-    if (a.n_tokens > 1 && b.n_tokens > 1 && a.token == b.token && a.token_major() && b.token_major()) {
+    if (a.n_tokens > 1 && a.token != b.token) return true;
+    if (a.n_tokens > 1 && a.token_major() && b.token_major()) {
         __int128 d = (b.base - a.base) % a.token;
         if (d < 0) d += a.token;
         // a covers [0, span_a) of every period, b covers [d, d + span_b)
-        return !(d >= a.heads_span() && d + b.heads_span() <= a.token);
+        if (d >= a.heads_span() && d + b.heads_span() <= a.token) return false;
     }
-    return true;
+    if (a.n_heads > 1 && b.n_heads > 1 && a.head != b.head) return true;
+    // two of their heads lie d + i token + j head apart: is that less than a head for any i and j?
+    const __int128 token = a.n_tokens > 1 ? a.token : 0, head = a.n_heads > 1 ? a.head : b.head, most = a.n_tokens - 1;
+    for (__int128 j = 1 - a.n_heads; j < b.n_heads; ++j) {
+        const __int128 x = b.base - a.base + j * head;
+        __int128 i = token > 0 ? -x / token : 0;                     // the nearest two are this and one beside it
+        for (__int128 k = i - 1; k <= i + 1; ++k) {
+            const __int128 at = k < -most ? -most : k > most ? most : k, gap = x + at * token;
+            if (gap < a.dim && -gap < a.dim) return true;
+        }
+    }
+    return false;
 }
 
 // ---- the cache in 4 bits ------------------------------------------------------------------------------------------
