@@ -553,8 +553,8 @@ def _modules():
     global _torch, _np, _bf16, _f32, _i32, _int64, _int32
     import numpy
     import torch
-    _np, _torch = numpy, torch
-    _bf16, _f32, _i32, _int64, _int32 = torch.bfloat16, torch.float32, torch.int32, numpy.dtype(numpy.int64), numpy.dtype(numpy.int32)
+    _np, _bf16, _f32, _i32, _int64, _int32 = numpy, torch.bfloat16, torch.float32, torch.int32, numpy.dtype(numpy.int64), numpy.dtype(numpy.int32)
+    _torch = torch                                       # last: a call that finds it, in another thread, uses the others
 
 
 def _call_stream(stream, dev):
