@@ -546,24 +546,27 @@ def ipkv_pack_blocks(shape, layout, k, v, n_tokens, dst, stream=None):
 # A decode step calls these once a layer, so what they check is checked with few attribute reads, and tables go to the
 # library as packed bytes.
 
-_torch = _np = _bf16 = _f32 = _i32 = _int64 = _int32 = None
+_torch = _np = _bf16 = _f32 = _i32 = _int64 = _int32 = _current_device = _current_stream = None
 
 
 def _modules():
-    global _torch, _np, _bf16, _f32, _i32, _int64, _int32
+    global _torch, _np, _bf16, _f32, _i32, _int64, _int32, _current_device, _current_stream
     import numpy
     import torch
     _np, _bf16, _f32, _i32, _int64, _int32 = numpy, torch.bfloat16, torch.float32, torch.int32, numpy.dtype(numpy.int64), numpy.dtype(numpy.int32)
+    # torch's own short ways to the current device and stream; where a release lacks them, the public ones
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
     _torch = torch                                       # last: a call that finds it, in another thread, uses the others
 
 
 def _call_stream(stream, dev):
     """The stream of a stateless call on tensors of CUDA device `dev`, as a number: the given one, or the current device's current
     one.  The call runs on the current device, so the tensors have to live there."""
-    if dev < 0 or dev != _torch._C._cuda_getDevice():
+    if dev < 0 or dev != _current_device():
         raise ValueError(f"the tensors are on device {dev} (-1: the host), the call runs on the current CUDA device")
     if stream is None:
-        return _torch._C._cuda_getCurrentRawStream(dev)
+        return _current_stream(dev)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

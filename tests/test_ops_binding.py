@@ -34,3 +34,20 @@ def test_a_call_that_finds_the_modules_finds_all_of_them(monkeypatch):
         sys.settrace(None)
     assert seen and binding._torch is torch
     assert all(not missing for there, missing in seen if there)
+
+
+def test_the_stream_is_found_without_the_names_that_torch_keeps_to_itself(monkeypatch):
+    class Stream:
+        cuda_stream = 77
+
+    for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream() if device == 3 else None)
+    fresh(monkeypatch)
+    binding._modules()
+    assert binding._call_stream(None, 3) == 77
+    assert binding._call_stream(5, 3) == 5 and binding._call_stream(Stream(), 3) == 77
+    for dev in (-1, 0):
+        with pytest.raises(ValueError):
+            binding._call_stream(None, dev)
