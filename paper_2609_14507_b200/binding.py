@@ -613,7 +613,7 @@ def make_rope(dim, rot_dim=None, *, theta=10000.0, sections=None, interleaved=Fa
 
 def ipkv_norm_rope(rope, parts, positions, stream=None):
     """parts: 1..4 tuples (x, weight or None, out or None): x and out [n_tokens, heads, dim] bf16 with any token and head
-    strides, out None means in place.  positions: int32 [n_axes, n_tokens] (or [n_tokens]), contiguous; None without a rotation."""
+    strides, out None means in place.  positions: int32 [n_axes, n_tokens] (or flat), contiguous; None without a rotation."""
     if _torch is None:
         _modules()
     bf16, dim = _bf16, rope.dim
@@ -647,8 +647,10 @@ def ipkv_norm_rope(rope, parts, positions, stream=None):
             wp = w.data_ptr()
         packed += _HEADS_FORMAT.pack(at, to, wp, n_heads, it, ih, ot, oh)
     if positions is not None:
-        if positions.dtype is not _i32 or positions.numel() != rope.n_axes * n_tokens or not positions.is_contiguous() or positions.get_device() != dev:
-            raise ValueError(f"positions are contiguous int32 [{rope.n_axes}, {n_tokens}] on the device of the heads")
+        axes = rope.n_axes
+        if (positions.dtype is not _i32 or positions.numel() != axes * n_tokens or not positions.is_contiguous() or positions.get_device() != dev
+                or (axes > 1 and positions.dim() > 1 and positions.shape[-1] != n_tokens)):
+            raise ValueError(f"positions are contiguous int32 [{axes}, {n_tokens}] on the device of the heads: got {positions.dtype} {tuple(positions.shape)}")
         positions = positions.data_ptr()
     rc = (_lib or lib()).ipkv_norm_rope(C.byref(rope), n_tokens, packed, len(parts), positions, _call_stream(stream, dev))
     if rc != OK:

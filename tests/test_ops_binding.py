@@ -51,3 +51,15 @@ def test_the_stream_is_found_without_the_names_that_torch_keeps_to_itself(monkey
     for dev in (-1, 0):
         with pytest.raises(ValueError):
             binding._call_stream(None, dev)
+
+
+def test_positions_lie_axis_by_axis():
+    """A table with one row per token has the same number of entries, and would be read as if its rows were axes."""
+    rope = binding.make_rope(64, sections=[8, 12, 12])
+    x = torch.zeros((5, 2, 64), dtype=torch.bfloat16)
+    for shape in ((5, 3), (3, 5, 1), (1, 15)):
+        with pytest.raises(ValueError, match="positions"):
+            binding.ipkv_norm_rope(rope, [(x, None, None)], torch.zeros(shape, dtype=torch.int32))
+    for rope, shape in ((rope, (3, 5)), (rope, (15,)), (binding.make_rope(64), (5,)), (binding.make_rope(64), (1, 5)), (binding.make_rope(64), (5, 1))):
+        with pytest.raises(ValueError, match="on device -1"):            # refused for nothing but being on the host
+            binding.ipkv_norm_rope(rope, [(x, None, None)], torch.zeros(shape, dtype=torch.int32))
