@@ -667,9 +667,15 @@ def ipkv_nibble_block_bytes(shape):
     return n
 
 
-def _table(rows, width):
-    """A host table of 64-bit words, [n][width]: a NumPy int64 array as it is, or rows whose first entry may be a tensor."""
+def _table(rows, width, dev):
+    """A host table of 64-bit words, [n][width]: a NumPy int64 array as it is, or rows whose first entry may be a tensor on device dev."""
     if not isinstance(rows, _np.ndarray):
+        for r in (rows, *rows):                          # a tensor's own entries would count as blocks
+            if isinstance(r, _torch.Tensor):
+                raise ValueError("a table of blocks is a list or a NumPy int64 array")
+        for r in rows:
+            if hasattr(r[0], "get_device") and r[0].get_device() != dev:
+                raise ValueError(f"blocks on device {r[0].get_device()} (-1: the host), the other tensors are on {dev}")
         rows = _np.array([[_ptr(r[0]) or 0, *r[1:]] for r in rows], dtype=_np.int64).reshape(-1, width)
     shape = rows.shape
     if rows.dtype != _int64 or len(shape) != 2 or shape[1] != width or not rows.flags.c_contiguous:
@@ -680,8 +686,8 @@ def _table(rows, width):
 def _move(name, shape, spans, k, v, stream):
     if _torch is None:
         _modules()
-    t = _table(spans, 3)
     heads, dim, size, dev, bf16 = shape.n_kv_heads, shape.dim_qk, k.shape, k.get_device(), _bf16
+    t = _table(spans, 3, dev)
     n = size[0]
     if k.dtype is not bf16 or v.dtype is not bf16 or len(size) != 3 or size[1] != heads or size[2] != dim or v.shape != size:
         raise ValueError(f"K and V are bfloat16 [tokens, {heads}, {dim}]: got {k.dtype} {tuple(size)}, {v.dtype} {tuple(v.shape)}")
@@ -721,17 +727,20 @@ def ipkv_nibble_attend(shape, runs, row_start, q, scratch, o_part, lse_part, sta
     an int32 array [rows + 1]; or, with row_start None, one list per row of (blocks, tokens) as for ipkv_attend_runs."""
     if _torch is None:
         _modules()
+    dev = q.get_device()
     if row_start is None:
+        if isinstance(runs, _torch.Tensor):
+            raise ValueError("the table of runs is a list per row, or a NumPy int64 array with row_start")
         row_start = _np.cumsum([0] + [len(r) for r in runs]).astype(_np.int32)
-        runs = _table([x for r in runs for x in r], 2)
+        runs = _table([x for r in runs for x in r], 2, dev)
     else:
-        runs = _table(runs, 2)
+        runs = _table(runs, 2, dev)
         if not isinstance(row_start, _np.ndarray) or row_start.dtype != _int32 or row_start.ndim != 1 or not row_start.flags.c_contiguous:
             raise ValueError("row_start is a contiguous int32 array [rows + 1]")
     rows = len(row_start) - 1
     if rows < 1 or row_start.item(-1) > len(runs):
         raise ValueError(f"row_start names runs that are not there: there are {len(runs)}")
-    heads, f32, dev = shape.n_q_heads, _f32, q.get_device()
+    heads, f32 = shape.n_q_heads, _f32
     want = (rows, heads, shape.dim_qk)
     if (q.dtype is not _bf16 or o_part.dtype is not f32 or lse_part.dtype is not f32 or q.shape != want or o_part.shape != want
             or lse_part.shape != (rows, heads) or not (q.is_contiguous() and o_part.is_contiguous() and lse_part.is_contiguous())

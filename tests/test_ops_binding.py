@@ -63,3 +63,45 @@ def test_positions_lie_axis_by_axis():
     for rope, shape in ((rope, (3, 5)), (rope, (15,)), (binding.make_rope(64), (5,)), (binding.make_rope(64), (1, 5)), (binding.make_rope(64), (5, 1))):
         with pytest.raises(ValueError, match="on device -1"):            # refused for nothing but being on the host
             binding.ipkv_norm_rope(rope, [(x, None, None)], torch.zeros(shape, dtype=torch.int32))
+
+
+def test_blocks_of_another_place_and_tables_that_are_tensors_are_refused():
+    """A row of a table that names a tensor means that tensor's memory: on the host, or on another device, a kernel would run into it.
+    A table that is a tensor itself would name the places of its own entries."""
+    class Elsewhere:                                     # a tensor of the second device, as far as the binding can see
+        def data_ptr(self): return 1 << 20
+        def get_device(self): return 1
+
+    shape = binding.make_shape(binding.GQA, 4, 2, 64, 64, 64, 0.0)
+    k = torch.zeros((3, 2, 64), dtype=torch.bfloat16)
+    q, o, lse, scratch = torch.zeros((1, 4, 64), dtype=torch.bfloat16), torch.zeros((1, 4, 64)), torch.zeros((1, 4)), torch.zeros(64, dtype=torch.uint8)
+    start = torch.tensor([0, 1], dtype=torch.int32).numpy()
+    blocks = torch.zeros(4608 * 2, dtype=torch.uint8)
+    for move in (binding.ipkv_nibble_pack, binding.ipkv_nibble_unpack):
+        with pytest.raises(ValueError, match="blocks"):
+            move(shape, [(Elsewhere(), 0, 3)], k, k)
+        with pytest.raises(ValueError, match="table"):
+            move(shape, torch.tensor([[1 << 20, 0, 3]]), k, k)
+        with pytest.raises(ValueError, match="on device -1"):            # blocks where K and V are: refused for being on the host
+            move(shape, [(blocks, 0, 3)], k, k)
+    with pytest.raises(ValueError, match="blocks"):
+        binding.ipkv_nibble_attend(shape, [[(Elsewhere(), 3)]], None, q, scratch, o, lse)
+    for runs, row_start in ((torch.tensor([[1 << 20, 3]]), start), (torch.tensor([[[1 << 20, 3]]]), None), ([torch.tensor([[1 << 20, 3]])], None)):
+        with pytest.raises(ValueError, match="table"):
+            binding.ipkv_nibble_attend(shape, runs, row_start, q, scratch, o, lse)
+    with pytest.raises(ValueError, match="on device -1"):
+        binding.ipkv_nibble_attend(shape, [[(blocks, 3)]], None, q, scratch, o, lse)
+
+
+@pytest.mark.gpu
+def test_host_blocks_are_refused_beside_device_tensors():
+    shape = binding.make_shape(binding.GQA, 4, 2, 64, 64, 64, 0.0)
+    k = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    blocks = torch.zeros(4608 * 2, dtype=torch.uint8)
+    for move in (binding.ipkv_nibble_pack, binding.ipkv_nibble_unpack):
+        with pytest.raises(ValueError, match="blocks"):
+            move(shape, [(blocks, 0, 3)], k, k)
+    q, o, lse = torch.zeros((1, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, 4, 64), device="cuda"), torch.zeros((1, 4), device="cuda")
+    scratch = torch.zeros(binding.ipkv_nibble_scratch_bytes(shape, 1, 1), dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError, match="blocks"):
+        binding.ipkv_nibble_attend(shape, [[(blocks, 3)]], None, q, scratch, o, lse)
