@@ -616,6 +616,8 @@ def ipkv_norm_rope(rope, parts, positions, stream=None):
     strides, out None means in place.  positions: int32 [n_axes, n_tokens] (or flat), contiguous; None without a rotation."""
     if _torch is None:
         _modules()
+    if not parts:
+        raise ValueError("a call takes 1 to 4 parts")
     bf16, dim = _bf16, rope.dim
     x = parts[0][0]
     n_tokens, dev = x.shape[0], x.get_device()

@@ -105,3 +105,8 @@ def test_host_blocks_are_refused_beside_device_tensors():
     scratch = torch.zeros(binding.ipkv_nibble_scratch_bytes(shape, 1, 1), dtype=torch.uint8, device="cuda")
     with pytest.raises(ValueError, match="blocks"):
         binding.ipkv_nibble_attend(shape, [[(blocks, 3)]], None, q, scratch, o, lse)
+
+
+def test_a_call_without_heads_is_refused():
+    with pytest.raises(ValueError, match="1 to 4"):
+        binding.ipkv_norm_rope(binding.make_rope(64), [], None)
