@@ -38,7 +38,8 @@
 // take them in turn.  At the end of a (row, head group) every warp writes its partial and goes on, and a second kernel joins the partials
 // in a fixed order; where one CTA has the whole group (WHOLE: short sequences) it does that itself.  (Joining a CTA's warps through shared memory first made each wait for the slowest: ragged 64 192 us, now 175
 // with that change alone.)  How rows and heads are shared out among CTAs: ops.h.
-// More than 8 query heads per KV head: several warps (one per octet of heads) share a tile, so it is still read once.
+// More than 8 query heads per KV head: they make octets, one octet to a warp.  An even number of octets goes by twos or fours, whose warps are
+// a team on one tile; other numbers of octets, and what is more than one group, read the tile once for each group (ops.h).
 // Every wait is bounded; a warp whose wait ran out does no more work.
 //
 // Bound by instruction issue, then by the copies: a product of 16 x 8 x 16 keeps its quarter of an SM busy for eight cycles, and a tile of
@@ -274,8 +275,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
 
     // ---------------- consumers ----------------
     const int g = lane >> 2, t = lane & 3;
-    const int team = warp / octets, octet = warp - team * octets;
-    const bool works = team < teams;
+    const int team = warp / octets, octet = warp - team * octets;        // octets divide the warps: every warp has a team
     bool dead = false;
     // Which tokens enter the output product complemented: 16u + 8h + g with g + h odd.
     const uint32_t odd = p.odd_tokens;           // g odd, as the halves of a word of V (an immediate here would cost an instruction a use)
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         float c[2];                              // log2 units per score, of heads 2t and 2t+1
         {
             const int hq = octet * 8 + (HALF ? (g & 3) : g);
-            const bool live = works && hq < n_heads;
+            const bool live = hq < n_heads;
             const uint4* src = reinterpret_cast<const uint4*>(p.q + (int64_t(x.row) * p.n_q_heads + head0 + hq) * (2 * D) + 32 * t);
             float v[P][16], top = 0.f;
 #pragma unroll
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
         const int it_end = it0 + x.n;
         int first = it0 / teams * teams + team;
         if (first < it0) first += teams;
-        for (int it = works ? first : it_end; it < it_end; it += teams) {
+        for (int it = first; it < it_end; it += teams) {
             if (!dead && !ptx::mbar_wait(ptx::smem_addr(&sm.full[st]), phase)) {
                 if (lane == 0 && p.status) atomicOr(p.status, kStatusNoTile);
                 dead = true;
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
 
         if (WHOLE) consumers_meet();             // the ring is free when every warp has done its tiles
         // ---- the warp's partial: every team writes its own (nobody waits for another warp), one without a tile an empty one ----
-        if (works) {
+        {
             float f[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
