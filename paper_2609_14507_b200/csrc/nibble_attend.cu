@@ -17,10 +17,10 @@
 // held as two fp16 numbers, head and remainder (22 bits): with at most 4 query heads per KV head they share one product (columns
 // 0-3 and 4-7), otherwise there are two.  The remainder is held times 2^11: a head that is cut at fp16's smallest step, 2^-24, leaves its
 // digits to a remainder that is cut at 2^-35.  (Without the factor both were cut at 2^-24: half of the tokens with weights of 2^-16 had
-// lost ten digits.)  sv is brought near 1 by a power of two per warp, so that fp16's range is spent on p.  It follows the largest scale among
-// tokens that count (with the largest of all, one token of no weight whose values were 2^20 times the others' took all but seven of their
-// digits) and leaves room for 2^4: a first token that outweighs the next by 2^12 and has no values would have every tile behind it
-// look again.  So a weight p is known to 22 bits or 2^-34 of the reference's, whichever is coarser.
+// lost ten digits.)  sv is brought near 1 by a power of two for each head of a warp, so that fp16's range is spent on p.  It follows the
+// largest scale among tokens that count for the head (with the largest of all, one token of no weight whose values were 2^20 times the
+// others' took all but seven of their digits) and leaves room for 2^4: a first token that outweighs the next by 2^12 and has no values would
+// have every tile behind it look again.  So a weight p is known to 22 bits or 2^-34 of the reference's, whichever is coarser.
 // The tensor cores add with two bits more than fp32 has and round towards zero, both counted from the largest exponent that
 // an operand's FORMAT shows (a subnormal counts as the smallest normal number).  Two things follow.  The codes must fill the
 // subnormal range: K's do in place as bf16 (7 bits of mantissa; bits 0..3 and 4..7), V's are shifted up to bits 3..6 and 7..10 of fp16,
@@ -90,9 +90,10 @@ __device__ __forceinline__ void mma_bf16_k8(float (&d)[4], uint32_t a0, uint32_t
         : "r"(a0), "r"(a1), "r"(b0));
 }
 // Two fp32 operations in one instruction, each rounded as if alone.
-__device__ __forceinline__ float2 mul2(float a0, float a1, float b) {
+__device__ __forceinline__ float2 mul2(float a0, float a1, float b0, float b1) {
     float2 r;
-    asm("{.reg .b64 p, q; mov.b64 p, {%2,%3}; mov.b64 q, {%4,%4}; mul.rn.f32x2 p, p, q; mov.b64 {%0,%1}, p;}" : "=f"(r.x), "=f"(r.y) : "f"(a0), "f"(a1), "f"(b));
+    asm("{.reg .b64 p, q; mov.b64 p, {%2,%3}; mov.b64 q, {%4,%5}; mul.rn.f32x2 p, p, q; mov.b64 {%0,%1}, p;}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
     return r;
 }
 __device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
@@ -352,7 +353,10 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             for (int i = 0; i < 4; ++i) o[d][i] = 0.f;
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, oz[2] = {0.f, 0.f};      // l and oz: this lane's tokens only
         float limit[2] = {-INFINITY, -INFINITY};                                          // scores above it raise m
-        float v_limit = -1.f, fv = 0.f;          // value scales from v_limit on raise the power of two behind fv
+        // What value scales are multiplied with, 2^(127 - x) for a head, as the operands have it: times 64, and negative where a complement's
+        // weight is.  Scales from v_limit on may raise an x.
+        float v_limit = -1.f, f0[2] = {0.f, 0.f};
+        auto scaled_by = [&](int e) { return f0[e] == 0.f ? -1 : 260 - int(__float_as_uint(f0[e]) >> 23 & 255u); };     // x, -1: not yet
 
         // the tiles of team `team`: it = team modulo teams
         const int it_end = it0 + x.n;
@@ -445,32 +449,39 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                         l[e] *= alpha[e]; oz[e] *= alpha[e];
                     }
                 }
-                if (v_top >= v_limit) {
+                if (__any_sync(0xffffffffu, v_top >= v_limit)) {
                     // scales of one order all count; otherwise a token's does in full from a weight of 2^-12 on, and less below
-                    float least = v_top, most = v_top;
+                    float least = v_top, most[2] = {v_top, v_top};
 #pragma unroll
                     for (int un = 0; un < 4; ++un) least = fminf(least, fminf(sv[un][0], sv[un][1]));
                     if (__any_sync(0xffffffffu, least * float(1 << kRoom) < v_top)) {
-                        most = 0.f;
 #pragma unroll
-                        for (int un = 0; un < 4; ++un)
+                        for (int e = 0; e < 2; ++e) {
+                            most[e] = 0.f;
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const float y = fmaxf(fmaf(s[un][2 * h], c[0], 12.f - m[0]), fmaf(s[un][2 * h + 1], c[1], 12.f - m[1]));
-                                most = fmaxf(most, sv[un][h] * fminf(ptx::ex2(y), 1.f));
-                            }
+                            for (int un = 0; un < 4; ++un)
 #pragma unroll
-                        for (int d = 1; d <= 16; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+                                for (int h = 0; h < 2; ++h) most[e] = fmaxf(most[e], sv[un][h] * fminf(ptx::ex2(fmaf(s[un][2 * h + e], c[e], 12.f - m[e])), 1.f));
+#pragma unroll
+                            for (int d = 4; d <= 16; d <<= 1) most[e] = fmaxf(most[e], __shfl_xor_sync(0xffffffffu, most[e], d));
+                        }
                     }
-                    if (most >= v_limit) {
-                        const int e = min(max(int(__float_as_uint(most) >> 23) + kRoom, 8), 250);
-                        const float f_new = __uint_as_float(uint32_t(254 - e) << 23);    // such scales times f_new lie below 2^(1 - kRoom)
-                        const float r = fv == 0.f ? 0.f : f_new / fv;
-                        alpha[0] *= r; alpha[1] *= r;
-                        fv = f_new;
-                        v_limit = __uint_as_float(uint32_t(e + 1) << 23);
-                        rescale = true;
+                    bool raised = false;
+                    int x_low = 255;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        int x = scaled_by(e);
+                        if (most[e] >= __uint_as_float(uint32_t(x + 1) << 23)) {
+                            const int x_new = min(max(int(__float_as_uint(most[e]) >> 23) + kRoom, 8), 250);     // such scales lie below 2^(1 - kRoom) then
+                            alpha[e] *= x < 0 ? 0.f : __uint_as_float(uint32_t(max(127 + x - x_new, 0)) << 23);
+                            f0[e] = __uint_as_float(uint32_t(260 - x_new) << 23 | (g & 1) << 31);
+                            x = x_new;
+                            raised = true;
+                        }
+                        x_low = min(x_low, x);
                     }
+                    v_limit = __uint_as_float(uint32_t(x_low + 1) << 23);
+                    rescale = __any_sync(0xffffffffu, raised) || rescale;
                 }
                 if (rescale) {
 #pragma unroll
@@ -483,22 +494,22 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
             // weights, and their products with the value scales as operands [token][head]
             uint32_t hi[4][2], lo[4][2];
             float zt[2] = {0.f, 0.f};
-            const float f0 = (g & 1) ? fv * -64.f : fv * 64.f, f1 = f0 * -0.0625f;   // a complement's weight is negative; codes of h = 1 are times 2^4
+            const float2 f1 = mul2(f0[0], f0[1], -0.0625f, -0.0625f);                    // codes of h = 1 are times 2^4, and complements where h = 0's are not
 #pragma unroll
             for (int un = 0; un < 4; ++un)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float svf = sv[un][h] * (h ? f1 : f0);
+                    const float2 svf = h ? mul2(f1.x, f1.y, sv[un][h], sv[un][h]) : mul2(f0[0], f0[1], sv[un][h], sv[un][h]);
                     const float2 y = fma2(s[un][2 * h], s[un][2 * h + 1], c[0], c[1], -m[0], -m[1]);
                     const float pr[2] = {ptx::ex2(y.x), ptx::ex2(y.y)};
                     add2(l[0], l[1], pr[0], pr[1]);
 #pragma unroll
                     for (int e = 0; e < 2; ++e) zt[e] = fmaf(pr[e], zv[un][h], zt[e]);
-                    float2 w = mul2(pr[0], pr[1], svf);
+                    float2 w = mul2(pr[0], pr[1], svf.x, svf.y);
                     const uint32_t big = pack_f16(w.x, w.y);
                     const float2 back = unpack_f16(big);
                     add2(w.x, w.y, -back.x, -back.y);
-                    w = mul2(w.x, w.y, kRest);
+                    w = mul2(w.x, w.y, kRest, kRest);
                     const uint32_t rest = pack_f16(w.x, w.y);
                     if (HALF) hi[un][h] = transpose8x8(t < 2 ? big : rest);              // columns 4-7 repeat heads 0-3
                     else { hi[un][h] = transpose8x8(big); lo[un][h] = transpose8x8(rest); }
@@ -548,7 +559,9 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
                 }
                 f[e] = l[e] == 0.f ? 0.f : 1.f / l[e];
             }
-            const float undo = fv > 0.f ? 0x1p15f : 0.f, inv_fv = fv > 0.f ? 1.f / fv : 0.f;   // 2^21 / 64, then 1 / fv
+            float undo[2];                       // 2^(x - 127), behind 2^15: 2^21 / 64
+#pragma unroll
+            for (int e = 0; e < 2; ++e) undo[e] = __uint_as_float(uint32_t(max(scaled_by(e), 0)) << 23);
             const int hb = octet * 8 + 2 * t;    // of the head group
             const int64_t row0 = (int64_t(x.slot) * teams + team) * p.rows_per_part + hb;      // (of the ring's memory: slot 0)
             const bool inside = !kChecked || WHOLE || (row0 >= 0 && row0 + min(2, n_heads - hb) <= p.part_rows);      // the partial must lie inside the scratch
@@ -562,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, kNibbleCtasPerSm) nibble_attend_kern
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if (HALF) o[d][i] = fmaf(__shfl_xor_sync(0xffffffffu, o[d][i], 2), 1.f / kRest, o[d][i]);
-                        o[d][i] = fmaf(o[d][i] * undo, inv_fv, oz[i & 1]) * f[i & 1];
+                        o[d][i] = fmaf(o[d][i] * 0x1p15f, undo[i & 1], oz[i & 1]) * f[i & 1];
                     }
 #pragma unroll
                     for (int e = 0; e < 2; ++e)

@@ -181,3 +181,30 @@ def test_a_value_far_out_takes_no_digits_from_the_others(hq, hkv, at, factor, ga
     size = np.sqrt((p ** 2 * (vd ** 2).sum(-1).T[:, None]).sum(-1)).reshape(-1)
     assert miss(o[0], want, size * RELATIVE + np.sqrt((rest ** 2).sum(-1).max()) * FLOOR) <= 1
     assert (np.abs(lse[0] - want_lse) <= LSE + np.abs(want_lse) * 2.0 ** -22).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (8, 1), (32, 2)])
+@pytest.mark.parametrize("at", [0, 300, 699])
+@pytest.mark.parametrize("factor", [10, 20, 30])
+def test_what_one_head_looks_at_takes_no_digits_from_the_heads_beside_it(hq, hkv, at, factor):
+    """The token with values far out has all of every other head's weight and nothing of the rest's."""
+    d, n = 128, 700
+    rng = np.random.default_rng(factor * 1000 + at)
+    sh = shape_of(hq, hkv, d, 64, 1.0)
+    sign = np.where(rng.random(d) < 0.5, -1.0, 1.0)
+    k = rng.standard_normal((n, hkv, d)) * 0.02
+    k[at, :, :64] += sign[:64] * 20 * np.log(2) / 64
+    k[at, :, 64:] -= sign[64:] * 80 * np.log(2) / 64
+    q = np.zeros((1, hq, d))
+    q[0, ::2, :64] = sign[:64]
+    q[0, 1::2, 64:] = sign[64:]
+    v = rng.standard_normal((n, hkv, d)).astype(np.float32)
+    v[at] *= np.float32(2.0) ** factor
+    q, k, v = (synth.f32_to_bf16_bits(x.astype(np.float32)) for x in (q, k, v))
+    o, lse = attend(sh, [[(packed(sh, k, v), n)]], q)
+    p, vd, want, want_lse = exact(sh, q[0], k, v)
+    size = np.sqrt((p ** 2 * (vd ** 2).sum(-1).T[:, None]).sum(-1)).reshape(-1)
+    floor = np.sqrt((np.delete(vd, at, 0) ** 2).sum(-1).max()) * FLOOR
+    assert miss(o[0], want, size * RELATIVE + floor) <= 1
+    assert (np.abs(lse[0] - want_lse) <= LSE + np.abs(want_lse) * 2.0 ** -22).all()
