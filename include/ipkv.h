@@ -436,7 +436,7 @@ int64_t ipkv_block_bytes(const ipkv_attn_shape* shape);
  *   y = x * rsqrt(mean(x^2) + eps) * weight            (over the head's dim columns; skipped where weight_dev is NULL)
  *   (a, b) -> (a cos t - b sin t, b cos t + a sin t)   (pair i of y's first rot_dim columns; the others stay)
  *   t = positions[pair_axis[i]][token] * frequency i
- * bf16 in and out, fp32 in between, one rounding.  The angle is the product modulo a turn, off by at most 2^-24 of a
+ * bf16 in and out, fp32 in between, one rounding (the sum of a head's squares has to stay within fp32).  The angle is the product modulo a turn, off by at most 2^-24 of a
  * turn for every 32-bit position and frequencies up to one turn per position (an fp32 product of a far position is not). */
 typedef struct {
   int32_t dim;               /* columns of a head: 64, 128 or 256                                              */
@@ -515,7 +515,7 @@ ipkv_status ipkv_nibble_unpack(const ipkv_attn_shape* shape, int32_t n_spans, co
  * the blocks hold behind them may be anything).  runs and row_run_start are host arrays, copied by the call; small tables travel
  * with the launch, so that the call can be captured into a CUDA graph like ipkv_attend_runs.  q_dev [n_rows][n_q_heads][dim] bf16.
  * Outputs fp32: o_part_dev [n_rows][n_q_heads][dim] normalised, lse_part_dev [n_rows][n_q_heads] natural log; a row without
- * tokens gives (0, -inf), a head whose query or tokens hold a NaN gives NaN.  They join partials over other tokens (a bf16
+ * tokens gives (0, -inf), a head whose query or whose tokens' scales or zeros hold a NaN gives NaN.  They join partials over other tokens (a bf16
  * window, the CPU side) through ipkv_merge.
  * scratch_dev: at least ipkv_nibble_scratch_bytes, 256-byte aligned, private to this call until its work on `stream` has
  * completed (calls captured into graphs that may run at the same time need scratch of their own).  status_dev as in

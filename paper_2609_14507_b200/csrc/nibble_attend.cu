@@ -28,9 +28,9 @@
 // codes are never negative, but an output is a mean of many values of either sign, so a sum of p sv code would exceed it by
 // 2.5 sqrt(tokens); every other token enters complemented, code = 15 - (15 - code): the complement costs nothing in the mask, its
 // weight is negative, 15 sv joins zv, and the excesses of the two halves meet in the same product (and in either half of its
-// 16 tokens: with tokens 0-7 plain and 8-15 complemented the cut was one-sided, 4.2e-6 of the output at 1M tokens instead of 8e-7).
+// 16 tokens: with tokens 0-7 plain and 8-15 complemented the cut was one-sided, 4.2e-6 of the output at 1M tokens, now 9.5e-7).
 // Remainders have sums of their own: added to the heads' they would be cut at the heads' exponent.  Without all this the output of
-// 32K tokens was off by 5e-4 of itself; it is off by 1e-6 (a computation in fp32: 6e-7).
+// 32K tokens was off by 5e-4 of itself; it is off by less than 1e-6 (a computation in fp32: 4e-7 to 1.5e-6).
 //
 // One warp works on one tile (64 tokens of a KV head) at a time, alone: its online softmax has its own reference maximum, raised
 // only when a score exceeds it by 2^8 (then everything is rescaled), which costs one vote per tile in place of a reduction over lanes.  A
@@ -44,10 +44,11 @@
 //
 // Bound by instruction issue, then by the copies: a product of 16 x 8 x 16 keeps its quarter of an SM busy for eight cycles, and a tile of
 // 128 columns takes 68 of them (4 query heads per KV head) or 100, beside 750 to 900 other instructions; the tiles of three
-// CTAs with four such warps and 73 KB of ring each are under way on an SM (fewer or larger CTAs: 3 to 15 % slower).  Measured, 128 columns:
-// 64 ragged rows of up to 24K tokens, 8 KV heads of 4 query heads: 158 us for 932 MB, 5.9 TB/s, 0.90 of a copy's rate; 16 rows of 32K,
-// 4 KV heads of 8: 62.7 us, 4.7 TB/s; one of 1M, 16 query heads on one KV head (every tile unpacked by two warps): 64 us,
-// 2.2 TB/s; one of 4K: 8.6 us, two launches of which neither does much.
+// CTAs with four such warps and 73 KB of ring each are under way on an SM (fewer or larger CTAs: 3 to 15 % slower).  Measured, 128 columns,
+// back to back for seconds (in brackets: a few calls, before the board reaches its power limit and leaves 1965 MHz):
+// 64 ragged rows of up to 24K tokens, 8 KV heads of 4 query heads: 190 us at 1.67 GHz (163) for 932 MB, 4.9 TB/s (5.7), 0.75 of a copy's
+// rate (0.87); 16 rows of 32K, 4 KV heads of 8: 69 us at 1.75 GHz (61.5), 4.3 TB/s (4.8); one of 1M, 16 query heads on one KV head
+// (every tile unpacked by two warps): 62 us, 2.3 TB/s; one of 4K: 8.4 us, two launches of which neither does much.
 #include <cuda_fp16.h>
 
 #include "kernels.h"

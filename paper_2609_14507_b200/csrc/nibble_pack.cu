@@ -13,12 +13,12 @@
 // exactly the tokens that share its words of V.  All 8 loads of a thread are issued before the first is used.  Groups are reduced
 // among the lanes of a token by shuffles; the tile's image is put together in shared memory and leaves in 16-byte stores.
 // A tile that the span covers in part keeps the other tokens' codes: its image is loaded first.
-// 32K tokens of 4 heads of 128 columns, written and read back: 33 us for 171 MB, 5.2 TB/s, 0.79 of a copy's rate (issue slots 79 %
-// busy in pack, 72 % in unpack); with K and V of a tile in one CTA 36, seven ragged chunks of up to 2.5K tokens 8.3 and 15 (half as many
+// 32K tokens of 4 heads of 128 columns, written and read back: 32.7 us for 171 MB, 5.2 TB/s, 0.80 of a copy's rate (issue slots 79 %
+// busy in pack, 72 % in unpack), 33.8 back to back for seconds (1.89 GHz); with K and V of a tile in one CTA 36, seven ragged chunks of up to 2.5K tokens 7.9 and 15 (half as many
 // CTAs, each twice as long); a scale computed by every lane, and fp32 values in unpack, 45.5.
 //
 // Single tokens (a decode step: one token per sequence) would move 9 KB each way for 140 bytes: they have kernels of their own, which write
-// the token's K words and its nibble of every V word in place (64 tokens of 8 heads, both ways: 4.8 us, two launches).
+// the token's K words and its nibble of every V word in place (64 tokens of 8 heads, both ways: 4.4 us, two launches).
 #include <cuda_bf16.h>
 
 #include "launch.cuh"

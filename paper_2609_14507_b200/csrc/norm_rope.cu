@@ -13,9 +13,9 @@
 // token: every lane takes D/64 pairs' sine and cosine and the lanes that need them fetch them by shuffles, and the weights are
 // multiplied into them, so that a pair costs six fp32 operations a head: out_a = (a r)(w_a c) - (b r)(w_b s), out_b = (b r)(w_b c) + (a r)(w_a s).
 // The copies of a warp's next steps are under way while it computes, across its tokens, through a ring of 16-byte slots in shared
-// memory that each lane fills and reads for itself.  32K tokens of 36 heads of 128: 96 us, 96 % of the measured copy rate; with loads
-// into registers one step ahead 137 us (too few bytes under way), with sines by every lane for itself and the weights by
-// themselves 141 us (bound by its instructions).  With few tokens the steps of a token are divided among warps (`split`), so
+// memory that each lane fills and reads for itself.  32K tokens of 36 heads of 128: 95.5 us in a few calls, 97 % of the measured copy rate, and
+// 100 us back to back for seconds (the board at its power limit, 1.73 GHz); with loads into registers one step ahead 137 us (too few bytes
+// under way), with sines by every lane for itself and the weights by themselves 141 us (bound by its instructions), in a few calls both.  With few tokens the steps of a token are divided among warps (`split`), so
 // that one token of 36 heads is not one warp's nine steps in a row.
 #include <cuda_bf16.h>
 

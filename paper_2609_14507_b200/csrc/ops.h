@@ -127,6 +127,9 @@ struct NibbleAttend {
 // Head groups of a KV head's `group` query heads, and heads in each.  One warp per 8 heads works on a tile, and the tile is read once for a
 // group: as many octets as divide both the computing warps and the octets there are, so that no warp is idle (40 heads on one KV head, 200K
 // tokens: 36 us; in two groups of 24 and 16, three warps of four busy, 51, though the tiles were read twice in place of five times).
+// Sharing reads a tile once and gives a group fewer teams, so it wins where the copies bound and loses a little elsewhere.  In us, shared
+// and (in brackets) one octet a group, 128 columns: 32 heads on one KV head, 200K tokens 30.9 (37.7), 20K 12.2 (11.2), 8 rows of 20K 27.9
+// (26.9); 16 heads, 1M 61.8 (63.0), 200K 27.6 (24.9), 8 x 20K 19.3 (18.1), 40 x 600 9.6 (9.0), 1K 7.3 (7.7); 48 heads, 200K 39.8 (39.8).
 inline int nibble_group_octets(int group) {
     const int n = (group + 7) / 8;
     return n % 4 == 0 ? 4 : n % 2 == 0 ? 2 : 1;
@@ -139,7 +142,8 @@ static_assert(kNibbleWarps == 4, "octets of a group");
 // A team that works off k tiles takes about (us, 128 columns, 4 query heads per KV head; 8 take a sixth more)
 //   7 + 1.3 k with one CTA to an SM,   9.3 + 1.75 k with two,   9.5 + 2.5 k with three,
 // and the chunks, which fill all SMs to the same degree but meet two pairs and more, with r rounds of tiles on three CTAs,
-//   11.5 + 2.4 r, 5.5 more if there are several pairs.
+//   11.5 + 2.4 r, 5.5 more if there are several pairs
+// (fitted there, and used as they are for 64 columns and for teams of several warps).
 // Whole CTAs win where there is little work for each SM (one row of 4K tokens of 4 KV heads 8.6 us against 10.6, 16 rows of 2K 12.7 against
 // 18.2, 32 ragged rows of up to 2K and 8 KV heads 17.5 against 27), chunks with more (16 rows of 32K 66 us against 71, 48 ragged rows
 // of up to 8K 45 against 58).  One CTA to a pair saves the join, 2.5 us, and its launch on the host: a call on one row of 768 tokens and 4 KV
