@@ -292,7 +292,7 @@ ipkv_status ipkv_norm_rope(const ipkv_rope* rope, int64_t n_tokens, const ipkv_h
     for (int i = 0; i < n_parts; ++i)
         for (int k = 0; k < n_parts; ++k) {
             if (i != k && may_overlap(out[i], out[k])) return IPKV_EINVAL;
-            if (may_overlap(out[i], in[k]) && !(i == k && same_view(out[i], in[k]))) return IPKV_EINVAL;
+            if (!(i == k && same_view(out[i], in[k])) && may_overlap(out[i], in[k])) return IPKV_EINVAL;
         }
     constexpr long double kTurnsPerRadian = 0.159154943091895335768883763372514362L;
     // theta^(-2i / rot_dim) by repeated multiplication (one power a call instead of one a pair): at most 127 roundings of 2^-64
