@@ -58,6 +58,19 @@ def test_no_views_that_share_bytes_are_taken():
     assert taken > 500
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are not real")
+@pytest.mark.parametrize("ts,n", [(1 << 40, 1 << 18), (1 << 48, 1 << 20), (1 << 48, (1 << 31) - 1)])
+def test_views_whose_extent_passes_63_bits(ts, n):
+    d = 128
+    rope = binding.make_rope(d)
+    part = lambda at, heads=3: Heads(BASE + at, BASE + at, None, heads, ts, 2 * d, ts, 2 * d)
+    assert rc(rope, [part(0), part(2 * d)], n) == ECUDA
+    assert rc(rope, [part(0), part(2 * d - 16)], n) == EINVAL
+    assert rc(rope, [part(0), part(2 * ts * 5 + 2 * d)], n) == ECUDA     # a token further on, between the heads again
+    assert rc(rope, [part(0), part(2 * ts * 5 + 2 * d + 16)], n) == EINVAL
+    assert rc(rope, [part(0), part(2 * ts * 5 + 4 * 3 * d)], n) == ECUDA     # behind the other's heads
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n", [1, 3, 300])
 @pytest.mark.parametrize("inter", [False, True])
