@@ -525,6 +525,73 @@ ipkv_status ipkv_nibble_attend(const ipkv_attn_shape* shape, int32_t n_rows, con
                                const void* q_dev, void* scratch_dev, size_t scratch_bytes, float* o_part_dev, float* lse_part_dev,
                                uint32_t* status_dev, void* stream);
 
+/* ---- a paged cache of bounded length (no handle) ------------------------------------------------------------------
+ * TILE blocks in a pool, named by a page table.  Pool, table, lengths and what the slots carry are device memory, so that a decode step
+ * captured into a CUDA graph is replayed as sequences grow, change pages or end: no call reads them on the host, and none writes
+ * the table or the lengths (all layers of a model share them).  Grouped-query shapes, dim 64 or 128, block_tokens 16, 32 or a multiple of
+ * 64.  Slot s of row r lies in block table[r][s / block_tokens] at token offset s % block_tokens.  Keys are cached after their
+ * rotation, so the order of a row's slots means nothing to the attention: an eviction fills holes in place of closing ranks, and
+ * what has to be known of a slot's token moves along (positions_dev, weights_dev; per KV head, since each keeps other tokens).
+ * A block may serve several rows as long as no call writes it (a shared prefix). */
+typedef struct {
+  void* pool_dev;               /* n_blocks TILE blocks (ipkv_block_bytes each), 16-byte aligned                        */
+  int64_t n_blocks;
+  const int32_t* table_dev;     /* [n_rows][table_stride]: a row's blocks in the order of its slots; entries behind its length are
+                                   not read                                                                             */
+  const int32_t* lengths_dev;   /* [n_rows]: slots of the row, 0 .. max_blocks * block_tokens                             */
+  int32_t n_rows, max_blocks;   /* max_blocks: entries of a row's table                                                  */
+  int64_t table_stride;         /* elements, >= max_blocks                                                               */
+  float* weights_dev;           /* [n_rows][n_kv_heads][slot_stride]: attention that the slot's token has been given; or NULL  */
+  int32_t* positions_dev;       /* the same shape: its position in the sequence; or NULL                                 */
+  int64_t slot_stride;          /* elements, a multiple of 4 and >= max_blocks * block_tokens (0 without both); both arrays 16-byte aligned */
+} ipkv_paged;
+
+/* Bits that the calls below OR into *status_dev (may be NULL), beside those of ipkv_attend_runs: a length outside
+ * 0 .. max_blocks * block_tokens, or a needed table entry outside 0 .. n_blocks - 1.  Such a token is left out: nothing outside the pool
+ * is read or written. */
+#define IPKV_STATUS_BAD_PAGE 16u
+
+/* Write new tokens.  k_dev, v_dev [n_tokens][n_kv_heads][dim] bf16, 16-byte aligned; *_token_stride: elements between tokens (multiples of 8; 0: dense).
+ * row_start_dev: device int32 [n_rows + 1], tokens row_start[r] .. row_start[r+1] are row r's; tokens behind row_start[n_rows] are
+ * ignored.  NULL: one token per row (n_tokens == n_rows).  The lengths already count the new tokens: the last new
+ * token of a row goes to slot lengths[r] - 1; one that the length does not count is not written (a row of length 0 takes none).
+ * positions: token_positions_dev int32 [n_tokens] goes to the slots of all KV heads (required with cache->positions_dev);
+ * the slots' weights become 0.  Rows and slots of one call must not share blocks.  Works on the current device. */
+ipkv_status ipkv_paged_append(const ipkv_attn_shape* shape, const ipkv_paged* cache, int64_t n_tokens, const void* k_dev, const void* v_dev,
+                              int64_t k_token_stride, int64_t v_token_stride, const int32_t* row_start_dev,
+                              const int32_t* token_positions_dev, uint32_t* status_dev, void* stream);
+
+/* Attention of one query per row over its slots.  window 0: all of them; else slot t of n is visible if t >= n - window or t < first_tokens
+ * (a sliding window of the last `window` slots, and first ones that stay visible).  q_dev [n_rows][n_q_heads][dim] bf16, q_row_stride
+ * elements between rows (a multiple of 8; 0: dense).  Outputs as in ipkv_attend_runs, fp32: o_part_dev [n_rows][n_q_heads][dim] normalised, lse_part_dev
+ * [n_rows][n_q_heads] natural log, (0, -inf) for a row without visible slots; they join other partials through ipkv_merge.  Invisible slots
+ * may hold anything; a NaN or an infinity in a visible one makes the outputs that it takes part in NaN or infinite.
+ * weights_out_dev: NULL, or shaped like cache->weights_dev: for every visible slot
+ *   weights_out = weights + sum over the KV head's query heads of the slot's softmax weight in this call
+ * (weights: cache->weights_dev, zeros if that is NULL; the same array for an update in place, else one that does not overlap it).  Other slots are not written.
+ * scratch_dev: at least ipkv_paged_scratch_bytes (of the same n_rows, max_blocks, window, first_tokens; weigh: weights_out_dev is given),
+ * 256-byte aligned, private to this call until its work on `stream` has completed (calls captured into graphs that may run at the same
+ * time need scratch of their own).  Results are bit-reproducible.  Works on the current device. */
+ipkv_status ipkv_paged_scratch_bytes(const ipkv_attn_shape* shape, int32_t n_rows, int32_t max_blocks, int32_t window, int32_t first_tokens,
+                                     int32_t weigh, size_t* out_bytes);
+ipkv_status ipkv_paged_attend(const ipkv_attn_shape* shape, const ipkv_paged* cache, const void* q_dev, int64_t q_row_stride, int32_t window,
+                              int32_t first_tokens, float* weights_out_dev, void* scratch_dev, size_t scratch_bytes, float* o_part_dev,
+                              float* lse_part_dev, uint32_t* status_dev, void* stream);
+
+/* Cut every row to at most `budget` slots, for every KV head by itself.  Of a row's n > budget slots those are kept whose token's position is
+ * below first_tokens or among the last `recent` (position > newest - recent, newest: the largest position of the head's slots), then those with the largest weights; a NaN
+ * counts as less than every number, equal weights go by the lower slot.  first_tokens + recent <= budget.  The i-th kept slot at or behind
+ * `budget` moves to the i-th slot below it that is not kept (K, V, weight, position); other slots below the budget stay as they are, those behind it keep
+ * what they held.  The lengths are the caller's to change, after all layers: min(length, budget).
+ * weights_out_dev, positions_out_dev: where the first min(n, budget) slots' weights and positions go; NULL: in place (else they do not overlap the
+ * cache's).  kept_dev: NULL, or int32 [n_rows][n_kv_heads][budget]: the slot that each slot's token comes from (the first
+ * min(n, budget) of every row are written).  Rows must not share blocks.  scratch_dev as above, at least
+ * ipkv_paged_evict_scratch_bytes.  Works on the current device. */
+ipkv_status ipkv_paged_evict_scratch_bytes(const ipkv_attn_shape* shape, int32_t n_rows, int32_t max_blocks, int32_t budget, size_t* out_bytes);
+ipkv_status ipkv_paged_evict(const ipkv_attn_shape* shape, const ipkv_paged* cache, int32_t budget, int32_t first_tokens, int32_t recent,
+                             float* weights_out_dev, int32_t* positions_out_dev, int32_t* kept_dev, void* scratch_dev, size_t scratch_bytes,
+                             uint32_t* status_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

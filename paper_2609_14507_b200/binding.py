@@ -31,6 +31,7 @@ EXPORTS = [
     "ipkv_selftest_expire_wait", "ipkv_selftest_fail_next_launch", "ipkv_selftest_declare_bounds", "ipkv_probe_umma",
     "ipkv_norm_rope", "ipkv_nibble_block_bytes", "ipkv_nibble_pack", "ipkv_nibble_unpack",
     "ipkv_nibble_scratch_bytes", "ipkv_nibble_attend",
+    "ipkv_paged_append", "ipkv_paged_scratch_bytes", "ipkv_paged_attend", "ipkv_paged_evict_scratch_bytes", "ipkv_paged_evict",
 ]
 
 
@@ -91,6 +92,12 @@ class Span(C.Structure):
     _fields_ = [("blocks_dev", C.c_void_p), ("first_token", C.c_int64), ("n_tokens", C.c_int64)]
 
 
+class Paged(C.Structure):
+    _fields_ = [("pool_dev", C.c_void_p), ("n_blocks", C.c_int64), ("table_dev", C.c_void_p), ("lengths_dev", C.c_void_p),
+                ("n_rows", C.c_int32), ("max_blocks", C.c_int32), ("table_stride", C.c_int64),
+                ("weights_dev", C.c_void_p), ("positions_dev", C.c_void_p), ("slot_stride", C.c_int64)]
+
+
 class Roofline(C.Structure):
     _fields_ = [("A", C.c_double), ("B", C.c_double), ("C_cpu", C.c_double), ("C_gpu", C.c_double)]
 
@@ -149,6 +156,11 @@ def lib():
         "ipkv_nibble_unpack": [C.POINTER(AttnShape), i32, vp, i64, vp, vp, i64, i64, vp],
         "ipkv_nibble_scratch_bytes": [C.POINTER(AttnShape), i32, i32, C.POINTER(C.c_size_t)],
         "ipkv_nibble_attend": [C.POINTER(AttnShape), i32, vp, vp, vp, vp, C.c_size_t, vp, vp, vp, vp],
+        "ipkv_paged_append": [C.POINTER(AttnShape), C.POINTER(Paged), i64, vp, vp, i64, i64, vp, vp, vp, vp],
+        "ipkv_paged_scratch_bytes": [C.POINTER(AttnShape), i32, i32, i32, i32, i32, C.POINTER(C.c_size_t)],
+        "ipkv_paged_attend": [C.POINTER(AttnShape), C.POINTER(Paged), vp, i64, i32, i32, vp, vp, C.c_size_t, vp, vp, vp, vp],
+        "ipkv_paged_evict_scratch_bytes": [C.POINTER(AttnShape), i32, i32, i32, C.POINTER(C.c_size_t)],
+        "ipkv_paged_evict": [C.POINTER(AttnShape), C.POINTER(Paged), i32, i32, i32, vp, vp, vp, vp, C.c_size_t, vp, vp],
         "ipkv_attend_runs_noalloc": [C.POINTER(AttnShape), i32, C.POINTER(Run), C.POINTER(i32), vp, i32, vp, vp, vp, vp],
     }
     L.ipkv_version.restype = C.c_char_p
@@ -755,3 +767,145 @@ def ipkv_nibble_attend(shape, runs, row_start, q, scratch, o_part, lse_part, sta
                                             o_part.data_ptr(), lse_part.data_ptr(), _ptr(status), _call_stream(stream, dev))
     if rc != OK:
         raise IpkvError(rc, "ipkv_nibble_attend")
+
+
+# ---- a paged cache of bounded length ----
+
+def make_paged(shape, pool, table, lengths, weights=None, positions=None):
+    """What the ipkv_paged_* calls work on: pool, contiguous, any type, a whole number of TILE blocks of `shape`; table int32 [rows, blocks a row
+    at most] (rows any stride apart), lengths int32 [rows]; weights float32 and positions int32 [rows, n_kv_heads, slots], contiguous, at least
+    table.shape[1] * block_tokens slots, a multiple of 4.  The object keeps the tensors; what they hold may change between calls, also under a captured graph."""
+    if _torch is None:
+        _modules()
+    dev, (block, per_row) = pool.get_device(), (ipkv_block_bytes(shape), table.shape[1] if table.dim() == 2 else 0)
+    if block <= 0 or not pool.is_contiguous() or pool.nbytes % block != 0 or pool.nbytes == 0:
+        raise ValueError(f"a pool is contiguous, a whole number of blocks of {block} bytes: got {pool.nbytes}")
+    if table.dtype is not _i32 or table.dim() != 2 or per_row < 1 or (per_row > 1 and table.stride(1) != 1) or table.get_device() != dev:
+        raise ValueError(f"a page table is int32 [rows, blocks] on the device of the pool: got {table.dtype} {tuple(table.shape)}")
+    rows = table.shape[0]
+    if lengths.dtype is not _i32 or lengths.shape != (rows,) or not lengths.is_contiguous() or lengths.get_device() != dev:
+        raise ValueError(f"lengths are contiguous int32 [{rows}] on the device of the pool: got {lengths.dtype} {tuple(lengths.shape)}")
+    stride = table.stride(0) if rows > 1 else per_row
+    if stride < per_row:
+        raise ValueError("the rows of a page table lie apart")
+    slots = 0
+    for x, dtype, name in ((weights, _f32, "weights"), (positions, _i32, "positions")):
+        if x is not None:
+            slots = slots or x.shape[-1]
+            if x.dtype is not dtype or x.shape != (rows, shape.n_kv_heads, slots) or not x.is_contiguous() or x.get_device() != dev:
+                raise ValueError(f"{name} are contiguous {dtype} [{rows}, {shape.n_kv_heads}, slots] on the device of the pool: got {x.dtype} {tuple(x.shape)}")
+    if slots and (slots < per_row * shape.block_tokens or slots % 4):
+        raise ValueError(f"{slots} slots: at least {per_row * shape.block_tokens}, a multiple of 4")
+    c = Paged(pool.data_ptr(), pool.nbytes // block, table.data_ptr(), lengths.data_ptr(), rows, per_row, stride, _ptr(weights), _ptr(positions), slots)
+    c._tensors, c._dev, c._slots = (pool, table, lengths, weights, positions), dev, (rows, shape.n_kv_heads, slots or per_row * shape.block_tokens)
+    c.slot_stride = c._slots[2]
+    return c
+
+
+def _slots_like(x, dtype, cache, name):
+    """An output shaped like the cache's weights and positions, as an address."""
+    if x is None:
+        return None
+    if x.dtype is not dtype or x.shape != cache._slots or not x.is_contiguous() or x.get_device() != cache._dev:
+        raise ValueError(f"{name} is contiguous {dtype} {cache._slots} on the device of the pool: got {x.dtype} {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _status_word(status, dev):
+    if status is None:
+        return None
+    if status.get_device() != dev or status.dtype not in (_i32, _torch.uint32):
+        raise ValueError("the status word (32 bits) is on the device of the pool")
+    return status.data_ptr()
+
+
+def _scratch(scratch, dev):
+    if scratch.get_device() != dev or not scratch.is_contiguous():
+        raise ValueError("scratch is contiguous, on the device of the pool")
+    return scratch.data_ptr(), scratch.nbytes
+
+
+def ipkv_paged_append(shape, cache, k, v, positions=None, row_start=None, status=None, stream=None):
+    """Write new tokens k and v [tokens, n_kv_heads, dim] bf16: one per row, or with row_start, int32 [rows + 1] on the device, the tokens
+    row_start[r] .. row_start[r + 1] to row r.  cache.lengths count them already.  positions: int32 [tokens]."""
+    heads, dim, size, dev, bf16 = shape.n_kv_heads, shape.dim_qk, k.shape, cache._dev, _bf16
+    n = size[0]
+    if k.dtype is not bf16 or v.dtype is not bf16 or len(size) != 3 or size[1] != heads or size[2] != dim or v.shape != size:
+        raise ValueError(f"K and V are bfloat16 [tokens, {heads}, {dim}]: got {k.dtype} {tuple(size)}, {v.dtype} {tuple(v.shape)}")
+    (kt, kh, kc), (vt, vh, vc) = k.stride(), v.stride()
+    if n <= 1:                                           # the stride of a dimension of one is never used
+        kt = vt = 0
+    elif kt == 0 or vt == 0:
+        kc = 0
+    if kc != 1 or vc != 1 or (heads > 1 and (kh != dim or vh != dim)) or k.get_device() != dev or v.get_device() != dev:
+        raise ValueError("the heads of a token lie side by side, its tokens apart, and K and V are on the device of the pool")
+    rs = at = None
+    if row_start is not None:
+        if row_start.dtype is not _i32 or row_start.shape != (cache.n_rows + 1,) or not row_start.is_contiguous() or row_start.get_device() != dev:
+            raise ValueError(f"row_start is contiguous int32 [{cache.n_rows + 1}] on the device of the pool")
+        rs = row_start.data_ptr()
+    elif n != cache.n_rows:
+        raise ValueError(f"{n} tokens for {cache.n_rows} rows: row_start says whose they are")
+    if positions is not None:
+        if positions.dtype is not _i32 or positions.numel() != n or not positions.is_contiguous() or positions.get_device() != dev:
+            raise ValueError(f"positions are contiguous int32 [{n}] on the device of the pool")
+        at = positions.data_ptr()
+    elif cache.positions_dev and n:
+        raise ValueError("the cache has positions: the new tokens need theirs")
+    rc = (_lib or lib()).ipkv_paged_append(C.byref(shape), C.byref(cache), n, k.data_ptr(), v.data_ptr(), kt, vt, rs, at, _status_word(status, dev),
+                                           _call_stream(stream, dev))
+    if rc != OK:
+        raise IpkvError(rc, "ipkv_paged_append")
+
+
+def ipkv_paged_scratch_bytes(shape, cache, window=0, first=0, weigh=False):
+    out = C.c_size_t()
+    rc = lib().ipkv_paged_scratch_bytes(C.byref(shape), cache.n_rows, cache.max_blocks, window, first, 1 if weigh else 0, C.byref(out))
+    if rc != OK:
+        raise IpkvError(rc, "ipkv_paged_scratch_bytes")
+    return out.value
+
+
+def ipkv_paged_attend(shape, cache, q, scratch, o_part, lse_part, window=0, first=0, weights_out=None, status=None, stream=None):
+    """Attention of one query per row, q [rows, n_q_heads, dim] bf16 (rows any stride apart), over the row's slots: all, or with a window the last `window` and the
+    `first` first ones.  weights_out: where the cache's weights go with this call's softmax weights added (may be the cache's own)."""
+    dev, f32, heads = cache._dev, _f32, shape.n_q_heads
+    want = (cache.n_rows, heads, shape.dim_qk)
+    if (q.dtype is not _bf16 or o_part.dtype is not f32 or lse_part.dtype is not f32 or q.shape != want or o_part.shape != want or lse_part.shape != want[:2]
+            or not (o_part.is_contiguous() and lse_part.is_contiguous()) or q.get_device() != dev or o_part.get_device() != dev or lse_part.get_device() != dev):
+        raise ValueError(f"q is bfloat16 {want}, o_part float32 {want} and lse_part float32 {want[:2]}, contiguous, on the device of the pool: got "
+                         + ", ".join(f"{x.dtype} {tuple(x.shape)} {x.device}" for x in (q, o_part, lse_part)))
+    qt, qh, qc = q.stride()
+    if qc != 1 or (heads > 1 and qh != want[2]):
+        raise ValueError("the heads of a query lie side by side")
+    if want[0] <= 1:
+        qt = 0
+    elif qt == 0:
+        raise ValueError("the queries of two rows lie apart")
+    at, size = _scratch(scratch, dev)
+    rc = (_lib or lib()).ipkv_paged_attend(C.byref(shape), C.byref(cache), q.data_ptr(), qt, window, first, _slots_like(weights_out, f32, cache, "weights_out"),
+                                           at, size, o_part.data_ptr(), lse_part.data_ptr(), _status_word(status, dev), _call_stream(stream, dev))
+    if rc != OK:
+        raise IpkvError(rc, "ipkv_paged_attend")
+
+
+def ipkv_paged_evict_scratch_bytes(shape, cache, budget):
+    out = C.c_size_t()
+    rc = lib().ipkv_paged_evict_scratch_bytes(C.byref(shape), cache.n_rows, cache.max_blocks, budget, C.byref(out))
+    if rc != OK:
+        raise IpkvError(rc, "ipkv_paged_evict_scratch_bytes")
+    return out.value
+
+
+def ipkv_paged_evict(shape, cache, budget, first, recent, scratch, weights_out=None, positions_out=None, kept=None, status=None, stream=None):
+    """Cut every row to at most `budget` slots per KV head: the `first` first and the `recent` most recent tokens stay, of the others
+    those with the largest weights.  cache.lengths stay as they are: the caller sets them to min(length, budget) after all layers."""
+    dev = cache._dev
+    if kept is not None and (kept.dtype is not _i32 or kept.shape != (cache.n_rows, shape.n_kv_heads, budget) or not kept.is_contiguous() or kept.get_device() != dev):
+        raise ValueError(f"kept is contiguous int32 {(cache.n_rows, shape.n_kv_heads, budget)} on the device of the pool")
+    at, size = _scratch(scratch, dev)
+    rc = (_lib or lib()).ipkv_paged_evict(C.byref(shape), C.byref(cache), budget, first, recent, _slots_like(weights_out, _f32, cache, "weights_out"),
+                                          _slots_like(positions_out, _i32, cache, "positions_out"), _ptr(kept), at, size, _status_word(status, dev),
+                                          _call_stream(stream, dev))
+    if rc != OK:
+        raise IpkvError(rc, "ipkv_paged_evict")
