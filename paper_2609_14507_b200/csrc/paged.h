@@ -37,119 +37,144 @@ struct PagedAppend {
 cudaError_t launch_paged_append(const PagedAppend& a, cudaStream_t s);
 
 // ---- attention (paged_attend.cu) -----------------------------------------------------------------------------------
-// What a query sees of a row's n slots, in tiles of 64: all of them, or the tiles of the first slots and those of the window.
+// Work is counted in units: 32 tokens of one KV head for 128 columns, 64 for 64, 16 KB either way.  One warp takes a unit at a time; with fewer
+// tokens to a warp (64 shared by four) the chain of a softmax step was as long and the products stood in a row behind it: 580
+// instructions for 16 tokens of 16 heads of 128 columns, 500K tokens 60 us.
+constexpr int kPagedUnitBytes = 16 * 1024;
+IPKV_HD int32_t paged_unit(int32_t dim) { return kPagedUnitBytes / (4 * dim); }
+// What a query sees of a row's n slots, in units: all of them, or the units of the first slots and those of the window.
 struct PagedSeen {
     int32_t n, first, lo;                        // slot t is visible if t < n and (t >= lo or t < first)
-    int32_t head, skip;                          // tiles of the first slots; invisible tiles behind them
-    int32_t tiles;
-    IPKV_HD int32_t tile(int32_t j) const { return j < head ? j : j + skip; }
+    int32_t head, skip;                          // units of the first slots; invisible units behind them
+    int32_t units;
+    IPKV_HD int32_t unit(int32_t j) const { return j < head ? j : j + skip; }
     IPKV_HD bool sees(int32_t t) const { return t < n && (t >= lo || t < first); }
     // any (all) of the slots a .. b - 1
     IPKV_HD bool sees_any(int32_t a, int32_t b) const { return a < n && ((b < n ? b : n) > lo || a < first); }
     IPKV_HD bool sees_all(int32_t a, int32_t b) const { return b <= n && (a >= lo || b <= first); }
 };
-IPKV_HD PagedSeen paged_seen(int32_t n, int32_t window, int32_t first) {
-    PagedSeen s{n, 0, 0, 0, 0, (n + kTileTokens - 1) / kTileTokens};
+IPKV_HD PagedSeen paged_seen(int32_t n, int32_t window, int32_t first, int32_t unit) {
+    PagedSeen s{n, 0, 0, 0, 0, (n + unit - 1) / unit};
     if (window > 0 && int64_t(window) + first < n) {
         s.first = first;
         s.lo = n - window;
-        const int32_t head = (first + kTileTokens - 1) / kTileTokens, from = s.lo / kTileTokens;
-        if (from > head) { s.head = head; s.skip = from - head; s.tiles -= s.skip; }
+        const int32_t head = (first + unit - 1) / unit, from = s.lo / unit;
+        if (from > head) { s.head = head; s.skip = from - head; s.units -= s.skip; }
     }
     return s;
 }
-// Tiles that a row of at most `capacity` slots can show.
-inline int64_t paged_most_tiles(int64_t capacity, int64_t window, int64_t first) {
-    const int64_t all = (capacity + kTileTokens - 1) / kTileTokens;
-    const int64_t seen = (first + kTileTokens - 1) / kTileTokens + window / kTileTokens + 2;
+// Units that a row of at most `capacity` slots can show.
+inline int64_t paged_most_units(int64_t capacity, int64_t window, int64_t first, int32_t unit) {
+    const int64_t all = (capacity + unit - 1) / unit;
+    const int64_t seen = (first + unit - 1) / unit + window / unit + 2;
     return window > 0 && seen < all ? seen : all;
 }
 
 // A pair is a row and a head group (a KV head and some of its query heads).  Lengths are on the device, so every CTA works the shares out
 // for itself, from the same numbers.  Two ways:
-//  - whole CTAs to every pair: ceil(tiles / share) of them, each an equal part of the pair's tiles, pair after pair;
-//  - equal chunks: work is counted in units, a pair's tiles and kPagedPairCost in front of them, pair after pair, and CTA c of n takes
-//    units [units c / n, units (c + 1) / n).
-// A part that holds all tiles of its pair is written out as the result; of the others a CTA has two at most, the chunk's first and last, and
-// leaves them at places 2 c and 2 c + 1.
-constexpr int kPagedPairCost = 2;                // queries read, the pipeline drained, a result written: as long as so many tiles
+//  - whole CTAs to every pair: ceil(units / share) of them, each an equal part of the pair's units, pair after pair;
+//  - equal chunks: a pair costs its units and kPagedPairCost in front of them, pair after pair, and every CTA takes an equal part of all cost.
+// A part that holds all units of its pair is written out as the result; of the others a CTA has two at most, the chunk's first and last, and
+// leaves them at places 2 c and 2 c + 1.  All counts of a launch fit 32 bits.
+constexpr int kPagedPairCost = 4;                // queries read, the pipeline drained, a result written: as long as so many units
 constexpr int kPagedRowsPerLaunch = 1024;        // the shares of so many rows are held in shared memory
-constexpr int kPagedCtasPerSm = 2;
-constexpr int kPagedSingleTiles = 4;             // tiles of a pair up to which one CTA takes it and no join follows
-struct PagedShare {
-    int32_t share;                               // tiles of a CTA at most; 0: chunks
-    int32_t units, ctas;                         // chunks: all units, and the CTAs that they are shared out to
-};
-IPKV_HD int32_t paged_units(int32_t tiles, const PagedShare& s) {
-    return s.share > 0 ? (tiles + s.share - 1) / s.share : tiles > 0 ? tiles + kPagedPairCost : 0;
+constexpr int kPagedCtasPerSm = 2, kPagedWarps = 4;
+// Where every pair has few units, which the host sees by the table's width or the window alone, a thread-block cluster takes it, joins
+// in distributed shared memory and adds the weights up: one launch in place of two or three.
+constexpr int kPagedMostCluster = 8;
+constexpr int kPagedClusterUnits = 16;           // units of a CTA up to which it wins
+inline int paged_cluster(int64_t pairs, int64_t most_units, int group, int ctas) {
+    if (group > 16 || pairs > ctas) return 0;            // (above, a KV head's heads are not in one CTA)
+    int n = 1;
+    while (n < kPagedMostCluster && pairs * n * 2 <= ctas && most_units > kPagedWarps * n) n *= 2;
+    return most_units <= int64_t(kPagedClusterUnits) * n ? n : 0;
 }
-IPKV_HD int32_t paged_chunk_begin(const PagedShare& s, int32_t c) { return int32_t(int64_t(s.units) * c / s.ctas); }
-// the last CTA whose chunk begins at or before a unit: the one that has it
-IPKV_HD int32_t paged_cta_of(const PagedShare& s, int32_t unit) { return int32_t(((int64_t(unit) + 1) * s.ctas - 1) / s.units); }
-// The share that whole CTAs to every pair would take is looked for among 32 values, from what `ctas` CTAs have to take of n_gh * tiles at least
-// up to twice that; chunks, if none of them gives every pair whole CTAs within `ctas`.
-IPKV_HD int32_t paged_share_tried(int64_t tiles, int32_t ctas, int32_t i) {
-    const int64_t least = tiles > 0 ? (tiles + ctas - 1) / ctas : 1;
-    return int32_t(least + (least * i + 30) / 31);
+struct PagedShare {
+    int32_t share;                               // units of a CTA at most; 0: chunks
+    int32_t cost, ctas;                          // chunks: of all pairs, and the CTAs that it is shared out to
+};
+IPKV_HD int32_t paged_cost(int32_t units, const PagedShare& s) {
+    return s.share > 0 ? (units + s.share - 1) / s.share : units > 0 ? units + kPagedPairCost : 0;
+}
+// Chunks: n things in `parts` equal parts, the first n % parts of them one larger (in 32 bits: the latency of a 64-bit division is half a microsecond).
+IPKV_HD int32_t paged_split(int32_t n, int32_t parts, int32_t i) {
+    const int32_t q = n / parts, r = n - q * parts;
+    return i * q + (i < r ? i : r);
+}
+// the part that has thing x of n >= parts
+IPKV_HD int32_t paged_part_of(int32_t n, int32_t parts, int32_t x) {
+    const int32_t q = n / parts, r = n - q * parts, large = r * (q + 1);
+    return x < large ? x / (q + 1) : r + (x - large) / q;
+}
+// The share that whole CTAs to every pair would take is looked for among 32 values, multiples of the teams that work in a CTA, from what `ctas`
+// CTAs have to take of all units at least up to twice that.  Chunks, if none of them gives every pair whole CTAs within `ctas`, or if the
+// share is more than a chunk by this much (rows of different lengths: 256 pairs of 80 to 129 units gave 120 units to a CTA, 93 in chunks).
+constexpr int kPagedUneven = 4;
+IPKV_HD int32_t paged_share_tried(int32_t units, int32_t ctas, int32_t teams, int32_t i) {
+    const int32_t least = units > 0 ? ((units - 1) / ctas + teams) / teams : 1;
+    return teams * (least + int32_t(uint32_t(least + 30) / 31u) * i);
+}
+IPKV_HD bool paged_share_wins(int32_t share, int32_t units, int32_t pairs, int32_t ctas) {
+    return share <= (units + pairs * kPagedPairCost) / ctas + kPagedUneven;
 }
 
-// A CTA's parts of pairs, one after the other.  cum[r]: units (with a share: parts) of a head group in the rows before r; n[r]: slots.
+// A CTA's parts of pairs, one after the other.  cum[r]: cost (with a share: parts) of a head group in the rows before r; n[r]: slots.
 struct PagedPart {
-    int32_t row, gh, t0, t1, place;
-    bool whole;                                  // all tiles of the pair
+    int32_t row, gh, u0, u1, place;
+    bool whole;                                  // all units of the pair
     PagedSeen seen;
 };
 struct PagedParts {
     const int32_t *cum, *n;
     PagedShare share;
-    int32_t n_rows, n_gh, window, first, cta;
-    int32_t u, u1;
-    // the row whose units hold unit u
-    IPKV_HD int32_t row_of(int32_t unit) const {
+    int32_t n_rows, n_gh, window, first, unit, cta;
+    int32_t at, end;
+    // the row whose cost holds x
+    IPKV_HD int32_t row_of(int32_t x) const {
         int32_t lo = 0, hi = n_rows - 1;
         while (lo < hi) {
             const int32_t mid = (lo + hi + 1) >> 1;
-            if (cum[mid] * n_gh <= unit) lo = mid; else hi = mid - 1;
+            if (cum[mid] * n_gh <= x) lo = mid; else hi = mid - 1;
         }
         return lo;
     }
-    // the part from unit u on of the pair (x.row, x.gh); u moves behind the pair
+    // the part from `at` on of the pair (x.row, x.gh); `at` moves behind the pair
     IPKV_HD void set(PagedPart& x, int32_t place) {
         const int32_t all = cum[x.row + 1] - cum[x.row], p0 = cum[x.row] * n_gh + x.gh * all;
-        const int32_t end = u1 - p0 < all ? u1 - p0 : all;
-        x.seen = paged_seen(n[x.row], window, first);
-        x.t0 = u - p0 > kPagedPairCost ? u - p0 - kPagedPairCost : 0;
-        x.t1 = end > kPagedPairCost ? end - kPagedPairCost : 0;
-        x.whole = x.t1 - x.t0 == x.seen.tiles;
+        const int32_t to = end - p0 < all ? end - p0 : all;
+        x.seen = paged_seen(n[x.row], window, first, unit);
+        x.u0 = at - p0 > kPagedPairCost ? at - p0 - kPagedPairCost : 0;
+        x.u1 = to > kPagedPairCost ? to - kPagedPairCost : 0;
+        x.whole = x.u1 - x.u0 == x.seen.units;
         x.place = place;
-        u = p0 + all;
+        at = p0 + all;
     }
     // false: no (more) part
     IPKV_HD bool begin(PagedPart& x) {
-        u = 0; u1 = 0;
+        at = 0; end = 0;
         if (share.share > 0) {
             if (cta >= cum[n_rows] * n_gh) return false;
             x.row = row_of(cta);
-            const int32_t parts = cum[x.row + 1] - cum[x.row], at = cta - cum[x.row] * n_gh, part = at % parts;
-            x.gh = at / parts;
-            x.seen = paged_seen(n[x.row], window, first);
-            x.t0 = int32_t(int64_t(x.seen.tiles) * part / parts);
-            x.t1 = int32_t(int64_t(x.seen.tiles) * (part + 1) / parts);
+            const int32_t parts = cum[x.row + 1] - cum[x.row], i = cta - cum[x.row] * n_gh, part = i % parts;
+            x.gh = i / parts;
+            x.seen = paged_seen(n[x.row], window, first, unit);
+            x.u0 = paged_split(x.seen.units, parts, part);
+            x.u1 = paged_split(x.seen.units, parts, part + 1);
             x.whole = parts == 1;
             x.place = 2 * cta;
             return true;
         }
         if (cta >= share.ctas) return false;
-        u = paged_chunk_begin(share, cta);
-        u1 = paged_chunk_begin(share, cta + 1);
-        if (u >= u1) return false;
-        x.row = row_of(u);
-        x.gh = (u - cum[x.row] * n_gh) / (cum[x.row + 1] - cum[x.row]);
+        at = paged_split(share.cost, share.ctas, cta);
+        end = paged_split(share.cost, share.ctas, cta + 1);
+        if (at >= end) return false;
+        x.row = row_of(at);
+        x.gh = (at - cum[x.row] * n_gh) / (cum[x.row + 1] - cum[x.row]);
         set(x, 2 * cta);
         return true;
     }
     IPKV_HD bool next(PagedPart& x) {
-        if (u >= u1) return false;
+        if (at >= end) return false;
         if (++x.gh == n_gh) {
             x.gh = 0;
             do ++x.row; while (cum[x.row + 1] == cum[x.row]);
@@ -158,18 +183,19 @@ struct PagedParts {
         return true;
     }
 };
-// The partials of a pair that has tiles: partial i of n is at place 2 (c0 + i), the first one at the next if it is not its CTA's first part.
+// The partials of a pair that has units: partial i of n is at place 2 (c0 + i), the first one at the next if it is not its CTA's first part.
 // One alone is no partial, but the result, written out.
 struct PagedPartials { int32_t c0, n, odd; };
 IPKV_HD PagedPartials paged_partials(const PagedShare& s, int32_t cum, int32_t all, int32_t n_gh, int32_t gh) {
     const int32_t first = cum * n_gh + gh * all;
     if (s.share > 0) return {first, all, 0};
-    const int32_t c0 = paged_cta_of(s, first + kPagedPairCost);
-    return {c0, paged_cta_of(s, first + all - 1) - c0 + 1, paged_chunk_begin(s, c0) < first};
+    const int32_t c0 = paged_part_of(s.cost, s.ctas, first + kPagedPairCost);
+    return {c0, paged_part_of(s.cost, s.ctas, first + all - 1) - c0 + 1, paged_split(s.cost, s.ctas, c0) < first};
 }
 
-// Head groups: a tile is read once for a head group.  Up to 16 query heads are the rows of one product (as one group of 4, 8 or 16 rows);
-// more make sixteens, as many to a group as divide both their number and the four computing warps.
+// Head groups: a unit is read once for a head group.  Up to 16 query heads are the rows of one product (as one group of 4, 8 or 16 rows);
+// more make sixteens, one to a warp: as many to a group as divide both their number and the four computing warps, which are then so
+// many teams fewer.
 inline int paged_rows(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
 inline int paged_sixteens(int group) {
     const int n = (group + 15) / 16;
@@ -180,7 +206,7 @@ inline int paged_rows_per_part(int group) { return paged_rows(group) * paged_six
 
 struct PagedHeader {                             // in front of the scratch, written by the attention for the join
     PagedShare share;
-    int32_t cum[kPagedRowsPerLaunch + 1];        // units (parts) of the rows before
+    int32_t cum[kPagedRowsPerLaunch + 1];        // see PagedParts
 };
 struct PagedAttend {
     PagedCache c;
@@ -190,15 +216,15 @@ struct PagedAttend {
     float* part_o;                               // [2 n_ctas][rows_per_part][dim]: sums of weight times value, not divided
     float2* part_ml;                             // [2 n_ctas][rows_per_part]: reference maximum (log2) and sum of weights against it
     float2* head_ml;                             // [n_rows][n_q_heads]: maximum and 1 / sum, for the weights; null without
-    float* scores;                               // [n_rows][n_gh][most_tiles][64 rows_per_part], null without weights
+    float* scores;                               // [n_rows][n_gh][most_units][unit * rows_per_part], null without weights
     float* weights_out;
     float* out_o;
     float* out_lse;
     uint32_t* status;
-    int32_t window, first, most_tiles;
+    int32_t window, first, unit, most_units;
     int32_t n_q_heads, group, groups_per_kv, n_gh, rows_per_part, sixteens;
     int32_t n_ctas;
-    int32_t single;                              // one CTA to every pair, which writes the result: no join
+    int32_t cluster;                             // CTAs that take a pair together and write its result; 0: shares, and a join
     float scale_log2;
 };
 cudaError_t launch_paged_attend(const PagedAttend& a, cudaStream_t s);

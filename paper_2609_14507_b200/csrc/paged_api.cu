@@ -61,21 +61,23 @@ bool apart(const ipkv_attn_shape* sh, const ipkv_paged* c, const void* in, const
 // Head groups of a row, rows of one launch and its scratch.
 struct AttendPlan {
     int group, groups_per_kv, n_gh, rows_per_part, sixteens;
-    int64_t most_tiles;
-    int32_t rows;                                // rows of a launch at most: shares held in shared memory, units in 32 bits
+    int32_t unit;
+    int64_t most_units;
+    int32_t rows;                                // rows of a launch at most: shares held in shared memory, costs in 32 bits
     size_t header, partials, head_ml, scores;
     AttendPlan(const ipkv_attn_shape* sh, int32_t n_rows, int32_t max_blocks, int32_t window, int32_t first, bool weigh)
         : group(sh->n_q_heads / sh->n_kv_heads), groups_per_kv(paged_groups_per_kv(group)), n_gh(sh->n_kv_heads * groups_per_kv),
           rows_per_part(paged_rows_per_part(group)), sixteens(paged_sixteens(group)),
-          most_tiles(paged_most_tiles(int64_t(max_blocks) * sh->block_tokens, window, first)) {
-        const int64_t fit = int64_t(INT32_MAX) / (n_gh * (most_tiles + kPagedPairCost));
+          unit(paged_unit(sh->dim_qk)),
+          most_units(paged_most_units(int64_t(max_blocks) * sh->block_tokens, window, first, unit)) {
+        const int64_t fit = int64_t(INT32_MAX) / (n_gh * (most_units + kPagedPairCost));
         const int64_t grid = int64_t(INT32_MAX) / 2 / sh->n_q_heads;      // the join's
         rows = int32_t(std::min<int64_t>(std::min<int64_t>(n_rows, kPagedRowsPerLaunch), std::min(fit, grid)));
         header = align_up(sizeof(PagedHeader), 256);
         const size_t parts = size_t(2) * kSmCount * kPagedCtasPerSm * rows_per_part;
         partials = align_up(parts * sh->dim_qk * sizeof(float), 256) + align_up(parts * sizeof(float2), 256);
         head_ml = weigh ? align_up(size_t(rows) * sh->n_q_heads * sizeof(float2), 256) : 0;
-        scores = weigh ? size_t(rows) * n_gh * size_t(most_tiles) * kTileTokens * rows_per_part * sizeof(float) : 0;
+        scores = weigh ? size_t(rows) * n_gh * size_t(most_units) * unit * rows_per_part * sizeof(float) : 0;
     }
     size_t scratch() const { return header + partials + head_ml + scores; }
 };
@@ -145,7 +147,7 @@ ipkv_status ipkv_paged_attend(const ipkv_attn_shape* sh, const ipkv_paged* c, co
     a.q_row = 2 * (q_row_stride ? q_row_stride : row);
     a.status = status_dev;
     a.window = window; a.first = window > 0 ? first_tokens : 0;
-    a.most_tiles = int32_t(plan.most_tiles);
+    a.unit = plan.unit; a.most_units = int32_t(plan.most_units);
     a.n_q_heads = sh->n_q_heads; a.group = plan.group; a.groups_per_kv = plan.groups_per_kv; a.n_gh = plan.n_gh;
     a.rows_per_part = plan.rows_per_part; a.sixteens = plan.sixteens;
     const float scale = sh->softmax_scale > 0.f ? sh->softmax_scale : 1.0f / std::sqrt(float(sh->dim_qk));
@@ -158,8 +160,8 @@ ipkv_status ipkv_paged_attend(const ipkv_attn_shape* sh, const ipkv_paged* c, co
         a.out_lse = lse_part_dev + int64_t(r0) * sh->n_q_heads;
         a.weights_out = weights_out_dev ? weights_out_dev + int64_t(r0) * sh->n_kv_heads * c->slot_stride : nullptr;
         const int64_t pairs = int64_t(n) * plan.n_gh, most = int64_t(kSmCount) * kPagedCtasPerSm;
-        a.single = pairs <= most && plan.most_tiles <= kPagedSingleTiles;
-        a.n_ctas = int32_t(a.single ? pairs : std::min(most, pairs * plan.most_tiles));
+        a.cluster = paged_cluster(pairs, plan.most_units, plan.group, int(most));
+        a.n_ctas = int32_t(a.cluster ? pairs * a.cluster : std::min(most, pairs * plan.most_units));
         if (launch_paged_attend(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return IPKV_ECUDA;
     }
     return IPKV_OK;

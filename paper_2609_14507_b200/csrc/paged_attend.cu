@@ -3,55 +3,55 @@
 //
 //   s_t = scale q . k_t,   O = sum_t p_t v_t,   p_t = 2^(s_t log2 e - m) / z,   LSE = m ln 2 + ln z      (t visible)
 //
-// Bound by the K/V bytes (4 dim per token and KV head for 4 dim flops and query head).  A producer warp brings tiles of 64 tokens of one
-// KV head (32 KB for 128 columns, contiguous in a page of 64 tokens or less: one bulk copy a page) into a ring of stages; four
-// warps compute, each on 16 tokens of every tile, with an online softmax of its own.  The query heads of a KV head are the rows of
+// Bound by the K/V bytes (4 dim per token and KV head for 4 dim flops and query head).  A producer warp brings units of one KV head (16 KB: 32 tokens
+// of 128 columns, 64 of 64) into a ring of stages; a page of a unit or less is one bulk copy, of larger ones a unit is one
+// a panel.  Four warps compute, each on a unit of its own with an online softmax of its own.  The query heads of a KV head are the rows of
 // the products (m16n8k16).  Page table and lengths are read here, so a captured call follows them.
 //
 // Exactness.  Products of bf16 are exact, sums fp32.  A softmax weight enters the second product as bf16 pieces that add up to
-// it, 24 bits in three pieces: with two (16 to 18 bits) the output was off by 2.4e-6 of itself, more than a computation in fp32 is.  Up to 4
+// it, 24 bits in three pieces: two (16 to 18 bits) would leave the output 2.4e-6 of itself off, more than a computation in fp32 does.  Up to 4
 // query heads per KV head the three share the 16 rows of one product (rows 0-3, 4-7, 8-11: the queries are in
-// rows 0-3 and 4-7, so that both have the weights); up to 8 two pieces share one and the third takes another; above, three.  A tile's
+// rows 0-3 and 4-7, so that both have the weights); up to 8 two pieces share one and the third takes another; above, three.  A unit's
 // sums start from zero and join the state by a rounded multiply-add: the tensor cores round towards zero, which would add up along a row.
 //
-// At the end of a pair the four warps' states are joined in the stage of the pair's last tile, which nobody reads any more, and
-// leave as the result, or as one partial for the join kernel.
+// At the end of a pair the warps' states are joined in the stages of their last units, which nobody reads any more, and
+// leave as the result, or as one partial for the join kernel.  Every wait is bounded.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <atomic>
-#include <cstddef>
 
 #include "kernels.h"
 #include "launch.cuh"
 #include "paged.h"
 #include "ptx.cuh"
 
+namespace cg = cooperative_groups;
+
 namespace ipkvi {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = (kWarps + 1) * 32;
+constexpr int kWarps = kPagedWarps, kThreads = (kWarps + 1) * 32;
 constexpr float kLn2 = 0.6931471805599453f;
 
-template <int D>
-struct Plan {
-    static constexpr int kStage = 64 * D * 4;    // K and V of 64 tokens
-    static constexpr int kStages = D == 128 ? 3 : 6;
-};
+constexpr int kStages = 6, kRing = kStages * kPagedUnitBytes;
 
 struct Smem {
-    uint64_t full[8], empty[8];
-    int32_t slices[8];                           // of a stage: bit i: tokens 16 i .. 16 i + 15 are there
-    float2 ml[2][kWarps * 16];                   // maximum and sum of every warp's rows; in turn, since a warp may be a part ahead of one that still reads
-    int32_t gave_up, scan[kThreads / 32 + 1];
-    int32_t tiles, pairs, fit[32];
+    uint64_t full[kStages], empty[kStages], met;
+    uint32_t tag[kStages];                       // of a stage: which unit of the CTA's (times 16); bit i: its tokens 16 i .. 16 i + 15 are there
+    float2 ml[kWarps * 16];                      // maximum and sum of every warp's rows
+    int32_t where[kWarps];                       // the stage that holds a warp's sums
+    int32_t scan[kThreads / 32];
+    int32_t units, pairs, fit[32];
     PagedShare share;
-    int32_t cum[kPagedRowsPerLaunch + 1], n[kPagedRowsPerLaunch];
+    float2 part_ml[16], head_ml[16];             // cluster: the CTA's partial and, in place of the arrays of rows, its sums; the pair's maxima and 1 / sum
+    alignas(16) int32_t cum[kPagedRowsPerLaunch + 1];
+    int32_t n[kPagedRowsPerLaunch];
 };
-// up to the arrays of rows
-inline size_t smem_bytes(int stage_bytes, int n_rows) {
-    return 1024 + size_t(stage_bytes) + offsetof(Smem, cum) + size_t(2 * kPagedRowsPerLaunch + 1) * 4 - size_t(kPagedRowsPerLaunch - n_rows) * 4;
-}
+static_assert(16 * 128 * 4 <= sizeof(int32_t) * (2 * kPagedRowsPerLaunch + 1), "a partial of 16 heads");
+// (a cluster's partial takes as much as all rows)
+inline size_t smem_bytes(int n_rows) { return 1024 + kRing + sizeof(Smem) - size_t(kPagedRowsPerLaunch - n_rows) * 4; }
 
 __device__ __forceinline__ void or_status(uint32_t* status, uint32_t bits) {
     if (status) atomicOr(status, bits);
@@ -65,135 +65,167 @@ __device__ __forceinline__ int length_of(const PagedAttend& p, int row, bool tel
     return n < 0 ? 0 : cap;
 }
 
-// Lengths, and from them the shares: see paged.h.  All threads of the CTA.
-__device__ void share_out(const PagedAttend& p, Smem& sm) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, R = p.c.n_rows;
-    int tiles = 0, rows = 0;
-    for (int r = tid; r < R; r += kThreads) {
-        const int n = length_of(p, r, blockIdx.x == 0);
-        const int t = paged_seen(n, p.window, p.first).tiles;
-        sm.n[r] = n;
-        sm.cum[r] = t;
-        tiles += t; rows += t > 0;
-    }
-    if (tid < 32) sm.fit[tid] = 0;
-    for (int d = 16; d > 0; d >>= 1) {
-        tiles += __shfl_xor_sync(0xffffffffu, tiles, d);
-        rows += __shfl_xor_sync(0xffffffffu, rows, d);
-    }
-    if (lane == 0) { atomicAdd(&sm.tiles, tiles); atomicAdd(&sm.pairs, rows * p.n_gh); }
-    __syncthreads();
-    // the fewest tiles a CTA with which whole CTAs to every pair stay within the grid
-    const int mine = paged_share_tried(int64_t(sm.tiles) * p.n_gh, p.n_ctas, lane);
-    const bool few = sm.pairs <= p.n_ctas;
-    if (few) {
-        int parts = 0;
-        for (int r = warp; r < R; r += kThreads / 32) parts += (sm.cum[r] + mine - 1) / mine;
-        atomicAdd(&sm.fit[lane], parts);
-    }
-    __syncthreads();
-    if (warp == 0) {
-        const unsigned fits = __ballot_sync(0xffffffffu, few && int64_t(sm.fit[lane]) * p.n_gh <= p.n_ctas);
-        const int which = __ffs(int(fits)) - 1;
-        const int best = __shfl_sync(0xffffffffu, mine, which < 0 ? 0 : which);
-        if (lane == 0) {
-            sm.share.share = which < 0 ? 0 : best;
-            sm.share.ctas = 0; sm.share.units = 0;
+// A team must not take another team's older unit in a stage for its own: the stage's barrier tells a lap from the next, but not from the one after
+// that, and copies land in any order.  So a computing warp first looks for its unit's number, which the producer leaves once the stage is
+// free, then waits for the copy.
+__device__ __forceinline__ void leave_tag(uint32_t* tag, uint32_t x) {
+    asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(ptx::smem_addr(tag)), "r"(x) : "memory");
+}
+__device__ __forceinline__ bool wait_tag(const uint32_t* tag, uint32_t unit, uint32_t& slices) {
+    uint64_t t0 = 0;
+    for (uint32_t n = 0;; ++n) {
+        uint32_t x;
+        asm volatile("ld.acquire.cta.shared::cta.u32 %0, [%1];" : "=r"(x) : "r"(ptx::smem_addr(tag)) : "memory");
+        slices = x & 15u;
+        if ((x >> 4) == (unit & 0x0fffffffu)) return true;
+        if ((n & 63u) == 0) {
+            const uint64_t now = ptx::globaltimer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > ptx::kWaitLimitNs) return false;
         }
     }
-    __syncthreads();
-    // prefix sums over the rows
-    int carry = 0;
-    for (int r0 = 0; r0 < R; r0 += kThreads) {
-        const int r = r0 + tid;
-        const int u = r < R ? paged_units(sm.cum[r], sm.share) : 0;
-        int x = u;
+}
+
+// Lengths, and from them the shares: see paged.h.  All threads of the CTA.
+__device__ PagedShare share_out(const PagedAttend& p, Smem& sm, int teams) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, R = p.c.n_rows;
+    PagedShare share{0, 0, 0};
+    // the first of the 32 shares with which whole CTAs to every pair stay within the grid
+    auto choose = [&](int mine, int parts, int units, int pairs) {
+        const unsigned fits = __ballot_sync(0xffffffffu, pairs <= p.n_ctas && int64_t(parts) * p.n_gh <= p.n_ctas);
+        const int share = fits == 0 ? 0 : __shfl_sync(0xffffffffu, mine, __ffs(int(fits)) - 1);
+        return paged_share_wins(share, units, pairs, p.n_ctas) ? share : 0;
+    };
+    auto scan = [&](int x) {
         for (int d = 1; d < 32; d <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, d);
             if (lane >= d) x += y;
         }
-        if (lane == 31) sm.scan[warp] = x;
-        __syncthreads();
-        int before = carry;
-        for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) before += sm.scan[w];
-            carry += sm.scan[w];
+        return x;
+    };
+    if (R <= 32) {                               // every warp for itself: all write the same
+        const int n = lane < R ? length_of(p, lane, tid < 32 && blockIdx.x == 0) : 0;
+        const int units = paged_seen(n, p.window, p.first, p.unit).units;
+        const int sum = __reduce_add_sync(0xffffffffu, unsigned(units)), pairs = __popc(__ballot_sync(0xffffffffu, units > 0)) * p.n_gh;
+        const int mine = paged_share_tried(sum * p.n_gh, p.n_ctas, teams, lane);
+        if (pairs <= p.n_ctas) {
+            int parts = 0;
+#pragma unroll 4
+            for (int r = 0; r < R; ++r) parts += (unsigned(__shfl_sync(0xffffffffu, units, r)) + unsigned(mine) - 1) / unsigned(mine);
+            share.share = choose(mine, parts, sum * p.n_gh, pairs);
         }
-        if (r < R) sm.cum[r] = before + x - u;
+        const int cost = paged_cost(units, share), upto = scan(cost);
+        if (lane < R) { sm.n[lane] = n; sm.cum[lane] = upto - cost; }
+        if (lane == 31) sm.cum[R] = upto;
+        __syncwarp();
+        if (share.share == 0) {
+            share.cost = sm.cum[R] * p.n_gh;
+            share.ctas = min(p.n_ctas, share.cost);
+        }
+    } else {
+        int units = 0, rows = 0;
+        for (int r = tid; r < R; r += kThreads) {
+            const int n = length_of(p, r, blockIdx.x == 0), u = paged_seen(n, p.window, p.first, p.unit).units;
+            sm.n[r] = n;
+            sm.cum[r] = u;
+            units += u; rows += u > 0;
+        }
+        if (tid < 32) sm.fit[tid] = 0;
+        units = int(__reduce_add_sync(0xffffffffu, unsigned(units)));
+        rows = int(__reduce_add_sync(0xffffffffu, unsigned(rows)));
+        if (lane == 0) { atomicAdd(&sm.units, units); atomicAdd(&sm.pairs, rows * p.n_gh); }
+        __syncthreads();
+        const int mine = paged_share_tried(sm.units * p.n_gh, p.n_ctas, teams, lane);
+        const bool few = sm.pairs <= p.n_ctas;
+        if (few) {
+            int parts = 0;
+#pragma unroll 4
+            for (int r = warp; r < R; r += kThreads / 32) parts += (unsigned(sm.cum[r]) + unsigned(mine) - 1) / unsigned(mine);
+            atomicAdd(&sm.fit[lane], parts);
+        }
+        __syncthreads();
+        share.share = choose(mine, sm.fit[lane], sm.units * p.n_gh, sm.pairs);
+        int carry = 0;                           // prefix sums over the rows
+        for (int r0 = 0; r0 < R; r0 += kThreads) {
+            const int r = r0 + tid, cost = r < R ? paged_cost(sm.cum[r], share) : 0, upto = scan(cost);
+            if (lane == 31) sm.scan[warp] = upto;
+            __syncthreads();
+            int before = carry;
+            for (int w = 0; w < kThreads / 32; ++w) {
+                if (w < warp) before += sm.scan[w];
+                carry += sm.scan[w];
+            }
+            if (r < R) sm.cum[r] = before + upto - cost;
+            __syncthreads();
+        }
+        if (tid == 0) sm.cum[R] = carry;
+        if (share.share == 0) {
+            share.cost = carry * p.n_gh;
+            share.ctas = min(p.n_ctas, share.cost);
+        }
         __syncthreads();
     }
-    if (tid == 0) {
-        sm.cum[R] = carry;
-        if (sm.share.share == 0) {
-            sm.share.units = carry * p.n_gh;
-            sm.share.ctas = min(p.n_ctas, sm.share.units);
-        }
+    if (blockIdx.x == 0 && warp == 0) {
+        for (int r = lane; r <= R; r += 32) p.header->cum[r] = sm.cum[r];
+        if (lane == 0) p.header->share = share;
     }
-    __syncthreads();
-    if (blockIdx.x == 0) {
-        for (int r = tid; r <= R; r += kThreads) p.header->cum[r] = sm.cum[r];
-        if (tid == 0) p.header->share = sm.share;
-    }
+    return share;
 }
 
 // ROWS: rows of the products that hold queries, see above.
 template <int D, int ROWS>
 __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel(const __grid_constant__ PagedAttend p) {
-    constexpr int kStage = Plan<D>::kStage, kStages = Plan<D>::kStages;
+    constexpr int U = kPagedUnitBytes / (4 * D), kSlices = U / 16;
     extern __shared__ unsigned char smem_dyn[];
     unsigned char* ring = smem_dyn + ((1024u - (ptx::smem_addr(smem_dyn) & 1023u)) & 1023u);      // 1024: rows of a panel on distinct banks
-    Smem& sm = *reinterpret_cast<Smem*>(ring + kStages * kStage);
+    Smem& sm = *reinterpret_cast<Smem*>(ring + kRing);
     const uint32_t s_ring = ptx::smem_addr(ring);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int sixteens = ROWS == 16 ? p.sixteens : 1, teams = kWarps / sixteens;
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             ptx::mbar_init(ptx::smem_addr(&sm.full[s]), 1);
-            ptx::mbar_init(ptx::smem_addr(&sm.empty[s]), kWarps);
+            ptx::mbar_init(ptx::smem_addr(&sm.empty[s]), sixteens);
+            sm.tag[s] = 0xffffffffu;
         }
+        ptx::mbar_init(ptx::smem_addr(&sm.met), kWarps);
         ptx::mbar_fence_init();
-        sm.gave_up = 0; sm.tiles = 0; sm.pairs = 0;
+        sm.units = 0; sm.pairs = 0;
     }
     __syncthreads();
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    if (p.single) {
-        if (tid == 0) {
-            const int row = int(blockIdx.x) / p.n_gh;
-            sm.n[row] = length_of(p, row, int(blockIdx.x) == row * p.n_gh);
-        }
-        __syncthreads();
-    } else {
-        share_out(p, sm);
-    }
-    const int T = min(p.c.g.bt, kTileTokens);            // tokens of a page that a tile takes at once
     PagedPart x;
-    PagedParts parts{sm.cum, sm.n, sm.share, p.c.n_rows, p.n_gh, p.window, p.first, int(blockIdx.x), 0, 0};
+    PagedParts parts{sm.cum, sm.n, PagedShare{0, 0, 0}, p.c.n_rows, p.n_gh, p.window, p.first, U, int(blockIdx.x), 0, 0};
+    if (p.cluster == 0) parts.share = share_out(p, sm, teams);
     auto begin = [&]() {
-        if (!p.single) return parts.begin(x);
-        x.row = int(blockIdx.x) / p.n_gh; x.gh = int(blockIdx.x) - x.row * p.n_gh;
-        x.seen = paged_seen(sm.n[x.row], p.window, p.first);
-        x.t0 = 0; x.t1 = x.seen.tiles; x.whole = true; x.place = 0;
-        parts.u = parts.u1 = 0;
+        if (p.cluster == 0) return parts.begin(x);
+        const int pair = int(blockIdx.x) / p.cluster, rank = int(blockIdx.x) - pair * p.cluster;
+        x.row = pair / p.n_gh; x.gh = pair - x.row * p.n_gh;
+        x.seen = paged_seen(length_of(p, x.row, x.gh == 0 && rank == 0 && tid == 0), p.window, p.first, U);
+        x.u0 = paged_split(x.seen.units, p.cluster, rank); x.u1 = paged_split(x.seen.units, p.cluster, rank + 1);
+        x.whole = false; x.place = 0;
         return true;
     };
+    const int T = min(p.c.g.bt, U);              // tokens of a page that a unit takes at once
 
     if (warp == kWarps) {
         // ---------------- producer ----------------
         const uint64_t pol = ptx::l2_evict_first_policy();
-        const int per_tile = kTileTokens / T;            // pages of a tile
+        const int per_unit = U / T, batch = 32 / per_unit;       // pages of a unit; units whose pages the lanes look up at once
         const int64_t head_bytes = p.c.g.head_bytes(), block_bytes = p.c.g.block_bytes();
-        int it = 0;
+        const int64_t extent = kChecked && p.status ? p.c.n_blocks * block_bytes : 0;
+        int st = 0, lap = 0, it = 0;
         bool ok = true;
         for (bool more = begin(); more && ok; more = parts.next(x)) {
             const int32_t* table = p.c.table + int64_t(x.row) * p.c.table_stride;
             const char* head = p.c.pool + (x.gh / p.groups_per_kv) * head_bytes;
-            const int batch = 32 / per_tile;
-            // lane l: the page of tile l / per_tile of a batch, its part l % per_tile; -1: nothing of it is seen, -2: a bad one
+            // lane l: the page of unit j + l / per_unit, its part l % per_unit; -1: nothing of it is seen, -2: a bad one
             auto page_of = [&](int j) {
-                const int tile = j + lane / per_tile;
+                const int u = j + lane / per_unit;
                 int page = -1;
-                if (tile < x.t1) {
-                    const int a = x.seen.tile(tile) * kTileTokens + (lane % per_tile) * T;
+                if (u < x.u1) {
+                    const int a = x.seen.unit(u) * U + (lane % per_unit) * T;
                     if (x.seen.sees_any(a, a + T)) {
                         page = table[a / p.c.g.bt];
                         if (page < 0 || page >= p.c.n_blocks) { or_status(p.status, kStatusBadPage); page = -2; }
@@ -201,43 +233,42 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 }
                 return page;
             };
-            int page = page_of(x.t0);
-            for (int j0 = x.t0; j0 < x.t1 && ok; j0 += batch) {
+            int page = page_of(x.u0);
+            for (int j0 = x.u0; j0 < x.u1 && ok; j0 += batch) {
                 const int pages = page;
-                if (j0 + batch < x.t1) page = page_of(j0 + batch);
-                for (int j = j0; j < min(j0 + batch, x.t1) && ok; ++j, ++it) {
-                    const int st = it % kStages;
-                    if (it >= kStages) ok = ptx::mbar_wait(ptx::smem_addr(&sm.empty[st]), ((it / kStages) - 1) & 1);
+                if (j0 + batch < x.u1) page = page_of(j0 + batch);
+                for (int j = j0; j < min(j0 + batch, x.u1); ++j) {
+                    if (lap > 0) ok = ptx::mbar_wait(ptx::smem_addr(&sm.empty[st]), (lap - 1) & 1);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    // the lanes that hold this tile's pages issue their copies
-                    const int sub = lane - (j - j0) * per_tile;
-                    const bool mine = sub >= 0 && sub < per_tile && pages >= 0;
-                    const unsigned there = __ballot_sync(0xffffffffu, mine) >> ((j - j0) * per_tile);
-                    const uint32_t bar = ptx::smem_addr(&sm.full[st]), dst = s_ring + st * kStage;
+                    const int lane0 = (j - j0) * per_unit;                  // the lane that holds the unit's first page
+                    const unsigned there = (__ballot_sync(0xffffffffu, pages >= 0) >> lane0) & ((1u << per_unit) - 1u);
+                    const uint32_t bar = ptx::smem_addr(&sm.full[st]), dst = s_ring + st * kPagedUnitBytes;
                     if (lane == 0) {
                         int slices = 0;
-                        for (int i = 0; i < 4; ++i) slices |= int((there >> (i * 16 / T)) & 1u) << i;
-                        sm.slices[st] = slices;
-                        ptx::mbar_expect_tx(bar, uint32_t(__popc(there & ((1u << per_tile) - 1u))) * T * D * 4);
+#pragma unroll
+                        for (int i = 0; i < kSlices; ++i) slices |= int((there >> (i * 16 / T)) & 1u) << i;
+                        leave_tag(&sm.tag[st], uint32_t(it) << 4 | uint32_t(slices));
+                        ptx::mbar_expect_tx(bar, uint32_t(__popc(there)) * T * D * 4);
                     }
                     __syncwarp();
-                    if (mine) {
-                        const char* src = head + int64_t(pages) * block_bytes;
-                        const int64_t extent = kChecked ? p.c.n_blocks * block_bytes : 0;
-                        if (p.c.g.bt <= kTileTokens) {
-                            ptx::bulk_g2s_hint(dst + sub * T * D * 4, ptx::checked_src<kChecked>(src, T * D * 4, p.c.pool, p.status ? extent : 0, p.status, kStatusBadIndex),
+                    if (p.c.g.bt <= U) {
+                        const int sub = lane - lane0;
+                        if (sub >= 0 && sub < per_unit && pages >= 0) {
+                            const char* src = head + int64_t(pages) * block_bytes;
+                            ptx::bulk_g2s_hint(dst + sub * T * D * 4, ptx::checked_src<kChecked>(src, T * D * 4, p.c.pool, extent, p.status, kStatusBadIndex),
                                                T * D * 4, bar, pol);
-                        } else {
-                            const int r0 = x.seen.tile(j) * kTileTokens % p.c.g.bt;
-#pragma unroll
-                            for (int i = 0; i < D / 32; ++i) {           // panels of K, then of V
-                                const char* from = src + (int64_t(i) * p.c.g.bt + r0) * 128;
-                                ptx::bulk_g2s_hint(dst + i * 8192, ptx::checked_src<kChecked>(from, 8192, p.c.pool, p.status ? extent : 0, p.status, kStatusBadIndex), 8192,
-                                                   bar, pol);
-                            }
+                        }
+                    } else {
+                        const int64_t at = __shfl_sync(0xffffffffu, pages, lane0);
+                        if (there && lane < D / 32) {            // a panel a lane, of K, then of V
+                            const char* src = head + at * block_bytes + (int64_t(lane) * p.c.g.bt + x.seen.unit(j) * U % p.c.g.bt) * 128;
+                            ptx::bulk_g2s_hint(dst + lane * (U * 128), ptx::checked_src<kChecked>(src, U * 128, p.c.pool, extent, p.status, kStatusBadIndex), U * 128,
+                                               bar, pol);
                         }
                     }
+                    ++it;
+                    if (++st == kStages) { st = 0; ++lap; }
                 }
             }
         }
@@ -250,39 +281,27 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     }
 
     // ---------------- computing warps ----------------
-    const int sixteens = ROWS == 16 ? p.sixteens : 1, hg = ROWS == 16 ? warp % sixteens : 0;      // which sixteen of the group's heads
+    const int team = warp / sixteens, hg = warp - team * sixteens;       // whose turn it is; which sixteen of the group's heads
     const int mi = lane >> 3, r8 = lane & 7;
     const int r0 = lane >> 2, c0 = 2 * (lane & 3);
-    // rows that lanes address for ldmatrix: K tokens (mi >> 1) * 8 + r8 of a slice of 16, V tokens (mi & 1) * 8 + r8
-    const uint32_t panel = uint32_t(T) * 128, v_off = uint32_t(T) * D * 2;
+    // offsets in a stage: panels, V, slices of 16 tokens (a page's K and V lie together)
+    const uint32_t panel = uint32_t(T) * 128, v_off = uint32_t(T) * D * 2, odd = T == 16 ? 16u * D * 4 : 2048u, pair = T >= 64 ? 4096u : 32u * D * 4;
     uint32_t qa[D / 16][4];
     float o[D / 8][4];
-    int it = 0, turn = 0;
+    int it0 = 0, meets = 0;                      // units of the parts before this one
     bool ok = true;
-
-    // The four warps.  The barrier has no limit of its own; the order of events bounds it: a warp comes here after a tile that the others wait
-    // for as well, each with a limit that began no earlier, and one that gave up has said so before that.
-    auto meet = [&]() -> bool {
+    auto meet = [&]() -> bool {                  // the four warps; they may wait for units of their own first
         __syncwarp();
-        if (*reinterpret_cast<volatile int32_t*>(&sm.gave_up)) return false;
-        asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-        return true;
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.met));
+        return ptx::mbar_wait(ptx::smem_addr(&sm.met), meets++ & 1, 2 * ptx::kWaitLimitNs);
     };
 
     for (bool more = begin(); more && ok; more = parts.next(x)) {
         const int kv = x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part;
         const int n_heads = min(p.rows_per_part, p.group - in_kv);       // of the part
         const int64_t item0 = int64_t(x.row) * p.n_q_heads + kv * p.group + in_kv;
-        if (x.t0 == x.t1) {
-            // an empty row (single), or a chunk that ends before the pair's first tile (nothing to leave)
-            if (x.whole)
-                for (int i = tid; i < n_heads * D; i += kWarps * 32) {
-                    p.out_o[item0 * D + i] = 0.f;
-                    if (i < n_heads) {
-                        p.out_lse[item0 + i] = -INFINITY;
-                        if (p.head_ml) p.head_ml[item0 + i] = make_float2(0.f, 0.f);
-                    }
-                }
+        if (x.u0 == x.u1) {                      // a chunk that ends before the pair's first unit, or a cluster's CTA without one
+            if (p.cluster > 0 && tid < 16) sm.part_ml[tid] = make_float2(-INFINITY, 0.f);
             continue;
         }
         {
@@ -301,97 +320,109 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
 #pragma unroll
         for (int nt = 0; nt < D / 8; ++nt) { o[nt][0] = o[nt][1] = o[nt][2] = o[nt][3] = 0.f; }
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-        float* scores = p.scores ? p.scores + (int64_t(x.row) * p.n_gh + x.gh) * p.most_tiles * (64 * p.rows_per_part) : nullptr;
+        float* scores = p.scores ? p.scores + (int64_t(x.row) * p.n_gh + x.gh) * p.most_units * (U * p.rows_per_part) + hg * (ROWS * 16) : nullptr;
+        const int n_units = x.u1 - x.u0;
+        int held = -1;                           // the stage of this warp's last unit
 
-        for (int j = x.t0; j < x.t1; ++j, ++it) {
-            const int st = it % kStages;
-            if (!ptx::mbar_wait(ptx::smem_addr(&sm.full[st]), (it / kStages) & 1)) {
-                *reinterpret_cast<volatile int32_t*>(&sm.gave_up) = 1;
+        for (int i = (team - it0 % teams + teams) % teams; i < n_units; i += teams) {
+            const int it = it0 + i, st = it % kStages, lap = it / kStages;
+            uint32_t there;
+            if (!wait_tag(&sm.tag[st], uint32_t(it), there) || !ptx::mbar_wait(ptx::smem_addr(&sm.full[st]), lap & 1)) {
                 ok = false;
                 break;
             }
-            const int slices = sm.slices[st], t_tile = x.seen.tile(j) * kTileTokens;
-            const uint32_t stage = s_ring + st * kStage;
-            bool wrote = false;
-            for (int sl = warp / sixteens; sl < 4; sl += kWarps / sixteens) {
-                const int ta = t_tile + sl * 16;
-                if (!x.seen.sees_any(ta, ta + 16)) continue;
-                float* to = scores ? scores + (int64_t(j) * 4 + sl) * (16 * p.rows_per_part) + hg * (ROWS * 16) : nullptr;
-                if (!((slices >> sl) & 1)) {     // its page was bad: no weight
-                    if (to)
-                        for (int i = lane; i < 16 * ROWS; i += 32) to[i] = -INFINITY;
-                    continue;
+            const int u = x.seen.unit(x.u0 + i), ta = u * U;
+            const uint32_t stage = s_ring + st * kPagedUnitBytes;
+            auto slice = [&](int sl) { return stage + (sl & 1) * odd + (sl >> 1) * pair; };
+            float s[2 * kSlices][4];
+#pragma unroll
+            for (int nt = 0; nt < 2 * kSlices; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const int chunk = ks * 2 + (mi & 1);             // K: matrices 0, 1 tokens 0-7 of a slice, 2, 3 tokens 8-15
+#pragma unroll
+                for (int sl = 0; sl < kSlices; ++sl) {
+                    uint32_t b0, b1, b2, b3;
+                    ptx::ldmatrix_x4(slice(sl) + ((mi >> 1) * 8 + r8) * 128 + (ks >= 4 ? panel : 0u) + (((chunk & 7) ^ r8) << 4), b0, b1, b2, b3);
+                    ptx::mma_bf16(s[2 * sl], qa[ks], b0, b1);
+                    ptx::mma_bf16(s[2 * sl + 1], qa[ks], b2, b3);
                 }
-                const uint32_t base = stage + uint32_t(sl * 16 / T) * (T * D * 4) + uint32_t(sl * 16 % T) * 128;
-                float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-                {
-                    const uint32_t kb = base + ((mi >> 1) * 8 + r8) * 128;
+            }
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks) {
-                        const int chunk = ks * 2 + (mi & 1);
-                        uint32_t b0, b1, b2, b3;
-                        ptx::ldmatrix_x4(kb + (ks >= 4 ? panel : 0u) + (((chunk & 7) ^ r8) << 4), b0, b1, b2, b3);
-                        ptx::mma_bf16(s[0], qa[ks], b0, b1);
-                        ptx::mma_bf16(s[1], qa[ks], b2, b3);
-                    }
+            for (int nt = 0; nt < 2 * kSlices; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[nt][e] *= p.scale_log2;
+            if (!x.seen.sees_all(ta, ta + U) || there != (1u << kSlices) - 1u) {
+                // Slots that are not seen, or whose page is bad, may hold anything: their scores are replaced, and their values by zeros (0 times a NaN
+                // is one).
+#pragma unroll
+                for (int nt = 0; nt < 2 * kSlices; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!x.seen.sees(ta + nt * 8 + c0 + (e & 1)) || !((there >> (nt / 2)) & 1)) s[nt][e] = -INFINITY;
+                for (int k = lane; k < U * (D / 8); k += 32) {
+                    const int t = k / (D / 8), chunk = k % (D / 8);
+                    if (!x.seen.sees(ta + t) || !((there >> (t / 16)) & 1))
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
+                                     ::"r"(slice(t / 16) + v_off + (chunk >> 3) * panel + (t % 16) * 128 + (chunk & 7) * 16), "r"(0) : "memory");
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // before the stage goes back to the copy engine
+                __syncwarp();
+            }
+            if (scores) {
+                float* to = scores + int64_t(x.u0 + i) * (U * p.rows_per_part);
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[nt][e] *= p.scale_log2;
-                if (!x.seen.sees_all(ta, ta + 16)) {
-                    // invisible slots may hold anything: their scores are replaced, and their values by zeros (0 times a NaN is one)
-#pragma unroll
-                    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (!x.seen.sees(ta + nt * 8 + c0 + (e & 1))) s[nt][e] = -INFINITY;
-                    for (int i = lane; i < 16 * (D / 8); i += 32) {
-                        const int t = i / (D / 8), chunk = i % (D / 8);
-                        if (!x.seen.sees(ta + t))
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + v_off + (chunk >> 3) * panel + t * 128 + (chunk & 7) * 16), "r"(0) : "memory");
-                    }
-                    wrote = true;
-                    __syncwarp();
+                for (int nt = 0; nt < 2 * kSlices; ++nt) {
+                    float* at = to + (nt / 2) * (16 * p.rows_per_part) + (nt & 1) * (ROWS * 8) + r0 * 8 + c0;
+                    if (ROWS > 4 || r0 < 4) *reinterpret_cast<float2*>(at) = make_float2(s[nt][0], s[nt][1]);
+                    if (ROWS == 16) *reinterpret_cast<float2*>(at + 64) = make_float2(s[nt][2], s[nt][3]);
                 }
-                if (to) {
+            }
+            // online softmax in the log2 domain; rows r0 and, with 16, r0 + 8
+            float a0, a1 = 0.f;
+            {
+                float mx0 = s[0][0], mx1 = s[0][2];
 #pragma unroll
-                    for (int nt = 0; nt < 2; ++nt) {
-                        if (ROWS > 4 || r0 < 4) *reinterpret_cast<float2*>(to + nt * (ROWS * 8) + r0 * 8 + c0) = make_float2(s[nt][0], s[nt][1]);
-                        if (ROWS == 16) *reinterpret_cast<float2*>(to + nt * (ROWS * 8) + (r0 + 8) * 8 + c0) = make_float2(s[nt][2], s[nt][3]);
-                    }
+                for (int nt = 0; nt < 2 * kSlices; ++nt) {
+                    mx0 = fmaxf(mx0, fmaxf(s[nt][0], s[nt][1]));
+                    if (ROWS == 16) mx1 = fmaxf(mx1, fmaxf(s[nt][2], s[nt][3]));
                 }
-                // online softmax in the log2 domain; rows r0 and, with 16, r0 + 8
-                float mx0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
                 mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
-                mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
-                const float mn0 = fmaxf(m0, mx0), ms0 = mn0 == -INFINITY ? 0.f : mn0;
-                const float a0 = ptx::ex2(m0 - ms0);
-                m0 = mn0;
-                float a1 = a0, ms1 = ms0;
+                if (ROWS == 16) mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
+                mx0 = fmaxf(m0, fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2)));
+                const float ms0 = mx0 == -INFINITY ? 0.f : mx0;
+                a0 = ptx::ex2(m0 - ms0);
+                m0 = mx0;
+                float ms1 = 0.f;
                 if (ROWS == 16) {
-                    float mx1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-                    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
-                    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
-                    const float mn1 = fmaxf(m1, mx1);
-                    ms1 = mn1 == -INFINITY ? 0.f : mn1;
+                    mx1 = fmaxf(m1, fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2)));
+                    ms1 = mx1 == -INFINITY ? 0.f : mx1;
                     a1 = ptx::ex2(m1 - ms1);
-                    m1 = mn1;
+                    m1 = mx1;
                 }
-                float pr[2][4];
+                float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
+                for (int nt = 0; nt < 2 * kSlices; ++nt) {
+                    s[nt][0] = ptx::ex2(s[nt][0] - ms0); s[nt][1] = ptx::ex2(s[nt][1] - ms0);
+                    sum0 += s[nt][0] + s[nt][1];
+                    if (ROWS == 16) {
+                        s[nt][2] = ptx::ex2(s[nt][2] - ms1); s[nt][3] = ptx::ex2(s[nt][3] - ms1);
+                        sum1 += s[nt][2] + s[nt][3];
+                    }
+                }
+                l0 = fmaf(l0, a0, sum0);
+                if (ROWS == 16) l1 = fmaf(l1, a1, sum1);
+            }
+            // the weights in three pieces, as operands: [0] and [2] are rows r0, [1] and [3] rows r0 + 8
+            constexpr int kProducts = ROWS == 16 ? 3 : ROWS == 8 ? 2 : 1;
+            uint32_t pa[kSlices][kProducts][4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) pr[nt][e] = (ROWS == 16 || e < 2) ? ptx::ex2(s[nt][e] - (e < 2 ? ms0 : ms1)) : 0.f;
-                l0 = l0 * a0 + ((pr[0][0] + pr[0][1]) + (pr[1][0] + pr[1][1]));
-                if (ROWS == 16) l1 = l1 * a1 + ((pr[0][2] + pr[0][3]) + (pr[1][2] + pr[1][3]));
-                // the weights in three pieces, as operands: [0] and [2] are rows r0, [1] and [3] rows r0 + 8
-                uint32_t pa[3][4];
+            for (int sl = 0; sl < kSlices; ++sl)
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
                     for (int h = 0; h < (ROWS == 16 ? 2 : 1); ++h) {
-                        float y0 = pr[nt][2 * h], y1 = pr[nt][2 * h + 1];
+                        float y0 = s[2 * sl + half][2 * h], y1 = s[2 * sl + half][2 * h + 1];
                         uint32_t piece[3];
 #pragma unroll
                         for (int k = 0; k < 3; ++k) {
@@ -400,60 +431,88 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                         }
                         if (ROWS == 16) {
 #pragma unroll
-                            for (int k = 0; k < 3; ++k) pa[k][2 * nt + h] = piece[k];
+                            for (int k = 0; k < 3; ++k) pa[sl][k % kProducts][2 * half + h] = piece[k];
                         } else if (ROWS == 8) {
-                            pa[0][2 * nt] = piece[0]; pa[0][2 * nt + 1] = piece[1];
-                            pa[1][2 * nt] = piece[2]; pa[1][2 * nt + 1] = 0u;
+                            pa[sl][0][2 * half] = piece[0]; pa[sl][0][2 * half + 1] = piece[1];
+                            pa[sl][1 % kProducts][2 * half] = piece[2]; pa[sl][1 % kProducts][2 * half + 1] = 0u;
                         } else {
-                            pa[0][2 * nt] = r0 < 4 ? piece[0] : piece[1];
-                            pa[0][2 * nt + 1] = r0 < 4 ? piece[2] : 0u;
+                            pa[sl][0][2 * half] = r0 < 4 ? piece[0] : piece[1];
+                            pa[sl][0][2 * half + 1] = r0 < 4 ? piece[2] : 0u;
                         }
                     }
-                }
-                const uint32_t vb = base + v_off + ((mi & 1) * 8 + r8) * 128;
 #pragma unroll
-                for (int jj = 0; jj < D / 16; ++jj) {
-                    const int chunk = 2 * jj + (mi >> 1);
-                    uint32_t b0, b1, b2, b3;
-                    ptx::ldmatrix_x4_trans(vb + (jj >= 4 ? panel : 0u) + (((chunk & 7) ^ r8) << 4), b0, b1, b2, b3);
-                    float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int jj = 0; jj < D / 16; ++jj) {
+                const int chunk = 2 * jj + (mi >> 1);            // V: matrices 0, 2 tokens 0-7 of a slice, 1, 3 tokens 8-15
+                uint32_t b[kSlices][4];
 #pragma unroll
-                    for (int k = (ROWS == 16 ? 3 : ROWS == 8 ? 2 : 1) - 1; k >= 0; --k) {        // the small pieces first
-                        ptx::mma_bf16(t0, pa[k], b0, b1);
-                        ptx::mma_bf16(t1, pa[k], b2, b3);
+                for (int sl = 0; sl < kSlices; ++sl)
+                    ptx::ldmatrix_x4_trans(slice(sl) + v_off + ((mi & 1) * 8 + r8) * 128 + (jj >= 4 ? panel : 0u) + (((chunk & 7) ^ r8) << 4), b[sl][0], b[sl][1], b[sl][2], b[sl][3]);
+                float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = kProducts - 1; k >= 0; --k)         // the small pieces first
+#pragma unroll
+                    for (int sl = 0; sl < kSlices; ++sl) {
+                        ptx::mma_bf16(t0, pa[sl][k], b[sl][0], b[sl][1]);
+                        ptx::mma_bf16(t1, pa[sl][k], b[sl][2], b[sl][3]);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        o[2 * jj][e] = fmaf(o[2 * jj][e], e < 2 ? a0 : a1, t0[e]);
-                        o[2 * jj + 1][e] = fmaf(o[2 * jj + 1][e], e < 2 ? a0 : a1, t1[e]);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const float a = ROWS < 16 || e < 2 ? a0 : a1;
+                    o[2 * jj][e] = fmaf(o[2 * jj][e], a, t0[e]);
+                    o[2 * jj + 1][e] = fmaf(o[2 * jj + 1][e], a, t1[e]);
                 }
             }
-            if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // before the stage goes back to the copy engine
             __syncwarp();
-            if (j + 1 < x.t1 && lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[st]));
+            if (i + teams < n_units) {
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[st]));
+            } else {
+                held = st;
+            }
         }
         if (!ok) break;
+        it0 += n_units;
 
-        // ---- the part's end: the warps' states meet in the last tile's stage ----
-        const int st = (it - 1) % kStages;
-        const uint32_t buf = s_ring + st * kStage;
-        float2* ml = sm.ml[turn];
-        turn ^= 1;
+        // ---- the part's end ----
         l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
         l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
         if (ROWS == 16) {
             l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
             l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
         }
-        if ((lane & 3) == 0 && r0 < ROWS) {
-            ml[warp * 16 + r0] = make_float2(m0, l0);
-            if (ROWS == 16) ml[warp * 16 + r0 + 8] = make_float2(m1, l1);
+        auto leave = [&](int head, float m, float z) {           // the part's maximum and sum; returns what the sums are divided by
+            if (x.whole) {
+                p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
+                if (p.head_ml) p.head_ml[item0 + head] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
+            } else if (p.cluster > 0) {
+                sm.part_ml[head] = make_float2(m, z);
+            } else {
+                p.part_ml[int64_t(x.place) * p.rows_per_part + head] = make_float2(m, z);
+            }
+        };
+        float* const out = x.whole ? p.out_o + item0 * D : p.cluster > 0 ? reinterpret_cast<float*>(sm.cum) : p.part_o + int64_t(x.place) * p.rows_per_part * D;
+        if (ROWS == 16 && teams == 1) {          // no two warps have the same head
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int head = hg * 16 + r0 + 8 * h;
+                const float m = h ? m1 : m0, z = h ? l1 : l0, f = !x.whole ? 1.f : z == 0.f ? 0.f : 1.f / z;
+                if (head < n_heads) {
+#pragma unroll
+                    for (int nt = 0; nt < D / 8; ++nt) *reinterpret_cast<float2*>(out + head * D + nt * 8 + c0) = make_float2(o[nt][2 * h] * f, o[nt][2 * h + 1] * f);
+                    if ((lane & 3) == 0) leave(head, m, z);
+                }
+            }
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[held]));
+            continue;
         }
-        if (!meet()) { ok = false; break; }      // every warp is done with the tile
-        {
+        if (sixteens > 1 && !meet()) { ok = false; break; }      // the warps of a team have read their unit
+        if ((lane & 3) == 0 && r0 < ROWS) {
+            sm.ml[warp * 16 + r0] = make_float2(m0, l0);
+            if (ROWS == 16) sm.ml[warp * 16 + r0 + 8] = make_float2(m1, l1);
+        }
+        if (held >= 0) {
+            if (lane == 0) sm.where[warp] = held;
             // pairs of columns are swapped by row, so that rows lie on distinct banks
-            const uint32_t to = buf + (warp * ROWS + r0) * (D * 4);
+            const uint32_t to = s_ring + held * kPagedUnitBytes + (hg * ROWS + r0) * (D * 4);
 #pragma unroll
             for (int nt = 0; nt < D / 8; ++nt) {
                 float y0 = o[nt][0], y1 = o[nt][1];
@@ -469,50 +528,97 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         }
         if (!meet()) { ok = false; break; }
         for (int i = tid; i < n_heads * (D / 4); i += kWarps * 32) {
-            const int head = i / (D / 4), col = i - head * (D / 4), w0 = ROWS == 16 ? head / 16 : 0, row = ROWS == 16 ? head % 16 : head;
+            const int head = i / (D / 4), col = i - head * (D / 4), g = ROWS == 16 ? head / 16 : 0, row = ROWS == 16 ? head % 16 : head;
             float m = -INFINITY, z = 0.f;
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = w0; w < kWarps; w += sixteens) m = fmaxf(m, ml[w * 16 + row].x);
-            for (int w = w0; w < kWarps; w += sixteens) {
-                const float2 y = ml[w * 16 + row];
+            for (int w = g; w < kWarps; w += sixteens) m = fmaxf(m, sm.ml[w * 16 + row].x);
+            for (int w = g; w < kWarps; w += sixteens) {
+                const float2 y = sm.ml[w * 16 + row];
                 if (y.y == 0.f) continue;        // nothing seen
                 const float f = ptx::ex2(y.x - (m == -INFINITY ? 0.f : m));
                 float4 v;
-                const uint32_t from = buf + (w * ROWS + row) * (D * 4) + (uint32_t(2 * col) ^ ((row & 7) << 2)) * 8;
+                const uint32_t from = s_ring + sm.where[w] * kPagedUnitBytes + (g * ROWS + row) * (D * 4) + (uint32_t(2 * col) ^ ((row & 7) << 2)) * 8;
                 asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(from) : "memory");
                 acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
                 z += f * y.y;
             }
-            if (x.whole) {
-                const float inv = z == 0.f ? 0.f : 1.f / z;
-                reinterpret_cast<float4*>(p.out_o + (item0 + head) * D)[col] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-                if (col == 0) {
-                    p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
-                    if (p.head_ml) p.head_ml[item0 + head] = make_float2(z == 0.f ? 0.f : m, inv);
-                }
-            } else {
-                const int64_t at = int64_t(x.place) * p.rows_per_part + head;
-                reinterpret_cast<float4*>(p.part_o + at * D)[col] = acc;
-                if (col == 0) p.part_ml[at] = make_float2(m, z);
-            }
+            const float f = !x.whole ? 1.f : z == 0.f ? 0.f : 1.f / z;
+            reinterpret_cast<float4*>(out + head * D)[col] = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+            if (col == 0) leave(head, m, z);
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[st]));
+        if (parts.at < parts.end) {              // the stages are needed again once all have read them
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            if (!meet()) { ok = false; break; }
+            if (held >= 0 && lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[held]));
+        }
     }
     if (!ok && lane == 0) or_status(p.status, kStatusNoTile);
+    if (p.cluster == 0) return;
+
+    // ---- a cluster: its CTAs' partials are joined, every CTA a share of the outputs (also after a wait that ran out: the others read here) ----
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    const int kv = x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part, n_heads = min(p.rows_per_part, p.group - in_kv);
+    const int64_t item0 = int64_t(x.row) * p.n_q_heads + kv * p.group + in_kv;
+    const int rank = int(cluster.block_rank());
+    auto state_of = [&](int head, float& m, float& z) {
+        m = -INFINITY; z = 0.f;
+        for (int c = 0; c < p.cluster; ++c) m = fmaxf(m, cluster.map_shared_rank(&sm.part_ml[head], c)->x);
+        for (int c = 0; c < p.cluster; ++c) {
+            const float2 y = *cluster.map_shared_rank(&sm.part_ml[head], c);
+            if (y.y != 0.f) z += ptx::ex2(y.x - (m == -INFINITY ? 0.f : m)) * y.y;
+        }
+    };
+    for (int i = rank * (kWarps * 32) + tid; i < n_heads * (D / 4); i += p.cluster * (kWarps * 32)) {
+        const int head = i / (D / 4), col = i - head * (D / 4);
+        float m, z;
+        state_of(head, m, z);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c = 0; c < p.cluster; ++c) {
+            const float2 y = *cluster.map_shared_rank(&sm.part_ml[head], c);
+            if (y.y == 0.f) continue;
+            const float f = ptx::ex2(y.x - (m == -INFINITY ? 0.f : m));
+            const float4 v = reinterpret_cast<const float4*>(cluster.map_shared_rank(sm.cum, c))[i];
+            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+        }
+        const float inv = z == 0.f ? 0.f : 1.f / z;
+        reinterpret_cast<float4*>(p.out_o + item0 * D)[i] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+        if (col == 0) p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
+    }
+    if (p.scores && tid < n_heads) {
+        float m, z;
+        state_of(tid, m, z);
+        sm.head_ml[tid] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
+    }
+    cluster.sync();                              // nobody reads another CTA's shared memory any more; the scores are written
+    if (!p.scores) return;
+    // the weights of this CTA's units (all heads of the KV head are in one group here)
+    const int64_t w0 = (int64_t(x.row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
+    const float* scores = p.scores + (int64_t(x.row) * p.n_gh + x.gh) * p.most_units * (U * ROWS);
+    for (int k = x.u0 * U + tid; k < x.u1 * U; k += kWarps * 32) {
+        const int t = x.seen.unit(k / U) * U + k % U;
+        if (!x.seen.sees(t)) continue;
+        const float before = p.c.weights ? p.c.weights[w0 + t] : 0.f;
+        const float* s = scores + int64_t(k >> 4) * (16 * ROWS) + ((k >> 3) & 1) * (ROWS * 8) + (k & 7);
+        float given = 0.f;
+#pragma unroll
+        for (int h = 0; h < ROWS; ++h)
+            if (h < n_heads && sm.head_ml[h].y != 0.f) given += ptx::ex2(s[h * 8] - sm.head_ml[h].x) * sm.head_ml[h].y;
+        p.weights_out[w0 + t] = before + given;
+    }
 }
 
 // Joins the partials of every (row, query head) whose pair more than one CTA had: with partial i's maximum m_i (log2), sum l_i and sums o_i,
 //   m = max m_i,  z = sum 2^(m_i - m) l_i,  O = sum 2^(m_i - m) o_i / z,  LSE = m ln 2 + ln z,   in a fixed order.
-// One CTA per (row, head): D / 4 column groups times slices of the partials.
-template <int D, int THREADS>
+// One CTA per (row, head, COLS columns): COLS / 4 column groups times slices of the partials.
+template <int D, int COLS, int THREADS>
 __global__ void __launch_bounds__(THREADS) paged_join_kernel(const __grid_constant__ PagedAttend p) {
-    constexpr int kCols = D / 4, kSlices = THREADS / kCols;
-    __shared__ float4 s_o[kSlices][kCols];
-    __shared__ float s_z[kSlices], s_m[THREADS / 32];
-    const int item = blockIdx.x, row = item / p.n_q_heads, head = item - row * p.n_q_heads;
-    const int tid = threadIdx.x, col = tid % kCols, slice = tid / kCols;
+    constexpr int kCols = COLS / 4, kSlices = THREADS / kCols, kSlabs = D / COLS;
+    __shared__ float4 s_o[THREADS / 32][kCols];
+    __shared__ float2 s_ml[THREADS / 32];
+    static_assert(kCols <= 32, "a warp has whole slices");
+    const int item = blockIdx.x / kSlabs, slab = blockIdx.x - item * kSlabs, row = item / p.n_q_heads, head = item - row * p.n_q_heads;
+    const int tid = threadIdx.x, slice = tid / kCols, col = slab * kCols + tid % kCols;
     const int kv = head / p.group, in_kv = head - kv * p.group, part_of = in_kv / p.rows_per_part, rin = in_kv - part_of * p.rows_per_part;
     const int gh = kv * p.groups_per_kv + part_of;
     ptx::grid_dependency_wait();
@@ -521,7 +627,7 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const __grid_consta
     const int u0 = p.header->cum[row], all = p.header->cum[row + 1] - u0;
     if (all == 0) {                              // nothing seen
         if (slice == 0) reinterpret_cast<float4*>(p.out_o + int64_t(item) * D)[col] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (tid == 0) {
+        if (tid == 0 && slab == 0) {
             p.out_lse[item] = -INFINITY;
             if (p.head_ml) p.head_ml[item] = make_float2(0.f, 0.f);
         }
@@ -531,63 +637,91 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const __grid_consta
     const int n = of.n;
     if (n == 1) return;                          // written by its CTA
     auto at = [&](int i) { return int64_t(2 * (of.c0 + i) + (i == 0 ? of.odd : 0)) * p.rows_per_part + rin; };
-    float m = -INFINITY;
-    for (int i = tid; i < n; i += THREADS) m = fmaxf(m, p.part_ml[at(i)].x);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    if ((tid & 31) == 0) s_m[tid >> 5] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) m = fmaxf(m, s_m[w]);
+    // every slice against its own maximum, then the slices
+    float m = -INFINITY, z = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float z = 0.f;
-#pragma unroll 4
-    for (int i = slice; i < n; i += kSlices) {
-        const float2 y = p.part_ml[at(i)];
-        const float4 v = reinterpret_cast<const float4*>(p.part_o + at(i) * D)[col];
-        if (y.y != 0.f) {                        // (a sum of NaN is not empty)
-            const float f = ptx::ex2(y.x - (m == -INFINITY ? 0.f : m));
-            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
-            z += f * y.y;
-        }
-    }
-    s_o[slice][col] = acc;
-    if (col == 0) s_z[slice] = z;
-    __syncthreads();
-    if (slice != 0) return;
+    constexpr int kAhead = 8;
+    for (int i0 = slice; i0 < n; i0 += kAhead * kSlices) {
+        float2 y[kAhead];
+        float4 v[kAhead];
 #pragma unroll
-    for (int k = 1; k < kSlices; ++k) {
-        const float4 v = s_o[k][col];
-        acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
-        z += s_z[k];
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = i0 + k * kSlices;
+            y[k] = make_float2(-INFINITY, 0.f);
+            if (i < n) {
+                y[k] = p.part_ml[at(i)];
+                v[k] = reinterpret_cast<const float4*>(p.part_o + at(i) * D)[col];
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) top = fmaxf(top, y[k].x);
+        const float base = top == -INFINITY ? 0.f : top, a = ptx::ex2(m - base);
+        acc.x *= a; acc.y *= a; acc.z *= a; acc.w *= a; z *= a;
+        m = top;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (y[k].y != 0.f) {                 // (a sum of NaN is not empty)
+                const float f = ptx::ex2(y[k].x - base);
+                acc.x += f * v[k].x; acc.y += f * v[k].y; acc.z += f * v[k].z; acc.w += f * v[k].w;
+                z += f * y[k].y;
+            }
+    }
+    // the slices of a warp, then the warps
+#pragma unroll
+    for (int d = kCols; d < 32; d <<= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, d), z2 = __shfl_xor_sync(0xffffffffu, z, d);
+        const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top, f = ptx::ex2(m - base), f2 = ptx::ex2(m2 - base);
+        acc.x = f * acc.x + f2 * __shfl_xor_sync(0xffffffffu, acc.x, d); acc.y = f * acc.y + f2 * __shfl_xor_sync(0xffffffffu, acc.y, d);
+        acc.z = f * acc.z + f2 * __shfl_xor_sync(0xffffffffu, acc.z, d); acc.w = f * acc.w + f2 * __shfl_xor_sync(0xffffffffu, acc.w, d);
+        z = f * z + f2 * z2;
+        m = top;
+    }
+    const int lane = tid & 31, warp = tid >> 5;
+    if (lane < kCols) s_o[warp][lane] = acc;
+    if (lane == 0) s_ml[warp] = make_float2(m, z);
+    __syncthreads();
+    if (tid >= kCols) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < THREADS / 32; ++k) top = fmaxf(top, s_ml[k].x);
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    z = 0.f;
+#pragma unroll
+    for (int k = 0; k < THREADS / 32; ++k) {
+        const float2 y = s_ml[k];
+        const float4 v = s_o[k][tid];
+        if (y.y == 0.f) continue;
+        const float f = ptx::ex2(y.x - (top == -INFINITY ? 0.f : top));
+        acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+        z += f * y.y;
     }
     const float inv = z == 0.f ? 0.f : 1.f / z;
     reinterpret_cast<float4*>(p.out_o + int64_t(item) * D)[col] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
     if (col == 0) {
-        p.out_lse[item] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
-        if (p.head_ml) p.head_ml[item] = make_float2(z == 0.f ? 0.f : m, inv);
+        p.out_lse[item] = z == 0.f ? -INFINITY : top * kLn2 + logf(z);
+        if (p.head_ml) p.head_ml[item] = make_float2(z == 0.f ? 0.f : top, inv);
     }
 }
 
 // weights_out[t] = weights[t] + sum over the KV head's query heads of 2^(s_t - m) / z, from the scores that the attention left.
-// One CTA for every splits-th group of four tiles of a (row, KV head); a thread per token.
+// One CTA for every splits-th 256 visible slots of a (row, KV head); a thread per slot.
 __global__ void __launch_bounds__(256) paged_weigh_kernel(const __grid_constant__ PagedAttend p, const int splits) {
     const int split = blockIdx.x % splits, pair = blockIdx.x / splits, kv = pair % p.c.g.n_kv_heads, row = pair / p.c.g.n_kv_heads;
-    const int tid = threadIdx.x, tok = tid & 63;
+    const int U = p.unit, per_cta = 256 / U, tok = int(threadIdx.x) % U;
     const int rows = p.rows_per_part / p.sixteens;       // of one product
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const int n = min(max(p.c.lengths[row], 0), p.c.max_blocks * p.c.g.bt);
-    const PagedSeen seen = paged_seen(n, p.window, p.first);
+    const PagedSeen seen = paged_seen(length_of(p, row, false), p.window, p.first, U);
     const float2* ml = p.head_ml + int64_t(row) * p.n_q_heads + kv * p.group;
     const int64_t w0 = (int64_t(row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
-    for (int j = split * 4 + (tid >> 6); j < seen.tiles; j += splits * 4) {
-        const int t = seen.tile(j) * kTileTokens + tok;
+    for (int j = split * per_cta + int(threadIdx.x) / U; j < seen.units; j += splits * per_cta) {
+        const int t = seen.unit(j) * U + tok;
         if (!seen.sees(t)) continue;
-        float sum = p.c.weights ? p.c.weights[w0 + t] : 0.f;
+        const float before = p.c.weights ? p.c.weights[w0 + t] : 0.f;
         float given = 0.f;
         for (int part = 0; part < p.groups_per_kv; ++part) {
-            const float* s = p.scores + ((int64_t(row) * p.n_gh + kv * p.groups_per_kv + part) * p.most_tiles + j) * (64 * p.rows_per_part) +
+            const float* s = p.scores + ((int64_t(row) * p.n_gh + kv * p.groups_per_kv + part) * p.most_units + j) * (U * p.rows_per_part) +
                              (tok >> 4) * (16 * p.rows_per_part) + ((tok >> 3) & 1) * (rows * 8) + (tok & 7);
             const int heads = min(p.rows_per_part, p.group - part * p.rows_per_part);
 #pragma unroll 8
@@ -597,7 +731,7 @@ __global__ void __launch_bounds__(256) paged_weigh_kernel(const __grid_constant_
                 if (y.y != 0.f) given += ptx::ex2(x - y.x) * y.y;
             }
         }
-        p.weights_out[w0 + t] = sum + given;
+        p.weights_out[w0 + t] = before + given;
     }
 }
 
@@ -607,13 +741,35 @@ cudaError_t launch(const PagedAttend& a, cudaStream_t s) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    constexpr int kRing = Plan<D>::kStage * Plan<D>::kStages;
     if (dev < 0 || dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(paged_attend_kernel<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes(kRing, kPagedRowsPerLaunch)));
+        e = cudaFuncSetAttribute(paged_attend_kernel<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes(kPagedRowsPerLaunch)));
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) configured[dev].store(true, std::memory_order_release);
     }
-    return launch_overlapped(paged_attend_kernel<D, ROWS>, a.n_ctas, kThreads, smem_bytes(kRing, a.c.n_rows), s, a);
+    if (a.cluster == 0) return launch_overlapped(paged_attend_kernel<D, ROWS>, a.n_ctas, kThreads, smem_bytes(a.c.n_rows), s, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(a.n_ctas));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem_bytes(kPagedRowsPerLaunch);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = overlap_launches() ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(a.cluster); attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, paged_attend_kernel<D, ROWS>, a);
+}
+
+// Many partials for every head (few pairs): slabs of 32 columns with many slices.
+constexpr int kManyPartials = 24;
+
+template <int D>
+cudaError_t launch_join(const PagedAttend& a, cudaStream_t s) {
+    const int items = a.c.n_rows * a.n_q_heads, pairs = a.c.n_rows * a.n_gh;
+    if (a.n_ctas > kManyPartials * pairs) return launch_overlapped(paged_join_kernel<D, 32, 256>, items * (D / 32), 256, size_t(0), s, a);
+    return launch_overlapped(paged_join_kernel<D, D, 128>, items, 128, size_t(0), s, a);
 }
 
 }  // namespace
@@ -625,14 +781,11 @@ cudaError_t launch_paged_attend(const PagedAttend& a, cudaStream_t s) {
                   : rows == 8 ? (wide ? launch<128, 8>(a, s) : launch<64, 8>(a, s))
                               : (wide ? launch<128, 16>(a, s) : launch<64, 16>(a, s));
     if (e != cudaSuccess) return e;
-    if (!a.single) {
-        const int items = a.c.n_rows * a.n_q_heads;
-        e = wide ? launch_overlapped(paged_join_kernel<128, 256>, items, 256, size_t(0), s, a)
-                 : launch_overlapped(paged_join_kernel<64, 256>, items, 256, size_t(0), s, a);
-        if (e != cudaSuccess) return e;
-    }
+    if (a.cluster > 0) return cudaSuccess;
+    e = wide ? launch_join<128>(a, s) : launch_join<64>(a, s);
+    if (e != cudaSuccess) return e;
     if (a.weights_out) {
-        const int64_t pairs = int64_t(a.c.n_rows) * a.c.g.n_kv_heads, groups = (a.most_tiles + 3) / 4;
+        const int64_t pairs = int64_t(a.c.n_rows) * a.c.g.n_kv_heads, groups = (int64_t(a.most_units) * a.unit + 255) / 256;
         const int64_t want = (148 * 8 + pairs - 1) / pairs;
         const int splits = int(want < groups ? want : groups);
         return launch_overlapped(paged_weigh_kernel, int(pairs * splits), 256, size_t(0), s, a, splits);
