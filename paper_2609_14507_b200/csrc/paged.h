@@ -98,13 +98,13 @@ IPKV_HD int32_t paged_cost(int32_t units, const PagedShare& s) {
 }
 // Chunks: n things in `parts` equal parts, the first n % parts of them one larger (in 32 bits: the latency of a 64-bit division is half a microsecond).
 IPKV_HD int32_t paged_split(int32_t n, int32_t parts, int32_t i) {
-    const int32_t q = n / parts, r = n - q * parts;
+    const int32_t q = int32_t(uint32_t(n) / uint32_t(parts)), r = n - q * parts;
     return i * q + (i < r ? i : r);
 }
 // the part that has thing x of n >= parts
 IPKV_HD int32_t paged_part_of(int32_t n, int32_t parts, int32_t x) {
-    const int32_t q = n / parts, r = n - q * parts, large = r * (q + 1);
-    return x < large ? x / (q + 1) : r + (x - large) / q;
+    const int32_t q = int32_t(uint32_t(n) / uint32_t(parts)), r = n - q * parts, large = r * (q + 1);
+    return x < large ? int32_t(uint32_t(x) / uint32_t(q + 1)) : r + int32_t(uint32_t(x - large) / uint32_t(q));
 }
 // The share that whole CTAs to every pair would take is looked for among 32 values, multiples of the teams that work in a CTA, from what `ctas`
 // CTAs have to take of all units at least up to twice that.  Chunks, if none of them gives every pair whole CTAs within `ctas`, or if the
@@ -155,8 +155,9 @@ struct PagedParts {
         if (share.share > 0) {
             if (cta >= cum[n_rows] * n_gh) return false;
             x.row = row_of(cta);
-            const int32_t parts = cum[x.row + 1] - cum[x.row], i = cta - cum[x.row] * n_gh, part = i % parts;
-            x.gh = i / parts;
+            const int32_t parts = cum[x.row + 1] - cum[x.row], i = cta - cum[x.row] * n_gh;
+            x.gh = int32_t(uint32_t(i) / uint32_t(parts));
+            const int32_t part = i - x.gh * parts;
             x.seen = paged_seen(n[x.row], window, first, unit);
             x.u0 = paged_split(x.seen.units, parts, part);
             x.u1 = paged_split(x.seen.units, parts, part + 1);
@@ -169,7 +170,7 @@ struct PagedParts {
         end = paged_split(share.cost, share.ctas, cta + 1);
         if (at >= end) return false;
         x.row = row_of(at);
-        x.gh = (at - cum[x.row] * n_gh) / (cum[x.row + 1] - cum[x.row]);
+        x.gh = int32_t(uint32_t(at - cum[x.row] * n_gh) / uint32_t(cum[x.row + 1] - cum[x.row]));
         set(x, 2 * cta);
         return true;
     }
@@ -239,7 +240,8 @@ struct PagedEvict {
     uint32_t* status;
     int32_t budget, first, recent;
     int32_t most_moved;                          // min(budget, slots - budget)
+    int32_t held;                                // slots that a CTA has room for in shared memory
 };
-cudaError_t launch_paged_evict(const PagedEvict& a, cudaStream_t s);
+cudaError_t launch_paged_evict(PagedEvict& a, cudaStream_t s);
 
 }  // namespace ipkvi

@@ -1,6 +1,8 @@
-// New tokens into the pages of a paged cache: one warp per token moves the K and V rows of all its KV heads, 16 bytes a lane, and sets
-// the slots' positions and weights.  Bound by the bytes (read once, written once) and, for a decode step, by the launch: the
-// loads of K and V go out before the table is looked up, so that one latency covers both.
+// New tokens into the pages of a paged cache.  A CTA takes some tokens: every thread asks for its 16-byte chunks of their K and V rows, a thread
+// per token finds the row, the slot and the page meanwhile (four dependent reads, and more for the search among the rows), then
+// the chunks are stored.  Bound by the bytes (read once, written once) and, for a decode step, by the launch and that chain of reads.
+// Measured: nine chunks of prompts, 20743 tokens of 4 KV heads of 128 columns, 85 MB: 23.5 us with one warp to a token and its reads one behind
+// the other.
 #include "launch.cuh"
 #include "paged.h"
 #include "ptx.cuh"
@@ -9,71 +11,83 @@ namespace ipkvi {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32, kAhead = 8;
+constexpr int kThreads = 256, kAhead = 8;        // chunks of a thread under way
+constexpr int kMostTokens = 32;                  // of a CTA
 
-__global__ void __launch_bounds__(kThreads) paged_append_kernel(const __grid_constant__ PagedAppend p) {
-    const int lane = threadIdx.x & 31;
-    const int64_t token = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+__global__ void __launch_bounds__(kThreads) paged_append_kernel(const __grid_constant__ PagedAppend p, const int per_cta) {
+    __shared__ int s_row[kMostTokens], s_slot[kMostTokens], s_page[kMostTokens];
+    const int tid = threadIdx.x;
+    const int64_t token0 = int64_t(blockIdx.x) * per_cta;
+    const int tokens = int(p.n_tokens - token0 < per_cta ? p.n_tokens - token0 : per_cta);
+    const BlockGeom g = p.c.g;
+    const int per_row = g.dim_qk / 8, per_plane = g.n_kv_heads * per_row;        // 16-byte chunks of a head's row, of a token's K
+    const int chunks = tokens * 2 * per_plane;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    if (token >= p.n_tokens) return;
-    const BlockGeom g = p.c.g;
-    const int per_row = g.dim_qk / 8, per_head = 2 * per_row, chunks = g.n_kv_heads * per_head;      // 16-byte chunks: K row, V row of a head
     auto load = [&](int c) {
-        const int head = c / per_head, i = c - head * per_head;
-        const char* src = i < per_row ? p.k + token * p.k_token : p.v + token * p.v_token;
-        return __ldg(reinterpret_cast<const uint4*>(src + (int64_t(head) * per_row + (i < per_row ? i : i - per_row)) * 16));
+        const int t = c / (2 * per_plane), i = c - t * (2 * per_plane);
+        const char* src = i < per_plane ? p.k + (token0 + t) * p.k_token + i * 16 : p.v + (token0 + t) * p.v_token + (i - per_plane) * 16;
+        return __ldg(reinterpret_cast<const uint4*>(src));
     };
     uint4 x[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-        if (lane + 32 * k < chunks) x[k] = load(lane + 32 * k);
-    // the token's row, and which of its new tokens it is
-    int row, behind;                             // behind: new tokens of the row from this one on
-    if (p.row_start) {
-        int lo = 0, hi = p.c.n_rows - 1;         // the last row that begins at or before the token
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (p.row_start[mid] <= token) lo = mid; else hi = mid - 1;
+        if (tid + kThreads * k < chunks) x[k] = load(tid + kThreads * k);
+    if (tid < tokens) {
+        const int64_t token = token0 + tid;
+        int row = int(token), page = -1;
+        int64_t slot = -1;
+        if (p.row_start) {
+            int lo = 0, hi = p.c.n_rows - 1;     // the last row that begins at or before the token
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (p.row_start[mid] <= token) lo = mid; else hi = mid - 1;
+            }
+            row = lo;
+            const int begin = p.row_start[row], end = p.row_start[row + 1];
+            if (token >= begin && token < end) slot = int64_t(p.c.lengths[row]) - (end - token);       // (else behind the last row's)
+        } else {
+            slot = int64_t(p.c.lengths[row]) - 1;
         }
-        row = lo;
-        if (token < p.row_start[row] || token >= p.row_start[row + 1]) return;       // behind the last row's
-        behind = int(p.row_start[row + 1] - token);
-    } else {
-        row = int(token);
-        behind = 1;
+        if (slot >= 0) {                         // (else not counted by the length)
+            if (slot < int64_t(p.c.max_blocks) * g.bt) page = p.c.table[row * p.c.table_stride + slot / g.bt];
+            if (page < 0 || page >= p.c.n_blocks) {
+                page = -1;
+                if (p.status) atomicOr(p.status, kStatusBadPage);
+            }
+        }
+        s_row[tid] = row; s_slot[tid] = int(slot); s_page[tid] = page;
     }
-    const int64_t slot = int64_t(p.c.lengths[row]) - behind;
-    if (slot < 0) return;                        // not counted by the length
-    int page = -1;
-    if (slot < int64_t(p.c.max_blocks) * g.bt) page = p.c.table[row * p.c.table_stride + slot / g.bt];
-    if (page < 0 || page >= p.c.n_blocks) {
-        if (lane == 0 && p.status) atomicOr(p.status, kStatusBadPage);
-        return;
-    }
-    const int t = int(slot % g.bt);
-    char* block = p.c.pool + page * g.block_bytes();
+    __syncthreads();
     auto store = [&](int c, const uint4& y) {
-        const int head = c / per_head, i = c - head * per_head;
-        char* plane = block + head * g.head_bytes() + (i < per_row ? 0 : g.k_plane_bytes());
-        *reinterpret_cast<uint4*>(plane + tile_chunk_offset(g.bt, t, i < per_row ? i : i - per_row)) = y;
+        const int t = c / (2 * per_plane), i = c - t * (2 * per_plane), page = s_page[t];
+        if (page < 0) return;
+        const bool v = i >= per_plane;
+        const int of = v ? i - per_plane : i, head = of / per_row;
+        char* plane = p.c.pool + page * g.block_bytes() + head * g.head_bytes() + (v ? g.k_plane_bytes() : 0);
+        *reinterpret_cast<uint4*>(plane + tile_chunk_offset(g.bt, s_slot[t] % g.bt, of - head * per_row)) = y;
     };
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-        if (lane + 32 * k < chunks) store(lane + 32 * k, x[k]);
-    for (int c = lane + 32 * kAhead; c < chunks; c += 32) store(c, load(c));
+        if (tid + kThreads * k < chunks) store(tid + kThreads * k, x[k]);
+    for (int c = tid + kThreads * kAhead; c < chunks; c += kThreads) store(c, load(c));
     if (p.c.weights || p.c.positions)
-        for (int head = lane; head < g.n_kv_heads; head += 32) {
-            const int64_t at = (int64_t(row) * g.n_kv_heads + head) * p.c.slot_stride + slot;
+        for (int c = tid; c < tokens * g.n_kv_heads; c += kThreads) {
+            const int t = c / g.n_kv_heads, head = c - t * g.n_kv_heads;
+            if (s_page[t] < 0) continue;
+            const int64_t at = (int64_t(s_row[t]) * g.n_kv_heads + head) * p.c.slot_stride + s_slot[t];
             if (p.c.weights) p.c.weights[at] = 0.f;
-            if (p.c.positions) p.c.positions[at] = p.token_positions[token];
+            if (p.c.positions) p.c.positions[at] = p.token_positions[token0 + t];
         }
 }
 
 }  // namespace
 
 cudaError_t launch_paged_append(const PagedAppend& a, cudaStream_t s) {
-    return launch_overlapped(paged_append_kernel, int((a.n_tokens + kWarps - 1) / kWarps), kThreads, size_t(0), s, a);
+    // as many tokens to a CTA as its threads have under way, fewer while there are SMs without work
+    const int64_t chunks = int64_t(a.c.g.n_kv_heads) * a.c.g.dim_qk / 4, full = kThreads * kAhead / chunks, spread = a.n_tokens / (4 * 148);
+    const int per_cta = int(full < 1 || spread < 1 ? 1 : full < spread ? (full < kMostTokens ? full : kMostTokens) : (spread < kMostTokens ? spread : kMostTokens));
+    return launch_overlapped(paged_append_kernel, int((a.n_tokens + per_cta - 1) / per_cta), kThreads, size_t(0), s, a, per_cta);
 }
 
 }  // namespace ipkvi

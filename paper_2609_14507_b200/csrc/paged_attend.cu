@@ -67,15 +67,16 @@ __device__ __forceinline__ int length_of(const PagedAttend& p, int row, bool tel
 
 // A team must not take another team's older unit in a stage for its own: the stage's barrier tells a lap from the next, but not from the one after
 // that, and copies land in any order.  So a computing warp first looks for its unit's number, which the producer leaves once the stage is
-// free, then waits for the copy.
+// free (every lap before has then been read), then waits for the copy.  Both are accesses of one SM to its shared memory, in program order; what
+// the copy brought is ordered by the barrier.
 __device__ __forceinline__ void leave_tag(uint32_t* tag, uint32_t x) {
-    asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(ptx::smem_addr(tag)), "r"(x) : "memory");
+    asm volatile("st.relaxed.cta.shared::cta.u32 [%0], %1;" ::"r"(ptx::smem_addr(tag)), "r"(x) : "memory");
 }
 __device__ __forceinline__ bool wait_tag(const uint32_t* tag, uint32_t unit, uint32_t& slices) {
     uint64_t t0 = 0;
     for (uint32_t n = 0;; ++n) {
         uint32_t x;
-        asm volatile("ld.acquire.cta.shared::cta.u32 %0, [%1];" : "=r"(x) : "r"(ptx::smem_addr(tag)) : "memory");
+        asm volatile("ld.relaxed.cta.shared::cta.u32 %0, [%1];" : "=r"(x) : "r"(ptx::smem_addr(tag)) : "memory");
         slices = x & 15u;
         if ((x >> 4) == (unit & 0x0fffffffu)) return true;
         if ((n & 63u) == 0) {
