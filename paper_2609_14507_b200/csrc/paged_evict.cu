@@ -27,17 +27,20 @@ namespace ipkvi {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kMostCtas = 8;
+constexpr int kMostCtas = 8;
 constexpr int kHeldSlots = 24 * 1024;            // of a CTA, 8 bytes each in shared memory; of more, keys are computed again where they are needed
 constexpr int kAtOnce = 8;                       // rows that a warp has under way
 
+template <int THREADS>
 struct Smem {
+    static constexpr int kWarps = THREADS / 32;
     uint64_t landed;
     unsigned long long least;
     uint32_t hist[2][256];
-    int32_t newest, digit, need, gave_up;
-    int32_t scan[kWarps];
+    int32_t newest, digit, need, ties, gave_up;
+    int32_t scan[8];
     int32_t count[3][kWarps];                    // of every warp: ties; kept slots behind the budget, evicted ones before it
+    int32_t total[2];                            // of the CTA, the latter two
 };
 
 // Larger is kept before smaller.  A NaN is less than every number.
@@ -47,19 +50,23 @@ __device__ __forceinline__ uint32_t key_of(float w) {
 }
 constexpr uint32_t kStays = 0xffffffffu;
 
-__global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_constant__ PagedEvict p, const int ctas) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(const __grid_constant__ PagedEvict p, const int ctas) {
+    constexpr int kWarps = THREADS / 32;
     extern __shared__ __align__(16) uint32_t held[];     // weights, then keys, of the CTA's slots; positions behind them
-    __shared__ Smem sm;
+    __shared__ Smem<THREADS> sm;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = int(cluster.block_rank()), pair = int(blockIdx.x) / ctas, H = p.c.g.n_kv_heads, row = pair / H, head = pair - row * H;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    auto meet = [&]() {                          // all CTAs of the cluster
+        if (ctas == 1) __syncthreads(); else cluster.sync();
+    };
     if (tid == 0) {
         ptx::mbar_init(ptx::smem_addr(&sm.landed), 1);
         ptx::mbar_fence_init();
         sm.newest = INT32_MIN; sm.least = ~0ull; sm.gave_up = 0;
     }
-    sm.hist[tid >> 8][tid & 255] = 0;
-    static_assert(kThreads == 512, "a thread clears one word of the histograms");
+    if (tid < 256) sm.hist[0][tid] = sm.hist[1][tid] = 0;
     __syncthreads();
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
@@ -76,13 +83,48 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
     int32_t* positions_out = p.positions_out + slots0;
     int32_t* kept = p.kept ? p.kept + int64_t(pair) * b : nullptr;
     const bool in_place = weights_out == weights && positions_out == positions;
-    // this warp's slots
-    const int per_cta = ((n + ctas - 1) / ctas + 31) & ~31, per_warp = (((per_cta + kWarps - 1) / kWarps) + 31) & ~31;
+    // this warp's slots, in groups of 128: four a lane
+    const int per_cta = ((n + ctas - 1) / ctas + 31) & ~31, per_warp = (((per_cta + kWarps - 1) / kWarps) + 127) & ~127;
     const int cta0 = min(n, rank * per_cta), cta1 = min(n, cta0 + per_cta);
     const int w0 = min(cta1, cta0 + warp * per_warp), w1 = min(cta1, w0 + per_warp);
-    if (n <= b && in_place && !kept) return;
+    auto stays_put = [&](int i) {                // a slot below the budget whose token stays where it is
+        if (weights_out != weights) weights_out[i] = weights[i];
+        if (positions_out != positions) positions_out[i] = positions[i];
+        if (kept) kept[i] = i;
+    };
+    if (n <= b) {                                // all stay: copied, four slots a lane, where they go to arrays of their own
+        if (in_place && !kept) return;
+        constexpr int kGroups = 4;
+        for (int i0 = w0 + 4 * lane; i0 - 4 * lane < w1; i0 += 128 * kGroups) {
+            float4 w[kGroups];
+            int4 at[kGroups];
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k)
+                if (i0 + 128 * k + 3 < w1) {
+                    w[k] = *reinterpret_cast<const float4*>(weights + i0 + 128 * k);
+                    at[k] = *reinterpret_cast<const int4*>(positions + i0 + 128 * k);
+                }
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) {
+                const int i = i0 + 128 * k;
+                if (i + 3 < w1) {
+                    if (weights_out != weights) *reinterpret_cast<float4*>(weights_out + i) = w[k];
+                    if (positions_out != positions) *reinterpret_cast<int4*>(positions_out + i) = at[k];
+                } else {
+                    for (int e = i; e < w1; ++e) {
+                        if (weights_out != weights) weights_out[e] = weights[e];
+                        if (positions_out != positions) positions_out[e] = positions[e];
+                    }
+                }
+            }
+        }
+        if (kept)
+            for (int i = w0 + lane; i < w1; i += 32) kept[i] = i;
+        return;
+    }
+
+    // ---- keys ----
     const bool holds = per_cta <= kHeldSlots;
-    const float* w_held = reinterpret_cast<const float*>(held);
     const int32_t* p_held = reinterpret_cast<const int32_t*>(held) + p.held;
     if (holds && cta1 > cta0) {
         const uint32_t bytes = uint32_t(cta1 - cta0 + 3) / 4 * 16;      // (whole 16 bytes: the slots behind n are there, the stride is a multiple of four)
@@ -94,67 +136,76 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
         }
         if (!ptx::mbar_wait(ptx::smem_addr(&sm.landed), 0)) sm.gave_up = 1;
     }
-    const bool lost = __syncthreads_or(sm.gave_up);      // nothing is evicted then; the CTAs of the cluster hear of it below
-    if (lost && tid == 0) {
+    if (__syncthreads_or(sm.gave_up) && tid == 0) {      // nothing is evicted then; the CTAs of the cluster hear of it below
         if (p.status) atomicOr(p.status, kStatusNoTile);
         if (!ptx::mbar_wait(ptx::smem_addr(&sm.landed), 0) && p.status) atomicOr(p.status, kStatusCopyNotLanded);
     }
-    auto weight = [&](int i) { return holds ? w_held[i - cta0] : weights[i]; };
-    auto position = [&](int i) { return holds ? p_held[i - cta0] : positions[i]; };
-    if (n <= b) {
-        if (lost) return;
-        for (int i = w0 + lane; i < w1; i += 32) {
-            if (weights_out != weights) weights_out[i] = weight(i);
-            if (positions_out != positions) positions_out[i] = position(i);
-            if (kept) kept[i] = i;
-        }
-        return;
-    }
-
-    // ---- keys ----
     int newest = INT32_MIN;
-    for (int i = w0 + lane; i < w1; i += 32) newest = max(newest, position(i));
+    for (int i = w0 + 4 * lane; i < w1; i += 128) {
+        const int4 x = holds ? *reinterpret_cast<const int4*>(p_held + (i - cta0)) : *reinterpret_cast<const int4*>(positions + i);
+        newest = max(newest, x.x);
+        if (i + 1 < w1) newest = max(newest, x.y);
+        if (i + 2 < w1) newest = max(newest, x.z);
+        if (i + 3 < w1) newest = max(newest, x.w);
+    }
     newest = __reduce_max_sync(0xffffffffu, newest);
     if (lane == 0) atomicMax(&sm.newest, newest);
-    cluster.sync();
-    bool gave_up = false;
-    for (int r = 0; r < ctas; ++r) {
-        newest = max(newest, *cluster.map_shared_rank(&sm.newest, r));
-        gave_up |= *cluster.map_shared_rank(&sm.gave_up, r) != 0;
+    meet();
+    // (reads of other CTAs' shared memory are issued together here and below: one behind the other they took most of the time)
+    int others = 0;
+    if (lane < ctas) {
+        newest = *cluster.map_shared_rank(&sm.newest, lane);
+        others = *cluster.map_shared_rank(&sm.gave_up, lane);
+    }
+    newest = __reduce_max_sync(0xffffffffu, newest);
+    if (__any_sync(0xffffffffu, others != 0)) {
+        meet();                                  // (the others read this CTA's shared memory until here)
+        return;
     }
     const int64_t old = int64_t(newest) - p.recent;      // positions up to here are not recent
-    auto key = [&](int i) {
-        const int at = position(i);
-        return at < p.first || at > old ? kStays : key_of(weight(i));
+    // the keys of slots i .. i + 3 from weights and positions
+    auto make_keys = [&](int i) {
+        const float4 w = holds ? *reinterpret_cast<const float4*>(held + (i - cta0)) : *reinterpret_cast<const float4*>(weights + i);
+        const int4 at = holds ? *reinterpret_cast<const int4*>(p_held + (i - cta0)) : *reinterpret_cast<const int4*>(positions + i);
+        auto one = [&](float w, int at) { return at < p.first || at > old ? kStays : key_of(w); };
+        return make_uint4(one(w.x, at.x), one(w.y, at.y), one(w.z, at.z), one(w.w, at.w));
     };
-    // a slot below the budget whose token stays where it is
-    auto stays_put = [&](int i) {
-        if (weights_out != weights) weights_out[i] = weight(i);
-        if (positions_out != positions) positions_out[i] = position(i);
-        if (kept) kept[i] = i;
+    // calls f(i, keys) for all groups of the warp, i the lane's first slot; keys[e] counts if i + e < w1
+    auto for_groups = [&](auto&& f) {
+        for (int i = w0 + 4 * lane; i - 4 * lane < w1; i += 128) {
+            uint4 k = make_uint4(0u, 0u, 0u, 0u);
+            if (i < w1) k = holds ? *reinterpret_cast<const uint4*>(held + (i - cta0)) : make_keys(i);
+            const uint32_t keys[4] = {k.x, k.y, k.z, k.w};
+            f(i, keys);
+        }
     };
+    if (holds && n != b + 1)
+        for (int i = w0 + 4 * lane; i < w1; i += 128) *reinterpret_cast<uint4*>(held + (i - cta0)) = make_keys(i);
+
     const BlockGeom g = p.c.g;
     const int32_t* table = p.c.table + row * p.c.table_stride;
     const int per_row = g.dim_qk / 8, chunks = 2 * per_row;
     const int chunk = lane < per_row ? lane : lane - per_row;
-    const int64_t in_block = head * g.head_bytes() + (lane < per_row ? 0 : g.k_plane_bytes());      // of this lane's plane
-    auto page_of = [&](int slot) {
-        const int page = table[slot / g.bt];
-        return page >= 0 && page < p.c.n_blocks ? page : -1;
+    // of this lane's chunk in a block, apart from the slot's row and the swizzle
+    char* const lane_at = p.c.pool + head * g.head_bytes() + (lane < per_row ? 0 : g.k_plane_bytes()) + (chunk >> 3) * int64_t(g.bt) * 128;
+    // where a slot's row begins, from the pool on; -1: its page is bad
+    auto row_at = [&](int slot) {
+        const int j = slot / g.bt, page = table[j];
+        return page >= 0 && page < p.c.n_blocks ? page * g.block_bytes() + (slot - j * g.bt) * 128 : int64_t(-1);
     };
-    auto place = [&](int page, int slot) { return p.c.pool + page * g.block_bytes() + in_block + tile_chunk_offset(g.bt, slot % g.bt, chunk); };
-
-    if (gave_up) {
-        cluster.sync();                          // (the others read this CTA's shared memory until here)
-        return;
-    }
+    auto swizzle = [&](int slot) { return ((chunk & 7) ^ (slot & 7)) << 4; };
 
     // ---- one slot goes ----
     if (n == b + 1) {
         unsigned long long least = ~0ull;        // key, then the slot, the last one first
-        for (int i = w0 + lane; i < w1; i += 32) {
-            const unsigned long long x = (static_cast<unsigned long long>(key(i)) << 32) | uint32_t(~i);
-            least = x < least ? x : least;
+        for (int i = w0 + 4 * lane; i < w1; i += 128) {
+            const uint4 k = make_keys(i);
+            const uint32_t keys[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned long long x = (static_cast<unsigned long long>(keys[e]) << 32) | uint32_t(~(i + e));
+                if (i + e < w1 && x < least) least = x;
+            }
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) {
@@ -162,26 +213,31 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
             least = x < least ? x : least;
         }
         if (lane == 0) atomicMin(&sm.least, least);
-        cluster.sync();
-        least = ~0ull;
-        for (int r = 0; r < ctas; ++r) {
-            const unsigned long long x = *cluster.map_shared_rank(&sm.least, r);
+        meet();
+        least = lane < ctas ? *cluster.map_shared_rank(&sm.least, lane) : ~0ull;
+#pragma unroll
+        for (int d = kMostCtas / 2; d > 0; d >>= 1) {
+            const unsigned long long x = __shfl_xor_sync(0xffffffffu, least, d);
             least = x < least ? x : least;
         }
-        const int gone = int(~uint32_t(least));
+        const int gone = int(~uint32_t(__shfl_sync(0xffffffffu, least, 0)));
         if (!in_place || kept)
             for (int i = w0 + lane; i < w1; i += 32)
-                if (i < b && i != gone) stays_put(i);
-        cluster.sync();                          // nobody reads another CTA's shared memory any more
+                if (i < b && i != gone) {
+                    if (weights_out != weights) weights_out[i] = holds ? __uint_as_float(held[i - cta0]) : weights[i];
+                    if (positions_out != positions) positions_out[i] = holds ? p_held[i - cta0] : positions[i];
+                    if (kept) kept[i] = i;
+                }
+        if (ctas > 1) meet();                    // nobody reads another CTA's shared memory any more
         if (gone == b || rank != 0 || warp != 0) return;
-        const int src_page = page_of(b), dst_page = page_of(gone);
+        const int64_t src_at = row_at(b), dst_at = row_at(gone);
         if (lane == 0) {
             weights_out[gone] = weights[b];
             positions_out[gone] = positions[b];
             if (kept) kept[gone] = b;
         }
-        if (src_page >= 0 && dst_page >= 0) {
-            if (lane < chunks) *reinterpret_cast<uint4*>(place(dst_page, gone)) = *reinterpret_cast<const uint4*>(place(src_page, b));
+        if (src_at >= 0 && dst_at >= 0) {
+            if (lane < chunks) *reinterpret_cast<uint4*>(lane_at + dst_at + swizzle(gone)) = *reinterpret_cast<const uint4*>(lane_at + src_at + swizzle(b));
         } else if (lane == 0 && p.status) {
             atomicOr(p.status, kStatusBadPage);
         }
@@ -194,27 +250,37 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
     for (int pass = 0; pass < 4; ++pass) {
         const int shift = 24 - 8 * pass;
         uint32_t* hist = sm.hist[pass & 1];
-        for (int i = w0 + lane; i < w1; i += 32) {
-            const uint32_t k = key(i);
-            if (pass == 0 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
-        }
-        cluster.sync();
+        for_groups([&](int i, const uint32_t (&keys)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < w1 && (pass == 0 || (keys[e] >> (shift + 8)) == (prefix >> (shift + 8)))) atomicAdd(&hist[(keys[e] >> shift) & 255], 1u);
+        });
+        meet();
         // keys with a larger digit than this thread's
-        int c = 0;
-        if (tid < 256)
-            for (int r = 0; r < ctas; ++r) c += int(cluster.map_shared_rank(hist, r)[255 - tid]);
+        int c = 0, lower = 0;                    // of all CTAs; of those before this one
+        if (tid < 256) {
+            uint32_t of[kMostCtas];
+#pragma unroll
+            for (int r = 0; r < kMostCtas; ++r) of[r] = r < ctas ? cluster.map_shared_rank(hist, r)[255 - tid] : 0u;
+#pragma unroll
+            for (int r = 0; r < kMostCtas; ++r) {
+                c += int(of[r]);
+                if (r < rank) lower += int(of[r]);
+            }
+        }
         int x = c;
         for (int d = 1; d < 32; d <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, d);
             if (lane >= d) x += y;
         }
-        if (lane == 31) sm.scan[warp] = x;
+        if (lane == 31 && warp < 8) sm.scan[warp] = x;
         // the other histogram is the next pass's: every CTA has read it, or it would not have come to this pass's barrier
-        if (tid >= 256) sm.hist[(pass + 1) & 1][tid - 256] = 0;
+        if (tid < 256) sm.hist[(pass + 1) & 1][tid] = 0;
         __syncthreads();
         int before = x - c;
+#pragma unroll
         for (int w = 0; w < 8; ++w) before += w < warp ? sm.scan[w] : 0;
-        if (tid < 256 && before < need && need <= before + c) { sm.digit = 255 - tid; sm.need = need - before; }
+        if (tid < 256 && before < need && need <= before + c) { sm.digit = 255 - tid; sm.need = need - before; sm.ties = lower; }
         __syncthreads();
         prefix |= uint32_t(sm.digit) << shift;
         need = sm.need;
@@ -222,72 +288,112 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
     const uint32_t threshold = prefix;           // `need` of the keys equal to it are kept, the lowest slots'
 
     // ---- numbers ----
-    // sums over the warps before this one, of the whole cluster
-    auto before_us = [&](int which) {
-        int s = 0;
-        for (int r = 0; r <= rank; ++r) {
-            const int32_t* c = cluster.map_shared_rank(&sm.count[which][0], r);
-            if (lane < (r < rank ? kWarps : warp)) s += c[lane];
+    auto warp_scan = [&](int x) {                // sums up to and with this lane
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
         }
-        return int(__reduce_add_sync(0xffffffffu, unsigned(s)));
+        return x;
+    };
+    // warp 0: turns counts by warp into the sums before them in the CTA; returns the CTA's
+    auto scan = [&](int which) {
+        const int c = lane < kWarps ? sm.count[which][lane] : 0, upto = warp_scan(c);
+        if (lane < kWarps) sm.count[which][lane] = upto - c;
+        return __shfl_sync(0xffffffffu, upto, 31);
     };
     int ties = 0;
-    for (int i = w0 + lane; i < w1; i += 32) ties += key(i) == threshold;
+    for_groups([&](int i, const uint32_t (&keys)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ties += i + e < w1 && keys[e] == threshold;
+    });
     ties = int(__reduce_add_sync(0xffffffffu, unsigned(ties)));
     if (lane == 0) sm.count[0][warp] = ties;
-    cluster.sync();
-    const int ties0 = before_us(0);
-    // calls f(slot, kept) for all slots of the warp, a group of 32 at a time
-    auto for_slots = [&](auto&& f) {
+    __syncthreads();
+    if (warp == 0) scan(0);
+    __syncthreads();
+    const int ties0 = sm.ties + sm.count[0][warp];       // (the last pass counted those of the CTAs before this one)
+    // calls f(i, keep) for all groups, bit e of keep: slot i + e is kept
+    auto for_kept = [&](auto&& f) {
         int seen = ties0;
-        for (int i0 = w0; i0 < w1; i0 += 32) {
-            const int i = i0 + lane;
-            const uint32_t k = i < w1 ? key(i) : 0u;
-            const bool tie = i < w1 && k == threshold;
-            const unsigned tied = __ballot_sync(0xffffffffu, tie);
-            const bool keep = i < w1 && (k > threshold || (tie && seen + __popc(tied & ((1u << lane) - 1u)) < need));
-            seen += __popc(tied);
-            f(i, keep);
-        }
+        for_groups([&](int i, const uint32_t (&keys)[4]) {
+            unsigned above = 0, tied = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < w1) {
+                    above |= unsigned(keys[e] > threshold) << e;
+                    tied |= unsigned(keys[e] == threshold) << e;
+                }
+            if (__any_sync(0xffffffffu, tied != 0)) {
+                const int mine = __popc(tied), upto = warp_scan(mine);
+                int left = need - (seen + upto - mine);          // ties that are still kept from this lane's first on
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if ((tied >> e) & 1u) above |= unsigned(left-- > 0) << e;
+                seen += __shfl_sync(0xffffffffu, upto, 31);
+            }
+            f(i, above);
+        });
     };
+    // of the slots i .. i + 3: those below the budget, those that are there
+    auto below = [&](int i) { return i >= b ? 0u : b - i >= 4 ? 15u : (1u << (b - i)) - 1u; };
+    auto there = [&](int i) { return i >= w1 ? 0u : w1 - i >= 4 ? 15u : (1u << (w1 - i)) - 1u; };
     int behind = 0, holes = 0;
-    for_slots([&](int i, bool keep) {
-        behind += __popc(__ballot_sync(0xffffffffu, keep && i >= b));
-        holes += __popc(__ballot_sync(0xffffffffu, i < w1 && !keep && i < b));
+    for_kept([&](int i, unsigned keep) {
+        behind += __popc(keep & ~below(i));
+        holes += __popc(there(i) & ~keep & below(i));
     });
+    behind = int(__reduce_add_sync(0xffffffffu, unsigned(behind)));
+    holes = int(__reduce_add_sync(0xffffffffu, unsigned(holes)));
     if (lane == 0) { sm.count[1][warp] = behind; sm.count[2][warp] = holes; }
-    cluster.sync();
-    int behind0 = before_us(1), holes0 = before_us(2), moves = 0;
-    for (int r = 0; r < ctas; ++r) {
-        const int32_t* c = cluster.map_shared_rank(&sm.count[2][0], r);
-        if (lane < kWarps) moves += c[lane];
+    __syncthreads();
+    if (warp == 0) {
+        const int x = scan(1), y = scan(2);
+        if (lane == 0) { sm.total[0] = x; sm.total[1] = y; }
     }
-    moves = int(__reduce_add_sync(0xffffffffu, unsigned(moves)));
+    meet();
+    const int of0 = lane < ctas ? cluster.map_shared_rank(sm.total, lane)[0] : 0, of1 = lane < ctas ? cluster.map_shared_rank(sm.total, lane)[1] : 0;
+    int behind0 = sm.count[1][warp] + int(__reduce_add_sync(0xffffffffu, unsigned(lane < rank ? of0 : 0)));
+    int holes0 = sm.count[2][warp] + int(__reduce_add_sync(0xffffffffu, unsigned(lane < rank ? of1 : 0)));
+    const int moves = int(__reduce_add_sync(0xffffffffu, unsigned(of1)));
     int32_t* from = p.moved + int64_t(pair) * 2 * p.most_moved;
     int32_t* into = from + p.most_moved;
-    for_slots([&](int i, bool keep) {
-        const bool comes = keep && i >= b, hole = i < w1 && !keep && i < b;
-        const unsigned coming = __ballot_sync(0xffffffffu, comes), open = __ballot_sync(0xffffffffu, hole), lower = (1u << lane) - 1u;
-        if (comes) from[behind0 + __popc(coming & lower)] = i;
-        if (hole) into[holes0 + __popc(open & lower)] = i;
-        behind0 += __popc(coming);
-        holes0 += __popc(open);
-        if (keep && i < b) stays_put(i);
+    const bool tells = !in_place || kept;        // what stays where it is has to be written, too
+    for_kept([&](int i, unsigned keep) {
+        const unsigned comes = keep & ~below(i), open = there(i) & ~keep & below(i);
+        const int mine = __popc(comes) | __popc(open) << 16, upto = warp_scan(mine);
+        int x = behind0 + ((upto - mine) & 0xffff), y = holes0 + ((upto - mine) >> 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if ((comes >> e) & 1u) from[x++] = i + e;
+            if ((open >> e) & 1u) into[y++] = i + e;
+            if (!holds && tells && ((keep & below(i)) >> e) & 1u) stays_put(i + e);
+        }
+        const int all = __shfl_sync(0xffffffffu, upto, 31);
+        behind0 += all & 0xffff;
+        holes0 += all >> 16;
     });
-    cluster.sync();                              // the lists are written; nobody reads another CTA's shared memory any more
+    meet();                                      // the lists are written; nobody reads another CTA's shared memory any more
+    if (holds && tells)                          // (behind the barrier, which would wait for these writes; keys that are not held are gone once rows move)
+        for_kept([&](int i, unsigned keep) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (((keep & below(i)) >> e) & 1u) stays_put(i + e);
+        });
 
     // ---- moves: a warp looks 32 of them up at once, a lane each, then moves their rows, a 16-byte chunk of each a lane ----
     const int warps = ctas * kWarps, each = (moves + warps - 1) / warps, first = min(moves, (rank * kWarps + warp) * each), last = min(moves, first + each);
     for (int i0 = first; i0 < last; i0 += 32) {
-        int src = 0, dst = 0, src_page = -1, dst_page = -1;
+        int src = 0, dst = 0;
+        int64_t src_at = -1, dst_at = -1;
         if (i0 + lane < last) {
             src = from[i0 + lane]; dst = into[i0 + lane];
-            src_page = page_of(src); dst_page = page_of(dst);
+            src_at = row_at(src); dst_at = row_at(dst);
             weights_out[dst] = weights[src];
             positions_out[dst] = positions[src];
             if (kept) kept[dst] = src;
-            if (src_page < 0 || dst_page < 0) {
-                src_page = -1;
+            if (src_at < 0 || dst_at < 0) {
+                src_at = -1;
                 if (p.status) atomicOr(p.status, kStatusBadPage);
             }
         }
@@ -296,38 +402,34 @@ __global__ void __launch_bounds__(kThreads) paged_evict_kernel(const __grid_cons
             uint4 x[kAtOnce];
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
-                const int page = __shfl_sync(0xffffffffu, src_page, k0 + k), slot = __shfl_sync(0xffffffffu, src, k0 + k);
-                if (page >= 0 && lane < chunks) x[k] = *reinterpret_cast<const uint4*>(place(page, slot));
+                const int64_t at = __shfl_sync(0xffffffffu, src_at, k0 + k);
+                const int slot = __shfl_sync(0xffffffffu, src, k0 + k);
+                if (at >= 0 && lane < chunks) x[k] = *reinterpret_cast<const uint4*>(lane_at + at + swizzle(slot));
             }
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
-                const int there = __shfl_sync(0xffffffffu, src_page, k0 + k), page = __shfl_sync(0xffffffffu, dst_page, k0 + k), slot = __shfl_sync(0xffffffffu, dst, k0 + k);
-                if (there >= 0 && lane < chunks) *reinterpret_cast<uint4*>(place(page, slot)) = x[k];
+                const int64_t from_at = __shfl_sync(0xffffffffu, src_at, k0 + k), at = __shfl_sync(0xffffffffu, dst_at, k0 + k);
+                const int slot = __shfl_sync(0xffffffffu, dst, k0 + k);
+                if (from_at >= 0 && lane < chunks) *reinterpret_cast<uint4*>(lane_at + at + swizzle(slot)) = x[k];
             }
         }
     }
 }
 
-}  // namespace
-
-cudaError_t launch_paged_evict(PagedEvict& a, cudaStream_t s) {
-    const int pairs = a.c.n_rows * a.c.g.n_kv_heads, slots = a.c.max_blocks * a.c.g.bt;
-    int ctas = 1;
-    while (ctas < kMostCtas && int64_t(pairs) * ctas * 2 <= 2 * kSmCount && slots / (ctas * 2) >= 1024) ctas *= 2;
-    const int per_cta = ((slots + ctas - 1) / ctas + 31) & ~31;
-    a.held = per_cta <= kHeldSlots ? per_cta : kHeldSlots;
+template <int THREADS>
+cudaError_t launch(const PagedEvict& a, int ctas, cudaStream_t s) {
     static std::atomic<bool> configured[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(paged_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldSlots * 8);
+        e = cudaFuncSetAttribute(paged_evict_kernel<THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldSlots * 8);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) configured[dev].store(true, std::memory_order_release);
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(pairs * ctas));
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3(unsigned(a.c.n_rows * a.c.g.n_kv_heads * ctas));
+    cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = size_t(a.held) * 8;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -337,7 +439,19 @@ cudaError_t launch_paged_evict(PagedEvict& a, cudaStream_t s) {
     attr[1].val.programmaticStreamSerializationAllowed = overlap_launches() ? 1 : 0;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, paged_evict_kernel, a, ctas);
+    return cudaLaunchKernelEx(&cfg, paged_evict_kernel<THREADS>, a, ctas);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_evict(PagedEvict& a, cudaStream_t s) {
+    const int pairs = a.c.n_rows * a.c.g.n_kv_heads, slots = a.c.max_blocks * a.c.g.bt;
+    int ctas = 1;
+    while (ctas < kMostCtas && int64_t(pairs) * ctas * 2 <= kSmCount && slots / (ctas * 2) >= 1024) ctas *= 2;
+    const int per_cta = ((slots + ctas - 1) / ctas + 31) & ~31;
+    a.held = per_cta <= kHeldSlots ? per_cta : kHeldSlots;
+    // a CTA to an SM wants its threads; several to an SM, smaller ones
+    return int64_t(pairs) * ctas <= kSmCount ? launch<1024>(a, ctas, s) : launch<256>(a, ctas, s);
 }
 
 }  // namespace ipkvi
