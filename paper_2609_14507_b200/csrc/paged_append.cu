@@ -1,8 +1,8 @@
 // New tokens into the pages of a paged cache.  A CTA takes some tokens: every thread asks for its 16-byte chunks of their K and V rows, a thread
 // per token finds the row, the slot and the page meanwhile (four dependent reads, and more for the search among the rows), then
 // the chunks are stored.  Bound by the bytes (read once, written once) and, for a decode step, by the launch and that chain of reads.
-// Measured: nine chunks of prompts, 20743 tokens of 4 KV heads of 128 columns, 85 MB: 23.5 us with one warp to a token and its reads one behind
-// the other.
+// Measured: nine chunks of prompts, 20743 tokens of 4 KV heads of 128 columns, 85 MB: 19.3 us, 4.4 TB/s (23.5 with one warp to a token and its reads one
+// behind the other, 20.4 with 8 chunks a thread, 19.4 to 21 with other CTAs).  64 tokens, one for each row: 2.8 us.
 #include "launch.cuh"
 #include "paged.h"
 #include "ptx.cuh"
@@ -11,10 +11,10 @@ namespace ipkvi {
 
 namespace {
 
-constexpr int kThreads = 256, kAhead = 8;        // chunks of a thread under way
+constexpr int kThreads = 256, kAhead = 4;        // chunks of a thread under way
 constexpr int kMostTokens = 32;                  // of a CTA
 
-__global__ void __launch_bounds__(kThreads) paged_append_kernel(const __grid_constant__ PagedAppend p, const int per_cta) {
+__global__ void __launch_bounds__(kThreads, 5) paged_append_kernel(const __grid_constant__ PagedAppend p, const int per_cta) {
     __shared__ int s_row[kMostTokens], s_slot[kMostTokens];
     __shared__ int64_t s_at[kMostTokens];        // the token's row in its page, from the pool on; -1: it has no place
     const int tid = threadIdx.x;

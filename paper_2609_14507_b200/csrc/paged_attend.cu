@@ -16,7 +16,6 @@
 //
 // At the end of a pair the warps' states are joined in the stages of their last units, which nobody reads any more, and
 // leave as the result, or as one partial for the join kernel.  Every wait is bounded.
-#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -25,8 +24,6 @@
 #include "launch.cuh"
 #include "paged.h"
 #include "ptx.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace ipkvi {
 
@@ -45,8 +42,8 @@ struct Smem {
     int32_t scan[kThreads / 32];
     int32_t units, pairs, fit[32];
     PagedShare share;
-    float2 part_ml[16], head_ml[16];             // cluster: the CTA's partial and, in place of the arrays of rows, its sums; the pair's maxima and 1 / sum
-    alignas(16) int32_t cum[kPagedRowsPerLaunch + 1];
+    float2 part_ml[kPagedMostCluster][16], head_ml[16];  // cluster: maxima and sums of its CTAs' partials; the pair's maxima and 1 / sum
+    alignas(16) int32_t cum[kPagedRowsPerLaunch + 1];    // (and n: a cluster's CTAs leave here what this one joins)
     int32_t n[kPagedRowsPerLaunch];
 };
 static_assert(16 * 128 * 4 <= sizeof(int32_t) * (2 * kPagedRowsPerLaunch + 1), "a partial of 16 heads");
@@ -85,6 +82,22 @@ __device__ __forceinline__ bool wait_tag(const uint32_t* tag, uint32_t unit, uin
             else if (now - t0 > ptx::kWaitLimitNs) return false;
         }
     }
+}
+
+// Thread-block clusters: the barrier in its two halves, and stores to the shared memory of another CTA.
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t at_rank(uint32_t smem, uint32_t rank) {
+    uint32_t there;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem), "r"(rank));
+    return there;
+}
+__device__ __forceinline__ void put(uint32_t there, const float4& v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void put(uint32_t there, const float2& v) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
 }
 
 // Lengths, and from them the shares: see paged.h.  All threads of the CTA.
@@ -194,6 +207,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         sm.units = 0; sm.pairs = 0;
     }
     __syncthreads();
+    if (p.cluster > 0) cluster_arrive_relaxed();         // this CTA is there: the others may write to it behind their wait
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     PagedPart x;
@@ -218,6 +232,14 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         const int64_t extent = kChecked && p.status ? p.c.n_blocks * block_bytes : 0;
         int st = 0, lap = 0, it = 0;
         bool ok = true;
+        {   // a small table comes into the L1 cache while the lengths are on their way
+            const int rows = p.cluster > 0 ? 1 : p.c.n_rows, first = p.cluster > 0 ? int(blockIdx.x) / p.cluster / p.n_gh : 0, lines = (p.c.max_blocks + 31) / 32;
+            const int row = lane / lines;
+            if (rows * lines <= 32 && row < rows) {
+                int32_t unused;
+                asm volatile("ld.global.b32 %0, [%1];" : "=r"(unused) : "l"(p.c.table + (first + row) * p.c.table_stride + (lane - row * lines) * 32));
+            }
+        }
         for (bool more = begin(); more && ok; more = parts.next(x)) {
             const int32_t* table = p.c.table + int64_t(x.row) * p.c.table_stride;
             const char* head = p.c.pool + (x.gh / p.groups_per_kv) * head_bytes;
@@ -278,6 +300,8 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         if (lane == 0)
             for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
                 if (!ptx::mbar_wait(ptx::smem_addr(&sm.full[i % kStages]), (i / kStages) & 1)) or_status(p.status, kStatusCopyNotLanded);
+        __syncwarp();
+        if (p.cluster > 0) cluster_wait();
         return;
     }
 
@@ -289,8 +313,9 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     const uint32_t panel = uint32_t(T) * 128, v_off = uint32_t(T) * D * 2, odd = T == 16 ? 16u * D * 4 : 2048u, pair = T >= 64 ? 4096u : 32u * D * 4;
     uint32_t qa[D / 16][4];
     float o[D / 8][4];
+    const int rank = p.cluster > 0 ? int(blockIdx.x) % p.cluster : 0;
     int it0 = 0, meets = 0;                      // units of the parts before this one
-    bool ok = true;
+    bool ok = true, waited = false;
     auto meet = [&]() -> bool {                  // the four warps; they may wait for units of their own first
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.met));
@@ -301,10 +326,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         const int kv = x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part;
         const int n_heads = min(p.rows_per_part, p.group - in_kv);       // of the part
         const int64_t item0 = int64_t(x.row) * p.n_q_heads + kv * p.group + in_kv;
-        if (x.u0 == x.u1) {                      // a chunk that ends before the pair's first unit, or a cluster's CTA without one
-            if (p.cluster > 0 && tid < 16) sm.part_ml[tid] = make_float2(-INFINITY, 0.f);
-            continue;
-        }
+        if (x.u0 == x.u1) continue;              // a chunk that ends before the pair's first unit, or a cluster's CTA without one
         {
             const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q + x.row * p.q_row) + (kv * p.group + in_kv) * D;
             const int ha = hg * 16 + (ROWS == 4 ? r0 & 3 : r0), hb = hg * 16 + r0 + 8;
@@ -484,13 +506,11 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
             if (x.whole) {
                 p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
                 if (p.head_ml) p.head_ml[item0 + head] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
-            } else if (p.cluster > 0) {
-                sm.part_ml[head] = make_float2(m, z);
             } else {
                 p.part_ml[int64_t(x.place) * p.rows_per_part + head] = make_float2(m, z);
             }
         };
-        float* const out = x.whole ? p.out_o + item0 * D : p.cluster > 0 ? reinterpret_cast<float*>(sm.cum) : p.part_o + int64_t(x.place) * p.rows_per_part * D;
+        float* const out = x.whole ? p.out_o + item0 * D : p.part_o + int64_t(x.place) * p.rows_per_part * D;
         if (ROWS == 16 && teams == 1) {          // no two warps have the same head
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -528,6 +548,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
             }
         }
         if (!meet()) { ok = false; break; }
+        if (p.cluster > 0) { cluster_wait(); waited = true; }
         for (int i = tid; i < n_heads * (D / 4); i += kWarps * 32) {
             const int head = i / (D / 4), col = i - head * (D / 4), g = ROWS == 16 ? head / 16 : 0, row = ROWS == 16 ? head % 16 : head;
             float m = -INFINITY, z = 0.f;
@@ -543,6 +564,12 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
                 z += f * y.y;
             }
+            if (p.cluster > 0) {                 // to the CTA that joins these columns; maximum and sum to all
+                const int to = i & (p.cluster - 1);
+                put(at_rank(ptx::smem_addr(sm.cum) + (rank * (n_heads * (D / 4) / p.cluster) + i / p.cluster) * 16, to), acc);
+                if (col < p.cluster) put(at_rank(ptx::smem_addr(&sm.part_ml[rank][head]), col), make_float2(m, z));
+                continue;
+            }
             const float f = !x.whole ? 1.f : z == 0.f ? 0.f : 1.f / z;
             reinterpret_cast<float4*>(out + head * D)[col] = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
             if (col == 0) leave(head, m, z);
@@ -556,43 +583,54 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     if (!ok && lane == 0) or_status(p.status, kStatusNoTile);
     if (p.cluster == 0) return;
 
-    // ---- a cluster: its CTAs' partials are joined, every CTA a share of the outputs (also after a wait that ran out: the others read here) ----
-    cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();
+    // ---- a cluster: every CTA joins its share of the columns of all partials (also after a wait that ran out: the others wait for its word) ----
     const int kv = x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part, n_heads = min(p.rows_per_part, p.group - in_kv);
     const int64_t item0 = int64_t(x.row) * p.n_q_heads + kv * p.group + in_kv;
-    const int rank = int(cluster.block_rank());
-    auto state_of = [&](int head, float& m, float& z) {
+    __syncwarp();
+    if (!waited) {                               // no part, or a lost one
+        cluster_wait();
+        if (tid < 16 * p.cluster) put(at_rank(ptx::smem_addr(&sm.part_ml[rank][tid & 15]), tid >> 4), make_float2(-INFINITY, 0.f));
+    }
+    cluster_arrive();
+    cluster_wait();
+    auto state_of = [&](int head, float2 (&y)[kPagedMostCluster], float& m, float& z) {
         m = -INFINITY; z = 0.f;
-        for (int c = 0; c < p.cluster; ++c) m = fmaxf(m, cluster.map_shared_rank(&sm.part_ml[head], c)->x);
-        for (int c = 0; c < p.cluster; ++c) {
-            const float2 y = *cluster.map_shared_rank(&sm.part_ml[head], c);
-            if (y.y != 0.f) z += ptx::ex2(y.x - (m == -INFINITY ? 0.f : m)) * y.y;
+#pragma unroll
+        for (int c = 0; c < kPagedMostCluster; ++c) {
+            y[c] = c < p.cluster ? sm.part_ml[c][head] : make_float2(-INFINITY, 0.f);
+            m = fmaxf(m, y[c].x);
+        }
+#pragma unroll
+        for (int c = 0; c < kPagedMostCluster; ++c) {
+            y[c].x = ptx::ex2(y[c].x - (m == -INFINITY ? 0.f : m));
+            if (y[c].y != 0.f) z += y[c].x * y[c].y;
         }
     };
-    for (int i = rank * (kWarps * 32) + tid; i < n_heads * (D / 4); i += p.cluster * (kWarps * 32)) {
-        const int head = i / (D / 4), col = i - head * (D / 4);
+    const int per_cta = n_heads * (D / 4) / p.cluster;
+    for (int k = tid; k < per_cta; k += kWarps * 32) {
+        const int i = k * p.cluster + rank, head = i / (D / 4), col = i - head * (D / 4);
+        float2 y[kPagedMostCluster];
         float m, z;
-        state_of(head, m, z);
+        state_of(head, y, m, z);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c = 0; c < p.cluster; ++c) {
-            const float2 y = *cluster.map_shared_rank(&sm.part_ml[head], c);
-            if (y.y == 0.f) continue;
-            const float f = ptx::ex2(y.x - (m == -INFINITY ? 0.f : m));
-            const float4 v = reinterpret_cast<const float4*>(cluster.map_shared_rank(sm.cum, c))[i];
-            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
-        }
+#pragma unroll
+        for (int c = 0; c < kPagedMostCluster; ++c)
+            if (c < p.cluster && y[c].y != 0.f) {
+                const float4 v = reinterpret_cast<const float4*>(sm.cum)[c * per_cta + k];
+                acc.x += y[c].x * v.x; acc.y += y[c].x * v.y; acc.z += y[c].x * v.z; acc.w += y[c].x * v.w;
+            }
         const float inv = z == 0.f ? 0.f : 1.f / z;
         reinterpret_cast<float4*>(p.out_o + item0 * D)[i] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
         if (col == 0) p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
     }
-    if (p.scores && tid < n_heads) {
+    if (!p.scores) return;
+    if (tid < n_heads) {
+        float2 y[kPagedMostCluster];
         float m, z;
-        state_of(tid, m, z);
+        state_of(tid, y, m, z);
         sm.head_ml[tid] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
     }
-    cluster.sync();                              // nobody reads another CTA's shared memory any more; the scores are written
-    if (!p.scores) return;
+    asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");       // (all four warps come here without another wait)
     // the weights of this CTA's units (all heads of the KV head are in one group here)
     const int64_t w0 = (int64_t(x.row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
     const float* scores = p.scores + (int64_t(x.row) * p.n_gh + x.gh) * p.most_units * (U * ROWS);
@@ -707,31 +745,36 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const __grid_consta
 
 // weights_out[t] = weights[t] + sum over the KV head's query heads of 2^(s_t - m) / z, from the scores that the attention left.
 // One CTA for every splits-th 256 visible slots of a (row, KV head); a thread per slot.
+template <int ROWS>
 __global__ void __launch_bounds__(256) paged_weigh_kernel(const __grid_constant__ PagedAttend p, const int splits) {
     const int split = blockIdx.x % splits, pair = blockIdx.x / splits, kv = pair % p.c.g.n_kv_heads, row = pair / p.c.g.n_kv_heads;
     const int U = p.unit, per_cta = 256 / U, tok = int(threadIdx.x) % U;
-    const int rows = p.rows_per_part / p.sixteens;       // of one product
+    const float2* ml = p.head_ml + int64_t(row) * p.n_q_heads + kv * p.group;
+    const float* scores = p.scores + (int64_t(row) * p.n_gh + kv * p.groups_per_kv) * p.most_units * (U * p.rows_per_part) + (tok >> 4) * (16 * p.rows_per_part) +
+                          ((tok >> 3) & 1) * (ROWS * 8) + (tok & 7);
+    const int64_t w0 = (int64_t(row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     const PagedSeen seen = paged_seen(length_of(p, row, false), p.window, p.first, U);
-    const float2* ml = p.head_ml + int64_t(row) * p.n_q_heads + kv * p.group;
-    const int64_t w0 = (int64_t(row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
     for (int j = split * per_cta + int(threadIdx.x) / U; j < seen.units; j += splits * per_cta) {
         const int t = seen.unit(j) * U + tok;
         if (!seen.sees(t)) continue;
         const float before = p.c.weights ? p.c.weights[w0 + t] : 0.f;
         float given = 0.f;
-        for (int part = 0; part < p.groups_per_kv; ++part) {
-            const float* s = p.scores + ((int64_t(row) * p.n_gh + kv * p.groups_per_kv + part) * p.most_units + j) * (U * p.rows_per_part) +
-                             (tok >> 4) * (16 * p.rows_per_part) + ((tok >> 3) & 1) * (rows * 8) + (tok & 7);
-            const int heads = min(p.rows_per_part, p.group - part * p.rows_per_part);
-#pragma unroll 8
-            for (int h = 0; h < heads; ++h) {
-                const float2 y = ml[part * p.rows_per_part + h];
-                const float x = s[(h / rows) * (rows * 16) + (h % rows) * 8];
-                if (y.y != 0.f) given += ptx::ex2(x - y.x) * y.y;
+        for (int head0 = 0, part = 0; head0 < p.group; ++part)
+            for (int hg = 0; hg < p.sixteens && head0 < p.group; ++hg, head0 += ROWS) {
+                const float* s = scores + (int64_t(part) * p.most_units + j) * (U * p.rows_per_part) + hg * (ROWS * 16);
+                float x[ROWS];
+                float2 y[ROWS];
+#pragma unroll
+                for (int h = 0; h < ROWS; ++h) {
+                    y[h] = make_float2(0.f, 0.f);
+                    if (head0 + h < p.group) { x[h] = s[h * 8]; y[h] = ml[head0 + h]; }
+                }
+#pragma unroll
+                for (int h = 0; h < ROWS; ++h)
+                    if (y[h].y != 0.f) given += ptx::ex2(x[h] - y[h].x) * y[h].y;
             }
-        }
         p.weights_out[w0 + t] = before + given;
     }
 }
@@ -787,9 +830,10 @@ cudaError_t launch_paged_attend(const PagedAttend& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (a.weights_out) {
         const int64_t pairs = int64_t(a.c.n_rows) * a.c.g.n_kv_heads, groups = (int64_t(a.most_units) * a.unit + 255) / 256;
-        const int64_t want = (148 * 8 + pairs - 1) / pairs;
+        const int64_t want = (148 * 32 + pairs - 1) / pairs;             // a few CTAs behind every one that runs
         const int splits = int(want < groups ? want : groups);
-        return launch_overlapped(paged_weigh_kernel, int(pairs * splits), 256, size_t(0), s, a, splits);
+        return launch_overlapped(rows == 4 ? paged_weigh_kernel<4> : rows == 8 ? paged_weigh_kernel<8> : paged_weigh_kernel<16>, int(pairs * splits), 256, size_t(0), s,
+                                 a, splits);
     }
     return cudaSuccess;
 }
