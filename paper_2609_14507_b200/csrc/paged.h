@@ -82,12 +82,16 @@ constexpr int kPagedCtasPerSm = 2, kPagedWarps = 4;
 // Where every pair has few units, which the host sees by the table's width or the window alone, a thread-block cluster takes it, joins
 // in distributed shared memory and adds the weights up: one launch in place of two or three.
 constexpr int kPagedMostCluster = 8;
-constexpr int kPagedClusterUnits = 16;           // units of a CTA up to which it wins
+constexpr int kPagedClusterUnits = 24, kPagedClusterMore = 5;
 inline int paged_cluster(int64_t pairs, int64_t most_units, int group, int ctas) {
     if (group > 16 || pairs > ctas) return 0;            // (above, a KV head's heads are not in one CTA)
     int n = 1;
     while (n < kPagedMostCluster && pairs * n * 2 <= ctas && most_units > kPagedWarps * n) n *= 2;
-    return most_units <= int64_t(kPagedClusterUnits) * n ? n : 0;
+    // Units of a CTA, against those with whole CTAs over the GPU.  The launch saved is worth five (1 row of 4 KV heads, 8 and 4: 2K tokens 10.3 us against
+    // 10.9; 12 and 4: 12.5 and 11.7; 4 rows of 8 heads and 6K tokens, 24 and 20: 22.7 and 23.9).  Rows may be shorter than the table is wide, and
+    // clusters do not even them out: not above 24.
+    const int64_t mine = (most_units + n - 1) / n, others = pairs * most_units / ctas > kPagedWarps ? pairs * most_units / ctas : kPagedWarps;
+    return mine <= kPagedClusterUnits && mine <= others + kPagedClusterMore ? n : 0;
 }
 struct PagedShare {
     int32_t share;                               // units of a CTA at most; 0: chunks
@@ -106,16 +110,18 @@ IPKV_HD int32_t paged_part_of(int32_t n, int32_t parts, int32_t x) {
     const int32_t q = int32_t(uint32_t(n) / uint32_t(parts)), r = n - q * parts, large = r * (q + 1);
     return x < large ? int32_t(uint32_t(x) / uint32_t(q + 1)) : r + int32_t(uint32_t(x - large) / uint32_t(q));
 }
-// The share that whole CTAs to every pair would take is looked for among 32 values, multiples of the teams that work in a CTA, from what `ctas`
-// CTAs have to take of all units at least up to twice that.  Chunks, if none of them gives every pair whole CTAs within `ctas`, or if the
-// share is more than a chunk by this much (rows of different lengths: 256 pairs of 80 to 129 units gave 120 units to a CTA, 93 in chunks).
-constexpr int kPagedUneven = 4;
+// The share that whole CTAs to every pair would take is looked for among 32 values, from what `ctas` CTAs have to take of all units at least
+// up to twice that, in multiples of the teams that work in a CTA while it is few rounds of them.  Chunks, if none of them gives every pair
+// whole CTAs within `ctas`, or if the share is much more than a chunk (rows of different lengths: 256 pairs of 80 to 129 units gave 120
+// units to a CTA, 93 in chunks).  Where a chunk has the end of one pair and the beginning of the next it loses some 3 us, 8 units: 64 pairs of
+// 129 units 29.5 us by shares of 36, 31.1 in chunks of 29; 264 of 94 units 67.7 by 94 and 72 in chunks of 87.
 IPKV_HD int32_t paged_share_tried(int32_t units, int32_t ctas, int32_t teams, int32_t i) {
-    const int32_t least = units > 0 ? ((units - 1) / ctas + teams) / teams : 1;
-    return teams * (least + int32_t(uint32_t(least + 30) / 31u) * i);
+    const int32_t mean = units > 0 ? (units - 1) / ctas + 1 : 1, step = mean >= 8 * teams ? 1 : teams, least = (mean + step - 1) / step;
+    return step * (least + int32_t(uint32_t(least + 30) / 31u) * i);
 }
 IPKV_HD bool paged_share_wins(int32_t share, int32_t units, int32_t pairs, int32_t ctas) {
-    return share <= (units + pairs * kPagedPairCost) / ctas + kPagedUneven;
+    const int32_t mean = (units + pairs * kPagedPairCost) / ctas;
+    return share <= mean + mean / 16 + 8;
 }
 
 // A CTA's parts of pairs, one after the other.  cum[r]: cost (with a share: parts) of a head group in the rows before r; n[r]: slots.
@@ -225,6 +231,7 @@ struct PagedAttend {
     int32_t window, first, unit, most_units;
     int32_t n_q_heads, group, groups_per_kv, n_gh, rows_per_part, sixteens;
     int32_t n_ctas;
+    int32_t bt_shift;                            // log2 of the tokens of a block, -1 where there is none
     int32_t cluster;                             // CTAs that take a pair together and write its result; 0: shares, and a join
     float scale_log2;
 };

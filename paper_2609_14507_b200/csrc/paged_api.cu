@@ -150,6 +150,7 @@ ipkv_status ipkv_paged_attend(const ipkv_attn_shape* sh, const ipkv_paged* c, co
     a.unit = plan.unit; a.most_units = int32_t(plan.most_units);
     a.n_q_heads = sh->n_q_heads; a.group = plan.group; a.groups_per_kv = plan.groups_per_kv; a.n_gh = plan.n_gh;
     a.rows_per_part = plan.rows_per_part; a.sixteens = plan.sixteens;
+    a.bt_shift = (sh->block_tokens & (sh->block_tokens - 1)) == 0 ? __builtin_ctz(unsigned(sh->block_tokens)) : -1;
     const float scale = sh->softmax_scale > 0.f ? sh->softmax_scale : 1.0f / std::sqrt(float(sh->dim_qk));
     a.scale_log2 = scale * 1.4426950408889634f;
     for (int32_t r0 = 0; r0 < c->n_rows; r0 += plan.rows) {

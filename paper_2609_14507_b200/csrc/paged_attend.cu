@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 if (u < x.u1) {
                     const int a = x.seen.unit(u) * U + (lane % per_unit) * T;
                     if (x.seen.sees_any(a, a + T)) {
-                        page = table[a / p.c.g.bt];
+                        page = table[p.bt_shift >= 0 ? a >> p.bt_shift : a / p.c.g.bt];
                         if (page < 0 || page >= p.c.n_blocks) { or_status(p.status, kStatusBadPage); page = -2; }
                     }
                 }
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                     } else {
                         const int64_t at = __shfl_sync(0xffffffffu, pages, lane0);
                         if (there && lane < D / 32) {            // a panel a lane, of K, then of V
-                            const char* src = head + at * block_bytes + (int64_t(lane) * p.c.g.bt + x.seen.unit(j) * U % p.c.g.bt) * 128;
+                            const char* src = head + at * block_bytes + (int64_t(lane) * p.c.g.bt + (p.bt_shift >= 0 ? x.seen.unit(j) * U & (p.c.g.bt - 1) : x.seen.unit(j) * U % p.c.g.bt)) * 128;
                             ptx::bulk_g2s_hint(dst + lane * (U * 128), ptx::checked_src<kChecked>(src, U * 128, p.c.pool, extent, p.status, kStatusBadIndex), U * 128,
                                                bar, pol);
                         }
@@ -551,19 +551,26 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         if (p.cluster > 0) { cluster_wait(); waited = true; }
         for (int i = tid; i < n_heads * (D / 4); i += kWarps * 32) {
             const int head = i / (D / 4), col = i - head * (D / 4), g = ROWS == 16 ? head / 16 : 0, row = ROWS == 16 ? head % 16 : head;
+            float2 y[kWarps];
+            float4 v[kWarps];
             float m = -INFINITY, z = 0.f;
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = g; w < kWarps; w += sixteens) m = fmaxf(m, sm.ml[w * 16 + row].x);
-            for (int w = g; w < kWarps; w += sixteens) {
-                const float2 y = sm.ml[w * 16 + row];
-                if (y.y == 0.f) continue;        // nothing seen
-                const float f = ptx::ex2(y.x - (m == -INFINITY ? 0.f : m));
-                float4 v;
-                const uint32_t from = s_ring + sm.where[w] * kPagedUnitBytes + (g * ROWS + row) * (D * 4) + (uint32_t(2 * col) ^ ((row & 7) << 2)) * 8;
-                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(from) : "memory");
-                acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
-                z += f * y.y;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                y[w] = ROWS < 16 || (w & (sixteens - 1)) == g ? sm.ml[w * 16 + row] : make_float2(-INFINITY, 0.f);
+                m = fmaxf(m, y[w].x);
+                if (y[w].y != 0.f) {             // (else nothing seen)
+                    const uint32_t from = s_ring + sm.where[w] * kPagedUnitBytes + (g * ROWS + row) * (D * 4) + (uint32_t(2 * col) ^ ((row & 7) << 2)) * 8;
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[w].x), "=f"(v[w].y), "=f"(v[w].z), "=f"(v[w].w) : "r"(from) : "memory");
+                }
             }
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w)
+                if (y[w].y != 0.f) {
+                    const float f = ptx::ex2(y[w].x - (m == -INFINITY ? 0.f : m));
+                    acc.x += f * v[w].x; acc.y += f * v[w].y; acc.z += f * v[w].z; acc.w += f * v[w].w;
+                    z += f * y[w].y;
+                }
             if (p.cluster > 0) {                 // to the CTA that joins these columns; maximum and sum to all
                 const int to = i & (p.cluster - 1);
                 put(at_rank(ptx::smem_addr(sm.cum) + (rank * (n_heads * (D / 4) / p.cluster) + i / p.cluster) * 16, to), acc);
@@ -634,16 +641,30 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     // the weights of this CTA's units (all heads of the KV head are in one group here)
     const int64_t w0 = (int64_t(x.row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
     const float* scores = p.scores + (int64_t(x.row) * p.n_gh + x.gh) * p.most_units * (U * ROWS);
-    for (int k = x.u0 * U + tid; k < x.u1 * U; k += kWarps * 32) {
-        const int t = x.seen.unit(k / U) * U + k % U;
-        if (!x.seen.sees(t)) continue;
-        const float before = p.c.weights ? p.c.weights[w0 + t] : 0.f;
-        const float* s = scores + int64_t(k >> 4) * (16 * ROWS) + ((k >> 3) & 1) * (ROWS * 8) + (k & 7);
-        float given = 0.f;
+    constexpr int kAhead = 32 / ROWS;            // slots of a thread under way
+    for (int k0 = x.u0 * U + tid; k0 < x.u1 * U; k0 += kWarps * 32 * kAhead) {
+        float s[kAhead][ROWS], before[kAhead];
+        int t[kAhead];
 #pragma unroll
-        for (int h = 0; h < ROWS; ++h)
-            if (h < n_heads && sm.head_ml[h].y != 0.f) given += ptx::ex2(s[h * 8] - sm.head_ml[h].x) * sm.head_ml[h].y;
-        p.weights_out[w0 + t] = before + given;
+        for (int e = 0; e < kAhead; ++e) {
+            const int k = k0 + e * (kWarps * 32);
+            t[e] = k < x.u1 * U ? x.seen.unit(k / U) * U + k % U : -1;
+            if (t[e] >= 0 && !x.seen.sees(t[e])) t[e] = -1;
+            if (t[e] < 0) continue;
+            const float* from = scores + int64_t(k >> 4) * (16 * ROWS) + ((k >> 3) & 1) * (ROWS * 8) + (k & 7);
+            before[e] = p.c.weights ? p.c.weights[w0 + t[e]] : 0.f;
+#pragma unroll
+            for (int h = 0; h < ROWS; ++h) s[e][h] = h < n_heads ? from[h * 8] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            if (t[e] < 0) continue;
+            float given = 0.f;
+#pragma unroll
+            for (int h = 0; h < ROWS; ++h)
+                if (h < n_heads && sm.head_ml[h].y != 0.f) given += ptx::ex2(s[e][h] - sm.head_ml[h].x) * sm.head_ml[h].y;
+            p.weights_out[w0 + t[e]] = before[e] + given;
+        }
     }
 }
 
@@ -806,13 +827,13 @@ cudaError_t launch(const PagedAttend& a, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, paged_attend_kernel<D, ROWS>, a);
 }
 
-// Many partials for every head (few pairs): slabs of 32 columns with many slices.
+// Many partials for every head (few pairs): slabs of 16 columns with many slices.
 constexpr int kManyPartials = 24;
 
 template <int D>
 cudaError_t launch_join(const PagedAttend& a, cudaStream_t s) {
     const int items = a.c.n_rows * a.n_q_heads, pairs = a.c.n_rows * a.n_gh;
-    if (a.n_ctas > kManyPartials * pairs) return launch_overlapped(paged_join_kernel<D, 32, 256>, items * (D / 32), 256, size_t(0), s, a);
+    if (a.n_ctas > kManyPartials * pairs) return launch_overlapped(paged_join_kernel<D, 16, 256>, items * (D / 16), 256, size_t(0), s, a);
     return launch_overlapped(paged_join_kernel<D, D, 128>, items, 128, size_t(0), s, a);
 }
 
