@@ -83,14 +83,14 @@ constexpr int kPagedCtasPerSm = 2, kPagedWarps = 4;
 // in distributed shared memory and adds the weights up: one launch in place of two or three.
 constexpr int kPagedMostCluster = 8;
 constexpr int kPagedClusterUnits = 24, kPagedClusterMore = 5;
-inline int paged_cluster(int64_t pairs, int64_t most_units, int group, int ctas) {
-    if (group > 16 || pairs > ctas) return 0;            // (above, a KV head's heads are not in one CTA)
-    int n = 1;
-    while (n < kPagedMostCluster && pairs * n * 2 <= ctas && most_units > kPagedWarps * n) n *= 2;
+inline int paged_cluster(int64_t pairs, int64_t most_units, int group, int sixteens, int ctas) {
+    if (pairs > ctas) return 0;
+    int n = 1;                                           // (more heads than one product takes stay with one CTA)
+    while (group <= 16 && n < kPagedMostCluster && pairs * n * 2 <= ctas && most_units > kPagedWarps * n) n *= 2;
     // Units of a CTA, against those with whole CTAs over the GPU.  The launch saved is worth five (1 row of 4 KV heads, 8 and 4: 2K tokens 10.3 us against
     // 10.9; 12 and 4: 12.5 and 11.7; 4 rows of 8 heads and 6K tokens, 24 and 20: 22.7 and 23.9).  Rows may be shorter than the table is wide, and
-    // clusters do not even them out: not above 24.
-    const int64_t mine = (most_units + n - 1) / n, others = pairs * most_units / ctas > kPagedWarps ? pairs * most_units / ctas : kPagedWarps;
+    // clusters do not even them out: not above 24.  (Warps that share their units take as many times more.)
+    const int64_t mine = (most_units + n - 1) / n * sixteens, all = pairs * most_units / ctas, others = (all > kPagedWarps / sixteens ? all : kPagedWarps / sixteens) * sixteens;
     return mine <= kPagedClusterUnits && mine <= others + kPagedClusterMore ? n : 0;
 }
 struct PagedShare {

@@ -161,7 +161,7 @@ ipkv_status ipkv_paged_attend(const ipkv_attn_shape* sh, const ipkv_paged* c, co
         a.out_lse = lse_part_dev + int64_t(r0) * sh->n_q_heads;
         a.weights_out = weights_out_dev ? weights_out_dev + int64_t(r0) * sh->n_kv_heads * c->slot_stride : nullptr;
         const int64_t pairs = int64_t(n) * plan.n_gh, most = int64_t(kSmCount) * kPagedCtasPerSm;
-        a.cluster = paged_cluster(pairs, plan.most_units, plan.group, int(most));
+        a.cluster = paged_cluster(pairs, plan.most_units, plan.group, plan.sixteens, int(most));
         a.n_ctas = int32_t(a.cluster ? pairs * a.cluster : std::min(most, pairs * plan.most_units));
         if (launch_paged_attend(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return IPKV_ECUDA;
     }

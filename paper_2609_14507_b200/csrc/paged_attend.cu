@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         sm.units = 0; sm.pairs = 0;
     }
     __syncthreads();
-    if (p.cluster > 0) cluster_arrive_relaxed();         // this CTA is there: the others may write to it behind their wait
+    if (p.cluster > 1) cluster_arrive_relaxed();         // this CTA is there: the others may write to it behind their wait
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     PagedPart x;
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         x.row = pair / p.n_gh; x.gh = pair - x.row * p.n_gh;
         x.seen = paged_seen(length_of(p, x.row, x.gh == 0 && rank == 0 && tid == 0), p.window, p.first, U);
         x.u0 = paged_split(x.seen.units, p.cluster, rank); x.u1 = paged_split(x.seen.units, p.cluster, rank + 1);
-        x.whole = false; x.place = 0;
+        x.whole = p.cluster == 1; x.place = 0;
         return true;
     };
     const int T = min(p.c.g.bt, U);              // tokens of a page that a unit takes at once
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
             for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
                 if (!ptx::mbar_wait(ptx::smem_addr(&sm.full[i % kStages]), (i / kStages) & 1)) or_status(p.status, kStatusCopyNotLanded);
         __syncwarp();
-        if (p.cluster > 0) cluster_wait();
+        if (p.cluster > 1) cluster_wait();
         return;
     }
 
@@ -326,7 +326,17 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         const int kv = x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part;
         const int n_heads = min(p.rows_per_part, p.group - in_kv);       // of the part
         const int64_t item0 = int64_t(x.row) * p.n_q_heads + kv * p.group + in_kv;
-        if (x.u0 == x.u1) continue;              // a chunk that ends before the pair's first unit, or a cluster's CTA without one
+        if (x.u0 == x.u1) {                      // a chunk that ends before the pair's first unit, a cluster's CTA without one, or an empty row
+            if (x.whole)
+                for (int i = tid; i < n_heads * D; i += kWarps * 32) {
+                    p.out_o[item0 * D + i] = 0.f;
+                    if (i < n_heads) {
+                        p.out_lse[item0 + i] = -INFINITY;
+                        if (p.head_ml) p.head_ml[item0 + i] = make_float2(0.f, 0.f);
+                    }
+                }
+            continue;
+        }
         {
             const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q + x.row * p.q_row) + (kv * p.group + in_kv) * D;
             const int ha = hg * 16 + (ROWS == 4 ? r0 & 3 : r0), hb = hg * 16 + r0 + 8;
@@ -502,27 +512,38 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
             l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
             l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
         }
-        auto leave = [&](int head, float m, float z) {           // the part's maximum and sum; returns what the sums are divided by
+        auto leave = [&](int head, float m, float z) {           // the part's maximum and sum
             if (x.whole) {
+                const float2 y = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
                 p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
-                if (p.head_ml) p.head_ml[item0 + head] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
+                if (p.head_ml) p.head_ml[item0 + head] = y;
+                if (p.cluster == 1 && head < 16) sm.head_ml[head] = y;
             } else {
                 p.part_ml[int64_t(x.place) * p.rows_per_part + head] = make_float2(m, z);
             }
         };
         float* const out = x.whole ? p.out_o + item0 * D : p.part_o + int64_t(x.place) * p.rows_per_part * D;
-        if (ROWS == 16 && teams == 1) {          // no two warps have the same head
+        if (teams == 1 || (n_units == 1 && sixteens == 1 && p.cluster <= 1)) {       // no two warps have something of the same head
+            if (held >= 0) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int head = hg * 16 + r0 + 8 * h;
-                const float m = h ? m1 : m0, z = h ? l1 : l0, f = !x.whole ? 1.f : z == 0.f ? 0.f : 1.f / z;
-                if (head < n_heads) {
+                for (int h = 0; h < (ROWS == 16 ? 2 : 1); ++h) {
+                    const int head = hg * 16 + r0 + 8 * h;
+                    const bool mine = (ROWS > 4 || r0 < 4) && head < n_heads;
+                    const float m = h ? m1 : m0, z = h ? l1 : l0, f = !x.whole ? 1.f : z == 0.f ? 0.f : 1.f / z;
 #pragma unroll
-                    for (int nt = 0; nt < D / 8; ++nt) *reinterpret_cast<float2*>(out + head * D + nt * 8 + c0) = make_float2(o[nt][2 * h] * f, o[nt][2 * h + 1] * f);
-                    if ((lane & 3) == 0) leave(head, m, z);
+                    for (int nt = 0; nt < D / 8; ++nt) {
+                        float y0 = o[nt][2 * h], y1 = o[nt][2 * h + 1];
+                        if (ROWS < 16) { y0 += o[nt][2]; y1 += o[nt][3]; }       // the pieces' sums
+                        if (ROWS == 4) {
+                            y0 += __shfl_xor_sync(0xffffffffu, y0, 16);
+                            y1 += __shfl_xor_sync(0xffffffffu, y1, 16);
+                        }
+                        if (mine) *reinterpret_cast<float2*>(out + head * D + nt * 8 + c0) = make_float2(y0 * f, y1 * f);
+                    }
+                    if (mine && (lane & 3) == 0) leave(head, m, z);
                 }
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[held]));
             }
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.empty[held]));
             continue;
         }
         if (sixteens > 1 && !meet()) { ok = false; break; }      // the warps of a team have read their unit
@@ -548,7 +569,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
             }
         }
         if (!meet()) { ok = false; break; }
-        if (p.cluster > 0) { cluster_wait(); waited = true; }
+        if (p.cluster > 1) { cluster_wait(); waited = true; }
         for (int i = tid; i < n_heads * (D / 4); i += kWarps * 32) {
             const int head = i / (D / 4), col = i - head * (D / 4), g = ROWS == 16 ? head / 16 : 0, row = ROWS == 16 ? head % 16 : head;
             float2 y[kWarps];
@@ -571,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                     acc.x += f * v[w].x; acc.y += f * v[w].y; acc.z += f * v[w].z; acc.w += f * v[w].w;
                     z += f * y[w].y;
                 }
-            if (p.cluster > 0) {                 // to the CTA that joins these columns; maximum and sum to all
+            if (p.cluster > 1) {                 // to the CTA that joins these columns; maximum and sum to all
                 const int to = i & (p.cluster - 1);
                 put(at_rank(ptx::smem_addr(sm.cum) + (rank * (n_heads * (D / 4) / p.cluster) + i / p.cluster) * 16, to), acc);
                 if (col < p.cluster) put(at_rank(ptx::smem_addr(&sm.part_ml[rank][head]), col), make_float2(m, z));
@@ -594,49 +615,51 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     const int kv = x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part, n_heads = min(p.rows_per_part, p.group - in_kv);
     const int64_t item0 = int64_t(x.row) * p.n_q_heads + kv * p.group + in_kv;
     __syncwarp();
-    if (!waited) {                               // no part, or a lost one
+    if (p.cluster > 1) {
+        if (!waited) {                               // no part, or a lost one
+            cluster_wait();
+            if (tid < 16 * p.cluster) put(at_rank(ptx::smem_addr(&sm.part_ml[rank][tid & 15]), tid >> 4), make_float2(-INFINITY, 0.f));
+        }
+        cluster_arrive();
         cluster_wait();
-        if (tid < 16 * p.cluster) put(at_rank(ptx::smem_addr(&sm.part_ml[rank][tid & 15]), tid >> 4), make_float2(-INFINITY, 0.f));
-    }
-    cluster_arrive();
-    cluster_wait();
-    auto state_of = [&](int head, float2 (&y)[kPagedMostCluster], float& m, float& z) {
-        m = -INFINITY; z = 0.f;
+        auto state_of = [&](int head, float2 (&y)[kPagedMostCluster], float& m, float& z) {
+            m = -INFINITY; z = 0.f;
 #pragma unroll
-        for (int c = 0; c < kPagedMostCluster; ++c) {
-            y[c] = c < p.cluster ? sm.part_ml[c][head] : make_float2(-INFINITY, 0.f);
-            m = fmaxf(m, y[c].x);
-        }
-#pragma unroll
-        for (int c = 0; c < kPagedMostCluster; ++c) {
-            y[c].x = ptx::ex2(y[c].x - (m == -INFINITY ? 0.f : m));
-            if (y[c].y != 0.f) z += y[c].x * y[c].y;
-        }
-    };
-    const int per_cta = n_heads * (D / 4) / p.cluster;
-    for (int k = tid; k < per_cta; k += kWarps * 32) {
-        const int i = k * p.cluster + rank, head = i / (D / 4), col = i - head * (D / 4);
-        float2 y[kPagedMostCluster];
-        float m, z;
-        state_of(head, y, m, z);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int c = 0; c < kPagedMostCluster; ++c)
-            if (c < p.cluster && y[c].y != 0.f) {
-                const float4 v = reinterpret_cast<const float4*>(sm.cum)[c * per_cta + k];
-                acc.x += y[c].x * v.x; acc.y += y[c].x * v.y; acc.z += y[c].x * v.z; acc.w += y[c].x * v.w;
+            for (int c = 0; c < kPagedMostCluster; ++c) {
+                y[c] = c < p.cluster ? sm.part_ml[c][head] : make_float2(-INFINITY, 0.f);
+                m = fmaxf(m, y[c].x);
             }
-        const float inv = z == 0.f ? 0.f : 1.f / z;
-        reinterpret_cast<float4*>(p.out_o + item0 * D)[i] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-        if (col == 0) p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
+#pragma unroll
+            for (int c = 0; c < kPagedMostCluster; ++c) {
+                y[c].x = ptx::ex2(y[c].x - (m == -INFINITY ? 0.f : m));
+                if (y[c].y != 0.f) z += y[c].x * y[c].y;
+            }
+        };
+        const int per_cta = n_heads * (D / 4) / p.cluster;
+        for (int k = tid; k < per_cta; k += kWarps * 32) {
+            const int i = k * p.cluster + rank, head = i / (D / 4), col = i - head * (D / 4);
+            float2 y[kPagedMostCluster];
+            float m, z;
+            state_of(head, y, m, z);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < kPagedMostCluster; ++c)
+                if (c < p.cluster && y[c].y != 0.f) {
+                    const float4 v = reinterpret_cast<const float4*>(sm.cum)[c * per_cta + k];
+                    acc.x += y[c].x * v.x; acc.y += y[c].x * v.y; acc.z += y[c].x * v.z; acc.w += y[c].x * v.w;
+                }
+            const float inv = z == 0.f ? 0.f : 1.f / z;
+            reinterpret_cast<float4*>(p.out_o + item0 * D)[i] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+            if (col == 0) p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
+        }
+        if (p.scores && tid < n_heads) {
+            float2 y[kPagedMostCluster];
+            float m, z;
+            state_of(tid, y, m, z);
+            sm.head_ml[tid] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
+        }
     }
-    if (!p.scores) return;
-    if (tid < n_heads) {
-        float2 y[kPagedMostCluster];
-        float m, z;
-        state_of(tid, y, m, z);
-        sm.head_ml[tid] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
-    }
+    if (!p.scores || p.group > 16) return;       // (more heads of a KV head are not all here: a launch of its own)
     asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");       // (all four warps come here without another wait)
     // the weights of this CTA's units (all heads of the KV head are in one group here)
     const int64_t w0 = (int64_t(x.row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
@@ -811,7 +834,7 @@ cudaError_t launch(const PagedAttend& a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) configured[dev].store(true, std::memory_order_release);
     }
-    if (a.cluster == 0) return launch_overlapped(paged_attend_kernel<D, ROWS>, a.n_ctas, kThreads, smem_bytes(a.c.n_rows), s, a);
+    if (a.cluster <= 1) return launch_overlapped(paged_attend_kernel<D, ROWS>, a.n_ctas, kThreads, smem_bytes(a.cluster ? 0 : a.c.n_rows), s, a);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(a.n_ctas));
     cfg.blockDim = dim3(kThreads);
@@ -846,10 +869,11 @@ cudaError_t launch_paged_attend(const PagedAttend& a, cudaStream_t s) {
                   : rows == 8 ? (wide ? launch<128, 8>(a, s) : launch<64, 8>(a, s))
                               : (wide ? launch<128, 16>(a, s) : launch<64, 16>(a, s));
     if (e != cudaSuccess) return e;
-    if (a.cluster > 0) return cudaSuccess;
-    e = wide ? launch_join<128>(a, s) : launch_join<64>(a, s);
-    if (e != cudaSuccess) return e;
-    if (a.weights_out) {
+    if (a.cluster == 0) {
+        e = wide ? launch_join<128>(a, s) : launch_join<64>(a, s);
+        if (e != cudaSuccess) return e;
+    }
+    if (a.weights_out && (a.cluster == 0 || a.group > 16)) {
         const int64_t pairs = int64_t(a.c.n_rows) * a.c.g.n_kv_heads, groups = (int64_t(a.most_units) * a.unit + 255) / 256;
         const int64_t want = (148 * 32 + pairs - 1) / pairs;             // a few CTAs behind every one that runs
         const int splits = int(want < groups ? want : groups);

@@ -8,7 +8,7 @@ using namespace ipkvi;
 
 extern "C" {
 int shim_paged_most_units(int capacity, int window, int first, int unit) { return int(paged_most_units(capacity, window, first, unit)); }
-int shim_paged_cluster(int pairs, int most_units, int group, int ctas) { return paged_cluster(pairs, most_units, group, ctas); }
+int shim_paged_cluster(int pairs, int most_units, int group, int ctas) { return paged_cluster(pairs, most_units, group, paged_sixteens(group), ctas); }
 int shim_paged_group(int group, int* groups_per_kv, int* rows_per_part, int* sixteens) {
     *groups_per_kv = paged_groups_per_kv(group); *rows_per_part = paged_rows_per_part(group); *sixteens = paged_sixteens(group);
     return paged_rows(group);
