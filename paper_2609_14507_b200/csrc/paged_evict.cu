@@ -70,6 +70,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
     __syncthreads();
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
+    if (tid * 32 < p.c.max_blocks) {             // the row's table comes into the L1 cache meanwhile
+        int32_t unused;
+        asm volatile("ld.global.b32 %0, [%1];" : "=r"(unused) : "l"(p.c.table + row * p.c.table_stride + tid * 32));
+    }
     const int capacity = p.c.max_blocks * p.c.g.bt, b = p.budget;
     int n = p.c.lengths[row];
     if (n < 0 || n > capacity) {
@@ -356,8 +360,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
     int behind0 = sm.count[1][warp] + int(__reduce_add_sync(0xffffffffu, unsigned(lane < rank ? of0 : 0)));
     int holes0 = sm.count[2][warp] + int(__reduce_add_sync(0xffffffffu, unsigned(lane < rank ? of1 : 0)));
     const int moves = int(__reduce_add_sync(0xffffffffu, unsigned(of1)));
-    int32_t* from = p.moved + int64_t(pair) * 2 * p.most_moved;
-    int32_t* into = from + p.most_moved;
+    // the lists: a CTA's own, if short, where its histograms were
+    const bool here = ctas == 1 && moves <= 256;
+    int32_t* from = here ? reinterpret_cast<int32_t*>(sm.hist[0]) : p.moved + int64_t(pair) * 2 * p.most_moved;
+    int32_t* into = here ? reinterpret_cast<int32_t*>(sm.hist[1]) : from + p.most_moved;
     const bool tells = !in_place || kept;        // what stays where it is has to be written, too
     for_kept([&](int i, unsigned keep) {
         const unsigned comes = keep & ~below(i), open = there(i) & ~keep & below(i);
