@@ -534,8 +534,8 @@ ipkv_status ipkv_nibble_attend(const ipkv_attn_shape* shape, int32_t n_rows, con
  * what has to be known of a slot's token moves along (positions_dev, weights_dev; per KV head, since each keeps other tokens).
  * A block may serve several rows as long as no call writes it (a shared prefix). */
 typedef struct {
-  void* pool_dev;               /* n_blocks TILE blocks (ipkv_block_bytes each), 16-byte aligned                        */
-  int64_t n_blocks;
+  void* pool_dev;               /* TILE blocks (ipkv_block_bytes each), 16-byte aligned                                  */
+  int64_t pool_bytes;           /* n_blocks blocks: pool_bytes / ipkv_block_bytes, at least one and below 2^31           */
   const int32_t* table_dev;     /* [n_rows][table_stride]: a row's blocks in the order of its slots; entries behind its length are
                                    not read                                                                             */
   const int32_t* lengths_dev;   /* [n_rows]: slots of the row, 0 .. max_blocks * block_tokens                             */
@@ -551,15 +551,28 @@ typedef struct {
  * is read or written. */
 #define IPKV_STATUS_BAD_PAGE 16u
 
+/* The arguments of a call are a struct: a decode loop makes these calls once a layer, and a foreign-function interface takes its time
+ * for every argument. */
+
 /* Write new tokens.  k_dev, v_dev [n_tokens][n_kv_heads][dim] bf16, 16-byte aligned; *_token_stride: elements between tokens (multiples of 8; 0: dense).
  * row_start_dev: device int32 [n_rows + 1], tokens row_start[r] .. row_start[r+1] are row r's; tokens behind row_start[n_rows] are
  * ignored.  NULL: one token per row (n_tokens == n_rows).  The lengths already count the new tokens: the last new
  * token of a row goes to slot lengths[r] - 1; one that the length does not count is not written (a row of length 0 takes none).
  * positions: token_positions_dev int32 [n_tokens] goes to the slots of all KV heads (required with cache->positions_dev);
  * the slots' weights become 0.  Rows and slots of one call must not share blocks.  Works on the current device. */
-ipkv_status ipkv_paged_append(const ipkv_attn_shape* shape, const ipkv_paged* cache, int64_t n_tokens, const void* k_dev, const void* v_dev,
-                              int64_t k_token_stride, int64_t v_token_stride, const int32_t* row_start_dev,
-                              const int32_t* token_positions_dev, uint32_t* status_dev, void* stream);
+typedef struct {
+  const ipkv_attn_shape* shape;
+  const ipkv_paged* cache;
+  int64_t n_tokens;
+  const void* k_dev;
+  const void* v_dev;
+  int64_t k_token_stride, v_token_stride;
+  const int32_t* row_start_dev;
+  const int32_t* token_positions_dev;
+  uint32_t* status_dev;
+  void* stream;
+} ipkv_paged_append_call;
+ipkv_status ipkv_paged_append(const ipkv_paged_append_call* call);
 
 /* Attention of one query per row over its slots.  window 0: all of them; else slot t of n is visible if t >= n - window or t < first_tokens
  * (a sliding window of the last `window` slots, and first ones that stay visible).  q_dev [n_rows][n_q_heads][dim] bf16, q_row_stride
@@ -572,11 +585,23 @@ ipkv_status ipkv_paged_append(const ipkv_attn_shape* shape, const ipkv_paged* ca
  * scratch_dev: at least ipkv_paged_scratch_bytes (of the same n_rows, max_blocks, window, first_tokens; weigh: weights_out_dev is given),
  * 256-byte aligned, private to this call until its work on `stream` has completed (calls captured into graphs that may run at the same
  * time need scratch of their own).  Results are bit-reproducible.  Works on the current device. */
+typedef struct {
+  const ipkv_attn_shape* shape;
+  const ipkv_paged* cache;
+  const void* q_dev;
+  int64_t q_row_stride;
+  int32_t window, first_tokens;
+  float* weights_out_dev;
+  void* scratch_dev;
+  size_t scratch_bytes;
+  float* o_part_dev;
+  float* lse_part_dev;
+  uint32_t* status_dev;
+  void* stream;
+} ipkv_paged_attend_call;
 ipkv_status ipkv_paged_scratch_bytes(const ipkv_attn_shape* shape, int32_t n_rows, int32_t max_blocks, int32_t window, int32_t first_tokens,
                                      int32_t weigh, size_t* out_bytes);
-ipkv_status ipkv_paged_attend(const ipkv_attn_shape* shape, const ipkv_paged* cache, const void* q_dev, int64_t q_row_stride, int32_t window,
-                              int32_t first_tokens, float* weights_out_dev, void* scratch_dev, size_t scratch_bytes, float* o_part_dev,
-                              float* lse_part_dev, uint32_t* status_dev, void* stream);
+ipkv_status ipkv_paged_attend(const ipkv_paged_attend_call* call);
 
 /* Cut every row to at most `budget` slots, for every KV head by itself.  Of a row's n > budget slots those are kept whose token's position is
  * below first_tokens or among the last `recent` (position > newest - recent, newest: the largest position of the head's slots), then those with the largest weights; a NaN
@@ -587,10 +612,20 @@ ipkv_status ipkv_paged_attend(const ipkv_attn_shape* shape, const ipkv_paged* ca
  * cache's).  kept_dev: NULL, or int32 [n_rows][n_kv_heads][budget]: the slot that each slot's token comes from (the first
  * min(n, budget) of every row are written).  Rows must not share blocks.  scratch_dev as above, at least
  * ipkv_paged_evict_scratch_bytes.  Works on the current device. */
+typedef struct {
+  const ipkv_attn_shape* shape;
+  const ipkv_paged* cache;
+  int32_t budget, first_tokens, recent;
+  float* weights_out_dev;
+  int32_t* positions_out_dev;
+  int32_t* kept_dev;
+  void* scratch_dev;
+  size_t scratch_bytes;
+  uint32_t* status_dev;
+  void* stream;
+} ipkv_paged_evict_call;
 ipkv_status ipkv_paged_evict_scratch_bytes(const ipkv_attn_shape* shape, int32_t n_rows, int32_t max_blocks, int32_t budget, size_t* out_bytes);
-ipkv_status ipkv_paged_evict(const ipkv_attn_shape* shape, const ipkv_paged* cache, int32_t budget, int32_t first_tokens, int32_t recent,
-                             float* weights_out_dev, int32_t* positions_out_dev, int32_t* kept_dev, void* scratch_dev, size_t scratch_bytes,
-                             uint32_t* status_dev, void* stream);
+ipkv_status ipkv_paged_evict(const ipkv_paged_evict_call* call);
 
 #ifdef __cplusplus
 }

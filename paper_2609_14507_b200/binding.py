@@ -93,7 +93,7 @@ class Span(C.Structure):
 
 
 class Paged(C.Structure):
-    _fields_ = [("pool_dev", C.c_void_p), ("n_blocks", C.c_int64), ("table_dev", C.c_void_p), ("lengths_dev", C.c_void_p),
+    _fields_ = [("pool_dev", C.c_void_p), ("pool_bytes", C.c_int64), ("table_dev", C.c_void_p), ("lengths_dev", C.c_void_p),
                 ("n_rows", C.c_int32), ("max_blocks", C.c_int32), ("table_stride", C.c_int64),
                 ("weights_dev", C.c_void_p), ("positions_dev", C.c_void_p), ("slot_stride", C.c_int64)]
 
@@ -156,11 +156,11 @@ def lib():
         "ipkv_nibble_unpack": [C.POINTER(AttnShape), i32, vp, i64, vp, vp, i64, i64, vp],
         "ipkv_nibble_scratch_bytes": [C.POINTER(AttnShape), i32, i32, C.POINTER(C.c_size_t)],
         "ipkv_nibble_attend": [C.POINTER(AttnShape), i32, vp, vp, vp, vp, C.c_size_t, vp, vp, vp, vp],
-        "ipkv_paged_append": [C.POINTER(AttnShape), C.POINTER(Paged), i64, vp, vp, i64, i64, vp, vp, vp, vp],
+        "ipkv_paged_append": [vp],
         "ipkv_paged_scratch_bytes": [C.POINTER(AttnShape), i32, i32, i32, i32, i32, C.POINTER(C.c_size_t)],
-        "ipkv_paged_attend": [C.POINTER(AttnShape), C.POINTER(Paged), vp, i64, i32, i32, vp, vp, C.c_size_t, vp, vp, vp, vp],
+        "ipkv_paged_attend": [vp],
         "ipkv_paged_evict_scratch_bytes": [C.POINTER(AttnShape), i32, i32, i32, C.POINTER(C.c_size_t)],
-        "ipkv_paged_evict": [C.POINTER(AttnShape), C.POINTER(Paged), i32, i32, i32, vp, vp, vp, vp, C.c_size_t, vp, vp],
+        "ipkv_paged_evict": [vp],
         "ipkv_attend_runs_noalloc": [C.POINTER(AttnShape), i32, C.POINTER(Run), C.POINTER(i32), vp, i32, vp, vp, vp, vp],
     }
     L.ipkv_version.restype = C.c_char_p
@@ -771,6 +771,11 @@ def ipkv_nibble_attend(shape, runs, row_start, q, scratch, o_part, lse_part, sta
 
 # ---- a paged cache of bounded length ----
 
+_APPEND_CALL = struct.Struct("<QQqQQqqQQQQ")         # ipkv_paged_append_call
+_ATTEND_CALL = struct.Struct("<QQQqiiQQQQQQQ")       # ipkv_paged_attend_call
+_EVICT_CALL = struct.Struct("<QQiii4xQQQQQQQ")       # ipkv_paged_evict_call
+
+
 def make_paged(shape, pool, table, lengths, weights=None, positions=None):
     """What the ipkv_paged_* calls work on: pool, contiguous, any type, a whole number of TILE blocks of `shape`; table int32 [rows, blocks a row
     at most] (rows any stride apart), lengths int32 [rows]; weights float32 and positions int32 [rows, n_kv_heads, slots], contiguous, at least
@@ -796,64 +801,56 @@ def make_paged(shape, pool, table, lengths, weights=None, positions=None):
                 raise ValueError(f"{name} are contiguous {dtype} [{rows}, {shape.n_kv_heads}, slots] on the device of the pool: got {x.dtype} {tuple(x.shape)}")
     if slots and (slots < per_row * shape.block_tokens or slots % 4):
         raise ValueError(f"{slots} slots: at least {per_row * shape.block_tokens}, a multiple of 4")
-    c = Paged(pool.data_ptr(), pool.nbytes // block, table.data_ptr(), lengths.data_ptr(), rows, per_row, stride, _ptr(weights), _ptr(positions), slots)
-    c._tensors, c._dev, c._slots = (pool, table, lengths, weights, positions), dev, (rows, shape.n_kv_heads, slots or per_row * shape.block_tokens)
-    c.slot_stride = c._slots[2]
+    slots = slots or per_row * shape.block_tokens
+    c = Paged(pool.data_ptr(), pool.nbytes, table.data_ptr(), lengths.data_ptr(), rows, per_row, stride, _ptr(weights), _ptr(positions), slots)
+    c._tensors, c._at, c._dev, c._rows, c._slots = (pool, table, lengths, weights, positions), C.addressof(c), dev, rows, (rows, shape.n_kv_heads, slots)
     return c
 
 
 def _slots_like(x, dtype, cache, name):
     """An output shaped like the cache's weights and positions, as an address."""
     if x is None:
-        return None
+        return 0
     if x.dtype is not dtype or x.shape != cache._slots or not x.is_contiguous() or x.get_device() != cache._dev:
         raise ValueError(f"{name} is contiguous {dtype} {cache._slots} on the device of the pool: got {x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
 
 
 def _status_word(status, dev):
-    if status is None:
-        return None
     if status.get_device() != dev or status.dtype not in (_i32, _torch.uint32):
         raise ValueError("the status word (32 bits) is on the device of the pool")
     return status.data_ptr()
 
 
-def _scratch(scratch, dev):
-    if scratch.get_device() != dev or not scratch.is_contiguous():
-        raise ValueError("scratch is contiguous, on the device of the pool")
-    return scratch.data_ptr(), scratch.nbytes
-
-
 def ipkv_paged_append(shape, cache, k, v, positions=None, row_start=None, status=None, stream=None):
     """Write new tokens k and v [tokens, n_kv_heads, dim] bf16: one per row, or with row_start, int32 [rows + 1] on the device, the tokens
     row_start[r] .. row_start[r + 1] to row r.  cache.lengths count them already.  positions: int32 [tokens]."""
-    heads, dim, size, dev, bf16 = shape.n_kv_heads, shape.dim_qk, k.shape, cache._dev, _bf16
-    n = size[0]
-    if k.dtype is not bf16 or v.dtype is not bf16 or len(size) != 3 or size[1] != heads or size[2] != dim or v.shape != size:
+    size, dev, bf16 = k.shape, cache._dev, _bf16
+    heads, dim = cache._slots[1], shape.dim_qk
+    if k.dtype is not bf16 or v.dtype is not bf16 or len(size) != 3 or size[1] != heads or size[2] != dim or v.shape != size or shape.n_kv_heads != heads:
         raise ValueError(f"K and V are bfloat16 [tokens, {heads}, {dim}]: got {k.dtype} {tuple(size)}, {v.dtype} {tuple(v.shape)}")
-    (kt, kh, kc), (vt, vh, vc) = k.stride(), v.stride()
+    (kt, kh, kc), (vt, vh, vc), n = k.stride(), v.stride(), size[0]
     if n <= 1:                                           # the stride of a dimension of one is never used
         kt = vt = 0
     elif kt == 0 or vt == 0:
         kc = 0
     if kc != 1 or vc != 1 or (heads > 1 and (kh != dim or vh != dim)) or k.get_device() != dev or v.get_device() != dev:
         raise ValueError("the heads of a token lie side by side, its tokens apart, and K and V are on the device of the pool")
-    rs = at = None
+    rs = at = 0
     if row_start is not None:
-        if row_start.dtype is not _i32 or row_start.shape != (cache.n_rows + 1,) or not row_start.is_contiguous() or row_start.get_device() != dev:
-            raise ValueError(f"row_start is contiguous int32 [{cache.n_rows + 1}] on the device of the pool")
+        if row_start.dtype is not _i32 or row_start.shape != (cache._rows + 1,) or not row_start.is_contiguous() or row_start.get_device() != dev:
+            raise ValueError(f"row_start is contiguous int32 [{cache._rows + 1}] on the device of the pool")
         rs = row_start.data_ptr()
-    elif n != cache.n_rows:
-        raise ValueError(f"{n} tokens for {cache.n_rows} rows: row_start says whose they are")
+    elif n != cache._rows:
+        raise ValueError(f"{n} tokens for {cache._rows} rows: row_start says whose they are")
     if positions is not None:
         if positions.dtype is not _i32 or positions.numel() != n or not positions.is_contiguous() or positions.get_device() != dev:
             raise ValueError(f"positions are contiguous int32 [{n}] on the device of the pool")
         at = positions.data_ptr()
-    elif cache.positions_dev and n:
+    elif cache._tensors[4] is not None and n:
         raise ValueError("the cache has positions: the new tokens need theirs")
-    rc = (_lib or lib()).ipkv_paged_append(C.byref(shape), C.byref(cache), n, k.data_ptr(), v.data_ptr(), kt, vt, rs, at, _status_word(status, dev),
-                                           _call_stream(stream, dev))
+    rc = (_lib or lib()).ipkv_paged_append(_APPEND_CALL.pack(C.addressof(shape), cache._at, n, k.data_ptr(), v.data_ptr(), kt, vt, rs, at,
+                                                             0 if status is None else _status_word(status, dev), _call_stream(stream, dev) or 0))
     if rc != OK:
         raise IpkvError(rc, "ipkv_paged_append")
 
@@ -869,8 +866,10 @@ def ipkv_paged_scratch_bytes(shape, cache, window=0, first=0, weigh=False):
 def ipkv_paged_attend(shape, cache, q, scratch, o_part, lse_part, window=0, first=0, weights_out=None, status=None, stream=None):
     """Attention of one query per row, q [rows, n_q_heads, dim] bf16 (rows any stride apart), over the row's slots: all, or with a window the last `window` and the
     `first` first ones.  weights_out: where the cache's weights go with this call's softmax weights added (may be the cache's own)."""
-    dev, f32, heads = cache._dev, _f32, shape.n_q_heads
-    want = (cache.n_rows, heads, shape.dim_qk)
+    dev, f32, heads, rows = cache._dev, _f32, shape.n_q_heads, cache._rows
+    want = (rows, heads, shape.dim_qk)
+    if shape.n_kv_heads != cache._slots[1]:
+        raise ValueError(f"the cache has {cache._slots[1]} KV heads, the shape {shape.n_kv_heads}")
     if (q.dtype is not _bf16 or o_part.dtype is not f32 or lse_part.dtype is not f32 or q.shape != want or o_part.shape != want or lse_part.shape != want[:2]
             or not (o_part.is_contiguous() and lse_part.is_contiguous()) or q.get_device() != dev or o_part.get_device() != dev or lse_part.get_device() != dev):
         raise ValueError(f"q is bfloat16 {want}, o_part float32 {want} and lse_part float32 {want[:2]}, contiguous, on the device of the pool: got "
@@ -878,13 +877,16 @@ def ipkv_paged_attend(shape, cache, q, scratch, o_part, lse_part, window=0, firs
     qt, qh, qc = q.stride()
     if qc != 1 or (heads > 1 and qh != want[2]):
         raise ValueError("the heads of a query lie side by side")
-    if want[0] <= 1:
+    if rows <= 1:                                        # the stride of a dimension of one is never used
         qt = 0
     elif qt == 0:
         raise ValueError("the queries of two rows lie apart")
-    at, size = _scratch(scratch, dev)
-    rc = (_lib or lib()).ipkv_paged_attend(C.byref(shape), C.byref(cache), q.data_ptr(), qt, window, first, _slots_like(weights_out, f32, cache, "weights_out"),
-                                           at, size, o_part.data_ptr(), lse_part.data_ptr(), _status_word(status, dev), _call_stream(stream, dev))
+    if scratch.get_device() != dev or not scratch.is_contiguous():
+        raise ValueError("scratch is contiguous, on the device of the pool")
+    rc = (_lib or lib()).ipkv_paged_attend(_ATTEND_CALL.pack(C.addressof(shape), cache._at, q.data_ptr(), qt, window, first,
+                                                             0 if weights_out is None else _slots_like(weights_out, f32, cache, "weights_out"), scratch.data_ptr(), scratch.nbytes,
+                                                             o_part.data_ptr(), lse_part.data_ptr(), 0 if status is None else _status_word(status, dev),
+                                                             _call_stream(stream, dev) or 0))
     if rc != OK:
         raise IpkvError(rc, "ipkv_paged_attend")
 
@@ -901,11 +903,17 @@ def ipkv_paged_evict(shape, cache, budget, first, recent, scratch, weights_out=N
     """Cut every row to at most `budget` slots per KV head: the `first` first and the `recent` most recent tokens stay, of the others
     those with the largest weights.  cache.lengths stay as they are: the caller sets them to min(length, budget) after all layers."""
     dev = cache._dev
-    if kept is not None and (kept.dtype is not _i32 or kept.shape != (cache.n_rows, shape.n_kv_heads, budget) or not kept.is_contiguous() or kept.get_device() != dev):
-        raise ValueError(f"kept is contiguous int32 {(cache.n_rows, shape.n_kv_heads, budget)} on the device of the pool")
-    at, size = _scratch(scratch, dev)
-    rc = (_lib or lib()).ipkv_paged_evict(C.byref(shape), C.byref(cache), budget, first, recent, _slots_like(weights_out, _f32, cache, "weights_out"),
-                                          _slots_like(positions_out, _i32, cache, "positions_out"), _ptr(kept), at, size, _status_word(status, dev),
-                                          _call_stream(stream, dev))
+    if shape.n_kv_heads != cache._slots[1]:
+        raise ValueError(f"the cache has {cache._slots[1]} KV heads, the shape {shape.n_kv_heads}")
+    at = 0
+    if kept is not None:
+        if kept.dtype is not _i32 or kept.shape != (*cache._slots[:2], budget) or not kept.is_contiguous() or kept.get_device() != dev:
+            raise ValueError(f"kept is contiguous int32 {(*cache._slots[:2], budget)} on the device of the pool")
+        at = kept.data_ptr()
+    if scratch.get_device() != dev or not scratch.is_contiguous():
+        raise ValueError("scratch is contiguous, on the device of the pool")
+    rc = (_lib or lib()).ipkv_paged_evict(_EVICT_CALL.pack(C.addressof(shape), cache._at, budget, first, recent, _slots_like(weights_out, _f32, cache, "weights_out"),
+                                                           _slots_like(positions_out, _i32, cache, "positions_out"), at, scratch.data_ptr(), scratch.nbytes,
+                                                           0 if status is None else _status_word(status, dev), _call_stream(stream, dev) or 0))
     if rc != OK:
         raise IpkvError(rc, "ipkv_paged_evict")

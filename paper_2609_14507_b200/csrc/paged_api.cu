@@ -24,9 +24,10 @@ bool shape_ok(const ipkv_attn_shape* sh) {
 bool capacity_ok(const ipkv_attn_shape* sh, int32_t n_rows, int32_t max_blocks) {
     return n_rows >= 0 && max_blocks >= 1 && int64_t(max_blocks) * sh->block_tokens <= INT32_MAX - 4 * kTileTokens;
 }
+BlockGeom geom(const ipkv_attn_shape* sh) { return BlockGeom{sh->n_kv_heads, sh->dim_qk, sh->dim_v, sh->block_tokens}; }
 bool cache_ok(const ipkv_attn_shape* sh, const ipkv_paged* c) {
     if (!shape_ok(sh) || !c || !capacity_ok(sh, c->n_rows, c->max_blocks)) return false;
-    if (!c->pool_dev || !aligned(c->pool_dev, 16) || c->n_blocks < 1 || c->n_blocks > INT32_MAX) return false;
+    if (!c->pool_dev || !aligned(c->pool_dev, 16) || c->pool_bytes < geom(sh).block_bytes() || c->pool_bytes / geom(sh).block_bytes() > INT32_MAX) return false;
     if (!c->table_dev || !aligned(c->table_dev, 4) || !c->lengths_dev || !aligned(c->lengths_dev, 4)) return false;
     if (c->table_stride < c->max_blocks || c->table_stride > (int64_t(1) << 40)) return false;
     if (c->weights_dev || c->positions_dev) {
@@ -37,8 +38,8 @@ bool cache_ok(const ipkv_attn_shape* sh, const ipkv_paged* c) {
 }
 PagedCache cache_of(const ipkv_attn_shape* sh, const ipkv_paged* c) {
     PagedCache p;
-    p.g = BlockGeom{sh->n_kv_heads, sh->dim_qk, sh->dim_v, sh->block_tokens};
-    p.pool = static_cast<char*>(c->pool_dev); p.n_blocks = c->n_blocks;
+    p.g = geom(sh);
+    p.pool = static_cast<char*>(c->pool_dev); p.n_blocks = c->pool_bytes / p.g.block_bytes();
     p.table = c->table_dev; p.lengths = c->lengths_dev; p.table_stride = c->table_stride; p.slot_stride = c->slot_stride;
     p.weights = c->weights_dev; p.positions = c->positions_dev;
     p.n_rows = c->n_rows; p.max_blocks = c->max_blocks;
@@ -88,9 +89,9 @@ bool window_ok(int32_t window, int32_t first) { return window >= 0 && first >= 0
 
 extern "C" {
 
-ipkv_status ipkv_paged_append(const ipkv_attn_shape* sh, const ipkv_paged* c, int64_t n_tokens, const void* k_dev, const void* v_dev,
-                              int64_t k_token_stride, int64_t v_token_stride, const int32_t* row_start_dev,
-                              const int32_t* token_positions_dev, uint32_t* status_dev, void* stream) {
+ipkv_status ipkv_paged_append(const ipkv_paged_append_call* call) {
+    if (!call) return IPKV_EINVAL;
+    const auto [sh, c, n_tokens, k_dev, v_dev, k_token_stride, v_token_stride, row_start_dev, token_positions_dev, status_dev, stream] = *call;
     if (!cache_ok(sh, c) || n_tokens < 0 || n_tokens > INT32_MAX) return IPKV_EINVAL;
     const int64_t row = int64_t(sh->n_kv_heads) * sh->dim_qk;
     for (int64_t stride : {k_token_stride, v_token_stride})
@@ -116,9 +117,9 @@ ipkv_status ipkv_paged_scratch_bytes(const ipkv_attn_shape* sh, int32_t n_rows, 
     return IPKV_OK;
 }
 
-ipkv_status ipkv_paged_attend(const ipkv_attn_shape* sh, const ipkv_paged* c, const void* q_dev, int64_t q_row_stride, int32_t window,
-                              int32_t first_tokens, float* weights_out_dev, void* scratch_dev, size_t scratch_bytes, float* o_part_dev,
-                              float* lse_part_dev, uint32_t* status_dev, void* stream) {
+ipkv_status ipkv_paged_attend(const ipkv_paged_attend_call* call) {
+    if (!call) return IPKV_EINVAL;
+    const auto [sh, c, q_dev, q_row_stride, window, first_tokens, weights_out_dev, scratch_dev, scratch_bytes, o_part_dev, lse_part_dev, status_dev, stream] = *call;
     if (!cache_ok(sh, c) || !window_ok(window, first_tokens)) return IPKV_EINVAL;
     if (!(sh->softmax_scale >= 0.f) || std::isinf(sh->softmax_scale)) return IPKV_EINVAL;
     const int64_t row = int64_t(sh->n_q_heads) * sh->dim_qk;
@@ -175,9 +176,9 @@ ipkv_status ipkv_paged_evict_scratch_bytes(const ipkv_attn_shape* sh, int32_t n_
     return IPKV_OK;
 }
 
-ipkv_status ipkv_paged_evict(const ipkv_attn_shape* sh, const ipkv_paged* c, int32_t budget, int32_t first_tokens, int32_t recent,
-                             float* weights_out_dev, int32_t* positions_out_dev, int32_t* kept_dev, void* scratch_dev, size_t scratch_bytes,
-                             uint32_t* status_dev, void* stream) {
+ipkv_status ipkv_paged_evict(const ipkv_paged_evict_call* call) {
+    if (!call) return IPKV_EINVAL;
+    const auto [sh, c, budget, first_tokens, recent, weights_out_dev, positions_out_dev, kept_dev, scratch_dev, scratch_bytes, status_dev, stream] = *call;
     if (!cache_ok(sh, c) || budget < 1 || first_tokens < 0 || recent < 0 || int64_t(first_tokens) + recent > budget) return IPKV_EINVAL;
     if (!c->weights_dev || !c->positions_dev) return IPKV_EINVAL;
     if (!aligned(weights_out_dev, 16) || !aligned(positions_out_dev, 16) || !aligned(kept_dev, 4) || !aligned(status_dev, 4)) return IPKV_EINVAL;

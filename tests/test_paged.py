@@ -21,22 +21,44 @@ def shape_of(hq, hkv, d, bt, scale=0.0, kind=binding.GQA, dv=None):
 # ---- refusals --------------------------------------------------------------------------------------------------------
 
 def struct(**kw):
-    c = dict(pool_dev=BASE, n_blocks=10, table_dev=BASE, lengths_dev=BASE, n_rows=2, max_blocks=4, table_stride=4, weights_dev=BASE, positions_dev=BASE,
+    c = dict(pool_dev=BASE, pool_bytes=10 << 17, table_dev=BASE, lengths_dev=BASE, n_rows=2, max_blocks=4, table_stride=4, weights_dev=BASE, positions_dev=BASE,
              slot_stride=256)
     c.update(kw)
     return binding.Paged(**c)
 
 
 def append_rc(sh, c, n=2, k=BASE, v=BASE, ks=0, vs=0, start=None, at=BASE, status=None):
-    return binding.lib().ipkv_paged_append(C.byref(sh), C.byref(c), n, k, v, ks, vs, start, at, status, None)
+    return binding.lib().ipkv_paged_append(binding._APPEND_CALL.pack(C.addressof(sh), C.addressof(c), n, k or 0, v or 0, ks, vs, start or 0, at or 0, status or 0, 0))
 
 
 def attend_rc(sh, c, q=BASE, qs=0, window=0, first=0, w=None, scratch=BASE, size=1 << 40, o=BASE, lse=BASE, status=None):
-    return binding.lib().ipkv_paged_attend(C.byref(sh), C.byref(c), q, qs, window, first, w, scratch, size, o, lse, status, None)
+    return binding.lib().ipkv_paged_attend(binding._ATTEND_CALL.pack(C.addressof(sh), C.addressof(c), q or 0, qs, window, first, w or 0, scratch or 0, size, o or 0, lse or 0,
+                                                                     status or 0, 0))
 
 
 def evict_rc(sh, c, budget=100, first=4, recent=10, w=None, pos=None, kept=None, scratch=BASE, size=1 << 40, status=None):
-    return binding.lib().ipkv_paged_evict(C.byref(sh), C.byref(c), budget, first, recent, w, pos, kept, scratch, size, status, None)
+    return binding.lib().ipkv_paged_evict(binding._EVICT_CALL.pack(C.addressof(sh), C.addressof(c), budget, first, recent, w or 0, pos or 0, kept or 0, scratch or 0, size,
+                                                                   status or 0, 0))
+
+
+def test_the_packed_arguments_are_the_structs_of_the_header(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "sz.c"
+    last = {"ipkv_paged": "slot_stride", "ipkv_paged_append_call": "stream", "ipkv_paged_attend_call": "stream", "ipkv_paged_evict_call": "stream"}
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "ipkv.h"\nint main(void){'
+                   + "".join(f'printf("%zu %zu ", sizeof({t}), offsetof({t}, {m}));' for t, m in last.items())
+                   + 'printf("%zu %zu\\n", offsetof(ipkv_paged_attend_call, weights_out_dev), offsetof(ipkv_paged_evict_call, weights_out_dev));return 0;}\n')
+    exe = tmp_path / "sz"
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    want = [C.sizeof(binding.Paged), binding.Paged.slot_stride.offset]
+    for s in (binding._APPEND_CALL, binding._ATTEND_CALL, binding._EVICT_CALL):
+        want += [s.size, s.size - 8]
+    assert got == want + [40, 32]
+    for call in (binding.lib().ipkv_paged_append, binding.lib().ipkv_paged_attend, binding.lib().ipkv_paged_evict):
+        assert call(None) == EINVAL
 
 
 @pytest.mark.parametrize("sh", [shape_of(32, 5, 128, 64), shape_of(32, 4, 96, 64), shape_of(32, 4, 256, 64), shape_of(32, 4, 128, 8), shape_of(32, 4, 128, 48),
@@ -52,7 +74,7 @@ def test_shapes_without_the_operators_are_refused(sh):
 
 def test_bad_caches_are_refused():
     sh = shape_of(32, 4, 128, 64)
-    for kw in (dict(pool_dev=None), dict(pool_dev=BASE + 8), dict(n_blocks=0), dict(n_blocks=-1), dict(n_blocks=1 << 31), dict(table_dev=None),
+    for kw in (dict(pool_dev=None), dict(pool_dev=BASE + 8), dict(pool_bytes=0), dict(pool_bytes=-1), dict(pool_bytes=(1 << 17) - 1), dict(pool_bytes=1 << 48), dict(table_dev=None),
                dict(table_dev=BASE + 2), dict(lengths_dev=None), dict(lengths_dev=BASE + 1), dict(n_rows=-1), dict(max_blocks=0), dict(max_blocks=-3),
                dict(max_blocks=1 << 26, table_stride=1 << 26), dict(table_stride=3), dict(weights_dev=BASE + 4), dict(positions_dev=BASE + 8),
                dict(slot_stride=255), dict(slot_stride=252), dict(slot_stride=258)):
@@ -104,7 +126,7 @@ def test_the_binding_refuses_other_types_and_shapes():
         with pytest.raises(ValueError):
             binding.make_paged(sh, *a)
     c = binding.make_paged(sh, pool, table, lengths, w, pos)
-    assert (c.n_blocks, c.n_rows, c.max_blocks, c.table_stride, c.slot_stride) == (3, 2, 3, 3, 192)
+    assert (c.pool_bytes, c.n_rows, c.max_blocks, c.table_stride, c.slot_stride) == (3 * 32768, 2, 3, 3, 192)
     wide = binding.make_paged(sh, pool, torch.zeros((2, 7), dtype=torch.int32)[:, 2:5], lengths)
     assert wide.table_stride == 7 and wide.slot_stride == 192
     k = torch.zeros((2, 2, 64), dtype=torch.bfloat16)
@@ -125,6 +147,11 @@ def test_the_binding_refuses_other_types_and_shapes():
     for kw in (dict(weights_out=pos), dict(positions_out=w), dict(kept=torch.zeros((2, 2, 9), dtype=torch.int32)), dict(kept=torch.zeros((2, 2, 10)))):
         with pytest.raises(ValueError):
             binding.ipkv_paged_evict(sh, c, 10, 0, 0, scratch, **kw)
+    other = shape_of(4, 4, 64, 64)                       # more KV heads than the cache has
+    for call in (lambda: binding.ipkv_paged_append(other, c, k.repeat(1, 2, 1), k.repeat(1, 2, 1), positions=at), lambda: binding.ipkv_paged_attend(other, c, q, scratch, o, lse),
+                 lambda: binding.ipkv_paged_evict(other, c, 10, 0, 0, scratch)):
+        with pytest.raises(ValueError):
+            call()
     for call in (lambda: binding.ipkv_paged_append(sh, c, k, k, positions=at), lambda: binding.ipkv_paged_attend(sh, c, q, scratch, o, lse),
                  lambda: binding.ipkv_paged_evict(sh, c, 10, 0, 0, scratch)):
         with pytest.raises(ValueError, match="on device -1"):            # refused for nothing but being on the host
