@@ -32,11 +32,16 @@ namespace {
 constexpr int kWarps = kPagedWarps, kThreads = (kWarps + 1) * 32;
 constexpr float kLn2 = 0.6931471805599453f;
 
-constexpr int kStages = 6, kRing = kStages * kPagedUnitBytes;
+struct Part : PagedPart {
+    int32_t kv, in_kv, n_heads;                  // the KV head, the first of its query heads, how many
+};
+constexpr int kMostStages = 6, kRing = kMostStages * kPagedUnitBytes;
 
 struct Smem {
-    uint64_t full[kStages], empty[kStages], met;
-    uint32_t tag[kStages];                       // of a stage: which unit of the CTA's (times 16); bit i: its tokens 16 i .. 16 i + 15 are there
+    uint64_t full[kMostStages], empty[kMostStages], met;
+    PagedParts parts[kWarps + 1];                // every warp's; registers are short
+    Part part[kWarps + 1];
+    uint32_t tag[kMostStages];                       // of a stage: which unit of the CTA's (times 16); bit i: its tokens 16 i .. 16 i + 15 are there
     float2 ml[kWarps * 16];                      // maximum and sum of every warp's rows
     int32_t where[kWarps];                       // the stage that holds a warp's sums
     int32_t scan[kThreads / 32];
@@ -190,6 +195,9 @@ __device__ PagedShare share_out(const PagedAttend& p, Smem& sm, int teams) {
 template <int D, int ROWS>
 __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel(const __grid_constant__ PagedAttend p) {
     constexpr int U = kPagedUnitBytes / (4 * D), kSlices = U / 16;
+    // 16 rows of queries are read from shared memory for every unit, each warp's in the place of a stage: with them in registers, too, some 20 others
+    // were reloaded in every unit (64 heads on 2 KV heads, 4 rows of 50K tokens: 64 us).
+    constexpr int kStages = ROWS == 16 ? kMostStages - 1 : kMostStages;
     extern __shared__ unsigned char smem_dyn[];
     unsigned char* ring = smem_dyn + ((1024u - (ptx::smem_addr(smem_dyn) & 1023u)) & 1023u);      // 1024: rows of a panel on distinct banks
     Smem& sm = *reinterpret_cast<Smem*>(ring + kRing);
@@ -210,17 +218,45 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     if (p.cluster > 1) cluster_arrive_relaxed();         // this CTA is there: the others may write to it behind their wait
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    PagedPart x;
-    PagedParts parts{sm.cum, sm.n, PagedShare{0, 0, 0}, p.c.n_rows, p.n_gh, p.window, p.first, U, int(blockIdx.x), 0, 0};
-    if (p.cluster == 0) parts.share = share_out(p, sm, teams);
-    auto begin = [&]() {
-        if (p.cluster == 0) return parts.begin(x);
-        const int pair = int(blockIdx.x) / p.cluster, rank = int(blockIdx.x) - pair * p.cluster;
-        x.row = pair / p.n_gh; x.gh = pair - x.row * p.n_gh;
-        x.seen = paged_seen(length_of(p, x.row, x.gh == 0 && rank == 0 && tid == 0), p.window, p.first, U);
-        x.u0 = paged_split(x.seen.units, p.cluster, rank); x.u1 = paged_split(x.seen.units, p.cluster, rank + 1);
-        x.whole = p.cluster == 1; x.place = 0;
-        return true;
+    PagedShare share{0, 0, 0};
+    if (p.cluster == 0) share = share_out(p, sm, teams);
+    // Where registers are short (128 columns), a warp's part is kept in shared memory, by its first lane.
+    constexpr bool kLocal = D == 64;
+    Part local_part;
+    PagedParts local_parts;
+    Part& x = kLocal ? local_part : sm.part[warp];
+    PagedParts& parts = kLocal ? local_parts : sm.parts[warp];
+    auto heads = [&](bool more) {                // of the part that has just been found
+        const int kv = p.groups_per_kv == 1 ? x.gh : x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part;
+        x.kv = kv; x.in_kv = in_kv; x.n_heads = min(p.rows_per_part, p.group - in_kv);
+        return more;
+    };
+    auto begin = [&]() {                         // the warp's first part (next one)
+        bool more = true;
+        if (kLocal || lane == 0) {
+            if (p.cluster == 0) {
+                parts = PagedParts{sm.cum, sm.n, share, p.c.n_rows, p.n_gh, p.window, p.first, U, int(blockIdx.x), 0, 0};
+                more = parts.begin(x);
+            } else {
+                const int pair = int(blockIdx.x) / p.cluster, rank = int(blockIdx.x) - pair * p.cluster;
+                x.row = pair / p.n_gh; x.gh = pair - x.row * p.n_gh;
+                const PagedSeen seen = paged_seen(length_of(p, x.row, x.gh == 0 && rank == 0 && tid == 0), p.window, p.first, U);
+                x.seen = seen;
+                x.u0 = paged_split(seen.units, p.cluster, rank); x.u1 = paged_split(seen.units, p.cluster, rank + 1);
+                x.whole = p.cluster == 1; x.place = 0;
+                parts.at = parts.end = 0;
+            }
+            more = heads(more);
+        }
+        __syncwarp();
+        return kLocal ? more : __shfl_sync(0xffffffffu, int(more), 0) != 0;
+    };
+    auto next = [&]() {
+        bool more = false;
+        __syncwarp();
+        if ((kLocal || lane == 0) && parts.at < parts.end) more = heads(parts.next(x));
+        __syncwarp();
+        return kLocal ? more : __shfl_sync(0xffffffffu, int(more), 0) != 0;
     };
     const int T = min(p.c.g.bt, U);              // tokens of a page that a unit takes at once
 
@@ -240,27 +276,29 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 asm volatile("ld.global.b32 %0, [%1];" : "=r"(unused) : "l"(p.c.table + (first + row) * p.c.table_stride + (lane - row * lines) * 32));
             }
         }
-        for (bool more = begin(); more && ok; more = parts.next(x)) {
+        for (bool more = begin(); more && ok; more = next()) {
             const int32_t* table = p.c.table + int64_t(x.row) * p.c.table_stride;
-            const char* head = p.c.pool + (x.gh / p.groups_per_kv) * head_bytes;
+            const char* head = p.c.pool + x.kv * head_bytes;
+            const PagedSeen seen = x.seen;
+            const int u0 = x.u0, u1 = x.u1;
             // lane l: the page of unit j + l / per_unit, its part l % per_unit; -1: nothing of it is seen, -2: a bad one
             auto page_of = [&](int j) {
                 const int u = j + lane / per_unit;
                 int page = -1;
-                if (u < x.u1) {
-                    const int a = x.seen.unit(u) * U + (lane % per_unit) * T;
-                    if (x.seen.sees_any(a, a + T)) {
+                if (u < u1) {
+                    const int a = seen.unit(u) * U + (lane % per_unit) * T;
+                    if (seen.sees_any(a, a + T)) {
                         page = table[p.bt_shift >= 0 ? a >> p.bt_shift : a / p.c.g.bt];
                         if (page < 0 || page >= p.c.n_blocks) { or_status(p.status, kStatusBadPage); page = -2; }
                     }
                 }
                 return page;
             };
-            int page = page_of(x.u0);
-            for (int j0 = x.u0; j0 < x.u1 && ok; j0 += batch) {
+            int page = page_of(u0);
+            for (int j0 = u0; j0 < u1 && ok; j0 += batch) {
                 const int pages = page;
-                if (j0 + batch < x.u1) page = page_of(j0 + batch);
-                for (int j = j0; j < min(j0 + batch, x.u1); ++j) {
+                if (j0 + batch < u1) page = page_of(j0 + batch);
+                for (int j = j0; j < min(j0 + batch, u1); ++j) {
                     if (lap > 0) ok = ptx::mbar_wait(ptx::smem_addr(&sm.empty[st]), (lap - 1) & 1);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
@@ -285,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                     } else {
                         const int64_t at = __shfl_sync(0xffffffffu, pages, lane0);
                         if (there && lane < D / 32) {            // a panel a lane, of K, then of V
-                            const char* src = head + at * block_bytes + (int64_t(lane) * p.c.g.bt + (p.bt_shift >= 0 ? x.seen.unit(j) * U & (p.c.g.bt - 1) : x.seen.unit(j) * U % p.c.g.bt)) * 128;
+                            const char* src = head + at * block_bytes + (int64_t(lane) * p.c.g.bt + (p.bt_shift >= 0 ? seen.unit(j) * U & (p.c.g.bt - 1) : seen.unit(j) * U % p.c.g.bt)) * 128;
                             ptx::bulk_g2s_hint(dst + lane * (U * 128), ptx::checked_src<kChecked>(src, U * 128, p.c.pool, extent, p.status, kStatusBadIndex), U * 128,
                                                bar, pol);
                         }
@@ -311,7 +349,8 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     const int r0 = lane >> 2, c0 = 2 * (lane & 3);
     // offsets in a stage: panels, V, slices of 16 tokens (a page's K and V lie together)
     const uint32_t panel = uint32_t(T) * 128, v_off = uint32_t(T) * D * 2, odd = T == 16 ? 16u * D * 4 : 2048u, pair = T >= 64 ? 4096u : 32u * D * 4;
-    uint32_t qa[D / 16][4];
+    const uint32_t s_q = s_ring + kStages * kPagedUnitBytes + warp * 4096;       // ROWS == 16
+    uint32_t qa[ROWS == 16 ? 1 : D / 16][2];
     float o[D / 8][4];
     const int rank = p.cluster > 0 ? int(blockIdx.x) % p.cluster : 0;
     int it0 = 0, meets = 0;                      // units of the parts before this one
@@ -321,13 +360,13 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.met));
         return ptx::mbar_wait(ptx::smem_addr(&sm.met), meets++ & 1, 2 * ptx::kWaitLimitNs);
     };
+    auto item_of = [&]() { return int64_t(x.row) * p.n_q_heads + x.kv * p.group + x.in_kv; };      // of the outputs
 
-    for (bool more = begin(); more && ok; more = parts.next(x)) {
-        const int kv = x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part;
-        const int n_heads = min(p.rows_per_part, p.group - in_kv);       // of the part
-        const int64_t item0 = int64_t(x.row) * p.n_q_heads + kv * p.group + in_kv;
+    for (bool more = begin(); more && ok; more = next()) {
         if (x.u0 == x.u1) {                      // a chunk that ends before the pair's first unit, a cluster's CTA without one, or an empty row
-            if (x.whole)
+            if (x.whole) {
+                const int n_heads = x.n_heads;
+                const int64_t item0 = item_of();
                 for (int i = tid; i < n_heads * D; i += kWarps * 32) {
                     p.out_o[item0 * D + i] = 0.f;
                     if (i < n_heads) {
@@ -335,36 +374,47 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                         if (p.head_ml) p.head_ml[item0 + i] = make_float2(0.f, 0.f);
                     }
                 }
+            }
             continue;
         }
         {
-            const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q + x.row * p.q_row) + (kv * p.group + in_kv) * D;
-            const int ha = hg * 16 + (ROWS == 4 ? r0 & 3 : r0), hb = hg * 16 + r0 + 8;
-            const uint32_t* qa0 = reinterpret_cast<const uint32_t*>(q + ha * D + c0);
-            const uint32_t* qa1 = reinterpret_cast<const uint32_t*>(q + hb * D + c0);
+            const int n_heads = x.n_heads;
+            const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q + x.row * p.q_row) + (x.kv * p.group + x.in_kv) * D;
+            if (ROWS == 16) {
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                qa[ks][0] = ha < n_heads ? qa0[ks * 8] : 0u;
-                qa[ks][2] = ha < n_heads ? qa0[ks * 8 + 4] : 0u;
-                qa[ks][1] = ROWS == 16 ? (hb < n_heads ? qa1[ks * 8] : 0u) : 0u;
-                qa[ks][3] = ROWS == 16 ? (hb < n_heads ? qa1[ks * 8 + 4] : 0u) : 0u;
+                for (int k = 0; k < D / 16; ++k) {
+                    const int row = (k * 32 + lane) / (D / 8), chunk = lane % (D / 8), head = hg * 16 + row;
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (head < n_heads) v = *reinterpret_cast<const uint4*>(q + head * D + chunk * 8);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                 ::"r"(s_q + row * (D * 2) + ((chunk & 8) << 4) + (((chunk ^ row) & 7) << 4)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                }
+                __syncwarp();
+            } else {
+                const int head = ROWS == 4 ? r0 & 3 : r0;
+                const uint32_t* from = reinterpret_cast<const uint32_t*>(q + head * D + c0);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    qa[ks][0] = head < n_heads ? from[ks * 8] : 0u;
+                    qa[ks][1] = head < n_heads ? from[ks * 8 + 4] : 0u;
+                }
             }
         }
 #pragma unroll
         for (int nt = 0; nt < D / 8; ++nt) { o[nt][0] = o[nt][1] = o[nt][2] = o[nt][3] = 0.f; }
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-        float* scores = p.scores ? p.scores + (int64_t(x.row) * p.n_gh + x.gh) * p.most_units * (U * p.rows_per_part) + hg * (ROWS * 16) : nullptr;
+        float* scores = p.scores ? p.scores + ((int64_t(x.row) * p.n_gh + x.gh) * p.most_units + x.u0) * (U * p.rows_per_part) + hg * (ROWS * 16) : nullptr;
         const int n_units = x.u1 - x.u0;
         int held = -1;                           // the stage of this warp's last unit
 
         for (int i = (team - it0 % teams + teams) % teams; i < n_units; i += teams) {
-            const int it = it0 + i, st = it % kStages, lap = it / kStages;
+            const int it = it0 + i, st = it % kStages;
             uint32_t there;
-            if (!wait_tag(&sm.tag[st], uint32_t(it), there) || !ptx::mbar_wait(ptx::smem_addr(&sm.full[st]), lap & 1)) {
+            if (!wait_tag(&sm.tag[st], uint32_t(it), there) || !ptx::mbar_wait(ptx::smem_addr(&sm.full[st]), (it / kStages) & 1)) {
                 ok = false;
                 break;
             }
-            const int u = x.seen.unit(x.u0 + i), ta = u * U;
+            const int ta = x.seen.unit(x.u0 + i) * U;
             const uint32_t stage = s_ring + st * kPagedUnitBytes;
             auto slice = [&](int sl) { return stage + (sl & 1) * odd + (sl >> 1) * pair; };
             float s[2 * kSlices][4];
@@ -373,12 +423,19 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
                 const int chunk = ks * 2 + (mi & 1);             // K: matrices 0, 1 tokens 0-7 of a slice, 2, 3 tokens 8-15
+                uint32_t q[4] = {0u, 0u, 0u, 0u};
+                if (ROWS == 16) {                                // queries: matrices 0, 2 rows 0-7, 1, 3 rows 8-15
+                    const int at = ks * 2 + (mi >> 1);
+                    ptx::ldmatrix_x4(s_q + ((mi & 1) * 8 + r8) * (D * 2) + ((at & 8) << 4) + (((at ^ r8) & 7) << 4), q[0], q[1], q[2], q[3]);
+                } else {
+                    q[0] = qa[ks][0]; q[2] = qa[ks][1];
+                }
 #pragma unroll
                 for (int sl = 0; sl < kSlices; ++sl) {
                     uint32_t b0, b1, b2, b3;
                     ptx::ldmatrix_x4(slice(sl) + ((mi >> 1) * 8 + r8) * 128 + (ks >= 4 ? panel : 0u) + (((chunk & 7) ^ r8) << 4), b0, b1, b2, b3);
-                    ptx::mma_bf16(s[2 * sl], qa[ks], b0, b1);
-                    ptx::mma_bf16(s[2 * sl + 1], qa[ks], b2, b3);
+                    ptx::mma_bf16(s[2 * sl], q, b0, b1);
+                    ptx::mma_bf16(s[2 * sl + 1], q, b2, b3);
                 }
             }
 #pragma unroll
@@ -403,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 __syncwarp();
             }
             if (scores) {
-                float* to = scores + int64_t(x.u0 + i) * (U * p.rows_per_part);
+                float* to = scores + int64_t(i) * (U * p.rows_per_part);
 #pragma unroll
                 for (int nt = 0; nt < 2 * kSlices; ++nt) {
                     float* at = to + (nt / 2) * (16 * p.rows_per_part) + (nt & 1) * (ROWS * 8) + r0 * 8 + c0;
@@ -506,6 +563,8 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         it0 += n_units;
 
         // ---- the part's end ----
+        const int n_heads = x.n_heads;
+        const int64_t item0 = item_of();
         l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
         l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
         if (ROWS == 16) {
@@ -612,8 +671,8 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     if (p.cluster == 0) return;
 
     // ---- a cluster: every CTA joins its share of the columns of all partials (also after a wait that ran out: the others wait for its word) ----
-    const int kv = x.gh / p.groups_per_kv, in_kv = (x.gh - kv * p.groups_per_kv) * p.rows_per_part, n_heads = min(p.rows_per_part, p.group - in_kv);
-    const int64_t item0 = int64_t(x.row) * p.n_q_heads + kv * p.group + in_kv;
+    const int n_heads = x.n_heads;
+    const int64_t item0 = item_of();
     __syncwarp();
     if (p.cluster > 1) {
         if (!waited) {                               // no part, or a lost one
@@ -662,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     if (!p.scores || p.group > 16) return;       // (more heads of a KV head are not all here: a launch of its own)
     asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");       // (all four warps come here without another wait)
     // the weights of this CTA's units (all heads of the KV head are in one group here)
-    const int64_t w0 = (int64_t(x.row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
+    const int64_t w0 = (int64_t(x.row) * p.c.g.n_kv_heads + x.kv) * p.c.slot_stride;
     const float* scores = p.scores + (int64_t(x.row) * p.n_gh + x.gh) * p.most_units * (U * ROWS);
     constexpr int kAhead = 32 / ROWS;            // slots of a thread under way
     for (int k0 = x.u0 * U + tid; k0 < x.u1 * U; k0 += kWarps * 32 * kAhead) {
