@@ -548,7 +548,7 @@ typedef struct {
 
 /* Bits that the calls below OR into *status_dev (may be NULL), beside those of ipkv_attend_runs: a length outside
  * 0 .. max_blocks * block_tokens, or a needed table entry outside 0 .. n_blocks - 1.  Such a token is left out: nothing outside the pool
- * is read or written. */
+ * is read or written (an eviction moves its weight and position all the same). */
 #define IPKV_STATUS_BAD_PAGE 16u
 
 /* The arguments of a call are a struct: a decode loop makes these calls once a layer, and a foreign-function interface takes its time

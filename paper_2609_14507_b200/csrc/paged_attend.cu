@@ -581,6 +581,10 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 p.part_ml[int64_t(x.place) * p.rows_per_part + head] = make_float2(m, z);
             }
         };
+        if (kChecked && !x.whole && p.cluster == 0 && (x.place < 0 || x.place >= 2 * p.n_ctas)) {     // the partial must lie inside the scratch
+            if (lane == 0) or_status(p.status, kStatusBadIndex);
+            x.place = 0;
+        }
         float* const out = x.whole ? p.out_o + item0 * D : p.part_o + int64_t(x.place) * p.rows_per_part * D;
         if (teams == 1 || (n_units == 1 && sixteens == 1 && p.cluster <= 1)) {       // no two warps have something of the same head
             if (held >= 0) {

@@ -218,7 +218,7 @@ class Case:
 # ---- attention -------------------------------------------------------------------------------------------------------
 
 SHAPES = [(4, 1, 128, 64), (3, 1, 64, 16), (8, 8, 128, 32), (8, 1, 64, 64), (10, 2, 128, 16), (28, 4, 128, 128), (16, 1, 128, 64), (24, 2, 64, 32), (17, 1, 128, 64),
-          (32, 1, 64, 128), (40, 1, 128, 16), (64, 1, 128, 256), (128, 2, 64, 64)]
+          (32, 1, 64, 128), (40, 1, 128, 16), (64, 1, 128, 256), (128, 2, 64, 64), (40, 40, 64, 16), (50, 2, 128, 192)]
 LENGTHS = [[1], [0, 1, 0], [63, 64, 65, 16, 17, 15], [4097], [300, 0, 2000, 7, 129], [1000] * 40 + [0] * 3 + [5], [5000, 1, 20, 64] * 25]
 
 
@@ -527,6 +527,39 @@ def test_eviction_keeps_what_it_says(hkv, d, bt, lengths, budget, first, recent)
 
 
 @pytest.mark.gpu
+def test_eviction_with_one_array_in_place_and_one_apart():
+    for lengths, budget in (([1000, 200, 513], 200), ([201, 200, 0], 200), ([230000], 150000)):
+        for which in range(2):
+            c = Case(lengths, 1, 1, 64, 256)
+            w, pos = c.weights.clone(), c.positions.clone()
+            both = [torch.full_like(w, -9.0), torch.full_like(pos, -9)]
+            kept = torch.full((len(lengths), 1, budget), -9, dtype=torch.int32, device="cuda")
+            cache = c.cache()
+            scratch = torch.zeros(max(256, binding.ipkv_paged_evict_scratch_bytes(c.shape, cache, budget)), dtype=torch.uint8, device="cuda")
+            binding.ipkv_paged_evict(c.shape, cache, budget, 3, 50, scratch, both[0] if which == 0 else None, both[1] if which == 1 else None, kept, status=c.status)
+            assert int(c.status) == 0
+            for r, n in enumerate(lengths):
+                if n == 0:
+                    continue
+                src = torch.tensor(ref.kept(w[r, 0, :n].tolist(), pos[r, 0, :n].tolist(), budget, 3, 50), device="cuda")
+                assert torch.equal(kept[r, 0, :len(src)].long(), src)
+                got_w, got_pos = both[0] if which == 0 else c.weights, both[1] if which == 1 else c.positions
+                assert torch.equal(got_w[r, 0, :len(src)], w[r, 0][src]) and torch.equal(got_pos[r, 0, :len(src)], pos[r, 0][src])
+
+
+@pytest.mark.gpu
+def test_a_budget_that_nothing_exceeds_needs_no_scratch():
+    c = Case([128, 5, 0], 2, 2, 64, 64)
+    cache = c.cache()
+    assert binding.ipkv_paged_evict_scratch_bytes(c.shape, cache, 128) == 0
+    before = [x.clone() for x in (c.pool.data, c.weights, c.positions)]
+    binding.ipkv_paged_evict(c.shape, cache, 128, 4, 100, torch.empty(0, dtype=torch.uint8, device="cuda"), status=c.status)
+    torch.cuda.synchronize()
+    for x, y in zip((c.pool.data, c.weights, c.positions), before):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
+@pytest.mark.gpu
 def test_eviction_by_hard_weights():
     """Ties (the lower slot stays), nothing but ties, zeros of both signs, infinities, NaN, negative and subnormal weights, twice the same position."""
     for seed, values in enumerate(([1.0], [0.0, -0.0], [1.0, 2.0], [math.nan], [math.nan, 1.0, -1.0], [math.inf, -math.inf, 0.0, math.nan], [1e-45, -1e-45, 0.0, 1e-40],
@@ -655,6 +688,39 @@ def test_a_captured_decode_run_of_bounded_caches():
         kk, vv = c.pool.get(c.pages[r], list(range(len(tokens[r][0]))))
         for h in range(hkv):
             assert torch.equal(kk[:, h], torch.stack([t[0] for t in tokens[r][h]])) and torch.equal(vv[:, h], torch.stack([t[1] for t in tokens[r][h]]))
+
+
+@pytest.mark.gpu
+def test_calls_of_two_threads():
+    """Two host threads, a stream, a cache and scratch of their own each."""
+    import threading
+    cases = [Case([3000, 64, 777], 8, 2, 128, 64, seed=1), Case([100, 5000, 9], 16, 1, 64, 32, seed=2)]
+    torch.cuda.synchronize()
+    outs, faults = [None, None], []
+
+    def work(i):
+        try:
+            c, s = cases[i], torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                cache = c.cache()
+                scratch = torch.empty(binding.ipkv_paged_scratch_bytes(c.shape, cache), dtype=torch.uint8, device="cuda")
+                o, lse = torch.empty((3, c.hq, c.d), device="cuda"), torch.empty((3, c.hq), device="cuda")
+                for _ in range(200):
+                    binding.ipkv_paged_attend(c.shape, cache, c.q, scratch, o, lse, status=c.status)
+            s.synchronize()
+            outs[i] = (o, lse)
+        except Exception as e:                           # noqa: BLE001
+            faults.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not faults
+    for c, (o, lse) in zip(cases, outs):
+        assert int(c.status) == 0
+        c.check(o, lse)
 
 
 @pytest.mark.gpu
