@@ -37,7 +37,7 @@ struct Smem {
     uint64_t landed;
     unsigned long long least;
     uint32_t hist[2][256];
-    int32_t newest, digit, need, ties, gave_up;
+    int32_t newest, digit, need, ties, all, gave_up;
     int32_t scan[8];
     int32_t count[3][kWarps];                    // of every warp: ties; kept slots behind the budget, evicted ones before it
     int32_t total[2];                            // of the CTA, the latter two
@@ -284,10 +284,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
         int before = x - c;
 #pragma unroll
         for (int w = 0; w < 8; ++w) before += w < warp ? sm.scan[w] : 0;
-        if (tid < 256 && before < need && need <= before + c) { sm.digit = 255 - tid; sm.need = need - before; sm.ties = lower; }
+        if (tid < 256 && before < need && need <= before + c) { sm.digit = 255 - tid; sm.need = need - before; sm.ties = lower; sm.all = need == before + c; }
         __syncthreads();
         prefix |= uint32_t(sm.digit) << shift;
         need = sm.need;
+        if (sm.all && pass < 3) {                // all keys that begin so are kept (most often the one that does): the bits below do not matter
+            --prefix;
+            need = 0;
+            break;
+        }
     }
     const uint32_t threshold = prefix;           // `need` of the keys equal to it are kept, the lowest slots'
 
@@ -456,8 +461,10 @@ cudaError_t launch_paged_evict(PagedEvict& a, cudaStream_t s) {
     while (ctas < kMostCtas && int64_t(pairs) * ctas * 2 <= kSmCount && slots / (ctas * 2) >= 1024) ctas *= 2;
     const int per_cta = ((slots + ctas - 1) / ctas + 31) & ~31;
     a.held = per_cta <= kHeldSlots ? per_cta : kHeldSlots;
-    // a CTA to an SM wants its threads; several to an SM, smaller ones
-    return int64_t(pairs) * ctas <= kSmCount ? launch<1024>(a, ctas, s) : launch<256>(a, ctas, s);
+    // Threads by the slots of a CTA, as long as it has an SM to itself: barriers cost more with more warps (8 pairs of 261 slots 11.0 us with 1024, 8.9 with
+    // 256), passes and moves less (24 pairs of 15K 30.8 and 39.3; 24 of 3.5K, 1760 to a CTA, 16.9 and 14.7).
+    if (int64_t(pairs) * ctas > kSmCount || per_cta <= 512) return launch<256>(a, ctas, s);
+    return per_cta <= 2048 ? launch<512>(a, ctas, s) : launch<1024>(a, ctas, s);
 }
 
 }  // namespace ipkvi
