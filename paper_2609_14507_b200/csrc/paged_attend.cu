@@ -851,38 +851,61 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const __grid_consta
 }
 
 // weights_out[t] = weights[t] + sum over the KV head's query heads of 2^(s_t - m) / z, from the scores that the attention left.
-// One CTA for every splits-th 256 visible slots of a (row, KV head); a thread per slot.
+// Bound by issue slots, so what does not change from slot to slot is done once for some: CTA (kv, split), row takes every splits-th group of a
+// row's and KV head's visible slots, a thread kAhead of a group, a CTA's width apart.
+constexpr int kWeighThreads = 256;
 template <int ROWS>
-__global__ void __launch_bounds__(256) paged_weigh_kernel(const __grid_constant__ PagedAttend p, const int splits) {
-    const int split = blockIdx.x % splits, pair = blockIdx.x / splits, kv = pair % p.c.g.n_kv_heads, row = pair / p.c.g.n_kv_heads;
-    const int U = p.unit, per_cta = 256 / U, tok = int(threadIdx.x) % U;
+constexpr int weigh_ahead() { return ROWS == 4 ? 4 : 2; }
+template <int ROWS>
+__global__ void __launch_bounds__(kWeighThreads) paged_weigh_kernel(const __grid_constant__ PagedAttend p, const int splits) {
+    constexpr int kAhead = weigh_ahead<ROWS>();
+    const int row = int(blockIdx.y), kv = int(blockIdx.x) / splits, split = int(blockIdx.x) - kv * splits;
+    const int shift = p.unit == 64 ? 6 : 5;
     const float2* ml = p.head_ml + int64_t(row) * p.n_q_heads + kv * p.group;
-    const float* scores = p.scores + (int64_t(row) * p.n_gh + kv * p.groups_per_kv) * p.most_units * (U * p.rows_per_part) + (tok >> 4) * (16 * p.rows_per_part) +
-                          ((tok >> 3) & 1) * (ROWS * 8) + (tok & 7);
+    const float* scores = p.scores + (int64_t(row) * p.n_gh + kv * p.groups_per_kv) * p.most_units * (p.unit * p.rows_per_part);
     const int64_t w0 = (int64_t(row) * p.c.g.n_kv_heads + kv) * p.c.slot_stride;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const PagedSeen seen = paged_seen(length_of(p, row, false), p.window, p.first, U);
-    for (int j = split * per_cta + int(threadIdx.x) / U; j < seen.units; j += splits * per_cta) {
-        const int t = seen.unit(j) * U + tok;
-        if (!seen.sees(t)) continue;
-        const float before = p.c.weights ? p.c.weights[w0 + t] : 0.f;
-        float given = 0.f;
+    const PagedSeen seen = paged_seen(length_of(p, row, false), p.window, p.first, p.unit);
+    const int slots = seen.units << shift;
+    float2 y[ROWS];
+    auto heads_from = [&](int head0) {
+#pragma unroll
+        for (int h = 0; h < ROWS; ++h) y[h] = head0 + h < p.group ? ml[head0 + h] : make_float2(0.f, 0.f);
+    };
+    const bool few = p.group <= ROWS;
+    if (few) heads_from(0);
+    for (int k0 = split * (kWeighThreads * kAhead) + int(threadIdx.x); k0 < slots; k0 += splits * (kWeighThreads * kAhead)) {
+        int t[kAhead];
+        float before[kAhead], given[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const int k = k0 + e * kWeighThreads;
+            t[e] = (seen.unit(k >> shift) << shift) + (k & (p.unit - 1));
+            if (k >= slots || !seen.sees(t[e])) t[e] = -1;
+            given[e] = 0.f;
+            before[e] = t[e] >= 0 && p.c.weights ? p.c.weights[w0 + t[e]] : 0.f;
+        }
         for (int head0 = 0, part = 0; head0 < p.group; ++part)
             for (int hg = 0; hg < p.sixteens && head0 < p.group; ++hg, head0 += ROWS) {
-                const float* s = scores + (int64_t(part) * p.most_units + j) * (U * p.rows_per_part) + hg * (ROWS * 16);
-                float x[ROWS];
-                float2 y[ROWS];
+                if (!few) heads_from(head0);
+                const float* s = scores + int64_t(part) * p.most_units * (p.unit * p.rows_per_part) + hg * (ROWS * 16);
+                float x[kAhead][ROWS];
 #pragma unroll
-                for (int h = 0; h < ROWS; ++h) {
-                    y[h] = make_float2(0.f, 0.f);
-                    if (head0 + h < p.group) { x[h] = s[h * 8]; y[h] = ml[head0 + h]; }
+                for (int e = 0; e < kAhead; ++e) {
+                    const int k = k0 + e * kWeighThreads;
+                    const float* from = s + int64_t(k >> 4) * (16 * p.rows_per_part) + ((k >> 3) & 1) * (ROWS * 8) + (k & 7);
+#pragma unroll
+                    for (int h = 0; h < ROWS; ++h) x[e][h] = t[e] >= 0 && y[h].y != 0.f ? from[h * 8] : -INFINITY;
                 }
 #pragma unroll
-                for (int h = 0; h < ROWS; ++h)
-                    if (y[h].y != 0.f) given += ptx::ex2(x[h] - y[h].x) * y[h].y;
+                for (int e = 0; e < kAhead; ++e)
+#pragma unroll
+                    for (int h = 0; h < ROWS; ++h) given[e] += ptx::ex2(x[e][h] - y[h].x) * y[h].y;
             }
-        p.weights_out[w0 + t] = before + given;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+            if (t[e] >= 0) p.weights_out[w0 + t[e]] = before[e] + given[e];
     }
 }
 
@@ -937,11 +960,19 @@ cudaError_t launch_paged_attend(const PagedAttend& a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
     }
     if (a.weights_out && (a.cluster == 0 || a.group > 16)) {
-        const int64_t pairs = int64_t(a.c.n_rows) * a.c.g.n_kv_heads, groups = (int64_t(a.most_units) * a.unit + 255) / 256;
-        const int64_t want = (148 * 32 + pairs - 1) / pairs;             // a few CTAs behind every one that runs
+        const int64_t pairs = int64_t(a.c.n_rows) * a.c.g.n_kv_heads, group = kWeighThreads * (rows == 4 ? weigh_ahead<4>() : weigh_ahead<8>());
+        const int64_t groups = (int64_t(a.most_units) * a.unit + group - 1) / group, want = (148 * 8 + pairs - 1) / pairs;       // CTAs that run at once
         const int splits = int(want < groups ? want : groups);
-        return launch_overlapped(rows == 4 ? paged_weigh_kernel<4> : rows == 8 ? paged_weigh_kernel<8> : paged_weigh_kernel<16>, int(pairs * splits), 256, size_t(0), s,
-                                 a, splits);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(unsigned(a.c.g.n_kv_heads * splits), unsigned(a.c.n_rows));
+        cfg.blockDim = dim3(kWeighThreads);
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = overlap_launches() ? 1 : 0;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, rows == 4 ? paged_weigh_kernel<4> : rows == 8 ? paged_weigh_kernel<8> : paged_weigh_kernel<16>, a, splits);
     }
     return cudaSuccess;
 }
