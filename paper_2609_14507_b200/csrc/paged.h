@@ -105,6 +105,12 @@ IPKV_HD int32_t paged_split(int32_t n, int32_t parts, int32_t i) {
     const int32_t q = int32_t(uint32_t(n) / uint32_t(parts)), r = n - q * parts;
     return i * q + (i < r ? i : r);
 }
+// one part's beginning and end
+IPKV_HD void paged_split(int32_t n, int32_t parts, int32_t i, int32_t& begin, int32_t& end) {
+    const int32_t q = int32_t(uint32_t(n) / uint32_t(parts)), r = n - q * parts;
+    begin = i * q + (i < r ? i : r);
+    end = begin + q + (i < r ? 1 : 0);
+}
 // the part that has thing x of n >= parts
 IPKV_HD int32_t paged_part_of(int32_t n, int32_t parts, int32_t x) {
     const int32_t q = int32_t(uint32_t(n) / uint32_t(parts)), r = n - q * parts, large = r * (q + 1);
@@ -115,13 +121,15 @@ IPKV_HD int32_t paged_part_of(int32_t n, int32_t parts, int32_t x) {
 // whole CTAs within `ctas`, or if the share is much more than a chunk (rows of different lengths: 256 pairs of 80 to 129 units gave 120
 // units to a CTA, 93 in chunks).  Where a chunk has the end of one pair and the beginning of the next it loses some 3 us, 8 units: 64 pairs of
 // 129 units 29.5 us by shares of 36, 31.1 in chunks of 29; 264 of 94 units 67.7 by 94 and 72 in chunks of 87.
-IPKV_HD int32_t paged_share_tried(int32_t units, int32_t ctas, int32_t teams, int32_t i) {
-    const int32_t mean = units > 0 ? (units - 1) / ctas + 1 : 1, step = mean >= 8 * teams ? 1 : teams, least = (mean + step - 1) / step;
-    return step * (least + int32_t(uint32_t(least + 30) / 31u) * i);
+// (In fp32, by 1 / ctas: every CTA finds the same, and an integer division is a twentieth of a microsecond.)
+IPKV_HD int32_t paged_share_tried(int32_t units, float per_cta, int32_t teams, int32_t i) {
+    const int32_t mean = int32_t(float(units) * per_cta) + 1, least = mean >= 8 * teams ? mean : (mean + teams - 1) & -teams;
+    const int32_t step = mean >= 8 * teams ? 1 : teams;          // teams is 1, 2 or 4
+    return least + (((least >> 5) & -step) + step) * i;
 }
-IPKV_HD bool paged_share_wins(int32_t share, int32_t units, int32_t pairs, int32_t ctas) {
-    const int32_t mean = (units + pairs * kPagedPairCost) / ctas;
-    return share <= mean + mean / 16 + 8;
+IPKV_HD bool paged_share_wins(int32_t share, int32_t units, int32_t pairs, float per_cta) {
+    const float mean = float(units + pairs * kPagedPairCost) * per_cta;
+    return float(share) <= mean + mean * (1.f / 16.f) + 8.f;
 }
 
 // A CTA's parts of pairs, one after the other.  cum[r]: cost (with a share: parts) of a head group in the rows before r; n[r]: slots.
@@ -165,15 +173,13 @@ struct PagedParts {
             x.gh = int32_t(uint32_t(i) / uint32_t(parts));
             const int32_t part = i - x.gh * parts;
             x.seen = paged_seen(n[x.row], window, first, unit);
-            x.u0 = paged_split(x.seen.units, parts, part);
-            x.u1 = paged_split(x.seen.units, parts, part + 1);
+            paged_split(x.seen.units, parts, part, x.u0, x.u1);
             x.whole = parts == 1;
             x.place = 2 * cta;
             return true;
         }
         if (cta >= share.ctas) return false;
-        at = paged_split(share.cost, share.ctas, cta);
-        end = paged_split(share.cost, share.ctas, cta + 1);
+        paged_split(share.cost, share.ctas, cta, at, end);
         if (at >= end) return false;
         x.row = row_of(at);
         x.gh = int32_t(uint32_t(at - cum[x.row] * n_gh) / uint32_t(cum[x.row + 1] - cum[x.row]));
@@ -232,6 +238,9 @@ struct PagedAttend {
     int32_t n_q_heads, group, groups_per_kv, n_gh, rows_per_part, sixteens;
     int32_t n_ctas;
     int32_t bt_shift;                            // log2 of the tokens of a block, -1 where there is none
+    float per_cta;                               // 1 / n_ctas
+    uint32_t per_gh;                             // 2^32 / n_gh, rounded up
+    int32_t cluster_shift;
     int32_t cluster;                             // CTAs that take a pair together and write its result; 0: shares, and a join
     float scale_log2;
 };

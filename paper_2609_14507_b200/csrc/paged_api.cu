@@ -164,6 +164,9 @@ ipkv_status ipkv_paged_attend(const ipkv_paged_attend_call* call) {
         const int64_t pairs = int64_t(n) * plan.n_gh, most = int64_t(kSmCount) * kPagedCtasPerSm;
         a.cluster = paged_cluster(pairs, plan.most_units, plan.group, plan.sixteens, int(most));
         a.n_ctas = int32_t(a.cluster ? pairs * a.cluster : std::min(most, pairs * plan.most_units));
+        a.per_cta = 1.f / float(a.n_ctas);
+        a.per_gh = plan.n_gh > 1 ? uint32_t(((uint64_t(1) << 32) + plan.n_gh - 1) / plan.n_gh) : 0;
+        a.cluster_shift = a.cluster > 1 ? __builtin_ctz(unsigned(a.cluster)) : 0;
         if (launch_paged_attend(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return IPKV_ECUDA;
     }
     return IPKV_OK;

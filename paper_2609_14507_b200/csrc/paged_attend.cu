@@ -113,7 +113,7 @@ __device__ PagedShare share_out(const PagedAttend& p, Smem& sm, int teams) {
     auto choose = [&](int mine, int parts, int units, int pairs) {
         const unsigned fits = __ballot_sync(0xffffffffu, pairs <= p.n_ctas && int64_t(parts) * p.n_gh <= p.n_ctas);
         const int share = fits == 0 ? 0 : __shfl_sync(0xffffffffu, mine, __ffs(int(fits)) - 1);
-        return paged_share_wins(share, units, pairs, p.n_ctas) ? share : 0;
+        return paged_share_wins(share, units, pairs, p.per_cta) ? share : 0;
     };
     auto scan = [&](int x) {
         for (int d = 1; d < 32; d <<= 1) {
@@ -126,7 +126,7 @@ __device__ PagedShare share_out(const PagedAttend& p, Smem& sm, int teams) {
         const int n = lane < R ? length_of(p, lane, tid < 32 && blockIdx.x == 0) : 0;
         const int units = paged_seen(n, p.window, p.first, p.unit).units;
         const int sum = __reduce_add_sync(0xffffffffu, unsigned(units)), pairs = __popc(__ballot_sync(0xffffffffu, units > 0)) * p.n_gh;
-        const int mine = paged_share_tried(sum * p.n_gh, p.n_ctas, teams, lane);
+        const int mine = paged_share_tried(sum * p.n_gh, p.per_cta, teams, lane);
         if (pairs <= p.n_ctas) {
             int parts = 0;
 #pragma unroll 4
@@ -154,7 +154,7 @@ __device__ PagedShare share_out(const PagedAttend& p, Smem& sm, int teams) {
         rows = int(__reduce_add_sync(0xffffffffu, unsigned(rows)));
         if (lane == 0) { atomicAdd(&sm.units, units); atomicAdd(&sm.pairs, rows * p.n_gh); }
         __syncthreads();
-        const int mine = paged_share_tried(sm.units * p.n_gh, p.n_ctas, teams, lane);
+        const int mine = paged_share_tried(sm.units * p.n_gh, p.per_cta, teams, lane);
         const bool few = sm.pairs <= p.n_ctas;
         if (few) {
             int parts = 0;
@@ -214,6 +214,9 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         ptx::mbar_fence_init();
         sm.units = 0; sm.pairs = 0;
     }
+    // a cluster's pair and this CTA's rank in it, before the wait
+    const int c_pair = int(blockIdx.x) >> p.cluster_shift, rank = int(blockIdx.x) & ((1 << p.cluster_shift) - 1);
+    const int c_row = p.n_gh > 1 ? int(__umulhi(unsigned(c_pair), p.per_gh)) : c_pair, c_gh = c_pair - c_row * p.n_gh;      // (fewer pairs than CTAs: exact)
     __syncthreads();
     if (p.cluster > 1) cluster_arrive_relaxed();         // this CTA is there: the others may write to it behind their wait
     ptx::grid_dependency_wait();
@@ -238,11 +241,10 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 parts = PagedParts{sm.cum, sm.n, share, p.c.n_rows, p.n_gh, p.window, p.first, U, int(blockIdx.x), 0, 0};
                 more = parts.begin(x);
             } else {
-                const int pair = int(blockIdx.x) / p.cluster, rank = int(blockIdx.x) - pair * p.cluster;
-                x.row = pair / p.n_gh; x.gh = pair - x.row * p.n_gh;
-                const PagedSeen seen = paged_seen(length_of(p, x.row, x.gh == 0 && rank == 0 && tid == 0), p.window, p.first, U);
-                x.seen = seen;
-                x.u0 = paged_split(seen.units, p.cluster, rank); x.u1 = paged_split(seen.units, p.cluster, rank + 1);
+                const PagedSeen seen = paged_seen(length_of(p, c_row, c_gh == 0 && rank == 0 && tid == 0), p.window, p.first, U);
+                const int q = seen.units >> p.cluster_shift, r = seen.units - (q << p.cluster_shift);
+                x.row = c_row; x.gh = c_gh; x.seen = seen;
+                x.u0 = rank * q + min(rank, r); x.u1 = x.u0 + q + (rank < r ? 1 : 0);
                 x.whole = p.cluster == 1; x.place = 0;
                 parts.at = parts.end = 0;
             }
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         int st = 0, lap = 0, it = 0;
         bool ok = true;
         {   // a small table comes into the L1 cache while the lengths are on their way
-            const int rows = p.cluster > 0 ? 1 : p.c.n_rows, first = p.cluster > 0 ? int(blockIdx.x) / p.cluster / p.n_gh : 0, lines = (p.c.max_blocks + 31) / 32;
+            const int rows = p.cluster > 0 ? 1 : p.c.n_rows, first = p.cluster > 0 ? c_row : 0, lines = (p.c.max_blocks + 31) / 32;
             const int row = lane / lines;
             if (rows * lines <= 32 && row < rows) {
                 int32_t unused;
@@ -352,7 +354,6 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     const uint32_t s_q = s_ring + kStages * kPagedUnitBytes + warp * 4096;       // ROWS == 16
     uint32_t qa[ROWS == 16 ? 1 : D / 16][2];
     float o[D / 8][4];
-    const int rank = p.cluster > 0 ? int(blockIdx.x) % p.cluster : 0;
     int it0 = 0, meets = 0;                      // units of the parts before this one
     bool ok = true, waited = false;
     auto meet = [&]() -> bool {                  // the four warps; they may wait for units of their own first
@@ -657,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 }
             if (p.cluster > 1) {                 // to the CTA that joins these columns; maximum and sum to all
                 const int to = i & (p.cluster - 1);
-                put(at_rank(ptx::smem_addr(sm.cum) + (rank * (n_heads * (D / 4) / p.cluster) + i / p.cluster) * 16, to), acc);
+                put(at_rank(ptx::smem_addr(sm.cum) + (rank * (n_heads * (D / 4) >> p.cluster_shift) + (i >> p.cluster_shift)) * 16, to), acc);
                 if (col < p.cluster) put(at_rank(ptx::smem_addr(&sm.part_ml[rank][head]), col), make_float2(m, z));
                 continue;
             }
@@ -698,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 if (y[c].y != 0.f) z += y[c].x * y[c].y;
             }
         };
-        const int per_cta = n_heads * (D / 4) / p.cluster;
+        const int per_cta = n_heads * (D / 4) >> p.cluster_shift;
         for (int k = tid; k < per_cta; k += kWarps * 32) {
             const int i = k * p.cluster + rank, head = i / (D / 4), col = i - head * (D / 4);
             float2 y[kPagedMostCluster];

@@ -39,12 +39,12 @@ int shim_paged_play(const int* n, int n_rows, int n_gh, int window, int first, i
     }
     PagedShare s{0, 0, 0};
     for (int i = 0; i < 32 && pairs <= ctas && s.share == 0; ++i) {
-        const int share = paged_share_tried(int32_t(all * n_gh), ctas, teams, i);
+        const int share = paged_share_tried(int32_t(all * n_gh), 1.f / float(ctas), teams, i);
         int64_t parts = 0;
         for (int r = 0; r < n_rows; ++r) parts += (units[r] + share - 1) / share;
         if (parts * n_gh <= ctas) s.share = share;
     }
-    if (s.share > 0 && !paged_share_wins(s.share, int32_t(all * n_gh), int32_t(pairs), ctas)) s.share = 0;
+    if (s.share > 0 && !paged_share_wins(s.share, int32_t(all * n_gh), int32_t(pairs), 1.f / float(ctas))) s.share = 0;
     cum[0] = 0;
     for (int r = 0; r < n_rows; ++r) cum[r + 1] = cum[r] + paged_cost(units[r], s);
     if (s.share == 0) { s.cost = cum[n_rows] * n_gh; s.ctas = std::min(ctas, s.cost); }
