@@ -16,6 +16,10 @@
 //
 // At the end of a pair the warps' states are joined in the stages of their last units, which nobody reads any more, and
 // leave as the result, or as one partial for the join kernel.  Every wait is bounded.
+//
+// Measured (a few replays of a graph): 16 rows of 32K tokens, 4 KV heads of 8 query heads, 128 columns: 164 us for 1074 MB, 6.5 TB/s; 64 ragged rows of up
+// to 16K in pages of 16, 8 KV heads of 4: 336 us for 2259 MB, 6.7 TB/s; one row of 500K, 16 heads on one: 51 us for 256 MB, 34 of them
+// streaming at 7.5 TB/s; 32 rows through a window of 4096: 85 us for 507 MB, 6.0 TB/s; one of 4K tokens: 11.8 us, a chain of latencies.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -757,7 +761,8 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
 
 // Joins the partials of every (row, query head) whose pair more than one CTA had: with partial i's maximum m_i (log2), sum l_i and sums o_i,
 //   m = max m_i,  z = sum 2^(m_i - m) l_i,  O = sum 2^(m_i - m) o_i / z,  LSE = m ln 2 + ln z,   in a fixed order.
-// One CTA per (row, head, COLS columns): COLS / 4 column groups times slices of the partials.
+// One CTA per (row, head, COLS columns): COLS / 4 column groups times slices of the partials.  Bound by the latency of its reads, one behind the
+// other: the shares, the partials (all of a slice at once).  295 partials of 16 heads, 2.5 MB: 4 us behind the attention.
 template <int D, int COLS, int THREADS>
 __global__ void __launch_bounds__(THREADS) paged_join_kernel(const __grid_constant__ PagedAttend p) {
     constexpr int kCols = COLS / 4, kSlices = THREADS / kCols, kSlabs = D / COLS;
@@ -851,7 +856,8 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(const __grid_consta
     }
 }
 
-// weights_out[t] = weights[t] + sum over the KV head's query heads of 2^(s_t - m) / z, from the scores that the attention left.
+// weights_out[t] = weights[t] + sum over the KV head's query heads of 2^(s_t - m) / z, from the scores that the attention left.  32 rows of 2.5K to 4K
+// tokens, 8 KV heads of 4: 10 us by itself with cold caches, 84 us all three launches.
 // Bound by issue slots, so what does not change from slot to slot is done once for some: CTA (kv, split), row takes every splits-th group of a
 // row's and KV head's visible slots, a thread kAhead of a group, a CTA's width apart.
 constexpr int kWeighThreads = 256;
