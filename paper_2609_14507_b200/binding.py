@@ -807,6 +807,14 @@ def make_paged(shape, pool, table, lengths, weights=None, positions=None):
     return c
 
 
+def _packed(call, *args):
+    """A call's struct; numbers that its fields cannot hold are refused as other bad arguments are."""
+    try:
+        return call.pack(*args)
+    except struct.error as e:
+        raise ValueError(f"an argument is out of range: {e}") from None
+
+
 def _slots_like(x, dtype, cache, name):
     """An output shaped like the cache's weights and positions, as an address."""
     if x is None:
@@ -849,7 +857,7 @@ def ipkv_paged_append(shape, cache, k, v, positions=None, row_start=None, status
         at = positions.data_ptr()
     elif cache._tensors[4] is not None and n:
         raise ValueError("the cache has positions: the new tokens need theirs")
-    rc = (_lib or lib()).ipkv_paged_append(_APPEND_CALL.pack(C.addressof(shape), cache._at, n, k.data_ptr(), v.data_ptr(), kt, vt, rs, at,
+    rc = (_lib or lib()).ipkv_paged_append(_packed(_APPEND_CALL, C.addressof(shape), cache._at, n, k.data_ptr(), v.data_ptr(), kt, vt, rs, at,
                                                              0 if status is None else _status_word(status, dev), _call_stream(stream, dev) or 0))
     if rc != OK:
         raise IpkvError(rc, "ipkv_paged_append")
@@ -883,7 +891,7 @@ def ipkv_paged_attend(shape, cache, q, scratch, o_part, lse_part, window=0, firs
         raise ValueError("the queries of two rows lie apart")
     if scratch.get_device() != dev or not scratch.is_contiguous():
         raise ValueError("scratch is contiguous, on the device of the pool")
-    rc = (_lib or lib()).ipkv_paged_attend(_ATTEND_CALL.pack(C.addressof(shape), cache._at, q.data_ptr(), qt, window, first,
+    rc = (_lib or lib()).ipkv_paged_attend(_packed(_ATTEND_CALL, C.addressof(shape), cache._at, q.data_ptr(), qt, window, first,
                                                              0 if weights_out is None else _slots_like(weights_out, f32, cache, "weights_out"), scratch.data_ptr(), scratch.nbytes,
                                                              o_part.data_ptr(), lse_part.data_ptr(), 0 if status is None else _status_word(status, dev),
                                                              _call_stream(stream, dev) or 0))
@@ -912,7 +920,7 @@ def ipkv_paged_evict(shape, cache, budget, first, recent, scratch, weights_out=N
         at = kept.data_ptr()
     if scratch.get_device() != dev or not scratch.is_contiguous():
         raise ValueError("scratch is contiguous, on the device of the pool")
-    rc = (_lib or lib()).ipkv_paged_evict(_EVICT_CALL.pack(C.addressof(shape), cache._at, budget, first, recent, _slots_like(weights_out, _f32, cache, "weights_out"),
+    rc = (_lib or lib()).ipkv_paged_evict(_packed(_EVICT_CALL, C.addressof(shape), cache._at, budget, first, recent, _slots_like(weights_out, _f32, cache, "weights_out"),
                                                            _slots_like(positions_out, _i32, cache, "positions_out"), at, scratch.data_ptr(), scratch.nbytes,
                                                            0 if status is None else _status_word(status, dev), _call_stream(stream, dev) or 0))
     if rc != OK:

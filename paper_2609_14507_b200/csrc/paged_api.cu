@@ -28,7 +28,7 @@ BlockGeom geom(const ipkv_attn_shape* sh) { return BlockGeom{sh->n_kv_heads, sh-
 bool cache_ok(const ipkv_attn_shape* sh, const ipkv_paged* c) {
     if (!shape_ok(sh) || !c || !capacity_ok(sh, c->n_rows, c->max_blocks)) return false;
     if (!c->pool_dev || !aligned(c->pool_dev, 16) || c->pool_bytes < geom(sh).block_bytes() || c->pool_bytes / geom(sh).block_bytes() > INT32_MAX) return false;
-    if (!c->table_dev || !aligned(c->table_dev, 4) || !c->lengths_dev || !aligned(c->lengths_dev, 4)) return false;
+    if (!aligned(c->table_dev, 4) || !aligned(c->lengths_dev, 4) || (c->n_rows > 0 && (!c->table_dev || !c->lengths_dev))) return false;
     if (c->table_stride < c->max_blocks || c->table_stride > (int64_t(1) << 40)) return false;
     if (c->weights_dev || c->positions_dev) {
         if (!aligned(c->weights_dev, 16) || !aligned(c->positions_dev, 16)) return false;
@@ -125,7 +125,7 @@ ipkv_status ipkv_paged_attend(const ipkv_paged_attend_call* call) {
     const int64_t row = int64_t(sh->n_q_heads) * sh->dim_qk;
     if (q_row_stride != 0 && (q_row_stride < row || q_row_stride % 8 != 0 || q_row_stride > (int64_t(1) << 40))) return IPKV_EINVAL;
     if (!aligned(q_dev, 16) || !aligned(o_part_dev, 16) || !aligned(lse_part_dev, 4) || !aligned(status_dev, 4) || !aligned(weights_out_dev, 16)) return IPKV_EINVAL;
-    if (!scratch_dev || !aligned(scratch_dev, 256)) return IPKV_EINVAL;
+    if (!aligned(scratch_dev, 256) || (c->n_rows > 0 && !scratch_dev)) return IPKV_EINVAL;
     if (weights_out_dev) {
         if (c->slot_stride < int64_t(c->max_blocks) * sh->block_tokens || c->slot_stride % 4 != 0 || c->slot_stride > (int64_t(1) << 32)) return IPKV_EINVAL;
         if (!apart(sh, c, c->weights_dev, weights_out_dev)) return IPKV_EINVAL;
@@ -183,7 +183,7 @@ ipkv_status ipkv_paged_evict(const ipkv_paged_evict_call* call) {
     if (!call) return IPKV_EINVAL;
     const auto [sh, c, budget, first_tokens, recent, weights_out_dev, positions_out_dev, kept_dev, scratch_dev, scratch_bytes, status_dev, stream] = *call;
     if (!cache_ok(sh, c) || budget < 1 || first_tokens < 0 || recent < 0 || int64_t(first_tokens) + recent > budget) return IPKV_EINVAL;
-    if (!c->weights_dev || !c->positions_dev) return IPKV_EINVAL;
+    if (c->n_rows > 0 && (!c->weights_dev || !c->positions_dev)) return IPKV_EINVAL;
     if (!aligned(weights_out_dev, 16) || !aligned(positions_out_dev, 16) || !aligned(kept_dev, 4) || !aligned(status_dev, 4)) return IPKV_EINVAL;
     if (!aligned(scratch_dev, 256)) return IPKV_EINVAL;
     PagedEvict a;

@@ -729,6 +729,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     }
     if (!p.scores || p.group > 16) return;       // (more heads of a KV head are not all here: a launch of its own)
     asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");       // (all four warps come here without another wait)
+    if (!ok) return;
     // the weights of this CTA's units (all heads of the KV head are in one group here)
     const int64_t w0 = (int64_t(x.row) * p.c.g.n_kv_heads + x.kv) * p.c.slot_stride;
     const float* scores = p.scores + (int64_t(x.row) * p.n_gh + x.gh) * p.most_units * (U * ROWS);

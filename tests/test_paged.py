@@ -80,8 +80,8 @@ def test_bad_caches_are_refused():
                dict(slot_stride=255), dict(slot_stride=252), dict(slot_stride=258)):
         c = struct(**kw)
         assert append_rc(sh, c) == attend_rc(sh, c) == evict_rc(sh, c) == EINVAL, kw
-    none = struct(n_rows=0)
-    assert append_rc(sh, none, n=0) == attend_rc(sh, none) == evict_rc(sh, none) == 0       # nothing to do
+    for none in (struct(n_rows=0), struct(n_rows=0, table_dev=None, lengths_dev=None, weights_dev=None, positions_dev=None)):     # nothing to do
+        assert append_rc(sh, none, n=0) == attend_rc(sh, none) == attend_rc(sh, none, q=None, scratch=None, o=None, lse=None) == evict_rc(sh, none) == 0
 
 
 def test_bad_calls_are_refused():
@@ -152,6 +152,11 @@ def test_the_binding_refuses_other_types_and_shapes():
                  lambda: binding.ipkv_paged_evict(other, c, 10, 0, 0, scratch)):
         with pytest.raises(ValueError):
             call()
+    for kw in (dict(window=1 << 31), dict(first=1 << 31), dict(window=1.5)):
+        with pytest.raises(ValueError):
+            binding.ipkv_paged_attend(sh, c, q, scratch, o, lse, **kw)
+    with pytest.raises(ValueError):
+        binding.ipkv_paged_evict(sh, c, 1 << 40, 0, 0, scratch)
     for call in (lambda: binding.ipkv_paged_append(sh, c, k, k, positions=at), lambda: binding.ipkv_paged_attend(sh, c, q, scratch, o, lse),
                  lambda: binding.ipkv_paged_evict(sh, c, 10, 0, 0, scratch)):
         with pytest.raises(ValueError, match="on device -1"):            # refused for nothing but being on the host
@@ -375,6 +380,19 @@ def test_slots_beyond_32_bits_of_bytes():
     cache = binding.make_paged(c.shape, pool, table, c.lengths)
     o, lse = c.attend(cache=cache)
     c.check(o, lse)
+
+
+@pytest.mark.gpu
+def test_a_batch_without_rows():
+    sh = shape_of(4, 2, 64, 64)
+    pool = torch.zeros((3, 2, 2, 64 * 64), dtype=torch.bfloat16, device="cuda")
+    empty = lambda *s, t=torch.float32: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    c = binding.make_paged(sh, pool, empty(0, 3, t=torch.int32), empty(0, t=torch.int32), empty(0, 2, 192), empty(0, 2, 192, t=torch.int32))
+    scratch = empty(max(256, binding.ipkv_paged_scratch_bytes(sh, c)), t=torch.uint8)
+    binding.ipkv_paged_append(sh, c, empty(0, 2, 64, t=torch.bfloat16), empty(0, 2, 64, t=torch.bfloat16), positions=empty(0, t=torch.int32))
+    binding.ipkv_paged_attend(sh, c, empty(0, 4, 64, t=torch.bfloat16), scratch, empty(0, 4, 64), empty(0, 4))
+    binding.ipkv_paged_evict(sh, c, 10, 0, 0, scratch)
+    torch.cuda.synchronize()
 
 
 @pytest.mark.gpu
