@@ -93,15 +93,7 @@ __device__ __forceinline__ bool wait_tag(const uint32_t* tag, uint32_t unit, uin
     }
 }
 
-// Thread-block clusters: the barrier in its two halves, and stores to the shared memory of another CTA.
-__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ uint32_t at_rank(uint32_t smem, uint32_t rank) {
-    uint32_t there;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem), "r"(rank));
-    return there;
-}
+// To the shared memory of another CTA of the cluster.
 __device__ __forceinline__ void put(uint32_t there, const float4& v) {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
@@ -222,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     const int c_pair = int(blockIdx.x) >> p.cluster_shift, rank = int(blockIdx.x) & ((1 << p.cluster_shift) - 1);
     const int c_row = p.n_gh > 1 ? int(__umulhi(unsigned(c_pair), p.per_gh)) : c_pair, c_gh = c_pair - c_row * p.n_gh;      // (fewer pairs than CTAs: exact)
     __syncthreads();
-    if (p.cluster > 1) cluster_arrive_relaxed();         // this CTA is there: the others may write to it behind their wait
+    if (p.cluster > 1) ptx::cluster_arrive_relaxed();         // this CTA is there: the others may write to it behind their wait
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     PagedShare share{0, 0, 0};
@@ -345,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
             for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
                 if (!ptx::mbar_wait(ptx::smem_addr(&sm.full[i % kStages]), (i / kStages) & 1)) or_status(p.status, kStatusCopyNotLanded);
         __syncwarp();
-        if (p.cluster > 1) cluster_wait();
+        if (p.cluster > 1) ptx::cluster_wait();
         return;
     }
 
@@ -637,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
             }
         }
         if (!meet()) { ok = false; break; }
-        if (p.cluster > 1) { cluster_wait(); waited = true; }
+        if (p.cluster > 1) { ptx::cluster_wait(); waited = true; }
         for (int i = tid; i < n_heads * (D / 4); i += kWarps * 32) {
             const int head = i / (D / 4), col = i - head * (D / 4), g = ROWS == 16 ? head / 16 : 0, row = ROWS == 16 ? head % 16 : head;
             float2 y[kWarps];
@@ -662,8 +654,8 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 }
             if (p.cluster > 1) {                 // to the CTA that joins these columns; maximum and sum to all
                 const int to = i & (p.cluster - 1);
-                put(at_rank(ptx::smem_addr(sm.cum) + (rank * (n_heads * (D / 4) >> p.cluster_shift) + (i >> p.cluster_shift)) * 16, to), acc);
-                if (col < p.cluster) put(at_rank(ptx::smem_addr(&sm.part_ml[rank][head]), col), make_float2(m, z));
+                put(ptx::at_rank(ptx::smem_addr(sm.cum) + (rank * (n_heads * (D / 4) >> p.cluster_shift) + (i >> p.cluster_shift)) * 16, to), acc);
+                if (col < p.cluster) put(ptx::at_rank(ptx::smem_addr(&sm.part_ml[rank][head]), col), make_float2(m, z));
                 continue;
             }
             const float f = !x.whole ? 1.f : z == 0.f ? 0.f : 1.f / z;
@@ -685,11 +677,11 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     __syncwarp();
     if (p.cluster > 1) {
         if (!waited) {                               // no part, or a lost one
-            cluster_wait();
-            if (tid < 16 * p.cluster) put(at_rank(ptx::smem_addr(&sm.part_ml[rank][tid & 15]), tid >> 4), make_float2(-INFINITY, 0.f));
+            ptx::cluster_wait();
+            if (tid < 16 * p.cluster) put(ptx::at_rank(ptx::smem_addr(&sm.part_ml[rank][tid & 15]), tid >> 4), make_float2(-INFINITY, 0.f));
         }
-        cluster_arrive();
-        cluster_wait();
+        ptx::cluster_arrive();
+        ptx::cluster_wait();
         auto state_of = [&](int head, float2 (&y)[kPagedMostCluster], float& m, float& z) {
             m = -INFINITY; z = 0.f;
 #pragma unroll

@@ -4,16 +4,15 @@
 // A thread-block cluster takes one (row, KV head), every CTA of it a contiguous part of the slots, every warp a contiguous part of that:
 //   1. weights and positions come into shared memory by two bulk copies; the newest position (a maximum), then the keys, as integers of
 //      the same order;
-//   2. the budget-th largest key, eight bits at a time: a histogram in every CTA, read by all through distributed shared memory;
+//   2. the budget-th largest key, eight bits at a time: a histogram in every CTA, sent to all of the cluster;
 //   3. slots above it are kept, and of those equal to it the lowest; prefix sums number the kept slots behind the budget and the evicted
 //      ones before it, and the i-th of the ones meets the i-th of the others;
 //   4. the warps of the cluster move the K and V rows, an even share each, whatever parts of the slots they come from.
 // Where one slot goes (a full cache that makes room for the next token), it is the smallest key, of equal ones the last slot's: one
 // minimum in place of 2 and 3.
-// Bound by its meetings, some 2 us each in a cluster of eight with what is between them, then by the rows moved in pieces of 128 bytes.  Measured: 512 pairs,
-// one of 4096 slots 10.5 us (41 MB with arrays apart); 8 pairs of 32K to 4K 25.7 us, 8 of them for 29 MB of rows; 8 pairs of 261 to 243 slots 8.9 us.
-#include <cooperative_groups.h>
-
+// Bound by its chain of passes, 1.7 us each in a cluster of eight with 1024 threads (the sending itself takes 0.15, counting 0.6), then by the rows moved in
+// pieces of 128 bytes.  Measured: 512 pairs, one of 4096 slots 9.6 us (41 MB with arrays apart); 8 pairs of 32K to 4K 24.0 us, 7 to 9 of them for 29 MB of rows;
+// 8 pairs of 261 to 243 slots 8.2 us.
 #include <atomic>
 
 #include "kernels.h"
@@ -22,22 +21,23 @@
 #include "plan.hpp"
 #include "ptx.cuh"
 
-namespace cg = cooperative_groups;
-
 namespace ipkvi {
 
 namespace {
 
 constexpr int kMostCtas = 8;
 constexpr int kHeldSlots = 24 * 1024;            // of a CTA, 8 bytes each in shared memory; of more, keys are computed again where they are needed
+constexpr int kMeetings = 6;                     // the newest position; the smallest key, or the numbers of moves; a pass each
 constexpr int kAtOnce = 8;                       // rows that a warp has under way
 
 template <int THREADS>
 struct Smem {
     static constexpr int kWarps = THREADS / 32;
     uint64_t landed;
+    uint64_t told[kMeetings];                    // what the CTAs of the cluster send one another, eight bytes each or a histogram
+    unsigned long long got[2][kMostCtas];
     unsigned long long least;
-    uint32_t hist[2][256];
+    alignas(16) uint32_t hist[2][256];
     int32_t newest, digit, need, ties, all, gave_up;
     int32_t scan[8];
     int32_t count[3][kWarps];                    // of every warp: ties; kept slots behind the budget, evicted ones before it
@@ -56,19 +56,39 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
     constexpr int kWarps = THREADS / 32;
     extern __shared__ __align__(16) uint32_t held[];     // weights, then keys, of the CTA's slots; positions behind them
     __shared__ Smem<THREADS> sm;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int rank = int(cluster.block_rank()), pair = int(blockIdx.x) / ctas, H = p.c.g.n_kv_heads, row = pair / H, head = pair - row * H;
+    const int rank = int(blockIdx.x) % ctas, pair = int(blockIdx.x) / ctas, H = p.c.g.n_kv_heads, row = pair / H, head = pair - row * H;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    uint4* const hists = reinterpret_cast<uint4*>(held + 2 * p.held);      // [2][ctas][64]: the cluster's histograms, of two passes in turn
     auto meet = [&]() {                          // all CTAs of the cluster
-        if (ctas == 1) __syncthreads(); else cluster.sync();
+        if (ctas == 1) { __syncthreads(); return; }
+        ptx::cluster_arrive();
+        ptx::cluster_wait();
+    };
+    // A meeting whose outcome every CTA needs: each sends its part to all, counted by a barrier that serves once, and waits for theirs.
+    // One way through the cluster's network in place of the cluster's barrier and a read there and back (8 pairs of 32K to 4K 25.7 to 24.0 us).
+    auto there = [&](const void* here, int cta) { return ptx::at_rank(ptx::smem_addr(here), cta); };
+    auto tell = [&](int meeting, int which, unsigned long long x) {        // (warp 0)
+        if (lane < ctas) ptx::st_async_b64(there(&sm.got[which][rank], lane), x, there(&sm.told[meeting], lane));
+    };
+    bool lost = false;                           // a wait ran out
+    auto hear = [&](int meeting) { lost |= !ptx::mbar_wait_cluster(ptx::smem_addr(&sm.told[meeting]), 0); };
+    // after such a wait, by all threads of the CTA: nothing moves in the cluster, and no CTA leaves before the others have sent
+    auto give_up = [&]() {
+        if (tid == 0 && p.status) atomicOr(p.status, kStatusNoTile);
+        if (tid < ctas) asm volatile("st.shared::cluster.u32 [%0], 1;" ::"r"(there(&sm.gave_up, tid)) : "memory");
+        __syncwarp();
+        meet();
     };
     if (tid == 0) {
         ptx::mbar_init(ptx::smem_addr(&sm.landed), 1);
+        for (int k = 0; k < kMeetings; ++k) ptx::mbar_init(ptx::smem_addr(&sm.told[k]), 1);
         ptx::mbar_fence_init();
+        for (int k = 0; k < kMeetings; ++k) ptx::mbar_expect_tx(ptx::smem_addr(&sm.told[k]), uint32_t(ctas) * (k < 2 ? 8u : 1024u));
         sm.newest = INT32_MIN; sm.least = ~0ull; sm.gave_up = 0;
     }
     if (tid < 256) sm.hist[0][tid] = sm.hist[1][tid] = 0;
     __syncthreads();
+    if (ctas > 1) ptx::cluster_arrive();         // the barriers are there: waited for before the first of them is used
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     if (tid * 32 < p.c.max_blocks) {             // the row's table comes into the L1 cache meanwhile
@@ -98,6 +118,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
         if (kept) kept[i] = i;
     };
     if (n <= b) {                                // all stay: copied, four slots a lane, where they go to arrays of their own
+        if (ctas > 1) ptx::cluster_wait();
         if (in_place && !kept) return;
         constexpr int kGroups = 4;
         for (int i0 = w0 + 4 * lane; i0 - 4 * lane < w1; i0 += 128 * kGroups) {
@@ -155,16 +176,17 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
     }
     newest = __reduce_max_sync(0xffffffffu, newest);
     if (lane == 0) atomicMax(&sm.newest, newest);
-    meet();
-    // (reads of other CTAs' shared memory are issued together here and below: one behind the other they took most of the time)
-    int others = 0;
-    if (lane < ctas) {
-        newest = *cluster.map_shared_rank(&sm.newest, lane);
-        others = *cluster.map_shared_rank(&sm.gave_up, lane);
-    }
-    newest = __reduce_max_sync(0xffffffffu, newest);
-    if (__any_sync(0xffffffffu, others != 0)) {
-        meet();                                  // (the others read this CTA's shared memory until here)
+    __syncthreads();
+    newest = sm.newest;
+    if (ctas > 1) {
+        ptx::cluster_wait();
+        if (warp == 0) tell(0, 0, static_cast<unsigned long long>(uint32_t(sm.gave_up)) << 32 | uint32_t(newest));
+        hear(0);
+        if (__syncthreads_or(lost)) return give_up();
+        const unsigned long long x = lane < ctas ? sm.got[0][lane] : uint32_t(INT32_MIN);
+        newest = __reduce_max_sync(0xffffffffu, int(uint32_t(x)));
+        if (__any_sync(0xffffffffu, x >> 32 != 0)) return meet();
+    } else if (sm.gave_up) {
         return;
     }
     const int64_t old = int64_t(newest) - p.recent;      // positions up to here are not recent
@@ -218,14 +240,21 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
             least = x < least ? x : least;
         }
         if (lane == 0) atomicMin(&sm.least, least);
-        meet();
-        least = lane < ctas ? *cluster.map_shared_rank(&sm.least, lane) : ~0ull;
+        __syncthreads();
+        least = sm.least;
+        if (ctas > 1) {
+            if (warp == 0) tell(1, 1, least);
+            hear(1);
+            if (__syncthreads_or(lost)) return give_up();
+            least = sm.got[1][lane & (ctas - 1)];
 #pragma unroll
-        for (int d = kMostCtas / 2; d > 0; d >>= 1) {
-            const unsigned long long x = __shfl_xor_sync(0xffffffffu, least, d);
-            least = x < least ? x : least;
+            for (int d = kMostCtas / 2; d > 0; d >>= 1) {
+                const unsigned long long x = __shfl_xor_sync(0xffffffffu, least, d);
+                least = x < least ? x : least;
+            }
+            ptx::cluster_arrive();               // (no CTA leaves before the others have heard it)
         }
-        const int gone = int(~uint32_t(__shfl_sync(0xffffffffu, least, 0)));
+        const int gone = int(~uint32_t(least));
         if (!in_place || kept)
             for (int i = w0 + lane; i < w1; i += 32)
                 if (i < b && i != gone) {
@@ -233,7 +262,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
                     if (positions_out != positions) positions_out[i] = holds ? p_held[i - cta0] : positions[i];
                     if (kept) kept[i] = i;
                 }
-        if (ctas > 1) meet();                    // nobody reads another CTA's shared memory any more
+        if (ctas > 1) ptx::cluster_wait();
         if (gone == b || rank != 0 || warp != 0) return;
         const int64_t src_at = row_at(b), dst_at = row_at(gone);
         if (lane == 0) {
@@ -260,18 +289,25 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
             for (int e = 0; e < 4; ++e)
                 if (i + e < w1 && (pass == 0 || (keys[e] >> (shift + 8)) == (prefix >> (shift + 8)))) atomicAdd(&hist[(keys[e] >> shift) & 255], 1u);
         });
-        meet();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // (the histogram is sent by the copy engine)
+        __syncthreads();
         // keys with a larger digit than this thread's
         int c = 0, lower = 0;                    // of all CTAs; of those before this one
-        if (tid < 256) {
-            uint32_t of[kMostCtas];
+        if (ctas > 1) {
+            uint4* const to = hists + (pass & 1) * ctas * 64;
+            if (tid < ctas) ptx::bulk_s2s(there(to + rank * 64, tid), ptx::smem_addr(hist), 1024, there(&sm.told[2 + pass], tid));
+            hear(2 + pass);
+            if (tid < 256) {
+                const uint32_t* of = reinterpret_cast<const uint32_t*>(to) + 255 - tid;
 #pragma unroll
-            for (int r = 0; r < kMostCtas; ++r) of[r] = r < ctas ? cluster.map_shared_rank(hist, r)[255 - tid] : 0u;
-#pragma unroll
-            for (int r = 0; r < kMostCtas; ++r) {
-                c += int(of[r]);
-                if (r < rank) lower += int(of[r]);
+                for (int r = 0; r < kMostCtas; ++r) {
+                    const int x = r < ctas ? int(of[r * 256]) : 0;
+                    c += x;
+                    if (r < rank) lower += x;
+                }
             }
+        } else if (tid < 256) {
+            c = int(hist[255 - tid]);
         }
         int x = c;
         for (int d = 1; d < 32; d <<= 1) {
@@ -279,14 +315,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
             if (lane >= d) x += y;
         }
         if (lane == 31 && warp < 8) sm.scan[warp] = x;
-        // the other histogram is the next pass's: every CTA has read it, or it would not have come to this pass's barrier
+        // the other histogram is the next pass's (a CTA that sends into the room of two passes ago has heard from all that they are past it)
         if (tid < 256) sm.hist[(pass + 1) & 1][tid] = 0;
         __syncthreads();
         int before = x - c;
 #pragma unroll
         for (int w = 0; w < 8; ++w) before += w < warp ? sm.scan[w] : 0;
         if (tid < 256 && before < need && need <= before + c) { sm.digit = 255 - tid; sm.need = need - before; sm.ties = lower; sm.all = need == before + c; }
-        __syncthreads();
+        if (__syncthreads_or(lost)) return give_up();
         prefix |= uint32_t(sm.digit) << shift;
         need = sm.need;
         if (sm.all && pass < 3) {                // all keys that begin so are kept (most often the one that does): the bits below do not matter
@@ -347,11 +383,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
     };
     // of the slots i .. i + 3: those below the budget, those that are there
     auto below = [&](int i) { return i >= b ? 0u : b - i >= 4 ? 15u : (1u << (b - i)) - 1u; };
-    auto there = [&](int i) { return i >= w1 ? 0u : w1 - i >= 4 ? 15u : (1u << (w1 - i)) - 1u; };
+    auto present = [&](int i) { return i >= w1 ? 0u : w1 - i >= 4 ? 15u : (1u << (w1 - i)) - 1u; };
     int behind = 0, holes = 0;
     for_kept([&](int i, unsigned keep) {
         behind += __popc(keep & ~below(i));
-        holes += __popc(there(i) & ~keep & below(i));
+        holes += __popc(present(i) & ~keep & below(i));
     });
     behind = int(__reduce_add_sync(0xffffffffu, unsigned(behind)));
     holes = int(__reduce_add_sync(0xffffffffu, unsigned(holes)));
@@ -361,8 +397,16 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
         const int x = scan(1), y = scan(2);
         if (lane == 0) { sm.total[0] = x; sm.total[1] = y; }
     }
-    meet();
-    const int of0 = lane < ctas ? cluster.map_shared_rank(sm.total, lane)[0] : 0, of1 = lane < ctas ? cluster.map_shared_rank(sm.total, lane)[1] : 0;
+    __syncthreads();
+    int of0 = 0, of1 = 0;
+    if (ctas > 1) {
+        if (warp == 0) tell(1, 1, static_cast<unsigned long long>(uint32_t(sm.total[1])) << 32 | uint32_t(sm.total[0]));
+        hear(1);
+        if (__syncthreads_or(lost)) return give_up();
+        if (lane < ctas) { of0 = int(uint32_t(sm.got[1][lane])); of1 = int(sm.got[1][lane] >> 32); }
+    } else if (lane == 0) {
+        of0 = sm.total[0]; of1 = sm.total[1];
+    }
     int behind0 = sm.count[1][warp] + int(__reduce_add_sync(0xffffffffu, unsigned(lane < rank ? of0 : 0)));
     int holes0 = sm.count[2][warp] + int(__reduce_add_sync(0xffffffffu, unsigned(lane < rank ? of1 : 0)));
     const int moves = int(__reduce_add_sync(0xffffffffu, unsigned(of1)));
@@ -372,7 +416,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
     int32_t* into = here ? reinterpret_cast<int32_t*>(sm.hist[1]) : from + p.most_moved;
     const bool tells = !in_place || kept;        // what stays where it is has to be written, too
     for_kept([&](int i, unsigned keep) {
-        const unsigned comes = keep & ~below(i), open = there(i) & ~keep & below(i);
+        const unsigned comes = keep & ~below(i), open = present(i) & ~keep & below(i);
         const int mine = __popc(comes) | __popc(open) << 16, upto = warp_scan(mine);
         int x = behind0 + ((upto - mine) & 0xffff), y = holes0 + ((upto - mine) >> 16);
 #pragma unroll
@@ -385,7 +429,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
         behind0 += all & 0xffff;
         holes0 += all >> 16;
     });
-    meet();                                      // the lists are written; nobody reads another CTA's shared memory any more
+    meet();                                      // the lists are written
+    if (ctas > 1 && sm.gave_up) return;
     if (holds && tells)                          // (behind the barrier, which would wait for these writes; keys that are not held are gone once rows move)
         for_kept([&](int i, unsigned keep) {
 #pragma unroll
@@ -396,13 +441,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
     // ---- moves: a warp looks 32 of them up at once, a lane each, then moves their rows, a 16-byte chunk of each a lane ----
     const int warps = ctas * kWarps, each = (moves + warps - 1) / warps, first = min(moves, (rank * kWarps + warp) * each), last = min(moves, first + each);
     for (int i0 = first; i0 < last; i0 += 32) {
-        int src = 0, dst = 0;
+        int src = 0, dst = 0, position = 0;
+        float weight = 0.f;
         int64_t src_at = -1, dst_at = -1;
         if (i0 + lane < last) {
             src = from[i0 + lane]; dst = into[i0 + lane];
             src_at = row_at(src); dst_at = row_at(dst);
-            weights_out[dst] = weights[src];
-            positions_out[dst] = positions[src];
+            weight = weights[src]; position = positions[src];
             if (kept) kept[dst] = src;
             if (src_at < 0 || dst_at < 0) {
                 src_at = -1;
@@ -425,6 +470,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) paged_evict_kernel(co
                 if (from_at >= 0 && lane < chunks) *reinterpret_cast<uint4*>(lane_at + at + swizzle(slot)) = x[k];
             }
         }
+        if (lane < count) { weights_out[dst] = weight; positions_out[dst] = position; }
     }
 }
 
@@ -435,14 +481,14 @@ cudaError_t launch(const PagedEvict& a, int ctas, cudaStream_t s) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(paged_evict_kernel<THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldSlots * 8);
+        e = cudaFuncSetAttribute(paged_evict_kernel<THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldSlots * 8 + kMostCtas * 2048);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) configured[dev].store(true, std::memory_order_release);
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(a.c.n_rows * a.c.g.n_kv_heads * ctas));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = size_t(a.held) * 8;
+    cfg.dynamicSmemBytes = size_t(a.held) * 8 + (ctas > 1 ? size_t(ctas) * 2048 : 0);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -51,6 +51,46 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_
     return true;
 }
 
+// Thread-block clusters: the barrier in its two halves (whole warps), and an address of this CTA's shared memory in another one of the cluster.
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t at_rank(uint32_t smem, uint32_t rank) {
+    uint32_t there;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem), "r"(rank));
+    return there;
+}
+// The wait for what other CTAs of the cluster sent with st_async_*: acquires at the cluster's scope.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity) {
+    if (mbar_try_wait_cluster(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    uint32_t n = 0;
+    while (!mbar_try_wait_cluster(bar, parity)) {
+        if ((++n & 63u) == 0 && globaltimer_ns() - t0 > kWaitLimitNs) return false;
+    }
+    return true;
+}
+// To shared memory of a CTA of the cluster (`there`, `bar_there`: in the cluster's window, of one CTA); counted in bytes on its barrier.
+__device__ __forceinline__ void bulk_s2s(uint32_t there, uint32_t src, uint32_t bytes, uint32_t bar_there) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(there), "r"(src), "r"(bytes), "r"(bar_there)
+                 : "memory");
+}
+__device__ __forceinline__ void st_async_b64(uint32_t there, unsigned long long x, uint32_t bar_there) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(there), "l"(x), "r"(bar_there) : "memory");
+}
+
 // Global -> shared bulk copy through the TMA engine; completion is counted in bytes on `bar`.
 // Both addresses 16-byte aligned, size a multiple of 16.
 __device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
