@@ -81,14 +81,16 @@ constexpr int kPagedRowsPerLaunch = 1024;        // the shares of so many rows a
 constexpr int kPagedCtasPerSm = 2, kPagedWarps = 4;
 // Where every pair has few units, which the host sees by the table's width or the window alone, a thread-block cluster takes it, joins
 // in distributed shared memory and adds the weights up: one launch in place of two or three.
-constexpr int kPagedMostCluster = 8;
+// Sixteen CTAs, more than a portable cluster, for at most eight pairs: a GPC for each (1 row of 4 KV heads, 2K tokens: 8.0 us, with eight CTAs 9.5; 3K and 4K:
+// 9.8 and 10.9, with CTAs over the GPU and a join 11.6 and 11.7; sixteen pairs of sixteen 14.7 against 7.7, they take turns).
+constexpr int kPagedMostCluster = 16;
 constexpr int kPagedClusterUnits = 24, kPagedClusterMore = 5;
 inline int paged_cluster(int64_t pairs, int64_t most_units, int group, int sixteens, int ctas) {
     if (pairs > ctas) return 0;
     int n = 1;                                           // (more heads than one product takes stay with one CTA)
-    while (group <= 16 && n < kPagedMostCluster && pairs * n * 2 <= ctas && most_units > kPagedWarps * n) n *= 2;
-    // Units of a CTA, against those with whole CTAs over the GPU.  The launch saved is worth five (1 row of 4 KV heads, 8 and 4: 2K tokens 10.3 us against
-    // 10.9; 12 and 4: 12.5 and 11.7; 4 rows of 8 heads and 6K tokens, 24 and 20: 22.7 and 23.9).  Rows may be shorter than the table is wide, and
+    while (group <= 16 && n < kPagedMostCluster && pairs * n * 2 <= ctas && most_units > kPagedWarps * n && (n < 8 || pairs <= 8)) n *= 2;
+    // Units of a CTA, against those with whole CTAs over the GPU.  The launch saved is worth five (1 row of 4 KV heads in clusters of eight, 8 and 4: 2K tokens
+    // 10.3 us against 10.9; 12 and 4: 12.5 and 11.7; 4 rows of 8 heads and 6K tokens, 24 and 20: 22.7 and 23.9).  Rows may be shorter than the table is wide, and
     // clusters do not even them out: not above 24.  (Warps that share their units take as many times more.)
     const int64_t mine = (most_units + n - 1) / n * sixteens, all = pairs * most_units / ctas, others = (all > kPagedWarps / sixteens ? all : kPagedWarps / sixteens) * sixteens;
     return mine <= kPagedClusterUnits && mine <= others + kPagedClusterMore ? n : 0;

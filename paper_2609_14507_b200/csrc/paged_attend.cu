@@ -19,10 +19,11 @@
 //
 // Measured (a few replays of a graph): 16 rows of 32K tokens, 4 KV heads of 8 query heads, 128 columns: 164 us for 1074 MB, 6.5 TB/s; 64 ragged rows of up
 // to 16K in pages of 16, 8 KV heads of 4: 336 us for 2259 MB, 6.7 TB/s; one row of 500K, 16 heads on one: 51 us for 256 MB, 34 of them
-// streaming at 7.5 TB/s; 32 rows through a window of 4096: 85 us for 507 MB, 6.0 TB/s; one of 4K tokens: 11.8 us, a chain of latencies.
+// streaming at 7.5 TB/s; 32 rows through a window of 4096: 85 us for 507 MB, 6.0 TB/s; one of 4K tokens: 11.0 us, a chain of latencies.
 #include <cuda_bf16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "kernels.h"
 #include "launch.cuh"
@@ -678,46 +679,50 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     if (p.cluster > 1) {
         if (!waited) {                               // no part, or a lost one
             ptx::cluster_wait();
-            if (tid < 16 * p.cluster) put(ptx::at_rank(ptx::smem_addr(&sm.part_ml[rank][tid & 15]), tid >> 4), make_float2(-INFINITY, 0.f));
+            for (int k = tid; k < 16 * p.cluster; k += kWarps * 32) put(ptx::at_rank(ptx::smem_addr(&sm.part_ml[rank][k & 15]), k >> 4), make_float2(-INFINITY, 0.f));
         }
         ptx::cluster_arrive();
         ptx::cluster_wait();
-        auto state_of = [&](int head, float2 (&y)[kPagedMostCluster], float& m, float& z) {
-            m = -INFINITY; z = 0.f;
+        auto join = [&](auto most) {             // (for eight and for sixteen: what is not there costs smaller clusters 0.3 us)
+            constexpr int kMost = decltype(most)::value;
+            auto state_of = [&](int head, float2 (&y)[kMost], float& m, float& z) {
+                m = -INFINITY; z = 0.f;
 #pragma unroll
-            for (int c = 0; c < kPagedMostCluster; ++c) {
-                y[c] = c < p.cluster ? sm.part_ml[c][head] : make_float2(-INFINITY, 0.f);
-                m = fmaxf(m, y[c].x);
+                for (int c = 0; c < kMost; ++c) {
+                    y[c] = c < p.cluster ? sm.part_ml[c][head] : make_float2(-INFINITY, 0.f);
+                    m = fmaxf(m, y[c].x);
+                }
+#pragma unroll
+                for (int c = 0; c < kMost; ++c) {
+                    y[c].x = ptx::ex2(y[c].x - (m == -INFINITY ? 0.f : m));
+                    if (y[c].y != 0.f) z += y[c].x * y[c].y;
+                }
+            };
+            const int per_cta = n_heads * (D / 4) >> p.cluster_shift;
+            for (int k = tid; k < per_cta; k += kWarps * 32) {
+                const int i = k * p.cluster + rank, head = i / (D / 4), col = i - head * (D / 4);
+                float2 y[kMost];
+                float m, z;
+                state_of(head, y, m, z);
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int c = 0; c < kMost; ++c)
+                    if (c < p.cluster && y[c].y != 0.f) {
+                        const float4 v = reinterpret_cast<const float4*>(sm.cum)[c * per_cta + k];
+                        acc.x += y[c].x * v.x; acc.y += y[c].x * v.y; acc.z += y[c].x * v.z; acc.w += y[c].x * v.w;
+                    }
+                const float inv = z == 0.f ? 0.f : 1.f / z;
+                reinterpret_cast<float4*>(p.out_o + item0 * D)[i] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+                if (col == 0) p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
             }
-#pragma unroll
-            for (int c = 0; c < kPagedMostCluster; ++c) {
-                y[c].x = ptx::ex2(y[c].x - (m == -INFINITY ? 0.f : m));
-                if (y[c].y != 0.f) z += y[c].x * y[c].y;
+            if (p.scores && tid < n_heads) {
+                float2 y[kMost];
+                float m, z;
+                state_of(tid, y, m, z);
+                sm.head_ml[tid] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
             }
         };
-        const int per_cta = n_heads * (D / 4) >> p.cluster_shift;
-        for (int k = tid; k < per_cta; k += kWarps * 32) {
-            const int i = k * p.cluster + rank, head = i / (D / 4), col = i - head * (D / 4);
-            float2 y[kPagedMostCluster];
-            float m, z;
-            state_of(head, y, m, z);
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int c = 0; c < kPagedMostCluster; ++c)
-                if (c < p.cluster && y[c].y != 0.f) {
-                    const float4 v = reinterpret_cast<const float4*>(sm.cum)[c * per_cta + k];
-                    acc.x += y[c].x * v.x; acc.y += y[c].x * v.y; acc.z += y[c].x * v.z; acc.w += y[c].x * v.w;
-                }
-            const float inv = z == 0.f ? 0.f : 1.f / z;
-            reinterpret_cast<float4*>(p.out_o + item0 * D)[i] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-            if (col == 0) p.out_lse[item0 + head] = z == 0.f ? -INFINITY : m * kLn2 + logf(z);
-        }
-        if (p.scores && tid < n_heads) {
-            float2 y[kPagedMostCluster];
-            float m, z;
-            state_of(tid, y, m, z);
-            sm.head_ml[tid] = make_float2(z == 0.f ? 0.f : m, z == 0.f ? 0.f : 1.f / z);
-        }
+        if (p.cluster <= 8) join(std::integral_constant<int, 8>()); else join(std::integral_constant<int, kPagedMostCluster>());
     }
     if (!p.scores || p.group > 16) return;       // (more heads of a KV head are not all here: a launch of its own)
     asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");       // (all four warps come here without another wait)
@@ -917,6 +922,8 @@ cudaError_t launch(const PagedAttend& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
         e = cudaFuncSetAttribute(paged_attend_kernel<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes(kPagedRowsPerLaunch)));
+        if (e != cudaSuccess) return e;
+        e = cudaFuncSetAttribute(paged_attend_kernel<D, ROWS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) configured[dev].store(true, std::memory_order_release);
     }

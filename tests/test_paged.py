@@ -245,6 +245,20 @@ def test_attention_matches_64_bits(hq, hkv, d, bt, lengths):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d,bt", [(1, 1, 64, 64), (5, 1, 128, 16), (16, 2, 64, 256), (16, 1, 128, 64), (7, 1, 64, 32)])
+@pytest.mark.parametrize("lengths", [[2100], [33 * 32, 0, 1], [2049, 31, 500, 2100], [1, 0, 0, 4000], [64, 4200, 63, 65]], ids=str)
+def test_few_pairs_of_some_units_are_taken_by_large_clusters(hq, hkv, d, bt, lengths):
+    c = Case(lengths, hq, hkv, d, bt)
+    for window, first in ((0, 0), (2080, 33)):
+        base, out = c.weights.clone(), c.weights.clone()
+        o, lse = c.attend(window, first, out)
+        assert int(c.status) == 0
+        c.check(o, lse, window, first, out, base)
+        o2, lse2 = c.attend(window, first)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("hq,hkv,d,bt", [(4, 1, 128, 64), (12, 2, 64, 16), (8, 8, 128, 32), (40, 1, 64, 256), (16, 1, 128, 128)])
 @pytest.mark.parametrize("window,first", [(1, 0), (1, 1), (5, 3), (64, 0), (64, 64), (100, 70), (1000, 4), (3000, 200), (2 ** 31 - 1, 2 ** 31 - 1), (7, 5000), (4096, 0)])
 def test_a_window_and_first_tokens(hq, hkv, d, bt, window, first):
