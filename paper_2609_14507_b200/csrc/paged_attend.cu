@@ -298,8 +298,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
                 const int pages = page;
                 if (j0 + batch < u1) page = page_of(j0 + batch);
                 for (int j = j0; j < min(j0 + batch, u1); ++j) {
-                    if (lap > 0) ok = ptx::mbar_wait(ptx::smem_addr(&sm.empty[st]), (lap - 1) & 1);
-                    ok = __all_sync(0xffffffffu, ok);
+                    if (lap > 0) ok = ptx::mbar_wait_warp(ptx::smem_addr(&sm.empty[st]), (lap - 1) & 1);
                     if (!ok) break;
                     const int lane0 = (j - j0) * per_unit;                  // the lane that holds the unit's first page
                     const unsigned there = (__ballot_sync(0xffffffffu, pages >= 0) >> lane0) & ((1u << per_unit) - 1u);
@@ -356,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
     auto meet = [&]() -> bool {                  // the four warps; they may wait for units of their own first
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&sm.met));
-        return ptx::mbar_wait(ptx::smem_addr(&sm.met), meets++ & 1, 2 * ptx::kWaitLimitNs);
+        return ptx::mbar_wait_warp(ptx::smem_addr(&sm.met), meets++ & 1, 2 * ptx::kWaitLimitNs);
     };
     auto item_of = [&]() { return int64_t(x.row) * p.n_q_heads + x.kv * p.group + x.in_kv; };      // of the outputs
 
@@ -408,10 +407,8 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         for (int i = (team - it0 % teams + teams) % teams; i < n_units; i += teams) {
             const int it = it0 + i, st = it % kStages;
             uint32_t there;
-            if (!wait_tag(&sm.tag[st], uint32_t(it), there) || !ptx::mbar_wait(ptx::smem_addr(&sm.full[st]), (it / kStages) & 1)) {
-                ok = false;
-                break;
-            }
+            ok = ptx::warp_agrees(wait_tag(&sm.tag[st], uint32_t(it), there) && ptx::mbar_wait(ptx::smem_addr(&sm.full[st]), (it / kStages) & 1));
+            if (!ok) break;
             const int ta = x.seen.unit(x.u0 + i) * U;
             const uint32_t stage = s_ring + st * kPagedUnitBytes;
             auto slice = [&](int sl) { return stage + (sl & 1) * odd + (sl >> 1) * pair; };
@@ -725,6 +722,7 @@ __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel
         if (p.cluster <= 8) join(std::integral_constant<int, 8>()); else join(std::integral_constant<int, kPagedMostCluster>());
     }
     if (!p.scores || p.group > 16) return;       // (more heads of a KV head are not all here: a launch of its own)
+    __syncwarp();
     asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");       // (all four warps come here without another wait)
     if (!ok) return;
     // the weights of this CTA's units (all heads of the KV head are in one group here)
