@@ -539,7 +539,7 @@ typedef struct {
   const int32_t* table_dev;     /* [n_rows][table_stride]: a row's blocks in the order of its slots; entries behind its length are
                                    not read                                                                             */
   const int32_t* lengths_dev;   /* [n_rows]: slots of the row, 0 .. max_blocks * block_tokens                             */
-  int32_t n_rows, max_blocks;   /* max_blocks: entries of a row's table                                                  */
+  int32_t n_rows, max_blocks;   /* max_blocks: entries of a row's table; max_blocks * block_tokens <= 2^31 - 2^21 - 1    */
   int64_t table_stride;         /* elements, >= max_blocks                                                               */
   float* weights_dev;           /* [n_rows][n_kv_heads][slot_stride]: attention that the slot's token has been given; or NULL  */
   int32_t* positions_dev;       /* the same shape: its position in the sequence; or NULL                                 */

@@ -10,6 +10,10 @@ namespace ipkvi {
 
 constexpr uint32_t kStatusBadPage = 16u;         // a length or a table entry out of range; the tokens were left out
 
+// Slots of a row are counted in 32 bits, and so are the threads' steps along them: the largest, of the kernel that adds the weights up, goes
+// 148 * 8 CTAs of 1024 slots beyond the last one.
+constexpr int32_t kPagedMostSlots = INT32_MAX - (1 << 21);
+
 // The cache as the kernels see it.
 struct PagedCache {
     BlockGeom g;

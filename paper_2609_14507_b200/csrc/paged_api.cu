@@ -20,9 +20,8 @@ bool shape_ok(const ipkv_attn_shape* sh) {
            sh->n_q_heads % sh->n_kv_heads == 0 && sh->dim_qk == sh->dim_v && (sh->dim_qk == 64 || sh->dim_qk == 128) && sh->block_tokens > 0 &&
            sh->block_tokens <= (1 << 20) && (sh->block_tokens == 16 || sh->block_tokens == 32 || sh->block_tokens % kTileTokens == 0);
 }
-// Slots of a row are counted in 32 bits, with room for a tile and a window behind them.
 bool capacity_ok(const ipkv_attn_shape* sh, int32_t n_rows, int32_t max_blocks) {
-    return n_rows >= 0 && max_blocks >= 1 && int64_t(max_blocks) * sh->block_tokens <= INT32_MAX - 4 * kTileTokens;
+    return n_rows >= 0 && max_blocks >= 1 && int64_t(max_blocks) * sh->block_tokens <= kPagedMostSlots;
 }
 BlockGeom geom(const ipkv_attn_shape* sh) { return BlockGeom{sh->n_kv_heads, sh->dim_qk, sh->dim_v, sh->block_tokens}; }
 bool cache_ok(const ipkv_attn_shape* sh, const ipkv_paged* c) {

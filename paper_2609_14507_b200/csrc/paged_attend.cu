@@ -967,7 +967,7 @@ cudaError_t launch_paged_attend(const PagedAttend& a, cudaStream_t s) {
     if (a.weights_out && (a.cluster == 0 || a.group > 16)) {
         const int64_t pairs = int64_t(a.c.n_rows) * a.c.g.n_kv_heads, group = kWeighThreads * (rows == 4 ? weigh_ahead<4>() : weigh_ahead<8>());
         const int64_t groups = (int64_t(a.most_units) * a.unit + group - 1) / group, want = (148 * 8 + pairs - 1) / pairs;       // CTAs that run at once
-        const int splits = int(want < groups ? want : groups);
+        const int splits = int(want < groups ? want : groups);   // (at most 148 * 8: kPagedMostSlots has room for a step of all of them)
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(unsigned(a.c.g.n_kv_heads * splits), unsigned(a.c.n_rows));
         cfg.blockDim = dim3(kWeighThreads);
