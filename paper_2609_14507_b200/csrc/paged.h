@@ -87,12 +87,13 @@ constexpr int kPagedCtasPerSm = 2, kPagedWarps = 4;
 // in distributed shared memory and adds the weights up: one launch in place of two or three.
 // Sixteen CTAs, more than a portable cluster, for at most eight pairs: a GPC for each (1 row of 4 KV heads, 2K tokens: 8.0 us, with eight CTAs 9.5; 3K and 4K:
 // 9.8 and 10.9, with CTAs over the GPU and a join 11.6 and 11.7; sixteen pairs of sixteen 14.7 against 7.7, they take turns).
-constexpr int kPagedMostCluster = 16;
+// `largest`: what the device places (a part of a GPU may have no GPC with room for sixteen).
+constexpr int kPagedMostCluster = 16, kPagedPortableCluster = 8;
 constexpr int kPagedClusterUnits = 24, kPagedClusterMore = 5;
-inline int paged_cluster(int64_t pairs, int64_t most_units, int group, int sixteens, int ctas) {
+inline int paged_cluster(int64_t pairs, int64_t most_units, int group, int sixteens, int ctas, int largest = kPagedMostCluster) {
     if (pairs > ctas) return 0;
     int n = 1;                                           // (more heads than one product takes stay with one CTA)
-    while (group <= 16 && n < kPagedMostCluster && pairs * n * 2 <= ctas && most_units > kPagedWarps * n && (n < 8 || pairs <= 8)) n *= 2;
+    while (group <= 16 && n < largest && pairs * n * 2 <= ctas && most_units > kPagedWarps * n && (n < kPagedPortableCluster || pairs <= 8)) n *= 2;
     // Units of a CTA, against those with whole CTAs over the GPU.  The launch saved is worth five (1 row of 4 KV heads in clusters of eight, 8 and 4: 2K tokens
     // 10.3 us against 10.9; 12 and 4: 12.5 and 11.7; 4 rows of 8 heads and 6K tokens, 24 and 20: 22.7 and 23.9).  Rows may be shorter than the table is wide, and
     // clusters do not even them out: not above 24.  (Warps that share their units take as many times more.)
@@ -251,6 +252,8 @@ struct PagedAttend {
     float scale_log2;
 };
 cudaError_t launch_paged_attend(const PagedAttend& a, cudaStream_t s);
+// The largest cluster of its kernel that the current device places: kPagedMostCluster or kPagedPortableCluster.
+cudaError_t paged_largest_cluster(const PagedAttend& a, int& largest);
 
 // ---- eviction (paged_evict.cu) -------------------------------------------------------------------------------------
 struct PagedEvict {

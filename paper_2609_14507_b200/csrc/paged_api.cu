@@ -162,6 +162,11 @@ ipkv_status ipkv_paged_attend(const ipkv_paged_attend_call* call) {
         a.weights_out = weights_out_dev ? weights_out_dev + int64_t(r0) * sh->n_kv_heads * c->slot_stride : nullptr;
         const int64_t pairs = int64_t(n) * plan.n_gh, most = int64_t(kSmCount) * kPagedCtasPerSm;
         a.cluster = paged_cluster(pairs, plan.most_units, plan.group, plan.sixteens, int(most));
+        if (a.cluster > kPagedPortableCluster) {
+            int largest = 0;
+            if (paged_largest_cluster(a, largest) != cudaSuccess) return IPKV_ECUDA;
+            a.cluster = paged_cluster(pairs, plan.most_units, plan.group, plan.sixteens, int(most), largest);
+        }
         a.n_ctas = int32_t(a.cluster ? pairs * a.cluster : std::min(most, pairs * plan.most_units));
         a.per_cta = 1.f / float(a.n_ctas);
         a.per_gh = plan.n_gh > 1 ? uint32_t(((uint64_t(1) << 32) + plan.n_gh - 1) / plan.n_gh) : 0;

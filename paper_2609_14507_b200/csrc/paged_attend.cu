@@ -912,32 +912,55 @@ __global__ void __launch_bounds__(kWeighThreads) paged_weigh_kernel(const __grid
     }
 }
 
-template <int D, int ROWS>
-cudaError_t launch(const PagedAttend& a, cudaStream_t s) {
-    static std::atomic<bool> configured[64];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 0 || dev >= 64 || !configured[dev].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(paged_attend_kernel<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes(kPagedRowsPerLaunch)));
-        if (e != cudaSuccess) return e;
-        e = cudaFuncSetAttribute(paged_attend_kernel<D, ROWS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-        if (dev >= 0 && dev < 64) configured[dev].store(true, std::memory_order_release);
-    }
-    if (a.cluster <= 1) return launch_overlapped(paged_attend_kernel<D, ROWS>, a.n_ctas, kThreads, smem_bytes(a.cluster ? 0 : a.c.n_rows), s, a);
+// Clusters of `cluster` CTAs.
+cudaLaunchConfig_t in_clusters(int n_ctas, int cluster, cudaLaunchAttribute (&attr)[2], cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(a.n_ctas));
+    cfg.gridDim = dim3(unsigned(n_ctas));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem_bytes(kPagedRowsPerLaunch);
     cfg.stream = s;
-    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = overlap_launches() ? 1 : 0;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = unsigned(a.cluster); attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.x = unsigned(cluster); attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
+    return cfg;
+}
+
+// Sets the kernel up on the current device, once; tells the largest cluster that it places there.
+template <int D, int ROWS>
+cudaError_t configure(int& largest) {
+    static std::atomic<int> known[64];           // 0: not yet
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const bool kept = dev >= 0 && dev < 64;
+    largest = kept ? known[dev].load(std::memory_order_acquire) : 0;
+    if (largest) return cudaSuccess;
+    e = cudaFuncSetAttribute(paged_attend_kernel<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes(kPagedRowsPerLaunch)));
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr[2];
+    const cudaLaunchConfig_t cfg = in_clusters(kPagedMostCluster, kPagedMostCluster, attr, nullptr);
+    int clusters = 0;
+    if (cudaFuncSetAttribute(paged_attend_kernel<D, ROWS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&clusters, paged_attend_kernel<D, ROWS>, &cfg) != cudaSuccess) {
+        cudaGetLastError();                      // (told here, and no later call's)
+        clusters = 0;
+    }
+    largest = clusters > 0 ? kPagedMostCluster : kPagedPortableCluster;
+    if (kept) known[dev].store(largest, std::memory_order_release);
+    return cudaSuccess;
+}
+
+template <int D, int ROWS>
+cudaError_t launch(const PagedAttend& a, cudaStream_t s) {
+    int largest = 0;
+    const cudaError_t e = configure<D, ROWS>(largest);
+    if (e != cudaSuccess) return e;
+    if (a.cluster <= 1) return launch_overlapped(paged_attend_kernel<D, ROWS>, a.n_ctas, kThreads, smem_bytes(a.cluster ? 0 : a.c.n_rows), s, a);
+    cudaLaunchAttribute attr[2];
+    const cudaLaunchConfig_t cfg = in_clusters(a.n_ctas, a.cluster, attr, s);
     return cudaLaunchKernelEx(&cfg, paged_attend_kernel<D, ROWS>, a);
 }
 
@@ -952,6 +975,14 @@ cudaError_t launch_join(const PagedAttend& a, cudaStream_t s) {
 }
 
 }  // namespace
+
+cudaError_t paged_largest_cluster(const PagedAttend& a, int& largest) {
+    const bool wide = a.c.g.dim_qk == 128;
+    const int rows = a.rows_per_part / a.sixteens;
+    return rows == 4 ? (wide ? configure<128, 4>(largest) : configure<64, 4>(largest))
+         : rows == 8 ? (wide ? configure<128, 8>(largest) : configure<64, 8>(largest))
+                     : (wide ? configure<128, 16>(largest) : configure<64, 16>(largest));
+}
 
 cudaError_t launch_paged_attend(const PagedAttend& a, cudaStream_t s) {
     const bool wide = a.c.g.dim_qk == 128;

@@ -23,3 +23,27 @@ def test_rows_whose_slots_leave_no_room_for_a_step_are_refused(bt):
         assert binding.lib().ipkv_paged_evict_scratch_bytes(C.byref(sh), 1, blocks, 100, C.byref(n)) == EINVAL
     assert binding.lib().ipkv_paged_scratch_bytes(C.byref(sh), 1, MOST // bt, 0, 0, 1, C.byref(n)) == 0
     assert binding.lib().ipkv_paged_evict_scratch_bytes(C.byref(sh), 1, MOST // bt, 100, C.byref(n)) == 0
+
+
+def test_where_the_device_places_no_cluster_of_sixteen_eight_are_taken(tmp_path):
+    """The same rule for clusters of sixteen and for devices without: up to eight nothing differs, and what sixteen would have taken is
+    taken by eight where they would take it, or shared out and joined."""
+    import os
+    import random
+    import subprocess
+    here = os.path.dirname(os.path.abspath(__file__))
+    src, so = tmp_path / "cluster.cpp", tmp_path / "libcluster.so"
+    src.write_text('#include "paged.h"\nusing namespace ipkvi;\nextern "C" int cluster(int pairs, int units, int group, int ctas, int largest) {\n'
+                   '    return paged_cluster(pairs, units, group, paged_sixteens(group), ctas, largest); }\n')
+    subprocess.run(["g++", "-O1", "-std=c++17", "-fPIC", "-shared", "-I/usr/local/cuda/include", "-I", os.path.join(here, "..", "paper_2609_14507_b200", "csrc"), "-o", str(so), str(src)],
+                   check=True)
+    shim, rng, sixteens = C.CDLL(str(so)), random.Random(7), 0
+    for _ in range(3000):
+        pairs, units, group = rng.choice([1, 4, 8, 9, 37, 296, rng.randint(1, 400)]), rng.randint(1, 300), rng.choice([1, 4, 8, 16, 17, 64])
+        with16, with8 = shim.cluster(pairs, units, group, 296, 16), shim.cluster(pairs, units, group, 296, 8)
+        assert with8 in (0, 1, 2, 4, 8) and pairs * with8 <= 296 and units <= 24 * with8 + (with8 == 0) * 300
+        sixteens += with16 == 16
+        assert with16 == with8 or (pairs <= 8 and with16 in (0, 16)), (pairs, units, group)
+    assert sixteens > 50
+    assert shim.cluster(4, 64, 8, 296, 8) == 8 and shim.cluster(4, 64, 8, 296, 16) == 16
+    assert shim.cluster(4, 129, 8, 296, 8) == 0 and shim.cluster(4, 129, 8, 296, 16) == 16
