@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(kThreads, 5) paged_append_kernel(const __grid_
     load(i0);
     if (tid < tokens) {
         const int64_t token = token0 + tid;
-        int row = int(token);
+        int row = int(token), n = 0;
         int64_t slot = -1, at = -1;
         if (p.row_start) {
             int lo = 0, hi = p.c.n_rows - 1;     // the last row that begins at or before the token
@@ -49,10 +49,15 @@ __global__ void __launch_bounds__(kThreads, 5) paged_append_kernel(const __grid_
             }
             row = lo;
             const int begin = p.row_start[row], end = p.row_start[row + 1];
-            if (token >= begin && token < end) slot = int64_t(p.c.lengths[row]) - (end - token);       // (else behind the last row's)
+            if (token >= begin && token < end) {                 // (else behind the last row's)
+                n = p.c.lengths[row];
+                slot = int64_t(n) - (end - token);
+            }
         } else {
-            slot = int64_t(p.c.lengths[row]) - 1;
+            n = p.c.lengths[row];
+            slot = int64_t(n) - 1;
         }
+        if (n < 0 && p.status) atomicOr(p.status, kStatusBadPage);
         if (slot >= 0) {                         // (else not counted by the length)
             int page = -1;
             const int t = slot < int64_t(p.c.max_blocks) * g.bt ? int(slot) : 0, block = int(unsigned(t) / unsigned(g.bt));
