@@ -547,8 +547,8 @@ typedef struct {
 } ipkv_paged;
 
 /* Bits that the calls below OR into *status_dev (may be NULL), beside those of ipkv_attend_runs: a length outside
- * 0 .. max_blocks * block_tokens, or a needed table entry outside 0 .. n_blocks - 1.  Such a token is left out: nothing outside the pool
- * is read or written (an eviction moves its weight and position all the same). */
+ * 0 .. max_blocks * block_tokens (in an append, of a row that takes tokens), or a needed table entry outside 0 .. n_blocks - 1.  Such a token is
+ * left out: nothing outside the pool is read or written (an eviction moves its weight and position all the same). */
 #define IPKV_STATUS_BAD_PAGE 16u
 
 /* The arguments of a call are a struct: a decode loop makes these calls once a layer, and a foreign-function interface takes its time
@@ -578,7 +578,8 @@ ipkv_status ipkv_paged_append(const ipkv_paged_append_call* call);
  * (a sliding window of the last `window` slots, and first ones that stay visible).  q_dev [n_rows][n_q_heads][dim] bf16, q_row_stride
  * elements between rows (a multiple of 8; 0: dense).  Outputs as in ipkv_attend_runs, fp32: o_part_dev [n_rows][n_q_heads][dim] normalised, lse_part_dev
  * [n_rows][n_q_heads] natural log, (0, -inf) for a row without visible slots; they join other partials through ipkv_merge.  Invisible slots
- * may hold anything; a NaN or an infinity in a visible one makes the outputs that it takes part in NaN or infinite.
+ * may hold anything.  In a visible one a NaN makes the outputs that it takes part in NaN, and so does an infinite V (infinite or NaN) or a
+ * score (scale q.k) of +infinity; a score of -infinity is a weight of zero, and a row whose scores are all that is (0, -inf).
  * weights_out_dev: NULL, or shaped like cache->weights_dev: for every visible slot
  *   weights_out = weights + sum over the KV head's query heads of the slot's softmax weight in this call
  * (weights: cache->weights_dev, zeros if that is NULL; the same array for an update in place, else one that does not overlap it).  Other slots are not written.
