@@ -793,13 +793,13 @@ def make_paged(shape, pool, table, lengths, weights=None, positions=None):
     stride = table.stride(0) if rows > 1 else per_row
     if stride < per_row:
         raise ValueError("the rows of a page table lie apart")
-    slots = 0
+    slots = None
     for x, dtype, name in ((weights, _f32, "weights"), (positions, _i32, "positions")):
         if x is not None:
-            slots = slots or x.shape[-1]
+            slots = x.shape[-1] if slots is None and x.dim() == 3 else slots
             if x.dtype is not dtype or x.shape != (rows, shape.n_kv_heads, slots) or not x.is_contiguous() or x.get_device() != dev:
                 raise ValueError(f"{name} are contiguous {dtype} [{rows}, {shape.n_kv_heads}, slots] on the device of the pool: got {x.dtype} {tuple(x.shape)}")
-    if slots and (slots < per_row * shape.block_tokens or slots % 4):
+    if slots is not None and (rows or slots) and (slots < per_row * shape.block_tokens or slots % 4):
         raise ValueError(f"{slots} slots: at least {per_row * shape.block_tokens}, a multiple of 4")
     slots = slots or per_row * shape.block_tokens
     c = Paged(pool.data_ptr(), pool.nbytes, table.data_ptr(), lengths.data_ptr(), rows, per_row, stride, _ptr(weights), _ptr(positions), slots)

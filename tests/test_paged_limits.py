@@ -47,3 +47,20 @@ def test_where_the_device_places_no_cluster_of_sixteen_eight_are_taken(tmp_path)
     assert sixteens > 50
     assert shim.cluster(4, 64, 8, 296, 8) == 8 and shim.cluster(4, 64, 8, 296, 16) == 16
     assert shim.cluster(4, 129, 8, 296, 8) == 0 and shim.cluster(4, 129, 8, 296, 16) == 16
+
+
+def test_weights_and_positions_without_slots_are_refused():
+    """They would pass for arrays that are not there: weights silently not counted, positions silently not kept."""
+    torch = pytest.importorskip("torch")
+    sh = shape_of(4, 2, 64, 64)
+    pool = torch.zeros((3, 2, 2, 64 * 64), dtype=torch.bfloat16)
+    table, lengths = torch.zeros((2, 3), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    w, pos = torch.zeros((2, 2, 192)), torch.zeros((2, 2, 192), dtype=torch.int32)
+    for a in ((w[:, :, :0],), (w[:, :, :0], pos), (None, pos[:, :, :0]), (w, pos[:, :, :0]), (w[:, :, :0], pos[:, :, :0]), (torch.tensor(1.0),), (w, torch.tensor(1, dtype=torch.int32)),
+              (w[0, 0],), (w[None],)):
+        with pytest.raises(ValueError):
+            binding.make_paged(sh, pool, table, lengths, *a)
+    c = binding.make_paged(sh, pool, table, lengths, w, pos)
+    assert (c.slot_stride, binding.make_paged(sh, pool, table, lengths, None, pos).slot_stride, binding.make_paged(sh, pool, table, lengths).slot_stride) == (192, 192, 192)
+    none = binding.make_paged(sh, pool, table[:0], lengths[:0], w[:0, :, :0])        # without rows nothing needs a slot
+    assert none.n_rows == 0
