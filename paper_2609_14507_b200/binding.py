@@ -863,7 +863,15 @@ def ipkv_paged_append(shape, cache, k, v, positions=None, row_start=None, status
         raise IpkvError(rc, "ipkv_paged_append")
 
 
+def _in_32_bits(*numbers):
+    """Numbers that the calls' structs cannot hold are refused (ctypes cuts them off)."""
+    for x in numbers:
+        if not -1 << 31 <= x < 1 << 31 or x != int(x):
+            raise ValueError(f"an argument is out of range: {x}")
+
+
 def ipkv_paged_scratch_bytes(shape, cache, window=0, first=0, weigh=False):
+    _in_32_bits(window, first)
     out = C.c_size_t()
     rc = lib().ipkv_paged_scratch_bytes(C.byref(shape), cache.n_rows, cache.max_blocks, window, first, 1 if weigh else 0, C.byref(out))
     if rc != OK:
@@ -900,6 +908,7 @@ def ipkv_paged_attend(shape, cache, q, scratch, o_part, lse_part, window=0, firs
 
 
 def ipkv_paged_evict_scratch_bytes(shape, cache, budget):
+    _in_32_bits(budget)
     out = C.c_size_t()
     rc = lib().ipkv_paged_evict_scratch_bytes(C.byref(shape), cache.n_rows, cache.max_blocks, budget, C.byref(out))
     if rc != OK:

@@ -64,3 +64,22 @@ def test_weights_and_positions_without_slots_are_refused():
     assert (c.slot_stride, binding.make_paged(sh, pool, table, lengths, None, pos).slot_stride, binding.make_paged(sh, pool, table, lengths).slot_stride) == (192, 192, 192)
     none = binding.make_paged(sh, pool, table[:0], lengths[:0], w[:0, :, :0])        # without rows nothing needs a slot
     assert none.n_rows == 0
+
+
+def test_scratch_is_told_for_the_numbers_that_the_calls_take():
+    """2^32 + 5 would have been answered as 5."""
+    torch = pytest.importorskip("torch")
+    sh = shape_of(4, 2, 64, 64)
+    c = binding.make_paged(sh, torch.zeros((3, 2, 2, 64 * 64), dtype=torch.bfloat16), torch.zeros((2, 3), dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+    for kw in (dict(window=2 ** 32 + 5), dict(window=2 ** 31), dict(window=5, first=2 ** 32), dict(window=-2 ** 31 - 1), dict(window=1.5)):
+        with pytest.raises(ValueError):
+            binding.ipkv_paged_scratch_bytes(sh, c, **kw)
+    for budget in (2 ** 32 + 7, 2 ** 31, -2 ** 31 - 1, 1.5):
+        with pytest.raises(ValueError):
+            binding.ipkv_paged_evict_scratch_bytes(sh, c, budget)
+    with pytest.raises(binding.IpkvError):
+        binding.ipkv_paged_scratch_bytes(sh, c, window=-1)
+    with pytest.raises(binding.IpkvError):
+        binding.ipkv_paged_evict_scratch_bytes(sh, c, 0)
+    assert binding.ipkv_paged_scratch_bytes(sh, c, 2 ** 31 - 1, 2 ** 31 - 1) == binding.ipkv_paged_scratch_bytes(sh, c)
+    assert binding.ipkv_paged_evict_scratch_bytes(sh, c, 2 ** 31 - 1) == 0
