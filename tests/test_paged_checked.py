@@ -19,3 +19,12 @@ def test_bounds_checked_build_passes_the_paged_cache():
                        env=env, cwd=ROOT, capture_output=True, text=True, timeout=900)
     assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
     assert " passed" in r.stdout and "skipped" not in r.stdout.splitlines()[-1]
+
+
+@pytest.mark.gpu
+def test_bounds_checked_build_passes_bad_lengths_and_pages():
+    env = dict(os.environ, IPKV_LIB_VARIANT="checked")
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-m", "gpu", "-x", os.path.join(ROOT, "tests", "test_paged_faults.py")],
+                       env=env, cwd=ROOT, capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
+    assert " passed" in r.stdout and "skipped" not in r.stdout.splitlines()[-1]
