@@ -530,14 +530,15 @@ ipkv_status ipkv_nibble_attend(const ipkv_attn_shape* shape, int32_t n_rows, con
  * captured into a CUDA graph is replayed as sequences grow, change pages or end: no call reads them on the host, and none writes
  * the table or the lengths (all layers of a model share them).  Grouped-query shapes, dim 64 or 128, block_tokens 16, 32 or a multiple of
  * 64.  Slot s of row r lies in block table[r][s / block_tokens] at token offset s % block_tokens.  Keys are cached after their
- * rotation, so the order of a row's slots means nothing to the attention: an eviction fills holes in place of closing ranks, and
- * what has to be known of a slot's token moves along (positions_dev, weights_dev; per KV head, since each keeps other tokens).
+ * rotation, so the order of a row's slots means nothing to the attention over all of them: an eviction fills holes in place of closing
+ * ranks, and what has to be known of a slot's token moves along (positions_dev, weights_dev; per KV head, since each keeps other tokens).
+ * A window counts slots, so it is for rows whose slots are in the order of their tokens: those that nothing was evicted from.
  * A block may serve several rows as long as no call writes it (a shared prefix). */
 typedef struct {
   void* pool_dev;               /* TILE blocks (ipkv_block_bytes each), 16-byte aligned                                  */
   int64_t pool_bytes;           /* n_blocks blocks: pool_bytes / ipkv_block_bytes, at least one and below 2^31           */
-  const int32_t* table_dev;     /* [n_rows][table_stride]: a row's blocks in the order of its slots; entries behind its length are
-                                   not read                                                                             */
+  const int32_t* table_dev;     /* [n_rows][table_stride]: a row's blocks in the order of its slots; entries behind its length may
+                                   hold anything (a prefetch reads them, nothing goes by them)                          */
   const int32_t* lengths_dev;   /* [n_rows]: slots of the row, 0 .. max_blocks * block_tokens                             */
   int32_t n_rows, max_blocks;   /* max_blocks: entries of a row's table; max_blocks * block_tokens <= 2^31 - 2^21 - 1    */
   int64_t table_stride;         /* elements, >= max_blocks                                                               */
@@ -575,7 +576,8 @@ typedef struct {
 ipkv_status ipkv_paged_append(const ipkv_paged_append_call* call);
 
 /* Attention of one query per row over its slots.  window 0: all of them; else slot t of n is visible if t >= n - window or t < first_tokens
- * (a sliding window of the last `window` slots, and first ones that stay visible).  q_dev [n_rows][n_q_heads][dim] bf16, q_row_stride
+ * (a sliding window of the last `window` slots, and first ones that stay visible; an eviction puts recent tokens into any slot below its budget, so a
+ * row that was cut is attended with window 0: its budget is its window).  q_dev [n_rows][n_q_heads][dim] bf16, q_row_stride
  * elements between rows (a multiple of 8; 0: dense).  Outputs as in ipkv_attend_runs, fp32: o_part_dev [n_rows][n_q_heads][dim] normalised, lse_part_dev
  * [n_rows][n_q_heads] natural log, (0, -inf) for a row without visible slots; they join other partials through ipkv_merge.  Invisible slots
  * may hold anything.  In a visible one a NaN makes the outputs that it takes part in NaN, and so does an infinite V (infinite or NaN) or a
@@ -585,7 +587,9 @@ ipkv_status ipkv_paged_append(const ipkv_paged_append_call* call);
  * (weights: cache->weights_dev, zeros if that is NULL; the same array for an update in place, else one that does not overlap it).  Other slots are not written.
  * scratch_dev: at least ipkv_paged_scratch_bytes (of the same n_rows, max_blocks, window, first_tokens; weigh: weights_out_dev is given),
  * 256-byte aligned, private to this call until its work on `stream` has completed (calls captured into graphs that may run at the same
- * time need scratch of their own).  Results are bit-reproducible.  Works on the current device. */
+ * time need scratch of their own).  The launches and the scratch follow max_blocks and the window, not the lengths, which are on the
+ * device: a table wider than the rows need costs time where little is read, and scratch with weights.  Results are bit-reproducible.  Works
+ * on the current device. */
 typedef struct {
   const ipkv_attn_shape* shape;
   const ipkv_paged* cache;

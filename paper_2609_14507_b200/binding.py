@@ -881,7 +881,7 @@ def ipkv_paged_scratch_bytes(shape, cache, window=0, first=0, weigh=False):
 
 def ipkv_paged_attend(shape, cache, q, scratch, o_part, lse_part, window=0, first=0, weights_out=None, status=None, stream=None):
     """Attention of one query per row, q [rows, n_q_heads, dim] bf16 (rows any stride apart), over the row's slots: all, or with a window the last `window` and the
-    `first` first ones.  weights_out: where the cache's weights go with this call's softmax weights added (may be the cache's own)."""
+    `first` first ones (slots, not positions: rows that were cut by an eviction are attended without a window).  weights_out: where the cache's weights go with this call's softmax weights added (may be the cache's own)."""
     dev, f32, heads, rows = cache._dev, _f32, shape.n_q_heads, cache._rows
     want = (rows, heads, shape.dim_qk)
     if shape.n_kv_heads != cache._slots[1]:
@@ -918,7 +918,8 @@ def ipkv_paged_evict_scratch_bytes(shape, cache, budget):
 
 def ipkv_paged_evict(shape, cache, budget, first, recent, scratch, weights_out=None, positions_out=None, kept=None, status=None, stream=None):
     """Cut every row to at most `budget` slots per KV head: the `first` first and the `recent` most recent tokens stay, of the others
-    those with the largest weights.  cache.lengths stay as they are: the caller sets them to min(length, budget) after all layers."""
+    those with the largest weights.  cache.lengths stay as they are: the caller sets them to min(length, budget) after all layers.  Kept tokens fill the
+    slots of evicted ones: from then on a row's slots are in no order, and a window over them means nothing."""
     dev = cache._dev
     if shape.n_kv_heads != cache._slots[1]:
         raise ValueError(f"the cache has {cache._slots[1]} KV heads, the shape {shape.n_kv_heads}")

@@ -244,3 +244,22 @@ def test_an_append_and_an_eviction_beyond_32_bits_of_bytes():
         src = torch.tensor(ref.kept(w[0, h, :n].tolist(), list(range(n)), budget, 4, 30), device="cuda")
         assert torch.equal(k1[:budget, h], k[src, h]) and torch.equal(v1[:budget, h], v[src, h]) and torch.equal(c.positions[0, h, :budget], src.int())
         assert torch.equal(k1[budget:, h], k[budget:, h]) and torch.equal(v1[budget:, h], v[budget:, h])
+
+
+# ---- a window over rows that were cut --------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+def test_a_window_counts_slots_whatever_their_tokens():
+    """As the header says: after an eviction the last slots are not the last tokens."""
+    c = Case([600, 90], 4, 2, 64, 32)
+    c.positions[:] = torch.arange(c.positions.shape[-1], dtype=torch.int32, device="cuda")
+    scratch = torch.empty(binding.ipkv_paged_evict_scratch_bytes(c.shape, c.cache(), 200), dtype=torch.uint8, device="cuda")
+    binding.ipkv_paged_evict(c.shape, c.cache(), 200, 0, 50, scratch, status=c.status)
+    c.lengths.clamp_(max=200)
+    c.n = [200, 90]
+    recent = c.positions[0, 0, :200] >= 550              # moved in order, but only into holes: tokens that stayed are among the last slots
+    assert recent.sum() == 50 and not recent[150:].all()
+    for window, first in ((50, 3), (0, 0)):
+        o, lse = c.attend(window, first)
+        c.check(o, lse, window, first)
+    assert int(c.status) == 0
