@@ -84,9 +84,11 @@ constexpr int kPagedPairCost = 4;                // queries read, the pipeline d
 constexpr int kPagedRowsPerLaunch = 1024;        // the shares of so many rows are held in shared memory
 constexpr int kPagedCtasPerSm = 2, kPagedWarps = 4;
 // Where every pair has few units, which the host sees by the table's width or the window alone, a thread-block cluster takes it, joins
-// in distributed shared memory and adds the weights up: one launch in place of two or three.
+// in distributed shared memory and adds the weights up: one launch in place of two or three.  (A step of 16 rows of 2K, weighed, takes 14.4 us with a table of
+// 2048 slots, 15.7 with 4096, and in three launches 19.8 with 8192 and 21.5 with 32768; one row of 4K 11.1 with 4608, 12.0 with 8192 and 32768.)
 // Sixteen CTAs, more than a portable cluster, for at most eight pairs: a GPC for each (1 row of 4 KV heads, 2K tokens: 8.0 us, with eight CTAs 9.5; 3K and 4K:
-// 9.8 and 10.9, with CTAs over the GPU and a join 11.6 and 11.7; sixteen pairs of sixteen 14.7 against 7.7, they take turns).
+// 9.8 and 10.9, with CTAs over the GPU and a join 11.6 and 11.7; sixteen pairs of sixteen 14.7 against 7.7, they take turns).  At the border that the units below
+// set, nine a CTA: 4600 tokens of 128 columns 12.0 and 12.6 with a join, 9000 of 64 columns 9.6 and 10.6; beyond it, 6000 of 128 columns 12.9 and 12.7, 8000 14.4 and 12.0.
 // `largest`: what the device places (a part of a GPU may have no GPC with room for sixteen).
 constexpr int kPagedMostCluster = 16, kPagedPortableCluster = 8;
 constexpr int kPagedClusterUnits = 24, kPagedClusterMore = 5;

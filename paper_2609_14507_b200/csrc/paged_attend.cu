@@ -19,7 +19,9 @@
 //
 // Measured (a few replays of a graph): 16 rows of 32K tokens, 4 KV heads of 8 query heads, 128 columns: 164 us for 1074 MB, 6.5 TB/s; 64 ragged rows of up
 // to 16K in pages of 16, 8 KV heads of 4: 336 us for 2259 MB, 6.7 TB/s; one row of 500K, 16 heads on one: 51 us for 256 MB, 34 of them
-// streaming at 7.5 TB/s; 32 rows through a window of 4096: 85 us for 507 MB, 6.0 TB/s; one of 4K tokens: 11.0 us, a chain of latencies.
+// streaming at 7.5 TB/s; 32 rows through a window of 4096: 85 us for 507 MB, 6.0 TB/s; one of 4K tokens: 11.0 us, a chain of latencies.  More than 16 heads
+// on a KV head are bound by their products, a warp's three for every 16 heads: 4 rows of 50K, 64 heads on 2: 63 us for 205 MB, 3.2 TB/s (32 on 1: 39 us for 102 MB); an odd number of
+// sixteens reads K and V once for each: one row of 200K, 40 heads on one: 48 us for 102 MB.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -193,7 +195,8 @@ template <int D, int ROWS>
 __global__ void __launch_bounds__(kThreads, kPagedCtasPerSm) paged_attend_kernel(const __grid_constant__ PagedAttend p) {
     constexpr int U = kPagedUnitBytes / (4 * D), kSlices = U / 16;
     // 16 rows of queries are read from shared memory for every unit, each warp's in the place of a stage: with them in registers, too, some 20 others
-    // were reloaded in every unit (64 heads on 2 KV heads, 4 rows of 50K tokens: 64 us).
+    // were reloaded in every unit (64 heads on 2 KV heads, 4 rows of 50K tokens: 67 us against 60 when
+    // this was changed).
     constexpr int kStages = ROWS == 16 ? kMostStages - 1 : kMostStages;
     extern __shared__ unsigned char smem_dyn[];
     unsigned char* ring = smem_dyn + ((1024u - (ptx::smem_addr(smem_dyn) & 1023u)) & 1023u);      // 1024: rows of a panel on distinct banks

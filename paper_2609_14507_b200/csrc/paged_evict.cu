@@ -11,8 +11,9 @@
 // Where one slot goes (a full cache that makes room for the next token), it is the smallest key, of equal ones the last slot's: one
 // minimum in place of 2 and 3.
 // Bound by its chain of passes, 1.7 us each in a cluster of eight with 1024 threads (the sending itself takes 0.15, counting 0.6), then by the rows moved in
-// pieces of 128 bytes.  Measured: 512 pairs, one of 4096 slots 9.6 us (41 MB with arrays apart); 8 pairs of 32K to 4K 24.0 us, 7 to 9 of them for 29 MB of rows;
-// 8 pairs of 261 to 243 slots 8.2 us.
+// pieces of 128 bytes.  Measured (a few replays of a graph, 1965 MHz): 512 pairs, one of 4096 slots goes in every one, in place 8.2 us (17 MB read), 128 such pairs 5.6,
+// 8 5.1; with arrays apart 512 12.0; 512 pairs of 4000 to 4096 slots of which 32 are cut and 480 copied to arrays apart 9.6; 8 pairs of 32K to 4K 24.2 us, 7 to 9 of them
+// for 29 MB of rows (all weights equal: 21.1); 8 of 3K to 1K 16.6 (equal: 13.3); 8 pairs of 261 to 243 slots 8.2 us.
 #include <atomic>
 
 #include "kernels.h"
